@@ -633,6 +633,137 @@ enum {
 lattice_status lattice_set_timing(lattice *L, int mode);
 lattice_status lattice_get_timing(lattice *L, double *ms, int64_t *count);
 
+/*
+ * Dense operators of a training step around the lattice: the normalisation of
+ * vertex or point rows, the classifier's loss with its gradients, and the
+ * orthogonalised form of a weight gradient.  They work on plain row-major
+ * matrices and need no lattice: a lattice_dense is their handle.  It owns
+ * scratch that grows on demand and a device status word; all its work is
+ * enqueued on the stream given at creation, and no call but
+ * lattice_dense_get_status and lattice_dense_destroy synchronises with the
+ * host.  A call that needs more scratch than any before it allocates device
+ * memory (make one such call before capturing the call into a HIP graph).
+ * Arguments are checked synchronously; on an error nothing is enqueued and
+ * lattice_dense_last_error holds a message.  A handle is not thread safe.
+ *
+ * Strides are in values between the starts of consecutive rows (>= the row's
+ * values); a row's values are next to each other.  Rows may start at any
+ * multiple of an element's size.  Sums, statistics and states are fp32 or
+ * wider; storage LATTICE_BF16 rounds results to nearest even once, at the end,
+ * but for what the operators state.  Every result is the same, bit for bit, in
+ * two calls on the same inputs.
+ */
+typedef struct lattice_dense lattice_dense;
+
+/* Create the handle on the current device; stream as in lattice_create. */
+lattice_status lattice_dense_create(void *stream, lattice_dense **out);
+/* Release the handle (after synchronising its stream).  NULL is a no-op. */
+void lattice_dense_destroy(lattice_dense *D);
+/*
+ * Synchronise and return the device status since the last call of this
+ * function, clearing it: LATTICE_E_RANGE if a lattice_linear_cross_entropy met
+ * a label that is neither a class nor ignore_index.
+ */
+lattice_status lattice_dense_get_status(lattice_dense *D);
+const char *lattice_dense_last_error(const lattice_dense *D);
+
+/*
+ * lattice_layer_norm -- normalise each row over its channels:
+ *   mu = mean_c x_c,  r = 1 / sqrt(mean_c (x_c - mu)^2 + eps),
+ *   y_c = gamma_c r (x_c - mu) + beta_c.
+ *   rows_of       a lattice on the same device and stream: the rows are its
+ *                 vertices, V of them (read on the device), of which `rows` is
+ *                 an upper bound (lattice_max_vertices); NULL: `rows` rows.
+ *   x             dev [rows][C] stored as x_dtype, x_stride values a row.
+ *   rows          0 .. 2^31.       C  channels, 1 .. 2^20.
+ *   gamma, beta   dev fp32 [C], or NULL for ones and zeros.
+ *   eps           >= 0.
+ *   y             dev [rows][C] stored as y_dtype, y_stride values a row; may
+ *                 be x itself (same type and stride), otherwise no overlap.
+ *   mean, rstd    dev fp32 [rows] receive mu and r (what the backward pass
+ *                 takes), or NULL.
+ * Statistics in fp32, the variance from the differences (two passes over a row
+ * held in registers).
+ */
+lattice_status lattice_layer_norm(lattice_dense *D, const lattice *rows_of, const void *x, lattice_dtype x_dtype,
+                                  int64_t x_stride, int64_t rows, int C, const float *gamma, const float *beta,
+                                  float eps, void *y, lattice_dtype y_dtype, int64_t y_stride, float *mean,
+                                  float *rstd);
+
+/*
+ * lattice_layer_norm_backward -- its gradients, given g = dL/dy:
+ *   dx_c = r (u_c - mean(u) - h_c mean(u h)),  u = g gamma,  h = r (x - mu)
+ *   dgamma_c = sum over rows of g_c h_c,  dbeta_c = sum over rows of g_c.
+ *   rows_of, x, rows, C, gamma   as in the forward call.
+ *   grad_y        dev [rows][C] stored as g_dtype, g_stride values a row.
+ *   mean, rstd    dev fp32 [rows] of the forward call.
+ *   grad_x        dev [rows][C] stored as x_dtype, or NULL; may be grad_y (of
+ *                 the same type) or x itself for C up to 8192.
+ *   grad_gamma, grad_beta   dev fp32 [C], or NULL.  Zero without rows.
+ * At least one of the three.  The sums over rows are fp32 in a thread and fp64
+ * between workgroups, in a fixed order.
+ */
+lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows_of, const void *grad_y,
+                                           lattice_dtype g_dtype, int64_t g_stride, const void *x,
+                                           lattice_dtype x_dtype, int64_t x_stride, int64_t rows, int C,
+                                           const float *mean, const float *rstd, const float *gamma, void *grad_x,
+                                           int64_t grad_x_stride, float *grad_gamma, float *grad_beta);
+
+/*
+ * lattice_linear_cross_entropy -- a linear classifier with its softmax cross
+ * entropy, and in the same call its gradients, without the N x K logits in
+ * memory:
+ *   z_ik = x_i . w_k + bias_k,   lse_i = log sum_k exp z_ik
+ *   row_loss_i = lse_i - z_it, t = target_i (0 for a row without a label)
+ *   loss = sum of the row losses; with mean, over the rows that have a label
+ *          (0 without any)
+ *   grad_x, grad_w, grad_bias = the gradients of `loss`.
+ *   dtype         storage of x, w, grad_x and grad_w.  Products of fp32
+ *                 operands are as in LATTICE_F32; of bf16 ones they are exact,
+ *                 and d loss / dz is rounded to bf16 before the products that
+ *                 give grad_x and grad_w (not for grad_bias).
+ *   x             dev [N][C], x_stride values a row; N 0 .. 2^28, C 1 .. 2^14.
+ *   w             dev [K][C], w_stride values a row; K 1 .. 2^20.
+ *   bias          dev fp32 [K], or NULL.  -inf takes a class out.
+ *   target        dev int64 [N]: a class, or ignore_index for a row without a
+ *                 label.  Any other value counts as no label, and is reported
+ *                 by lattice_dense_get_status.
+ *   loss          dev fp32 [1].           row_loss  dev fp32 [N], or NULL.
+ *   grad_x        dev [N][C], or NULL; zero for rows without a label.
+ *   grad_w        dev [K][C], or NULL.    grad_bias dev fp32 [K], or NULL.
+ * What a row without a label holds (NaN, infinities) reaches no result.  fp32
+ * operands of 2^104 or more in magnitude give NaN.  The gradients overlap
+ * neither x nor w.
+ */
+#define LATTICE_LOSS_MAX_ROWS ((int64_t)1 << 28)
+#define LATTICE_LOSS_MAX_CHANNELS (1 << 14)
+#define LATTICE_LOSS_MAX_CLASSES (1 << 20)
+lattice_status lattice_linear_cross_entropy(lattice_dense *D, lattice_dtype dtype, const void *x, int64_t x_stride,
+                                            int64_t N, int C, const void *w, int64_t w_stride, int K,
+                                            const float *bias, const int64_t *target, int64_t ignore_index, int mean,
+                                            float *loss, float *row_loss, void *grad_x, void *grad_w,
+                                            float *grad_bias);
+
+/*
+ * lattice_orthogonalize -- Newton-Schulz steps on each of `batch` matrices,
+ * which move its singular values towards 1 and keep its singular vectors (the
+ * update that an optimiser subtracts in place of the gradient):
+ *   X = g / (|g|_F + eps), transposed if m > n;
+ *   `steps` times  S = X X^T,  X = a X + (b S + c S S) X;   transposed back.
+ *   g             dev [batch][m][n] stored as g_dtype, row_stride values a
+ *                 row, batch_stride between matrices; batch 0 .. 65535, m and
+ *                 n 1 .. 65536.
+ *   steps         0 .. 64.     coefficients  host: a, b, c.     eps  >= 0.
+ *   out           dev [batch][m][n] stored as out_dtype; no overlap with g.
+ * For an fp32 result X and S carry 24 bits between the products, for a bf16
+ * one 16.  A matrix of zeros gives zeros.
+ */
+#define LATTICE_UPDATE_MAX_BATCH 65535
+#define LATTICE_UPDATE_MAX_SIDE 65536
+lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dtype g_dtype, int64_t batch, int m,
+                                     int n, int64_t batch_stride, int64_t row_stride, int steps,
+                                     const float *coefficients, float eps, void *out, lattice_dtype out_dtype);
+
 /* Query the hash capacity and dimension of L. */
 int64_t lattice_hash_capacity(const lattice *L);
 int lattice_dim(const lattice *L);

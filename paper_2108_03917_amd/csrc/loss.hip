@@ -1,0 +1,599 @@
+// The linear classifier with softmax cross entropy, and its gradients, without
+// the logits in memory.
+//
+//   z_ik = x_i . w_k + b_k,   lse_i = log sum_k exp z_ik,   l_i = lse_i - z_it (t = target_i)
+//   L = sum_i s l_i,  s = 1, or 1 / (rows with a label);  rows without a label count for nothing
+//   G_ik = exp(z_ik - lse_i) - [k = t],   dx = s G w,   dw = s G^T x,   db_k = s sum_i G_ik.
+//
+// Rows are taken in pieces, and for the gradients classes too.  For a piece of
+// rows a first product passes over all classes and keeps, per tile of classes,
+// the running maximum and sum of each row; these are joined to lse.  Then, per
+// piece of classes, the logits are computed again, G is formed from them in the
+// product's epilogue, in both orders, and multiplied with w and x.  The
+// second product of the logits costs a third more operations than the gradients
+// need; keeping the logits instead would cost rows x classes of memory.
+//
+// The products run on the bf16 matrix cores (gemm.h): bf16 operands as they
+// are, fp32 ones as three planes.  G is rounded to bf16 for bf16 gradients (a
+// relative 2^-9 of each term, random in sign, as the gradients' own rounding
+// is; s is left out of it, or the entries near -s of all rows would be off by
+// the same part), and kept in three planes for fp32 ones.  The bias gradient is
+// summed from G before that rounding.  Sums are fp32, joined in a fixed order.
+#include "planes.h"
+#include "rowsum.h"
+
+namespace {
+
+constexpr int kCounts = 256;          // partial counts of rows with a label
+constexpr int64_t kMaxPiece = 65536;  // rows of a piece
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of G in both orders
+
+// Rows with a label, counted per workgroup; a label that is neither a class
+// nor `ignore` sets the status.
+__global__ __launch_bounds__(256) void k_count(const int64_t *__restrict__ target, int64_t N, int K, int64_t ignore,
+                                               int32_t *count, int32_t *status) {
+    int n = 0, bad = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = target[i];
+        if (t == ignore) continue;
+        if (t >= 0 && t < K)
+            ++n;
+        else
+            bad = 1;
+    }
+    if (bad) atomicOr(status, DENSE_ST_LABEL);
+    __shared__ int red[4];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) count[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+// The factor s of the rows with a label.  Called by whole wavefronts.
+__device__ __forceinline__ float row_factor(const int32_t *count, bool mean) {
+    if (!mean) return 1.f;
+    int64_t n = 0;
+    for (int i = threadIdx.x & 63; i < kCounts; i += 64) n += count[i];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
+    return n > 0 ? (float)(1.0 / (double)n) : 0.f;
+}
+
+// Biases of the classes, zeros without any; -inf from K on, so that the
+// classes that fill up the last tile have no share.
+__global__ __launch_bounds__(256) void k_bias(const float *bias, int K, int Kp, float *out) {
+    const int k = blockIdx.x * 256 + threadIdx.x;
+    if (k < Kp) out[k] = k < K ? (bias ? bias[k] : 0.f) : -INFINITY;
+}
+
+// What the epilogues need of a piece's rows.
+struct Rows {
+    const int32_t *label;  // class, or -1 for a row without one
+    const float *lse;
+    int n;
+};
+
+// The labels of a piece's rows, and the factor s.
+__global__ __launch_bounds__(256) void k_rows(const int64_t *__restrict__ target, int n, int K, int64_t ignore,
+                                              const int32_t *count, bool mean, int32_t *label, float *factor) {
+    if (blockIdx.x == 0 && threadIdx.x < 64) {
+        const float s = row_factor(count, mean);
+        if (threadIdx.x == 0) *factor = s;
+    }
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int64_t t = target[i];
+    label[i] = t != ignore && t >= 0 && t < K ? (int)t : -1;
+}
+
+// Epilogue of the first pass (rows of the product are classes, columns the
+// piece's rows): maximum and sum of exponentials per tile and row, and the
+// logit of the label.
+template <int P>
+struct Stats {
+    const float *bias;  // padded
+    const int32_t *label;
+    int n;
+    float2 *stats;      // [tiles of classes][n]
+    float *picked;      // [n]
+
+    template <class T>
+    static constexpr int lds() { return T::WM * T::BN * 8; }
+
+    template <class T>
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *lds) const {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int wm = wave / T::WN;
+        float2 *part = reinterpret_cast<float2 *>(lds);
+        float4 bb[T::TM][4];
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                bb[i][q] = *reinterpret_cast<const float4 *>(bias + at.row0 + 32 * i + 8 * q + 4 * (lane >> 5));
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j) {
+            const int col = at.col0 + 32 * j + (lane & 31);
+            const int t = col < n ? label[col] : -1;
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float4 b4 = bb[i][e >> 2];
+                    const float b = (e & 3) == 0 ? b4.x : (e & 3) == 1 ? b4.y : (e & 3) == 2 ? b4.z : b4.w;
+                    const float z = acc[i][j][e] * planes::kBack<P> + b;
+                    acc[i][j][e] = z;
+                    top = fmaxf(top, z);
+                    if (at.row0 + 32 * i + gemm::acc_row(e) == t) picked[col] = z;
+                }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float ref = top == -INFINITY ? 0.f : top;
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s += __expf(acc[i][j][e] - ref);
+            s += __shfl_xor(s, 32);
+            if (lane < 32) part[wm * T::BN + col - at.tile_n * T::BN] = make_float2(top, s);
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < T::BN; c += T::THREADS) {
+            const int col = at.tile_n * T::BN + c;
+            if (col >= n) continue;
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < T::WM; ++w) top = fmaxf(top, part[w * T::BN + c].x);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < T::WM; ++w) s += part[w * T::BN + c].y * __expf(part[w * T::BN + c].x - ref);
+            stats[(int64_t)at.tile_m * n + col] = make_float2(top, s);
+        }
+    }
+};
+
+// Joins the tiles' statistics to lse, and the rows' losses; one partial sum of
+// the losses a workgroup, in fp64.  Four threads a row share its tiles.
+__global__ __launch_bounds__(256) void k_lse(const float2 *__restrict__ stats, int tiles, int n,
+                                             const float *__restrict__ picked, const int32_t *__restrict__ label,
+                                             float *lse, float *rows, double *part) {
+    const int i = blockIdx.x * 64 + (threadIdx.x >> 2), q = threadIdx.x & 3;
+    double l = 0.0;
+    if (i < n) {
+        float top = -INFINITY, s = 0.f;
+        for (int t = q; t < tiles; t += 4) {
+            const float2 v = stats[(int64_t)t * n + i];
+            const float m = fmaxf(top, v.x);
+            const float ref = m == -INFINITY ? 0.f : m;
+            s = s * __expf(top - ref) + v.y * __expf(v.x - ref);
+            // a NaN in a tile's sum stays
+            top = m;
+        }
+#pragma unroll
+        for (int d = 1; d < 4; d *= 2) {
+            const float top2 = __shfl_xor(top, d), s2 = __shfl_xor(s, d);
+            const float m = fmaxf(top, top2);
+            const float ref = m == -INFINITY ? 0.f : m;
+            s = s * __expf(top - ref) + s2 * __expf(top2 - ref);
+            top = m;
+        }
+        const float v = top + logf(s);
+        if (q == 0) {
+            const float one = label[i] >= 0 ? v - picked[i] : 0.f;
+            lse[i] = v;
+            if (rows) rows[i] = one;
+            l = one;
+        }
+    }
+    __shared__ double red[4];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = l;
+    __syncthreads();
+    if (threadIdx.x == 0) part[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+// The loss from the workgroups' partial sums.
+__global__ __launch_bounds__(256) void k_total(const double *__restrict__ part, int64_t n, const int32_t *count,
+                                               bool mean, float *loss) {
+    double s = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 256) s += part[i];
+    int64_t c = 0;
+    for (int i = threadIdx.x; i < kCounts; i += 256) c += count[i];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        s += __shfl_xor(s, d);
+        c += __shfl_xor(c, d);
+    }
+    __shared__ double red[4];
+    __shared__ int64_t cred[4];
+    if ((threadIdx.x & 63) == 0) {
+        red[threadIdx.x >> 6] = s;
+        cred[threadIdx.x >> 6] = c;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = red[0] + red[1] + red[2] + red[3];
+        c = cred[0] + cred[1] + cred[2] + cred[3];
+        *loss = (float)(mean ? (c > 0 ? s / (double)c : 0.0) : s);
+    }
+}
+
+// Epilogue of the second pass over a piece of classes: G in both orders, and
+// partial sums of its columns.
+template <int P>
+struct Grad {
+    const float *bias;  // padded, of the piece's first class on
+    Rows rows;
+    int class0;         // of the piece
+    int K, ldg;         // classes of the piece, and padded
+    int64_t ldt;        // rows padded
+    uint16_t *g;        // [P][n][ldg], or null
+    uint16_t *gt;       // [P][K][ldt], or null
+    float *pbias;       // [tiles of rows * WN][K], or null
+    const float *factor;
+
+    template <class T>
+    static constexpr int lds() { return 0; }
+
+    template <class T>
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *) const {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int n = rows.n;
+        int t[T::TN];     // label in the piece's classes
+        bool on[T::TN];
+        float lse[T::TN];
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j) {
+            const int col = at.col0 + 32 * j + (lane & 31);
+            const int l = col < n ? rows.label[col] : -1;
+            on[j] = l >= 0;
+            t[j] = l - class0;
+            lse[j] = col < n ? rows.lse[col] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int row = at.row0 + 32 * i + 8 * q + 4 * (lane >> 5);
+                const float4 b4 = *reinterpret_cast<const float4 *>(bias + row);
+                const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j) {
+                    const int col = at.col0 + 32 * j + (lane & 31);
+                    uint16_t h[4][P];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float z = acc[i][j][4 * q + r] * planes::kBack<P> + b[r];
+                        float v = __expf(z - lse[j]);
+                        if (row + r == t[j]) v -= 1.f;
+                        if (!on[j]) v = 0.f;  // a row without a label, whatever it holds
+                        sum[r] += v;
+                        planes::split<P>(v, h[r]);
+                    }
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        if (g && col < n && row < ldg) {
+                            const uint2 u = make_uint2(h[0][p] | (uint32_t)h[1][p] << 16, h[2][p] | (uint32_t)h[3][p] << 16);
+                            *reinterpret_cast<uint2 *>(g + ((int64_t)p * n + col) * ldg + row) = u;
+                        }
+                        if (gt && col < ldt)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (row + r < K) gt[((int64_t)p * K + row + r) * ldt + col] = h[r][p];
+                    }
+                }
+                if (pbias) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                        for (int d = 1; d < 32; d *= 2) sum[r] += __shfl_xor(sum[r], d);
+                        if ((lane & 31) == 0 && row + r < K)
+                            pbias[((int64_t)at.tile_n * T::WN + wave % T::WN) * K + row + r] = sum[r] * *factor;
+                    }
+                }
+            }
+    }
+};
+
+// Epilogue of a gradient's product: fp32 partial sums [split][rows][cols],
+// begun or added to.
+template <int P>
+struct Part {
+    float *out;
+    int rows, cols;
+    bool add;
+
+    template <class T>
+    static constexpr int lds() { return 0; }
+
+    template <class T>
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *) const {
+        const int lane = threadIdx.x & 63;
+        float *o = out + (int64_t)at.split * rows * cols;
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int row = at.row0 + 32 * i + gemm::acc_row(e), col = at.col0 + 32 * j + (lane & 31);
+                    if (row >= rows || col >= cols) continue;
+                    float *to = o + (int64_t)row * cols + col;
+                    const float v = acc[i][j][e] * planes::kBack<P>;
+                    *to = add ? *to + v : v;
+                }
+    }
+};
+
+// The gradient from the partial sums of its product's splits and the factor s.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, int splits, int64_t n,
+                                              const float *factor, void *out) {
+    const float f = splits > 0 ? *factor : 0.f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        float s = 0.f;  // without any part, zeros
+        for (int k = 0; k < splits; ++k) s += part[k * n + i];
+        s *= f;
+        if (BF16)
+            reinterpret_cast<uint16_t *>(out)[i] = (uint16_t)pack_bf16(s, 0.f);
+        else
+            reinterpret_cast<float *>(out)[i] = s;
+    }
+}
+
+// Tiles: classes x rows for the logits, rows x channels and classes x channels
+// for the gradients.
+template <int P>
+struct Tiles;
+template <>
+struct Tiles<1> {
+    using Large = gemm::Tile<256, 256, 2, 4, 64, 1>;
+    using Middle = gemm::Tile<128, 128, 2, 2, 64, 1>;
+    using Few = gemm::Tile<128, 64, 4, 1, 64, 1>;
+};
+template <>
+struct Tiles<3> {
+    using Large = gemm::Tile<128, 128, 2, 2, 32, 3>;
+    using Middle = gemm::Tile<128, 128, 2, 2, 32, 3>;
+    using Few = gemm::Tile<128, 64, 4, 1, 32, 3>;
+};
+
+// 0: Large, 1: Middle, 2: Few.  The large tile reads the least; it is for
+// products with enough of them to go round, and the last is for few columns.
+template <int P>
+int tile_for(int64_t m, int64_t n, int cu) {
+    using L = typename Tiles<P>::Large;
+    if (n <= 64) return 2;
+    const int64_t large = (m + L::BM - 1) / L::BM * ((n + L::BN - 1) / L::BN);
+    return large * 4 >= (int64_t)cu * 3 ? 0 : 1;
+}
+
+template <int P>
+int64_t tile_count(int kind, int64_t m, int64_t n) {
+    using X = Tiles<P>;
+    const int64_t bm = kind == 0 ? X::Large::BM : kind == 1 ? X::Middle::BM : X::Few::BM;
+    const int64_t bn = kind == 0 ? X::Large::BN : kind == 1 ? X::Middle::BN : X::Few::BN;
+    return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
+}
+
+template <int P>
+int tile_m(int kind) { return kind == 0 ? Tiles<P>::Large::BM : kind == 1 ? Tiles<P>::Middle::BM : Tiles<P>::Few::BM; }
+
+// Columns' partial rows of the bias gradient that a product over n rows gives.
+template <int P>
+int64_t bias_rows(int kind, int64_t n) {
+    using X = Tiles<P>;
+    const int64_t bn = kind == 0 ? X::Large::BN : kind == 1 ? X::Middle::BN : X::Few::BN;
+    const int64_t wn = kind == 0 ? X::Large::WN : kind == 1 ? X::Middle::WN : X::Few::WN;
+    return (n + bn - 1) / bn * wn;
+}
+
+// Splits of a contraction of k for m x n tiles that do not fill the chip.
+template <int P>
+int splits_for(int kind, int64_t m, int64_t n, int64_t k, int cu) {
+    const int64_t t = tile_count<P>(kind, m, n);
+    int64_t s = (cu + t - 1) / t;
+    const int64_t most = k / 256 > 0 ? k / 256 : 1;
+    s = s < most ? s : most;
+    return (int)(s < 16 ? s : 16);
+}
+
+template <int P, class E>
+hipError_t product(hipStream_t st, int kind, const gemm::Operand &A, const gemm::Operand &B, int64_t K, int64_t part,
+                   const E &e) {
+    using X = Tiles<P>;
+    if (kind == 0) return gemm::launch<typename X::Large>(st, A, B, K, part, 1, false, e);
+    if (kind == 1) return gemm::launch<typename X::Middle>(st, A, B, K, part, 1, false, e);
+    return gemm::launch<typename X::Few>(st, A, B, K, part, 1, false, e);
+}
+
+// Sizes of the pieces and where everything lies in the scratch.
+template <int P>
+struct Plan {
+    int64_t R;           // rows of a piece
+    int64_t Kpad;        // classes in whole tiles
+    int64_t KP;          // classes of a piece
+    int fkind, gkind;    // tiles of the two passes over the logits
+    int xkind, wkind;    // of the gradients' products
+    int64_t xpart, wpart;      // lengths of their contractions' parts
+    int64_t xsplits, wsplits;  // and how many there are at most
+    bool own_x, own_w;   // operands that have to be laid out first
+    int64_t count, bias, label, factor, lse, picked, stats, part, xp, xt, wp, wt, g, gt, pbias, bias_acc, px, pw, bytes;
+    int64_t parts;       // partial sums of the loss
+
+    Plan(const lattice_dense *D, const LossArgs &a) {
+        const int cu = D->cu_count;
+        const int64_t C = a.C, K = a.K;
+        const int64_t Cp = gemm::padded(C);
+        Kpad = (K + 255) / 256 * 256;
+        R = a.N < kMaxPiece ? a.N : kMaxPiece;
+        // tiles' statistics of a piece: at most 256 MiB
+        const int64_t most = ((int64_t)1 << 25) / (Kpad / 128);
+        if (R > most) R = most < 256 ? 256 : most / 256 * 256;
+        if (R < 1) R = 1;
+        const int64_t Rp = gemm::padded(R);
+        KP = kPieceBytes / (Rp * P * 2 * 2) / 256 * 256;
+        KP = KP < 256 ? 256 : KP;
+        KP = KP < Kpad ? KP : Kpad;
+        const int64_t kp = KP < K ? KP : K;
+        fkind = tile_for<P>(K, R, cu);
+        gkind = tile_for<P>(kp, R, cu);
+        xkind = C <= 64 ? 2 : tile_for<P>(R, C, cu);
+        wkind = C <= 64 ? 2 : tile_for<P>(kp, C, cu);
+        xpart = gemm::part_length(gemm::padded(kp), splits_for<P>(xkind, R, C, kp, cu));
+        wpart = gemm::part_length(Rp, splits_for<P>(wkind, kp, C, R, cu));
+        xsplits = (gemm::padded(kp) + xpart - 1) / xpart;
+        wsplits = (Rp + wpart - 1) / wpart;
+        auto as_is = [&](const void *q, int64_t stride) {
+            return P == 1 && C % gemm::kPad == 0 && stride % 8 == 0 && stride < gemm::kMaxLd && ((uintptr_t)q & 15) == 0;
+        };
+        own_x = !as_is(a.x, a.x_stride);
+        own_w = !as_is(a.w, a.w_stride);
+        ScratchLayout s;
+        count = s.take(kCounts * 4);
+        bias = s.take(Kpad * 4);
+        label = s.take(R * 4);
+        factor = s.take(4);
+        lse = s.take(R * 4);
+        picked = s.take(R * 4);
+        const int64_t bm = tile_m<P>(fkind);
+        stats = s.take((K + bm - 1) / bm * R * 8);
+        parts = 0;
+        for (int64_t r = 0; r < a.N; r += R) parts += ((a.N - r < R ? a.N - r : R) + 63) / 64;
+        part = s.take(parts * 8);
+        xp = own_x ? s.take(P * R * Cp * 2) : 0;
+        wp = own_w ? s.take(P * K * Cp * 2) : 0;
+        xt = a.grad_w ? s.take(P * C * Rp * 2) : 0;
+        wt = a.grad_x ? s.take(P * C * gemm::padded(K) * 2) : 0;
+        g = a.grad_x ? s.take(P * R * gemm::padded(kp) * 2) : 0;
+        gt = a.grad_w ? s.take(P * kp * Rp * 2) : 0;
+        if (a.grad_bias) {
+            const int64_t rows = bias_rows<P>(gkind, R);
+            pbias = s.take((rows * kp + rowsum::scratch_floats(rows, kp)) * 4);
+            bias_acc = s.take((a.N + R - 1) / R * K * 4);
+        }
+        px = a.grad_x ? s.take(xsplits * R * C * 4) : 0;
+        pw = a.grad_w ? s.take(wsplits * K * C * 4) : 0;
+        bytes = s.bytes;
+    }
+};
+
+#define TRY(expr)                          \
+    do {                                   \
+        const hipError_t e_ = (expr);      \
+        if (e_ != hipSuccess) return e_;   \
+    } while (0)
+
+template <int P>
+hipError_t run(lattice_dense *D, const LossArgs &a) {
+    const Plan<P> p(D, a);
+    char *ws = reinterpret_cast<char *>(D->ws);
+    hipStream_t st = D->stream;
+    auto f = [&](int64_t at) { return reinterpret_cast<float *>(ws + at); };
+    auto h = [&](int64_t at) { return reinterpret_cast<uint16_t *>(ws + at); };
+    auto ints = [&](int64_t at) { return reinterpret_cast<int32_t *>(ws + at); };
+    const int C = a.C, K = a.K;
+    const int64_t Cp = gemm::padded(C);
+    const int esz = a.bf16 ? 2 : 4;
+    constexpr int BF = P == 1;
+
+    hipLaunchKernelGGL(k_count, dim3(kCounts), dim3(256), 0, st, a.target, a.N, K, a.ignore, ints(p.count), D->status);
+    hipLaunchKernelGGL(k_bias, dim3((unsigned)(p.Kpad / 256)), dim3(256), 0, st, a.bias, K, (int)p.Kpad, f(p.bias));
+    TRY(hipGetLastError());
+    gemm::Operand W = {reinterpret_cast<const uint16_t *>(a.w), a.w_stride, 0, 0, K};
+    if (p.own_w || a.grad_x) {
+        const planes::Source s = {a.w, a.w_stride, 0, K, C, nullptr, nullptr};
+        TRY(planes::launch<P>(st, a.bf16, s, 1, p.own_w ? h(p.wp) : nullptr, a.grad_x ? h(p.wt) : nullptr));
+        if (p.own_w) W = planes::operand(h(p.wp), K, C, P);
+    }
+    int64_t parts = 0;
+    int piece = 0;
+    for (int64_t r0 = 0; r0 < a.N; r0 += p.R, ++piece) {
+        const int n = (int)(a.N - r0 < p.R ? a.N - r0 : p.R);
+        const int64_t np = gemm::padded(n);
+        const char *x = reinterpret_cast<const char *>(a.x) + r0 * a.x_stride * esz;
+        hipLaunchKernelGGL(k_rows, dim3((n + 255) / 256), dim3(256), 0, st, a.target + r0, n, K, a.ignore,
+                           ints(p.count), a.mean, ints(p.label), f(p.factor));
+        TRY(hipGetLastError());
+        gemm::Operand X = {reinterpret_cast<const uint16_t *>(x), a.x_stride, 0, 0, n};
+        if (p.own_x || a.grad_w) {
+            const planes::Source s = {x, a.x_stride, 0, n, C, ints(p.label), nullptr};
+            TRY(planes::launch<P>(st, a.bf16, s, 1, p.own_x ? h(p.xp) : nullptr, a.grad_w ? h(p.xt) : nullptr));
+            if (p.own_x) X = planes::operand(h(p.xp), n, C, P);
+        }
+        const Stats<P> stats = {f(p.bias), ints(p.label), n, reinterpret_cast<float2 *>(ws + p.stats), f(p.picked)};
+        TRY((product<P>(st, p.fkind, W, X, Cp, Cp, stats)));
+        const int tiles = (K + tile_m<P>(p.fkind) - 1) / tile_m<P>(p.fkind);
+        const unsigned lse_grid = (n + 63) / 64;
+        hipLaunchKernelGGL(k_lse, dim3(lse_grid), dim3(256), 0, st, stats.stats, tiles, n, f(p.picked), ints(p.label),
+                           f(p.lse), a.rows ? a.rows + r0 : nullptr, reinterpret_cast<double *>(ws + p.part) + parts);
+        TRY(hipGetLastError());
+        parts += lse_grid;
+        if (!a.any_grad()) continue;
+        for (int64_t k0 = 0; k0 < K; k0 += p.KP) {
+            const int kn = (int)(K - k0 < p.KP ? K - k0 : p.KP);
+            const int64_t ldg = gemm::padded(kn);
+            gemm::Operand Wk = W;
+            Wk.p += k0 * W.ld;
+            Wk.rows = kn;
+            const Grad<P> grad = {f(p.bias) + k0, {ints(p.label), f(p.lse), n}, (int)k0, kn, (int)ldg, np,
+                                  a.grad_x ? h(p.g) : nullptr, a.grad_w ? h(p.gt) : nullptr,
+                                  a.grad_bias ? f(p.pbias) : nullptr, f(p.factor)};
+            TRY((product<P>(st, p.gkind, Wk, X, Cp, Cp, grad)));
+            if (a.grad_bias) {
+                const int64_t rows = bias_rows<P>(p.gkind, n);
+                TRY(rowsum::sum(st, f(p.pbias), rows, kn, f(p.pbias) + rows * kn,
+                                f(p.bias_acc) + (int64_t)piece * K + k0));
+            }
+            if (a.grad_x) {
+                gemm::Operand Wt = planes::operand(h(p.wt), C, K, P);
+                Wt.p += k0;
+                TRY((product<P>(st, p.xkind, planes::operand(h(p.g), n, kn, P), Wt, ldg, p.xpart,
+                                Part<P>{f(p.px), n, C, k0 > 0})));
+            }
+            if (a.grad_w) {
+                float *part = f(p.pw) + k0 * C * p.wsplits;
+                TRY((product<P>(st, p.wkind, planes::operand(h(p.gt), kn, n, P), planes::operand(h(p.xt), C, n, P), np,
+                                p.wpart, Part<P>{part, kn, C, r0 > 0})));
+                if (r0 + p.R >= a.N) {
+                    const int64_t v = (int64_t)kn * C;
+                    // a later piece of rows is no longer than the first, and has no more parts
+                    const int splits = (int)(piece > 0 ? p.wsplits : (np + p.wpart - 1) / p.wpart);
+                    hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, part,
+                                       splits, v, f(p.factor), reinterpret_cast<char *>(a.grad_w) + k0 * C * esz);
+                    TRY(hipGetLastError());
+                }
+            }
+        }
+        if (a.grad_x) {
+            const int64_t v = (int64_t)n * C;
+            hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, f(p.px),
+                               (int)p.xsplits, v, f(p.factor),
+                               reinterpret_cast<char *>(a.grad_x) + r0 * C * esz);
+            TRY(hipGetLastError());
+        }
+    }
+    hipLaunchKernelGGL(k_total, dim3(1), dim3(256), 0, st, reinterpret_cast<const double *>(ws + p.part), parts,
+                       ints(p.count), a.mean, a.loss);
+    TRY(hipGetLastError());
+    if (a.grad_bias) TRY(rowsum::sum(st, f(p.bias_acc), piece, K, nullptr, a.grad_bias));
+    if (a.N == 0 && a.grad_w) {
+        const int64_t v = (int64_t)K * C;
+        hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, nullptr, 0, v, nullptr,
+                           a.grad_w);
+        TRY(hipGetLastError());
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+int64_t loss_scratch(const lattice_dense *D, const LossArgs &a) {
+    return a.bf16 ? Plan<1>(D, a).bytes : Plan<3>(D, a).bytes;
+}
+
+hipError_t launch_loss(lattice_dense *D, const LossArgs &a) { return a.bf16 ? run<1>(D, a) : run<3>(D, a); }

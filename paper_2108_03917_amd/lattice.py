@@ -33,6 +33,8 @@ EXPORTS = (
     "lattice_splat_backward", "lattice_conv_backward", "lattice_downsample", "lattice_upsample",
     "lattice_distribute_pointnet", "lattice_conv_backward_noalloc", "lattice_downsample_backward",
     "lattice_upsample_backward", "lattice_deform_slice_backward", "lattice_distribute_pointnet_backward",
+    "lattice_dense_create", "lattice_dense_destroy", "lattice_dense_get_status", "lattice_dense_last_error",
+    "lattice_layer_norm", "lattice_layer_norm_backward", "lattice_linear_cross_entropy", "lattice_orthogonalize",
 )
 
 _lib = None
@@ -54,6 +56,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                            "(python -m paper_2108_03917_amd._build)")
     lib = ctypes.CDLL(path)
     P, I64, I, D, St = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_double, ctypes.c_int
+    F = ctypes.c_float
     sig = {
         "lattice_create": (St, [I, P, D, I64, I64, P, ctypes.POINTER(P)]),
         "lattice_destroy": (None, [P]),
@@ -87,6 +90,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "lattice_dim": (I, [P]),
         "lattice_status_string": (ctypes.c_char_p, [I]),
         "lattice_last_error": (ctypes.c_char_p, [P]),
+        "lattice_dense_create": (St, [P, ctypes.POINTER(P)]),
+        "lattice_dense_destroy": (None, [P]),
+        "lattice_dense_get_status": (St, [P]),
+        "lattice_dense_last_error": (ctypes.c_char_p, [P]),
+        "lattice_layer_norm": (St, [P, P, P, I, I64, I64, I, P, P, F, P, I, I64, P, P]),
+        "lattice_layer_norm_backward": (St, [P, P, P, I, I64, P, I, I64, I64, I, P, P, P, P, I64, P, P]),
+        "lattice_linear_cross_entropy": (St, [P, I, P, I64, I64, I, P, I64, I, P, P, I64, I, P, P, P, P, P]),
+        "lattice_orthogonalize": (St, [P, P, I, I64, I, I, I64, I64, I, P, F, P, I]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

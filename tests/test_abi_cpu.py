@@ -156,3 +156,17 @@ def test_distribute_binding_passes_the_output_storage(monkeypatch):
     assert list(a[7]) == [3, 16, 32] and abs(a[8].value - 1e-3) < 1e-9
     L.distribute_pointnet(torch.zeros((10, 3)), None, params, groups=[1, 4, 8])
     assert list(calls[-1][7]) == [1, 4, 8]
+
+
+def test_null_dense_handle_is_rejected():
+    lib = B.load_library()
+    assert lib.lattice_dense_create(None, None) == B.E_ARG
+    assert lib.lattice_dense_get_status(None) == B.E_ARG
+    assert lib.lattice_dense_last_error(None).decode() == "null handle"
+    assert lib.lattice_layer_norm(None, None, None, 0, 8, 1, 8, None, None, 0.0, None, 0, 8, None, None) == B.E_ARG
+    assert lib.lattice_layer_norm_backward(None, None, None, 0, 8, None, 0, 8, 1, 8, None, None, None, None, 8, None,
+                                           None) == B.E_ARG
+    assert lib.lattice_linear_cross_entropy(None, 0, None, 8, 1, 8, None, 8, 2, None, None, -100, 1, None, None, None,
+                                            None, None) == B.E_ARG
+    assert lib.lattice_orthogonalize(None, None, 0, 1, 8, 8, 64, 8, 5, None, 0.0, None, 0) == B.E_ARG
+    lib.lattice_dense_destroy(None)

@@ -1,0 +1,659 @@
+"""The dense operators of a training step (layer normalisation, classifier loss,
+orthogonalised update) against plain 64-bit implementations.
+
+Tolerances, fixed from the arithmetic.  fp32 results: REL_F32 of each element's
+sum of |terms|, terms being what its formula adds up (as for the lattice
+operators).  A result stored as bf16 may be off by half a unit in the last
+place more: 2^-8 of itself (8 significant bits, spacing 2^-7 above a power of
+two).  The loss's gradients of bf16 operands are products of an intermediate
+that is rounded to bf16: 2^-8 of each of their terms more.
+The orthogonalised update is 3 products a step, each value off by 2^-22 at most
+(24 bits and fp32 sums), and a step stretches relative errors by at most 5 for
+the well-conditioned matrices used here: 2e-5 of the norm for five steps; in 16
+bits the stored result's rounding rules (2^-16 takes the place of 2^-22): 2^-8.
+"""
+import math
+
+import pytest
+import torch
+
+from datagen.clouds import random_cloud
+from tests.gpu_util import REL_F32
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+HALF = 2.0 ** -8     # half a unit in the last place of bf16, relative
+T = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+@pytest.fixture(scope="module")
+def ops(_gpu):
+    from paper_2108_03917_amd import Dense
+
+    d = Dense()
+    yield d
+    torch.cuda.synchronize()
+    d.close()
+
+
+def rand(seed, *shape, dtype="f32"):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g, device=DEV).to(T[dtype])
+
+
+def check(got, ref, scale, rel, what):
+    """|got - ref| <= rel * scale, elementwise; NaN and infinities in the same places."""
+    got, ref, scale = got.double(), ref.double(), torch.as_tensor(scale, device=got.device).double()
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)), what
+    fine = torch.isfinite(ref)
+    assert torch.equal(torch.isfinite(got), fine), what
+    err = torch.where(fine, (got - ref).abs(), 0.0)
+    bound = rel * torch.where(fine, scale.expand_as(ref), 0.0) + 1e-30
+    worst = (err / bound).max().item() if err.numel() else 0.0
+    assert worst <= 1.0, f"{what}: error {worst:.3g} times the tolerance"
+
+
+# -- layer normalisation -------------------------------------------------------
+
+def norm_ref(x, gamma, beta, eps, g=None):
+    x = x.double()
+    C = x.shape[1]
+    ga = torch.ones(C, device=x.device).double() if gamma is None else gamma.double()
+    be = torch.zeros(C, device=x.device).double() if beta is None else beta.double()
+    mu = x.mean(1, keepdim=True)
+    r = ((x - mu) ** 2).mean(1, keepdim=True).add(eps).rsqrt()
+    h = (x - mu) * r
+    hs = h.abs() + r * (x.abs() + x.abs().mean(1, keepdim=True))    # what h is a difference of
+    y, ys = ga * h + be, ga.abs() * hs + be.abs()
+    if g is None:
+        return (y, ys), mu[:, 0], r[:, 0]
+    g = g.double()
+    u = g * ga
+    gx = r * (u - u.mean(1, keepdim=True) - h * (u * h).mean(1, keepdim=True))
+    gxs = r * (u.abs() + u.abs().mean(1, keepdim=True) + hs * (u.abs() * hs).mean(1, keepdim=True))
+    return (y, ys), (gx, gxs), ((g * h).sum(0), (g.abs() * hs).sum(0)), (g.sum(0), g.abs().sum(0))
+
+
+NORM = [(1, 1), (1, 64), (3, 5), (2, 8), (65, 63), (300, 100), (7, 257), (130, 512), (33, 1000), (5, 2050), (4, 8192),
+        (3, 16384), (2, 20001)]
+
+
+@pytest.mark.parametrize("xt,yt", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("rows,C", NORM)
+def test_layer_norm(ops, rows, C, xt, yt):
+    x = rand(1, rows, C, dtype=xt) * 2 + 0.5
+    gamma, beta, g = 1 + rand(2, C) * 0.3, rand(3, C), rand(4, rows, C, dtype=yt)
+    y, mean, rstd = ops.layer_norm(x, gamma, beta, out_dtype=yt, want_stats=True)
+    gx, gg, gb = ops.layer_norm_backward(g, x, mean, rstd, gamma)
+    ry, rgx, rgg, rgb = norm_ref(x, gamma, beta, 1e-5, g)
+    check(y, *ry, REL_F32 + (HALF if yt == "bf16" else 0), "y")
+    check(gx, *rgx, REL_F32 + (HALF if xt == "bf16" else 0), "grad_x")
+    check(gg, *rgg, REL_F32, "grad_gamma")
+    check(gb, *rgb, REL_F32, "grad_beta")
+    assert y.dtype == T[yt] and gx.dtype == T[xt]
+
+
+def test_layer_norm_without_gain_and_shift(ops):
+    x, g = rand(1, 50, 96), rand(2, 50, 96)
+    y, mean, rstd = ops.layer_norm(x, eps=1e-3, want_stats=True)
+    ry, rgx, rgg, _ = norm_ref(x, None, None, 1e-3, g)
+    check(y, *ry, REL_F32, "y")
+    gx, gg, gb = ops.layer_norm_backward(g, x, mean, rstd)
+    check(gx, *rgx, REL_F32, "grad_x")
+    check(gg, *rgg, REL_F32, "grad_gamma")
+    gx2, none, none2 = ops.layer_norm_backward(g, x, mean, rstd, want_params=False)
+    assert none is None and none2 is None and torch.equal(gx, gx2)
+    none, gg2, _ = ops.layer_norm_backward(g, x, mean, rstd, want_input=False)
+    assert none is None and torch.equal(gg, gg2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,offset,stride", [(100, 0, 131), (100, 3, 107), (64, 1, 65), (520, 7, 1041)])
+def test_layer_norm_strided_rows(ops, dtype, C, offset, stride):
+    """Rows that start at any element, with others' values between them."""
+    rows = 37
+    flat = rand(1, rows * stride + offset, dtype=dtype)
+    x = flat[offset:].as_strided((rows, C), (stride, 1))
+    out = torch.full((rows, stride), 7.0, device=DEV, dtype=T[dtype])
+    gamma, beta, g = rand(2, C), rand(3, C), rand(4, rows, C + 1, dtype=dtype)[:, 1:]
+    y, mean, rstd = ops.layer_norm(x, gamma, beta, out=out[:, :C], want_stats=True)
+    ry, rgx, rgg, _ = norm_ref(x, gamma, beta, 1e-5, g)
+    check(y, *ry, REL_F32 + (HALF if dtype == "bf16" else 0), "y")
+    assert torch.all(out[:, C:] == 7.0)
+    gx, gg, _ = ops.layer_norm_backward(g, x, mean, rstd, gamma)
+    check(gx, *rgx, REL_F32 + (HALF if dtype == "bf16" else 0), "grad_x")
+    check(gg, *rgg, REL_F32, "grad_gamma")
+
+
+def test_layer_norm_in_place_and_far_from_zero(ops):
+    x = rand(1, 40, 64) + 1000.0
+    keep = x.clone()
+    ops.layer_norm(x, out=x)
+    ry, _, _ = norm_ref(keep, None, None, 1e-5)
+    check(x, *ry, REL_F32, "in place")
+    g = rand(2, 40, 64)
+    y, mean, rstd = ops.layer_norm(keep, want_stats=True)
+    expect, _, _ = ops.layer_norm_backward(g, keep, mean, rstd)
+    got, _, _ = ops.layer_norm_backward(g, keep, mean, rstd, grad_x=g)
+    assert got is g and torch.equal(g, expect)
+
+
+def test_layer_norm_a_row_of_equal_or_infinite_values(ops):
+    x = rand(1, 6, 80)
+    x[1] = 3.0                       # no variance: the shift alone
+    x[2, 5] = float("inf")
+    x[3, 7] = float("nan")
+    beta = rand(2, 80)
+    y = ops.layer_norm(x, None, beta)
+    assert torch.equal(y[1], beta)
+    assert torch.isnan(y[2]).all() and torch.isnan(y[3]).all()
+    keep = [0, 1, 4, 5]
+    ry, _, _ = norm_ref(x[keep], None, beta, 1e-5)
+    check(y[keep], *ry, REL_F32, "the other rows")
+
+
+def test_layer_norm_no_rows(ops):
+    x = torch.empty((0, 32), device=DEV)
+    y, mean, rstd = ops.layer_norm(x, want_stats=True)
+    assert y.shape == (0, 32) and mean.shape == (0,)
+    gx, gg, gb = ops.layer_norm_backward(x, x, mean, rstd)
+    assert gx.shape == (0, 32) and torch.all(gg == 0) and torch.all(gb == 0)
+
+
+@pytest.mark.parametrize("C", [16, 300, 17000])
+def test_layer_norm_of_a_lattice(ops, C):
+    """Rows are the vertices: V is read on the device, rows past it are left."""
+    from paper_2108_03917_amd import Lattice
+
+    w = random_cloud(200, 3, seed=5, extent=1.0, C=1)
+    L = Lattice(3, 0.3, max_points=200)
+    L.splat(torch.from_numpy(w.pos).to(DEV), None, want_weight=False)
+    rows = L.max_vertices(200)
+    x, g = rand(1, rows, C), rand(2, rows, C)
+    out = torch.full((rows, C), 7.0, device=DEV)
+    y, mean, rstd = ops.layer_norm(x, lattice=L, out=out, want_stats=True)
+    left = torch.full((rows, C), 7.0, device=DEV)
+    gx, gg, gb = ops.layer_norm_backward(g, x, mean, rstd, lattice=L, grad_x=left)
+    V = L.num_vertices()
+    assert 0 < V < rows
+    ry, rgx, rgg, rgb = norm_ref(x[:V], None, None, 1e-5, g[:V])
+    check(y[:V], *ry, REL_F32, "y")
+    check(gx[:V], *rgx, REL_F32, "grad_x")
+    check(gg, *rgg, REL_F32, "grad_gamma")
+    check(gb, *rgb, REL_F32, "grad_beta")
+    assert torch.all(out[V:] == 7.0) and torch.all(left[V:] == 7.0)
+    L.splat(torch.empty((0, 3), device=DEV), None, want_weight=False)   # no vertex at all
+    _, gg, _ = ops.layer_norm_backward(g, x, mean, rstd, lattice=L)
+    assert torch.all(gg == 0)
+    L.close()
+
+
+def test_layer_norm_gradient_against_differences(ops):
+    rows, C, d = 4, 24, 1e-2
+    x, g, gamma, beta = rand(1, rows, C), rand(2, rows, C), 1 + 0.2 * rand(3, C), rand(4, C)
+    _, mean, rstd = ops.layer_norm(x, gamma, beta, want_stats=True)
+    gx, gg, gb = ops.layer_norm_backward(g, x, mean, rstd, gamma)
+
+    def loss(x, gamma, beta):
+        return (ops.layer_norm(x, gamma, beta).double() * g.double()).sum().item()
+
+    # a difference quotient is off by d^2 times the third derivative (of order
+    # |g| here) and by the results' 2^-23 |terms| / d
+    tol = 20 * d * d + 2.0 ** -23 * rows * C * 8 / d
+    for (i, j) in [(0, 0), (1, 7), (3, 23)]:
+        e = torch.zeros_like(x)
+        e[i, j] = d
+        assert abs((loss(x + e, gamma, beta) - loss(x - e, gamma, beta)) / (2 * d) - gx[i, j].item()) < tol
+    for j in (0, 11):
+        e = torch.zeros_like(gamma)
+        e[j] = d
+        assert abs((loss(x, gamma + e, beta) - loss(x, gamma - e, beta)) / (2 * d) - gg[j].item()) < tol
+        assert abs((loss(x, gamma, beta + e) - loss(x, gamma, beta - e)) / (2 * d) - gb[j].item()) < tol
+
+
+# -- classifier loss -----------------------------------------------------------
+
+IGN = -100
+
+
+def loss_ref(x, w, target, bias, mean):
+    """(value, scale) of the loss, row losses and gradients, in 64 bits."""
+    x, w = x.double(), w.double()
+    K = w.shape[0]
+    on = (target >= 0) & (target < K)
+    b = torch.zeros(K, device=x.device).double() if bias is None else bias.double()
+    xs = torch.where(on[:, None], x, 0.0)
+    z = xs @ w.t() + b
+    zs = (xs.abs() @ w.abs().t() + torch.where(torch.isfinite(b), b.abs(), 0.0)).amax(1, keepdim=True)
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    t = torch.where(on, target, 0)[:, None]
+    rows = torch.where(on, (lse - z.gather(1, t))[:, 0], 0.0)
+    s = (1.0 / max(1, int(on.sum()))) if mean else 1.0
+    p = torch.exp(z - lse)
+    one = torch.zeros_like(p).scatter_(1, t, 1.0)
+    G = torch.where(on[:, None], s * (p - one), 0.0)
+    Gs = torch.where(on[:, None], s * (p * (1 + zs) + one), 0.0)
+    return {"loss": (rows.sum() * s, ((lse.abs() + 2 * zs)[:, 0] * on).sum() * s),
+            "rows": (rows, (lse.abs() + 2 * zs)[:, 0]),
+            "grad_x": (G @ w, Gs @ w.abs(), G.abs() @ w.abs()),
+            "grad_w": (G.t() @ xs, Gs.t() @ xs.abs(), G.abs().t() @ xs.abs()),
+            "grad_bias": (G.sum(0), Gs.sum(0))}
+
+
+def check_loss(got, ref, dtype, what=""):
+    loss, rows, gx, gw, gb = got
+    check(loss, *ref["loss"], REL_F32, what + "loss")
+    if rows is not None:
+        check(rows, *ref["rows"], REL_F32, what + "rows")
+    for name, g in (("grad_x", gx), ("grad_w", gw)):
+        if g is None:
+            continue
+        v, scale, terms = ref[name]
+        # bf16: the rounding of the intermediate and of the result
+        if dtype == "bf16":
+            scale = scale + (HALF / REL_F32) * 2 * terms
+        check(g, v, scale, REL_F32, what + name)
+    if gb is not None:
+        check(gb, *ref["grad_bias"], REL_F32, what + "grad_bias")
+
+
+def labels(seed, N, K, share=0.1):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    t = torch.randint(0, K, (N,), generator=g, device=DEV)
+    t[torch.rand(N, generator=g, device=DEV) < share] = IGN
+    return t
+
+
+LOSS = [(1, 1, 1), (1, 64, 20), (2, 3, 2), (17, 16, 16), (64, 32, 33), (129, 64, 50), (1000, 100, 7), (333, 128, 64),
+        (90, 256, 32), (70, 65, 65), (65, 48, 128), (300, 130, 129), (64, 200, 1000), (1, 512, 5000), (513, 33, 777)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C,K", LOSS)
+def test_loss(ops, N, C, K, dtype):
+    x, w = rand(1, N, C, dtype=dtype), (rand(2, K, C) * 2 / math.sqrt(C)).to(T[dtype])
+    bias, t = rand(3, K), labels(4, N, K)
+    got = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    check_loss(got, loss_ref(x, w, t, bias, True), dtype)
+    assert got[2].dtype == T[dtype] and got[3].dtype == T[dtype] and got[4].dtype == torch.float32
+    # the loss alone, and without the row losses, is the same number
+    assert torch.equal(ops.linear_cross_entropy(x, w, t, bias), got[0])
+    # and two calls give the same bits
+    again = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C,K", [(200, 64, 20), (200, 96, 400)])
+def test_loss_sum_without_bias_and_parts(ops, N, C, K, dtype):
+    x, w, t = rand(1, N, C, dtype=dtype), rand(2, K, C, dtype=dtype) * 0.1, labels(3, N, K)
+    ref = loss_ref(x, w, t, None, False)
+    loss, gx, gw, gb = ops.linear_cross_entropy(x, w, t, reduction="sum", want_grad=True)
+    assert gb is None
+    check_loss((loss, None, gx, gw, None), ref, dtype)
+    only = [ops.linear_cross_entropy(x, w, t, reduction="sum", want_grad=True, want_input=i == 0, want_weight=i == 1,
+                                     want_bias=i == 2) for i in range(3)]
+    assert torch.equal(only[0][1], gx) and only[0][2] is None and only[0][3] is None
+    assert only[1][1] is None and torch.equal(only[1][2], gw)
+    check_loss((loss, None, None, None, only[2][3]), ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,K", [(64, 20), (64, 300), (61, 19)])
+def test_loss_rows_without_a_label_reach_nothing(ops, C, K, dtype):
+    N = 150
+    x, w, t = rand(1, N, C, dtype=dtype), rand(2, K, C, dtype=dtype) * 0.2, labels(3, N, K, 0.5)
+    bias = rand(4, K)
+    clean = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    off = t == IGN
+    dirty = x.clone()
+    dirty[off] = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], device=DEV).repeat(
+        N * C // 4 + 1)[: N * C].reshape(N, C).to(x.dtype)[off]
+    got = ops.linear_cross_entropy(dirty, w, t, bias, want_rows=True, want_grad=True)
+    assert all(torch.equal(a, b) for a, b in zip(clean, got))
+    assert torch.all(got[1][off] == 0) and torch.all(got[2][off] == 0)
+    check_loss(got, loss_ref(x, w, t, bias, True), dtype)
+    # no row with a label at all, and no row
+    none = torch.full_like(t, IGN)
+    for n in (N, 0):
+        loss, rows, gx, gw, gb = ops.linear_cross_entropy(dirty[:n], w, none[:n], bias, want_rows=True, want_grad=True)
+        assert loss.item() == 0 and all(torch.all(v == 0) for v in (rows, gx, gw, gb))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,K", [(64, 40), (64, 600)])
+def test_loss_masked_classes(ops, C, K, dtype):
+    """Classes taken out by a bias of -inf, or of the type's lowest value."""
+    N = 100
+    x, w = rand(1, N, C, dtype=dtype), rand(2, K, C, dtype=dtype) * 0.2
+    out = torch.arange(K, device=DEV) % 3 != 0
+    out[K // 2:] = True                  # whole tiles without a class
+    t = labels(3, N, (K // 2 + 2) // 3) * 3
+    t[t < 0] = IGN
+    results = []
+    for low in (-float("inf"), torch.finfo(torch.float32).min):
+        bias = torch.where(out, low, rand(4, K))
+        got = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+        check_loss(got, loss_ref(x, w, t, torch.where(out, -float("inf"), bias), True), dtype)
+        assert torch.all(got[3][out] == 0) and torch.all(got[4][out] == 0)
+        results.append(got)
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    # a label on a class that is out has no share: an infinite loss
+    t2 = t.clone()
+    t2[0] = 1
+    loss, rows = ops.linear_cross_entropy(x, w, t2, torch.where(out, -float("inf"), 0.0), want_rows=True)
+    assert rows[0].item() == float("inf") and loss.item() == float("inf")
+    assert torch.isfinite(rows[1:]).all()
+
+
+@pytest.mark.parametrize("K", [21, 700])
+def test_loss_large_logits(ops, K):
+    """Logits of thousands: the exponentials are of differences."""
+    N, C = 64, 32
+    x, w, t = rand(1, N, C) * 100, rand(2, K, C) * 10, labels(3, N, K)
+    got = ops.linear_cross_entropy(x, w, t, want_rows=True, want_grad=True)
+    ref = loss_ref(x, w, t, None, True)
+    check(got[0], *ref["loss"], REL_F32, "loss")
+    check(got[1], *ref["rows"], REL_F32, "rows")
+    assert all(torch.isfinite(g).all() for g in got[2:4])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,K,xs,ws,off", [(64, 20, 80, 72, 0), (64, 20, 67, 71, 3), (64, 300, 128, 72, 0),
+                                           (64, 300, 67, 71, 3), (50, 11, 51, 53, 1)])
+def test_loss_strided_operands(ops, C, K, xs, ws, off, dtype):
+    N = 83
+    x = rand(1, N * xs + off, dtype=dtype)[off:].as_strided((N, C), (xs, 1))
+    w = (rand(2, K * ws + off, dtype=dtype) * 0.2)[off:].as_strided((K, C), (ws, 1))
+    t, bias = labels(3, N, K), rand(4, K)
+    got = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    check_loss(got, loss_ref(x, w, t, bias, True), dtype)
+
+
+@pytest.mark.parametrize("K", [9, 300])
+def test_loss_reports_labels_that_are_no_class(ops, K):
+    N, C = 40, 16
+    x, w, t = rand(1, N, C), rand(2, K, C), labels(3, N, K)
+    assert ops.status() == 0
+    bad = t.clone()
+    bad[3], bad[5] = K, -1
+    good = t.clone()
+    good[3] = good[5] = IGN
+    got = ops.linear_cross_entropy(x, w, bad, want_rows=True, want_grad=True)
+    from paper_2108_03917_amd.lattice import E_RANGE
+
+    assert ops.status() == E_RANGE and ops.status() == 0
+    want = ops.linear_cross_entropy(x, w, good, want_rows=True, want_grad=True)
+    assert all(torch.equal(a, b) for a, b in zip(got[:4], want[:4])) and ops.status() == 0
+    # another ignore_index
+    other = torch.where(good == IGN, 7, good)
+    got = ops.linear_cross_entropy(x, w, other, ignore_index=7)
+    ref = loss_ref(x, w, torch.where(other == 7, IGN, other), None, True)
+    check(got, *ref["loss"], REL_F32, "ignore_index")
+
+
+@pytest.mark.parametrize("N,C,K,dtype", [(70001, 16, 300, "f32"), (66000, 8, 5000, "bf16"), (131073, 20, 21, "bf16"),
+                                         (131073, 24, 50, "f32")])
+def test_loss_in_pieces(ops, N, C, K, dtype):
+    """More rows, and more classes at so many rows, than go into one piece."""
+    x, w, t = rand(1, N, C, dtype=dtype), rand(2, K, C, dtype=dtype) * 0.3, labels(3, N, K)
+    bias = rand(4, K)
+    got = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    check_loss(got, loss_ref(x, w, t, bias, True), dtype)
+
+
+@pytest.mark.parametrize("K", [6, 200])
+def test_loss_gradient_against_differences(ops, K):
+    N, C, d = 5, 12, 1e-2
+    x, w, b, t = rand(1, N, C), rand(2, K, C) * 0.3, rand(3, K), labels(4, N, K, 0.2)
+    _, gx, gw, gb = ops.linear_cross_entropy(x, w, t, b, reduction="sum", want_grad=True)
+
+    def loss(x, w, b):
+        return ops.linear_cross_entropy(x, w, t, b, reduction="sum").double().item()
+
+    # d^2 times third derivatives of order |x|^3 N, and 2^-23 |loss| / d
+    tol = 30 * d * d + 2.0 ** -23 * 10 * N / d
+    for (i, j) in [(0, 0), (2, 5), (4, 11)]:
+        e = torch.zeros_like(x)
+        e[i, j] = d
+        assert abs((loss(x + e, w, b) - loss(x - e, w, b)) / (2 * d) - gx[i, j].item()) < tol
+    for k in (0, K - 1, int(t.max().item())):
+        e, f = torch.zeros_like(w), torch.zeros_like(b)
+        e[k, 3] = d
+        f[k] = d
+        assert abs((loss(x, w + e, b) - loss(x, w - e, b)) / (2 * d) - gw[k, 3].item()) < tol
+        assert abs((loss(x, w, b + f) - loss(x, w, b - f)) / (2 * d) - gb[k].item()) < tol
+
+
+# -- orthogonalised update -----------------------------------------------------
+
+NS = (3.4445, -4.7750, 2.0315)
+
+
+def update_ref(g, steps=5, coef=NS, eps=1e-7):
+    a, b, c = coef
+    x = g.double()
+    tall = g.shape[-2] > g.shape[-1]
+    x = x.mT if tall else x
+    x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + eps)
+    for _ in range(steps):
+        s = x @ x.mT
+        x = a * x + (b * s + c * (s @ s)) @ x
+    return x.mT if tall else x
+
+
+def check_update(got, ref, what=""):
+    assert got.shape == ref.shape
+    tol = 2.0 ** -8 if got.dtype == torch.bfloat16 else 2e-5
+    err = (got.double() - ref).norm(dim=(-2, -1))
+    assert torch.all(err <= tol * ref.norm(dim=(-2, -1)) + 1e-30), (what, (err / ref.norm(dim=(-2, -1))).max().item())
+
+
+UPDATE = [(1, 1), (1, 70), (70, 1), (2, 3), (16, 16), (33, 100), (64, 576), (130, 64), (64, 200), (128, 300), (129, 400),
+          (500, 150), (260, 700)]
+
+
+@pytest.mark.parametrize("gt,ot", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("m,n", UPDATE)
+def test_update(ops, m, n, gt, ot):
+    g = rand(1, m, n, dtype=gt)
+    got = ops.orthogonalize(g, out_dtype=ot)
+    assert got.dtype == T[ot]
+    check_update(got, update_ref(g))
+    assert torch.equal(got, ops.orthogonalize(g, out_dtype=ot))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,m,n", [(3, 20, 50), (5, 64, 576), (2, 200, 90), (4, 128, 260), (0, 8, 8)])
+def test_update_of_a_batch(ops, batch, m, n, dtype):
+    g = rand(1, batch, m, n, dtype=dtype)
+    got = ops.orthogonalize(g)
+    if batch:
+        check_update(got, update_ref(g))
+        # each as alone
+        assert torch.equal(got[batch - 1], ops.orthogonalize(g[batch - 1]))
+    assert got.shape == g.shape
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,rs", [(40, 90, 101), (90, 40, 47), (150, 333, 340)])
+def test_update_strided(ops, m, n, rs, dtype):
+    flat = rand(1, 3 * (m * rs + 5) + 1, dtype=dtype)
+    g = flat[1:].as_strided((3, m, n), (m * rs + 5, rs, 1))
+    check_update(ops.orthogonalize(g), update_ref(g))
+    # one matrix for all of a batch
+    same = g[:1].expand(3, m, n)
+    out = ops.orthogonalize(same)
+    assert torch.equal(out[0], out[2])
+
+
+@pytest.mark.parametrize("m,n", [(64, 144), (200, 250)])
+def test_update_scales_steps_and_coefficients(ops, m, n):
+    g = rand(1, m, n)
+    for scale in (1e-30, 1e30, 3e-6):
+        check_update(ops.orthogonalize(g * scale, eps=0.0), update_ref(g * scale, eps=0.0), scale)
+    for steps in (0, 1, 2, 3):
+        check_update(ops.orthogonalize(g, steps=steps), update_ref(g, steps), steps)
+    cubic = (1.5, -0.5, 0.0)
+    check_update(ops.orthogonalize(g, steps=4, coefficients=cubic), update_ref(g, 4, cubic), "cubic")
+
+
+@pytest.mark.parametrize("m,n", [(30, 64), (150, 170)])
+def test_update_zeros_and_non_finite_matrices_of_a_batch(ops, m, n):
+    g = rand(1, 4, m, n)
+    g[1] = 0
+    g[2, 3, 4] = float("nan")
+    got = ops.orthogonalize(g)
+    assert torch.all(got[1] == 0) and torch.isnan(got[2]).any()
+    for b in (0, 3):
+        check_update(got[b], update_ref(g[b]))
+
+
+def test_update_of_decaying_spectrum(ops):
+    """Singular values over three decades: what a step makes of the smallest is
+    a^5 = 485 times its error, so 485 * 2^-22 of the norm."""
+    u, _ = torch.linalg.qr(rand(1, 96, 96).double())
+    v, _ = torch.linalg.qr(rand(2, 300, 96).double())
+    g = (u * torch.logspace(0, -3, 96, device=DEV).double()) @ v.t()
+    g = g.float()
+    ref = update_ref(g)
+    got = ops.orthogonalize(g).double()
+    assert (got - ref).norm() <= 485 * 2.0 ** -22 * ref.norm()
+
+
+# -- the handle ----------------------------------------------------------------
+
+def test_another_current_stream(ops):
+    """Inputs made on another stream than the handle's, and used there after."""
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        x = rand(1, 4000, 256)
+        for _ in range(5):
+            x = x * 1.0
+        y = ops.layer_norm(x)
+        z = y * 2
+    s.synchronize()
+    ry, _, _ = norm_ref(x, None, None, 1e-5)
+    check(z, 2 * ry[0], 2 * ry[1], REL_F32, "z")
+
+
+def test_graph_replays(ops):
+    """Each operator captured once and replayed between eager work."""
+    from paper_2108_03917_amd import Dense
+
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        own = Dense(s)
+        x, w, t, b = rand(1, 300, 64), rand(2, 20, 64), labels(3, 300, 20), rand(4, 20)
+        big, tb = rand(5, 1000, 64), labels(6, 300, 1000)
+        g = rand(7, 64, 144)
+
+        def all_of():
+            y, mean, rstd = own.layer_norm(x, want_stats=True)
+            r = [y, *own.layer_norm_backward(x, x, mean, rstd)]
+            r += own.linear_cross_entropy(x, w, t, b, want_rows=True, want_grad=True)
+            r += own.linear_cross_entropy(x, big, tb, want_rows=True, want_grad=True)[:4]
+            return r + [own.orthogonalize(g), own.orthogonalize(x)]
+
+        all_of()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            out = all_of()
+        for i in range(4):
+            x.copy_(rand(10 + i, 300, 64))
+            g.copy_(rand(20 + i, 64, 144))
+            graph.replay()
+            s.synchronize()
+            eager = all_of()
+            s.synchronize()
+            assert all(torch.equal(a, c) for a, c in zip(out, eager)), i
+        own.close()
+
+
+def test_refusals(ops):
+    from paper_2108_03917_amd import LatticeError
+
+    x, w, t = rand(1, 10, 8), rand(2, 4, 8), labels(3, 10, 4)
+    g8, mean = rand(4, 8), rand(5, 10)
+    bad = [
+        lambda: ops.layer_norm(x.cpu()),
+        lambda: ops.layer_norm(x.double()),
+        lambda: ops.layer_norm(x[0]),
+        lambda: ops.layer_norm(x.t()),
+        lambda: ops.layer_norm(x, rand(1, 7)),
+        lambda: ops.layer_norm(x, g8.bfloat16()),
+        lambda: ops.layer_norm(x, out=torch.empty((9, 8), device=DEV)),
+        lambda: ops.layer_norm(x.expand(3, 10, 8)[:, 0, :].as_strided((3, 8), (0, 1))),
+        lambda: ops.layer_norm_backward(x, x, mean[:9], mean),
+        lambda: ops.layer_norm_backward(x[:9], x, mean, mean),
+        lambda: ops.layer_norm_backward(x, x, mean, mean, grad_x=x.bfloat16()),
+        lambda: ops.linear_cross_entropy(x, w.bfloat16(), t),
+        lambda: ops.linear_cross_entropy(x, w[:, :7], t),
+        lambda: ops.linear_cross_entropy(x, w, t.int()),
+        lambda: ops.linear_cross_entropy(x, w, t[:9]),
+        lambda: ops.linear_cross_entropy(x, w, t, rand(1, 5)),
+        lambda: ops.linear_cross_entropy(x, w, t, reduction="none"),
+        lambda: ops.orthogonalize(g8),
+        lambda: ops.orthogonalize(x.t()),
+        lambda: ops.orthogonalize(x, out=torch.empty((8, 10), device=DEV)),
+        lambda: ops.orthogonalize(x, coefficients=(1.0, 2.0)),
+    ]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    flat = rand(1, 200)
+    lib = [
+        lambda: ops.layer_norm(x, eps=-1.0),
+        lambda: ops.layer_norm(x, eps=float("nan")),
+        lambda: ops.layer_norm(flat[:80].view(10, 8), out=flat[8:88].view(10, 8)),
+        lambda: ops.layer_norm_backward(flat[:80].view(10, 8), x, mean, mean, grad_x=flat[8:88].view(10, 8)),
+        lambda: ops.layer_norm_backward(x, x, mean, mean, want_input=False, want_params=False),
+        lambda: ops.linear_cross_entropy(x, torch.empty((0, 8), device=DEV), t),
+        lambda: ops.orthogonalize(x, steps=-1),
+        lambda: ops.orthogonalize(x, steps=65),
+        lambda: ops.orthogonalize(x, eps=float("inf")),
+        lambda: ops.orthogonalize(x, coefficients=(1.0, float("nan"), 0.0)),
+        lambda: ops.orthogonalize(torch.empty((0, 8), device=DEV)),
+        lambda: ops.orthogonalize(flat[:80].view(10, 8), out=flat[8:88].view(10, 8)),
+    ]
+    for f in lib:
+        with pytest.raises(LatticeError):
+            f()
+    # nothing was enqueued, and the handle goes on working
+    torch.cuda.synchronize()
+    assert ops.status() == 0
+    ry, _, _ = norm_ref(x, None, None, 1e-5)
+    check(ops.layer_norm(x), *ry, REL_F32, "after refusals")
+
+
+def test_a_lattice_that_cannot_give_the_rows(ops):
+    from paper_2108_03917_amd import Dense, Lattice, LatticeError
+
+    L = Lattice(3, 0.3, max_points=10)
+    x = rand(1, 40, 8)
+    with pytest.raises(LatticeError):      # not splatted
+        ops.layer_norm(x, lattice=L)
+    L.splat(rand(2, 10, 3), None, want_weight=False)
+    with pytest.raises(ValueError):        # fewer rows than it may have vertices
+        ops.layer_norm(x[:3], lattice=L)
+    other = Dense(torch.cuda.Stream())
+    with pytest.raises(LatticeError):      # another stream than the lattice's
+        other.layer_norm(x, lattice=L)
+    other.close()
+    with pytest.raises(ValueError):
+        other.layer_norm(x)
+    L.close()
