@@ -22,7 +22,8 @@ LIB = os.path.join(LIBDIR, "liblattice.so")
 ARCH = "gfx950"
 
 SOURCES = ["lattice.hip", "splat.hip", "neighbors.hip", "conv.hip", "conv_seg.hip", "slice.hip", "deform.hip", "deform_bwd.hip",
-           "backward.hip", "distribute.hip", "dense.hip", "norm.hip", "loss.hip", "update.hip"]
+           "backward.hip", "distribute.hip", "dense.hip", "norm.hip", "loss.hip", "loss_fused.hip",
+           "update.hip"]
 EXTRA = {"splat.hip": ["-ffp-contract=off"]}
 PEAKS_SRC = "peaks.hip"
 PEAKS = os.path.join(LIBDIR, "peaks")

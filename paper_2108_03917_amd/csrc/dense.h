@@ -88,6 +88,11 @@ struct LossArgs {
 int64_t loss_scratch(const lattice_dense *D, const LossArgs &a);
 hipError_t launch_loss(lattice_dense *D, const LossArgs &a);
 
+// loss_fused.hip: few classes and channels
+bool loss_fused_covers(const LossArgs &a);
+int64_t loss_fused_scratch(const lattice_dense *D, const LossArgs &a);
+hipError_t launch_loss_fused(lattice_dense *D, const LossArgs &a);
+
 // update.hip
 struct UpdateArgs {
     const void *g;

@@ -593,7 +593,11 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
 }  // namespace
 
 int64_t loss_scratch(const lattice_dense *D, const LossArgs &a) {
+    if (loss_fused_covers(a)) return loss_fused_scratch(D, a);
     return a.bf16 ? Plan<1>(D, a).bytes : Plan<3>(D, a).bytes;
 }
 
-hipError_t launch_loss(lattice_dense *D, const LossArgs &a) { return a.bf16 ? run<1>(D, a) : run<3>(D, a); }
+hipError_t launch_loss(lattice_dense *D, const LossArgs &a) {
+    if (loss_fused_covers(a)) return launch_loss_fused(D, a);
+    return a.bf16 ? run<1>(D, a) : run<3>(D, a);
+}
