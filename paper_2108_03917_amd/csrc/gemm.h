@@ -8,8 +8,8 @@
 // sums the largest are taken: 1 of 1, 3 of 4, 6 of 9; sums are fp32.
 //
 // A workgroup computes a BM x BN tile.  Operand slices of BK values a row go
-// from memory straight into LDS (16 bytes a lane), one slice ahead of the one
-// that is multiplied, and from there as 16-byte reads into
+// from memory straight into LDS (16 bytes a lane), STAGES - 1 slices ahead of
+// the one that is multiplied, and from there as 16-byte reads into
 // v_mfma_f32_32x32x16_bf16.  16-byte chunks of the rows are XOR-swizzled so
 // that 16 consecutive rows read at one chunk index hit 16 different 16-byte
 // bank groups.
@@ -21,6 +21,9 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <atomic>
+#include <type_traits>
 
 #include "internal.h"
 
@@ -35,10 +38,15 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int kPad = 64;  // rows of operands hold a multiple of this many values
 inline int64_t padded(int64_t k) { return (k + kPad - 1) / kPad * kPad; }
+// Values from row to row of an operand laid out here: a row more than a
+// multiple of 1 KB long is left out of step by 128 bytes, since rows at such
+// distances fall on the same memory channels (a product with rows 128 KB apart
+// took 338 us, see loss.hip, and 278 with this).
+inline int64_t row_length(int64_t k) { return padded(k) % 512 == 0 ? padded(k) + 64 : padded(k); }
 
 // bf16 planes [P][rows][ld] of each of a batch.  ld < kMaxLd: offsets within a
 // tile are 32 bits.
-constexpr int64_t kMaxLd = (int64_t)1 << 23;
+constexpr int64_t kMaxLd = (int64_t)1 << 22;
 struct Operand {
     const uint16_t *p;
     int64_t ld, plane, batch;
@@ -52,31 +60,59 @@ struct Shape {
     bool lower;    // square and symmetric: only tiles with tile_m >= tile_n
 };
 
-template <int BM_, int BN_, int WM_, int WN_, int BK_, int P_>
+template <int BM_, int BN_, int WM_, int WN_, int BK_, int P_, int STAGES_ = 2>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = BK_, P = P_;
     static constexpr int NW = WM * WN, THREADS = 64 * NW;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // 32 x 32 blocks of a wavefront
     static constexpr int CPR = BK / 8;                          // 16-byte chunks of a row of a slice
     static constexpr int SLICE = P * (BM + BN) * CPR * 16;      // bytes
-    static constexpr int STAGES = 2;
+    static constexpr int STAGES = STAGES_;
     static constexpr int LDS = STAGES * SLICE;
-    static constexpr int INSTR = P * (BM + BN) * CPR / 64;      // direct loads of a slice, one per wavefront each
-    static constexpr int DMA = INSTR / NW;
-    static constexpr int RPI = 64 / CPR;                        // rows of one such load
+    static constexpr int RPI = 64 / CPR;                        // rows of a wavefront's direct load
+    static constexpr int DMA_A = BM / RPI / NW, DMA_B = BN / RPI / NW;  // its loads of one plane's slice
+    static constexpr int DMA = P * (DMA_A + DMA_B);
+    static constexpr int PRODUCTS = P * (P + 1) / 2 * TM * TN, READS = P * (TM + TN);  // of 16 values
     static_assert(BM % (32 * WM) == 0 && BN % (32 * WN) == 0, "wavefront blocks");
-    static_assert(INSTR % NW == 0 && BM % RPI == 0 && BN % RPI == 0, "direct loads");
-    static_assert((BK == 64 || BK == 32) && kPad % BK == 0, "slice");
+    static_assert(BM % (RPI * NW) == 0 && BN % (RPI * NW) == 0, "direct loads");
+    static_assert((BK == 64 || BK == 32) && kPad % BK == 0 && STAGES >= 2, "slice");
     static_assert(LDS <= 160 * 1024, "LDS");
     __device__ static __forceinline__ int key(int row) { return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 };
 
-// 16 bytes a lane from memory to 1024 bytes of LDS.
-__device__ __forceinline__ void dma16(const void *src, char *lds_wave_base) {
-    __builtin_amdgcn_global_load_lds(src, (lds_void *)lds_wave_base, 16, 0, 0);
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+// The 4 GiB from p on.
+__device__ __forceinline__ rsrc_t buffer(const void *p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, -1, 0x00020000);
 }
-// Wait for this wavefront's memory operations, then the workgroup barrier.
-__device__ __forceinline__ void drain_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// 16 bytes a lane from memory (lane offset v, common offset s) to 1024 bytes of LDS.
+__device__ __forceinline__ void dma16(rsrc_t from, uint32_t v, uint32_t s, char *lds_wave_base) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)lds_wave_base, 16, v, s, 0, 0);
+}
+// Wait until at most N of this wavefront's loads from memory are outstanding,
+// and none of its LDS operations, then the workgroup barrier.
+template <int N>
+__device__ __forceinline__ void wait_and_barrier() {
+    static_assert(N >= 0 && N < 64, "vmcnt");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void sched_barrier() { __builtin_amdgcn_sched_barrier(0); }
+// Orders what lies between two sched_barriers: the LDS reads among the first
+// half of the products, so that they are done when the next ones want them, and
+// the direct loads among the second, so that the matrix core never waits for a
+// run of either to be issued.
+template <int PRODUCTS, int READS, int LOADS, int I = 0>
+__device__ __forceinline__ void interleave() {
+    if constexpr (I < PRODUCTS) {
+        constexpr int H = PRODUCTS / 2;
+        constexpr int r = I < H ? (I + 1) * READS / H - I * READS / H : 0;
+        constexpr int l = I < H ? 0 : (I + 1 - H) * LOADS / (PRODUCTS - H) - (I - H) * LOADS / (PRODUCTS - H);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+        if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
+        interleave<PRODUCTS, READS, LOADS, I + 1>();
+    }
+}
 __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 __device__ __forceinline__ f32x16_t mfma(bf16x8_t a, bf16x8_t b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -111,6 +147,23 @@ __device__ __forceinline__ void tile_of(const Shape &s, int64_t b, int &tm, int 
     tn = in / high;
 }
 
+// An epilogue that wants nothing but the accumulators.
+struct Simple {
+    template <class T>
+    static constexpr int lds() { return 0; }
+    template <class T>
+    static constexpr int extra() { return 0; }
+    template <class T>
+    __device__ __forceinline__ void begin(const Place &, char *) const {}
+    // the accumulators start as zeros
+    template <class T>
+    __device__ __forceinline__ void init(f32x16_t (&)[T::TM][T::TN], const Place &) const {}
+};
+
+// LDS of the slices, which the epilogue may use after them.
+template <class T, class Epilogue>
+constexpr int room() { return T::LDS > Epilogue::template lds<T>() ? T::LDS : Epilogue::template lds<T>(); }
+
 template <class T, class Epilogue>
 __global__ __launch_bounds__(T::THREADS) void k_gemm(Operand A, Operand B, Shape s, Epilogue epi) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -127,31 +180,47 @@ __global__ __launch_bounds__(T::THREADS) void k_gemm(Operand A, Operand B, Shape
     const int k0 = blockIdx.y * s.k_split;
     const int k1 = k0 + s.k_split < s.K ? k0 + s.k_split : s.K;
 
-    // This wavefront's direct loads: load d brings RPI rows of one plane of A
-    // or B.  Lane l's 16 bytes land at chunk l of the load's 1024 bytes; it
-    // reads the chunk that the swizzle puts there.
-    const char *base[T::DMA];
-    uint32_t off[T::DMA];
-#pragma unroll
-    for (int d = 0; d < T::DMA; ++d) {
-        const int instr = wave + T::NW * d;
-        const int plane = instr / ((T::BM + T::BN) / T::RPI);
-        const int r0 = instr % ((T::BM + T::BN) / T::RPI) * T::RPI;  // row of the plane's BM + BN
-        const bool is_b = r0 >= T::BM;
-        const Operand &o = is_b ? B : A;
-        const int first = is_b ? n0 : m0;
-        int r = r0 + lane / T::CPR;
+    // This wavefront's direct loads of a slice: load d of an operand brings RPI
+    // rows of one of its planes.  Lane l's 16 bytes land at chunk l of the
+    // load's 1024 bytes; it reads the chunk that the swizzle puts there.
+    constexpr int DA = T::DMA_A, DB = T::DMA_B;
+    uint32_t off_a[DA], off_b[DB];
+    auto offset = [&](const Operand &o, int first, int r, int row) {
         const int chunk = (lane % T::CPR) ^ T::key(r);
-        r -= is_b ? T::BM : 0;
-        if (first + r > o.rows - 1) r = o.rows - 1 - first;
-        base[d] = reinterpret_cast<const char *>(o.p + at.batch * o.batch + plane * o.plane + (int64_t)first * o.ld + k0);
-        off[d] = (uint32_t)r * (uint32_t)(o.ld * 2) + chunk * 16;
+        const int last = o.rows - 1 - first;
+        return (uint32_t)(row < last ? row : last) * (uint32_t)(o.ld * 2) + chunk * 16;
+    };
+#pragma unroll
+    for (int d = 0; d < DA; ++d) {
+        const int row = (wave + T::NW * d) * T::RPI + lane / T::CPR;
+        off_a[d] = offset(A, m0, row, row);
+    }
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        const int row = (wave + T::NW * d) * T::RPI + lane / T::CPR;
+        off_b[d] = offset(B, n0, T::BM + row, row);
+    }
+    rsrc_t from_a[T::P], from_b[T::P];
+#pragma unroll
+    for (int p = 0; p < T::P; ++p) {
+        from_a[p] = buffer(A.p + at.batch * A.batch + p * A.plane + (int64_t)m0 * A.ld);
+        from_b[p] = buffer(B.p + at.batch * B.batch + p * B.plane + (int64_t)n0 * B.ld);
     }
     auto issue = [&](int buf, int step) {
+        const uint32_t k = (uint32_t)(k0 + step * T::BK) * 2;
 #pragma unroll
-        for (int d = 0; d < T::DMA; ++d)
-            dma16(base[d] + (int64_t)step * (T::BK * 2) + off[d], lds + buf * T::SLICE + (wave + T::NW * d) * 1024);
+        for (int p = 0; p < T::P; ++p) {
+            char *to = lds + buf * T::SLICE + p * (T::BM + T::BN) * T::CPR * 16 + wave * 1024;
+#pragma unroll
+            for (int d = 0; d < DA; ++d) dma16(from_a[p], off_a[d], k, to + T::NW * d * 1024);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) dma16(from_b[p], off_b[d], k, to + T::BM * T::CPR * 16 + T::NW * d * 1024);
+        }
     };
+
+    // what the epilogue wants in LDS, loaded while the products go on
+    constexpr int ROOM = room<T, Epilogue>();
+    epi.template begin<T>(at, lds + ROOM);
 
     f32x16_t acc[T::TM][T::TN];
 #pragma unroll
@@ -160,46 +229,95 @@ __global__ __launch_bounds__(T::THREADS) void k_gemm(Operand A, Operand B, Shape
         for (int j = 0; j < T::TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    epi.template init<T>(acc, at);
 
     const int steps = (k1 - k0) / T::BK;
     const int ar = wm * 32 * T::TM + (lane & 31), br = T::BM + wn * 32 * T::TN + (lane & 31);
-    issue(0, 0);
-    for (int step = 0; step < steps; ++step) {
-        // this slice is there, and the other buffer is read no more
-        drain_and_barrier();
-        if (step + 1 < steps) issue((step + 1) & 1, step + 1);
-        const char *slice = lds + (step & 1) * T::SLICE;
+    constexpr int KK = T::BK / 16;
+    // Operand fragments are read one 16-value step ahead of the products that
+    // use them, in two register sets, also across the slices: the barrier
+    // after which the next slice may be read and this one's buffer filled again
+    // comes before the products of a slice's last step.
+    bf16x8_t a[2][T::P][T::TM], b[2][T::P][T::TN];
+    auto read = [&](const char *slice, int kk, int set) {
+        const int chunk = 2 * kk + (lane >> 5);
 #pragma unroll
-        for (int kk = 0; kk < T::BK / 16; ++kk) {
-            bf16x8_t a[T::P][T::TM], b[T::P][T::TN];
-            const int chunk = 2 * kk + (lane >> 5);
+        for (int p = 0; p < T::P; ++p) {
+            const char *plane = slice + p * (T::BM + T::BN) * T::CPR * 16;
 #pragma unroll
-            for (int p = 0; p < T::P; ++p) {
-                const char *plane = slice + p * (T::BM + T::BN) * T::CPR * 16;
+            for (int i = 0; i < T::TM; ++i)
+                a[set][p][i] = *reinterpret_cast<const bf16x8_t *>(
+                    plane + ((ar + 32 * i) * T::CPR + (chunk ^ T::key(ar + 32 * i))) * 16);
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+                b[set][p][j] = *reinterpret_cast<const bf16x8_t *>(
+                    plane + ((br + 32 * j) * T::CPR + (chunk ^ T::key(br + 32 * j))) * 16);
+        }
+    };
+    auto multiply = [&](int set) {  // the smaller products first
+#pragma unroll
+        for (int t = T::P - 1; t >= 0; --t)
+#pragma unroll
+            for (int p = 0; p <= t; ++p)
 #pragma unroll
                 for (int i = 0; i < T::TM; ++i)
-                    a[p][i] = *reinterpret_cast<const bf16x8_t *>(
-                        plane + ((ar + 32 * i) * T::CPR + (chunk ^ T::key(ar + 32 * i))) * 16);
 #pragma unroll
-                for (int j = 0; j < T::TN; ++j)
-                    b[p][j] = *reinterpret_cast<const bf16x8_t *>(
-                        plane + ((br + 32 * j) * T::CPR + (chunk ^ T::key(br + 32 * j))) * 16);
-            }
-            // the smaller products first
+                    for (int j = 0; j < T::TN; ++j) acc[i][j] = mfma(a[set][p][i], b[set][t - p][j], acc[i][j]);
+    };
 #pragma unroll
-            for (int t = T::P - 1; t >= 0; --t)
+    for (int t = 0; t < T::STAGES; ++t)
+        if (t < steps) issue(t, t);
+    if (steps >= T::STAGES)
+        wait_and_barrier<(T::STAGES - 1) * T::DMA>();
+    else
+        wait_and_barrier<0>();
+    read(lds, 0, 0);
+    int buf = 0;
+    // One slice; its last step's products come after the switch to the next
+    // one.  MORE: a slice is left to be loaded into this one's buffer; NEXT:
+    // there is a next one.
+    auto slice = [&](int step, auto more, auto next) {
+        constexpr bool MORE = decltype(more)::value, NEXT = decltype(next)::value;
+        const char *at_ = lds + buf * T::SLICE;
+        const int after = buf + 1 == T::STAGES ? 0 : buf + 1;
 #pragma unroll
-                for (int p = 0; p <= t; ++p)
-#pragma unroll
-                    for (int i = 0; i < T::TM; ++i)
-#pragma unroll
-                        for (int j = 0; j < T::TN; ++j)
-                            acc[i][j] = mfma(a[p][i], b[t - p][j], acc[i][j]);
+        for (int kk = 0; kk < KK - 1; ++kk) {
+            read(at_, kk + 1, (kk + 1) & 1);
+            multiply(kk & 1);
+            interleave<T::PRODUCTS, T::READS, 0>();
+            sched_barrier();
         }
-    }
+        if constexpr (NEXT) {
+            // the next slice is there (the ones after it may be on their way),
+            // and no wavefront reads this one any more
+            wait_and_barrier<MORE ? (T::STAGES - 2) * T::DMA : 0>();
+            read(lds + after * T::SLICE, 0, 0);
+            if constexpr (MORE) issue(buf, step + T::STAGES);
+        }
+        multiply((KK - 1) & 1);
+        interleave<T::PRODUCTS, NEXT ? T::READS : 0, MORE ? T::DMA : 0>();
+        sched_barrier();
+        buf = after;
+    };
+    int step = 0;
+    for (; step + T::STAGES < steps; ++step) slice(step, std::true_type{}, std::true_type{});
+    for (; step + 1 < steps; ++step) slice(step, std::false_type{}, std::true_type{});
+    slice(step, std::false_type{}, std::false_type{});
     // the epilogue may use the slices' LDS
-    drain_and_barrier();
-    epi.template run<T>(acc, at, lds);
+    wait_and_barrier<0>();
+    epi.template run<T>(acc, at, lds, lds + ROOM);
+}
+
+// Allow a kernel more than 64 KB of LDS, once on each device.
+inline hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
 }
 
 template <class T, class Epilogue>
@@ -214,10 +332,11 @@ hipError_t launch(hipStream_t stream, const Operand &A, const Operand &B, int64_
     s.lower = lower;
     const int64_t tiles = lower ? (int64_t)s.tiles_m * (s.tiles_m + 1) / 2 : (int64_t)s.tiles_m * s.tiles_n;
     const int64_t parts = (K + s.k_split - 1) / s.k_split;
-    constexpr int LDS = T::LDS > Epilogue::template lds<T>() ? T::LDS : Epilogue::template lds<T>();
+    constexpr int LDS = room<T, Epilogue>() + Epilogue::template extra<T>();
+    static_assert(LDS <= 160 * 1024, "LDS");
     if (LDS > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_gemm<T, Epilogue>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = allow_lds(reinterpret_cast<const void *>(&k_gemm<T, Epilogue>), LDS, done);
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((k_gemm<T, Epilogue>), dim3((unsigned)tiles, (unsigned)parts, (unsigned)batch), dim3(T::THREADS),

@@ -28,24 +28,32 @@ constexpr int kCounts = 256;          // partial counts of rows with a label
 constexpr int64_t kMaxPiece = 65536;  // rows of a piece
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of G in both orders
 
-// Rows with a label, counted per workgroup; a label that is neither a class
-// nor `ignore` sets the status.
-__global__ __launch_bounds__(256) void k_count(const int64_t *__restrict__ target, int64_t N, int K, int64_t ignore,
-                                               int32_t *count, int32_t *status) {
-    int n = 0, bad = 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N; i += (int64_t)gridDim.x * 256) {
+__device__ __forceinline__ int label_of(int64_t t, int K, int64_t ignore) {
+    return t != ignore && t >= 0 && t < K ? (int)t : -1;
+}
+
+// Before the first piece: rows with a label, counted per workgroup (a label
+// that is neither a class nor `ignore` sets the status), the first piece's
+// labels, and the classes' biases, zeros without any and -inf from K on, so
+// that the classes that fill up the last tile have no share.
+__global__ __launch_bounds__(256) void k_begin(const int64_t *__restrict__ target, int64_t N, int n, int K,
+                                               int64_t ignore, int32_t *count, int32_t *status, int32_t *label,
+                                               const float *bias, int Kp, float *padded_bias) {
+    int c = 0, bad = 0;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+    for (int64_t i = at; i < N; i += step) {
         const int64_t t = target[i];
-        if (t == ignore) continue;
-        if (t >= 0 && t < K)
-            ++n;
-        else
-            bad = 1;
+        const int l = label_of(t, K, ignore);
+        c += l >= 0;
+        bad |= l < 0 && t != ignore;
+        if (i < n) label[i] = l;
     }
+    for (int64_t k = at; k < Kp; k += step) padded_bias[k] = k < K ? (bias ? bias[k] : 0.f) : -INFINITY;
     if (bad) atomicOr(status, DENSE_ST_LABEL);
     __shared__ int red[4];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+    for (int d = 1; d < 64; d *= 2) c += __shfl_xor(c, d);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
     __syncthreads();
     if (threadIdx.x == 0) count[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
@@ -60,12 +68,7 @@ __device__ __forceinline__ float row_factor(const int32_t *count, bool mean) {
     return n > 0 ? (float)(1.0 / (double)n) : 0.f;
 }
 
-// Biases of the classes, zeros without any; -inf from K on, so that the
-// classes that fill up the last tile have no share.
-__global__ __launch_bounds__(256) void k_bias(const float *bias, int K, int Kp, float *out) {
-    const int k = blockIdx.x * 256 + threadIdx.x;
-    if (k < Kp) out[k] = k < K ? (bias ? bias[k] : 0.f) : -INFINITY;
-}
+constexpr int kNoLabel = -(1 << 30);
 
 // What the epilogues need of a piece's rows.
 struct Rows {
@@ -74,24 +77,18 @@ struct Rows {
     int n;
 };
 
-// The labels of a piece's rows, and the factor s.
-__global__ __launch_bounds__(256) void k_rows(const int64_t *__restrict__ target, int n, int K, int64_t ignore,
-                                              const int32_t *count, bool mean, int32_t *label, float *factor) {
-    if (blockIdx.x == 0 && threadIdx.x < 64) {
-        const float s = row_factor(count, mean);
-        if (threadIdx.x == 0) *factor = s;
-    }
+// The labels of a later piece's rows.
+__global__ __launch_bounds__(256) void k_labels(const int64_t *__restrict__ target, int n, int K, int64_t ignore,
+                                                int32_t *label) {
     const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const int64_t t = target[i];
-    label[i] = t != ignore && t >= 0 && t < K ? (int)t : -1;
+    if (i < n) label[i] = label_of(target[i], K, ignore);
 }
 
 // Epilogue of the first pass (rows of the product are classes, columns the
 // piece's rows): maximum and sum of exponentials per tile and row, and the
 // logit of the label.
 template <int P>
-struct Stats {
+struct Stats : gemm::Simple {
     const float *bias;  // padded
     const int32_t *label;
     int n;
@@ -100,22 +97,40 @@ struct Stats {
 
     template <class T>
     static constexpr int lds() { return T::WM * T::BN * 8; }
+    template <class T>
+    static constexpr int extra() { return (T::BM + T::BN) * 4; }
+
+    // the tile's biases and labels
+    template <class T>
+    __device__ __forceinline__ void begin(const gemm::Place &at, char *own) const {
+        float *b = reinterpret_cast<float *>(own);
+        for (int x = threadIdx.x; x < T::BM + T::BN; x += T::THREADS) {
+            const int col = at.tile_n * T::BN + x - T::BM;
+            if (x < T::BM)
+                b[x] = bias[at.tile_m * T::BM + x];
+            else
+                reinterpret_cast<int32_t *>(b)[x] = col < n ? label[col] : -1;
+        }
+    }
 
     template <class T>
-    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *lds) const {
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *lds,
+                                        const char *own) const {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const int wm = wave / T::WN;
+        const float *own_bias = reinterpret_cast<const float *>(own) + at.row0 - at.tile_m * T::BM;
+        const int32_t *own_label = reinterpret_cast<const int32_t *>(own) + T::BM + at.col0 - at.tile_n * T::BN;
         float2 *part = reinterpret_cast<float2 *>(lds);
         float4 bb[T::TM][4];
 #pragma unroll
         for (int i = 0; i < T::TM; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                bb[i][q] = *reinterpret_cast<const float4 *>(bias + at.row0 + 32 * i + 8 * q + 4 * (lane >> 5));
+                bb[i][q] = *reinterpret_cast<const float4 *>(own_bias + 32 * i + 8 * q + 4 * (lane >> 5));
 #pragma unroll
         for (int j = 0; j < T::TN; ++j) {
             const int col = at.col0 + 32 * j + (lane & 31);
-            const int t = col < n ? label[col] : -1;
+            const int t = own_label[32 * j + (lane & 31)] - at.row0;
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < T::TM; ++i)
@@ -126,8 +141,14 @@ struct Stats {
                     const float z = acc[i][j][e] * planes::kBack<P> + b;
                     acc[i][j][e] = z;
                     top = fmaxf(top, z);
-                    if (at.row0 + 32 * i + gemm::acc_row(e) == t) picked[col] = z;
                 }
+            if (__any(t >= 0 && t < 32 * T::TM)) {  // few wavefronts hold a row's label
+#pragma unroll
+                for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (32 * i + gemm::acc_row(e) == t) picked[col] = acc[i][j][e];
+            }
             top = fmaxf(top, __shfl_xor(top, 32));
             const float ref = top == -INFINITY ? 0.f : top;
             float s = 0.f;
@@ -155,24 +176,30 @@ struct Stats {
 };
 
 // Joins the tiles' statistics to lse, and the rows' losses; one partial sum of
-// the losses a workgroup, in fp64.  Four threads a row share its tiles.
+// the losses a workgroup, in fp64.  Q threads a row share its tiles: few where
+// there are rows enough.  Also writes the factor s.
+template <int Q>
 __global__ __launch_bounds__(256) void k_lse(const float2 *__restrict__ stats, int tiles, int n,
                                              const float *__restrict__ picked, const int32_t *__restrict__ label,
-                                             float *lse, float *rows, double *part) {
-    const int i = blockIdx.x * 64 + (threadIdx.x >> 2), q = threadIdx.x & 3;
+                                             float *lse, float *rows, double *part, const int32_t *count, bool mean,
+                                             float *factor) {
+    if (blockIdx.x == 0 && threadIdx.x < 64) {
+        const float s = row_factor(count, mean);
+        if (threadIdx.x == 0) *factor = s;
+    }
+    const int i = blockIdx.x * (256 / Q) + threadIdx.x / Q, q = threadIdx.x % Q;
     double l = 0.0;
     if (i < n) {
         float top = -INFINITY, s = 0.f;
-        for (int t = q; t < tiles; t += 4) {
+        for (int t = q; t < tiles; t += Q) {
             const float2 v = stats[(int64_t)t * n + i];
             const float m = fmaxf(top, v.x);
             const float ref = m == -INFINITY ? 0.f : m;
             s = s * __expf(top - ref) + v.y * __expf(v.x - ref);
-            // a NaN in a tile's sum stays
             top = m;
         }
 #pragma unroll
-        for (int d = 1; d < 4; d *= 2) {
+        for (int d = 1; d < Q; d *= 2) {
             const float top2 = __shfl_xor(top, d), s2 = __shfl_xor(s, d);
             const float m = fmaxf(top, top2);
             const float ref = m == -INFINITY ? 0.f : m;
@@ -221,98 +248,229 @@ __global__ __launch_bounds__(256) void k_total(const double *__restrict__ part, 
     }
 }
 
+// Four lanes hold four 16-bit values each, (a.lo, a.hi, d.lo, d.hi); afterwards
+// lane c holds value c of the four lanes.
+__device__ __forceinline__ void transpose4(uint32_t &a, uint32_t &d) {
+    const int c = threadIdx.x & 3;
+    const uint32_t an = __builtin_amdgcn_mov_dpp(a, 0xB1, 0xF, 0xF, false);  // of lane c ^ 1
+    const uint32_t dn = __builtin_amdgcn_mov_dpp(d, 0xB1, 0xF, 0xF, false);
+    if (c & 1) {
+        a = (an >> 16) | (a & 0xffff0000u);
+        d = (dn >> 16) | (d & 0xffff0000u);
+    } else {
+        a = (a & 0xffffu) | (an << 16);
+        d = (d & 0xffffu) | (dn << 16);
+    }
+    const uint32_t ap = __builtin_amdgcn_mov_dpp(a, 0x4E, 0xF, 0xF, false);  // of lane c ^ 2
+    const uint32_t dp = __builtin_amdgcn_mov_dpp(d, 0x4E, 0xF, 0xF, false);
+    if (c & 2)
+        a = dp;
+    else
+        d = ap;
+}
+
+// The value of lane (this one ^ D).
+template <int D>
+__device__ __forceinline__ float from_lane(float v) {
+    if constexpr (D == 1)
+        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xF, 0xF, false));
+    else if constexpr (D == 2)
+        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xF, 0xF, false));
+    else
+        return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), D << 10 | 0x1f));
+}
+
+// Sums of 16 values over 32 lanes each (the two halves of a wavefront apart):
+// returns which of them this lane gets, in sum[0].
+__device__ __forceinline__ int sum32(float (&sum)[16]) {
+    const int lane = threadIdx.x & 63;
+    int which = 0;
+    auto round = [&](auto half, auto dist) {
+        constexpr int h = decltype(half)::value, d = decltype(dist)::value;
+        const bool up = lane & d;
+        which += up ? h : 0;
+#pragma unroll
+        for (int e = 0; e < h; ++e) {
+            const float keep = up ? sum[e + h] : sum[e], give = up ? sum[e] : sum[e + h];
+            sum[e] = keep + from_lane<d>(give);
+        }
+    };
+    using std::integral_constant;
+    round(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    round(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    round(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+    round(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    sum[0] += from_lane<16>(sum[0]);
+    return which;
+}
+
 // Epilogue of the second pass over a piece of classes: G in both orders, and
 // partial sums of its columns.
 template <int P>
-struct Grad {
+struct Grad : gemm::Simple {
     const float *bias;  // padded, of the piece's first class on
     Rows rows;
     int class0;         // of the piece
-    int K, ldg;         // classes of the piece, and padded
-    int64_t ldt;        // rows padded
-    uint16_t *g;        // [P][n][ldg], or null
-    uint16_t *gt;       // [P][K][ldt], or null
+    int K, Kp, np;      // classes of the piece, classes and rows padded
+    int64_t ldg, ldt;   // values between the rows of g and of gt
+    uint16_t *g;        // [P][n][ldg], classes up to Kp written, or null
+    uint16_t *gt;       // [P][K][ldt], rows up to np written, or null
     float *pbias;       // [tiles of rows * WN][K], or null
     const float *factor;
 
     template <class T>
-    static constexpr int lds() { return 0; }
+    static constexpr int lds() { return T::BM * T::BN * 2; }
+    template <class T>
+    static constexpr int extra() { return (T::BM + 2 * T::BN) * 4; }
+
+    // the tile's biases, labels (counted from the tile's first class; far below
+    // 0 without one) and lse
+    template <class T>
+    __device__ __forceinline__ void begin(const gemm::Place &at, char *own) const {
+        float *b = reinterpret_cast<float *>(own);
+        for (int x = threadIdx.x; x < T::BM + T::BN; x += T::THREADS) {
+            const int c = x - T::BM, col = at.tile_n * T::BN + c;
+            if (c < 0) {
+                b[x] = bias[at.tile_m * T::BM + x];
+            } else {
+                const int l = col < rows.n ? rows.label[col] : -1;
+                reinterpret_cast<int32_t *>(b)[x] = l < 0 ? kNoLabel : l - class0 - at.tile_m * T::BM;
+                b[x + T::BN] = col < rows.n ? rows.lse[col] : 0.f;
+            }
+        }
+    }
 
     template <class T>
-    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *) const {
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *lds,
+                                        const char *own) const {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const int n = rows.n;
-        int t[T::TN];     // label in the piece's classes
+        const int m0 = at.tile_m * T::BM, n0 = at.tile_n * T::BN;
+        const int r0 = at.row0 - m0, c0 = at.col0 - n0;
+        const float *own_bias = reinterpret_cast<const float *>(own) + r0;
+        const float *own_cols = reinterpret_cast<const float *>(own) + T::BM + c0;
+        int t[T::TN];  // label, counted from the wavefront's first class
         bool on[T::TN];
         float lse[T::TN];
+        bool here = false;
 #pragma unroll
         for (int j = 0; j < T::TN; ++j) {
-            const int col = at.col0 + 32 * j + (lane & 31);
-            const int l = col < n ? rows.label[col] : -1;
-            on[j] = l >= 0;
-            t[j] = l - class0;
-            lse[j] = col < n ? rows.lse[col] : 0.f;
+            const int l = __float_as_int(own_cols[32 * j + (lane & 31)]);
+            on[j] = l != kNoLabel;
+            t[j] = l - r0;
+            here |= t[j] >= 0 && t[j] < 32 * T::TM;
+            lse[j] = own_cols[T::BN + 32 * j + (lane & 31)];
         }
+        const bool labels = __any(here);  // few wavefronts hold a row's label
+        const float f = pbias ? *factor : 0.f;
+        uint32_t pk[T::TM][T::TN][4][2][P];  // four classes of a row, twice two
 #pragma unroll
-        for (int i = 0; i < T::TM; ++i)
+        for (int i = 0; i < T::TM; ++i) {
+            float sum[16];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int row = at.row0 + 32 * i + 8 * q + 4 * (lane >> 5);
-                const float4 b4 = *reinterpret_cast<const float4 *>(bias + row);
-                const float b[4] = {b4.x, b4.y, b4.z, b4.w};
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int e = 0; e < 16; ++e) sum[e] = 0.f;
 #pragma unroll
-                for (int j = 0; j < T::TN; ++j) {
-                    const int col = at.col0 + 32 * j + (lane & 31);
-                    uint16_t h[4][P];
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int row = 32 * i + 8 * q + 4 * (lane >> 5);
+                    const float4 b4 = *reinterpret_cast<const float4 *>(own_bias + row);
+                    const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+                    float v[4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float z = acc[i][j][4 * q + r] * planes::kBack<P> + b[r];
-                        float v = __expf(z - lse[j]);
-                        if (row + r == t[j]) v -= 1.f;
-                        if (!on[j]) v = 0.f;  // a row without a label, whatever it holds
-                        sum[r] += v;
-                        planes::split<P>(v, h[r]);
+                        v[r] = on[j] ? __expf(z - lse[j]) : 0.f;  // whatever a row without a label holds
                     }
+                    if (labels)
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        if (g && col < n && row < ldg) {
-                            const uint2 u = make_uint2(h[0][p] | (uint32_t)h[1][p] << 16, h[2][p] | (uint32_t)h[3][p] << 16);
-                            *reinterpret_cast<uint2 *>(g + ((int64_t)p * n + col) * ldg + row) = u;
-                        }
-                        if (gt && col < ldt)
+                        for (int r = 0; r < 4; ++r)
+                            if (row + r == t[j]) v[r] -= 1.f;
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (row + r < K) gt[((int64_t)p * K + row + r) * ldt + col] = h[r][p];
-                    }
+                    for (int r = 0; r < 4; ++r) sum[4 * q + r] += v[r];
+                    planes::split_pair<P>(v[0], v[1], pk[i][j][q][0]);
+                    planes::split_pair<P>(v[2], v[3], pk[i][j][q][1]);
                 }
-                if (pbias) {
+            if (pbias) {
+                // over the 32 lanes: halves of the values are exchanged, so that
+                // each lane adds half as many in the next round
+                const int e = sum32(sum);
+                const int row = at.row0 + 32 * i + gemm::acc_row(e);
+                if ((lane & 16) == 0 && row < K)
+                    pbias[((int64_t)at.tile_n * T::WN + wave % T::WN) * K + row] = sum[0] * f;
+            }
+        }
+        // Both orders go out through LDS, 16 bytes a lane along whole rows of
+        // the tile.
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
+        for (int p = 0; p < P; ++p) {
+            if (g) {
+                constexpr int CH = T::BM / 8;  // 16-byte chunks of a row
+                if (p > 0) __syncthreads();
 #pragma unroll
-                        for (int d = 1; d < 32; d *= 2) sum[r] += __shfl_xor(sum[r], d);
-                        if ((lane & 31) == 0 && row + r < K)
-                            pbias[((int64_t)at.tile_n * T::WN + wave % T::WN) * K + row + r] = sum[r] * *factor;
-                    }
+                for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int c = c0 + 32 * j + (lane & 31), chunk = (r0 + 32 * i + 8 * q) / 8;
+                            *reinterpret_cast<uint2 *>(lds + (c * CH + (chunk ^ (c & (CH - 1)))) * 16 + 8 * (lane >> 5)) =
+                                make_uint2(pk[i][j][q][0][p], pk[i][j][q][1][p]);
+                        }
+                __syncthreads();
+                uint16_t *to = g + ((int64_t)p * n + n0) * ldg + m0;
+                for (int x = threadIdx.x; x < T::BN * CH; x += T::THREADS) {
+                    const int c = x / CH, chunk = x % CH;
+                    if (n0 + c < n && m0 + 8 * chunk < Kp)
+                        *reinterpret_cast<uint4 *>(to + c * ldg + 8 * chunk) =
+                            *reinterpret_cast<const uint4 *>(lds + (c * CH + (chunk ^ (c & (CH - 1)))) * 16);
                 }
             }
+            if (gt) {
+                constexpr int CH = T::BN / 8;
+                // lanes of a write hold four (eight) rows and four chunks of each
+                auto key = [](int r) { return (r & (CH / 4 - 1)) * 4; };
+                if (p > 0 || g) __syncthreads();
+#pragma unroll
+                for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            // lane c of four takes class c of their four rows
+                            uint32_t a = pk[i][j][q][0][p], d = pk[i][j][q][1][p];
+                            transpose4(a, d);
+                            const int r = r0 + 32 * i + 8 * q + 4 * (lane >> 5) + (lane & 3);
+                            const int c = c0 + 32 * j + (lane & 28);
+                            *reinterpret_cast<uint2 *>(lds + (r * CH + ((c / 8) ^ key(r))) * 16 + 2 * (c & 4)) =
+                                make_uint2(a, d);
+                        }
+                __syncthreads();
+                uint16_t *to = gt + ((int64_t)p * K + m0) * ldt + n0;
+                for (int x = threadIdx.x; x < T::BM * CH; x += T::THREADS) {
+                    const int r = x / CH, chunk = x % CH;
+                    if (m0 + r < K && n0 + 8 * chunk < np)
+                        *reinterpret_cast<uint4 *>(to + r * ldt + 8 * chunk) =
+                            *reinterpret_cast<const uint4 *>(lds + (r * CH + (chunk ^ key(r))) * 16);
+                }
+            }
+        }
     }
 };
 
 // Epilogue of a gradient's product: fp32 partial sums [split][rows][cols],
-// begun or added to.
+// begun, or added to: the accumulators then start as them (reading them at the
+// end, with nothing left to multiply, took 55 of 330 us for 8192 x 1024 sums).
 template <int P>
-struct Part {
+struct Part : gemm::Simple {
     float *out;
     int rows, cols;
     bool add;
 
-    template <class T>
-    static constexpr int lds() { return 0; }
+    Part(float *out, int rows, int cols, bool add) : out(out), rows(rows), cols(cols), add(add) {}
 
-    template <class T>
-    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *) const {
-        const int lane = threadIdx.x & 63;
+    template <class T, class F>
+    __device__ __forceinline__ void each(const gemm::Place &at, F &&f) const {
         float *o = out + (int64_t)at.split * rows * cols;
 #pragma unroll
         for (int i = 0; i < T::TM; ++i)
@@ -320,12 +478,17 @@ struct Part {
             for (int j = 0; j < T::TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int row = at.row0 + 32 * i + gemm::acc_row(e), col = at.col0 + 32 * j + (lane & 31);
-                    if (row >= rows || col >= cols) continue;
-                    float *to = o + (int64_t)row * cols + col;
-                    const float v = acc[i][j][e] * planes::kBack<P>;
-                    *to = add ? *to + v : v;
+                    const int row = at.row0 + 32 * i + gemm::acc_row(e), col = at.col0 + 32 * j + (threadIdx.x & 31);
+                    if (row < rows && col < cols) f(o + (int64_t)row * cols + col, i, j, e);
                 }
+    }
+    template <class T>
+    __device__ __forceinline__ void init(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at) const {
+        if (add) each<T>(at, [&](const float *v, int i, int j, int e) { acc[i][j][e] = *v * (1.f / planes::kBack<P>); });
+    }
+    template <class T>
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *, char *) const {
+        each<T>(at, [&](float *v, int i, int j, int e) { *v = acc[i][j][e] * planes::kBack<P>; });
     }
 };
 
@@ -351,13 +514,13 @@ template <int P>
 struct Tiles;
 template <>
 struct Tiles<1> {
-    using Large = gemm::Tile<256, 256, 2, 4, 64, 1>;
+    using Large = gemm::Tile<256, 256, 4, 2, 64, 1>;
     using Middle = gemm::Tile<128, 128, 2, 2, 64, 1>;
     using Few = gemm::Tile<128, 64, 4, 1, 64, 1>;
 };
 template <>
 struct Tiles<3> {
-    using Large = gemm::Tile<128, 128, 2, 2, 32, 3>;
+    using Large = gemm::Tile<256, 128, 4, 2, 32, 3>;
     using Middle = gemm::Tile<128, 128, 2, 2, 32, 3>;
     using Few = gemm::Tile<128, 64, 4, 1, 32, 3>;
 };
@@ -402,6 +565,16 @@ int splits_for(int kind, int64_t m, int64_t n, int64_t k, int cu) {
     return (int)(s < 16 ? s : 16);
 }
 
+// The same for products whose contraction of k may be split: the large tile
+// too where parts of it that fill the chip are long.
+template <int P>
+int split_tile_for(int64_t m, int64_t n, int64_t k, int cu) {
+    const int kind = tile_for<P>(m, n, cu);
+    using L = typename Tiles<P>::Large;
+    if (kind != 1 || m < L::BM || n < L::BN) return kind;
+    return k / splits_for<P>(0, m, n, k, cu) >= 1024 ? 0 : 1;
+}
+
 template <int P, class E>
 hipError_t product(hipStream_t st, int kind, const gemm::Operand &A, const gemm::Operand &B, int64_t K, int64_t part,
                    const E &e) {
@@ -410,6 +583,11 @@ hipError_t product(hipStream_t st, int kind, const gemm::Operand &A, const gemm:
     if (kind == 1) return gemm::launch<typename X::Middle>(st, A, B, K, part, 1, false, e);
     return gemm::launch<typename X::Few>(st, A, B, K, part, 1, false, e);
 }
+
+// Workgroups of k_lse for n rows: 4 threads a row, or where that leaves CUs
+// without work a wavefront.
+bool lse_wide(const lattice_dense *D, int64_t n) { return n < (int64_t)64 * D->cu_count; }
+int64_t lse_blocks(const lattice_dense *D, int64_t n) { return lse_wide(D, n) ? (n + 3) / 4 : (n + 63) / 64; }
 
 // Sizes of the pieces and where everything lies in the scratch.
 template <int P>
@@ -428,22 +606,22 @@ struct Plan {
     Plan(const lattice_dense *D, const LossArgs &a) {
         const int cu = D->cu_count;
         const int64_t C = a.C, K = a.K;
-        const int64_t Cp = gemm::padded(C);
+        const int64_t Cl = gemm::row_length(C);
         Kpad = (K + 255) / 256 * 256;
         R = a.N < kMaxPiece ? a.N : kMaxPiece;
         // tiles' statistics of a piece: at most 256 MiB
         const int64_t most = ((int64_t)1 << 25) / (Kpad / 128);
         if (R > most) R = most < 256 ? 256 : most / 256 * 256;
         if (R < 1) R = 1;
-        const int64_t Rp = gemm::padded(R);
+        const int64_t Rp = gemm::padded(R), Rl = gemm::row_length(R);
         KP = kPieceBytes / (Rp * P * 2 * 2) / 256 * 256;
         KP = KP < 256 ? 256 : KP;
         KP = KP < Kpad ? KP : Kpad;
         const int64_t kp = KP < K ? KP : K;
         fkind = tile_for<P>(K, R, cu);
         gkind = tile_for<P>(kp, R, cu);
-        xkind = C <= 64 ? 2 : tile_for<P>(R, C, cu);
-        wkind = C <= 64 ? 2 : tile_for<P>(kp, C, cu);
+        xkind = split_tile_for<P>(R, C, kp, cu);
+        wkind = split_tile_for<P>(kp, C, R, cu);
         xpart = gemm::part_length(gemm::padded(kp), splits_for<P>(xkind, R, C, kp, cu));
         wpart = gemm::part_length(Rp, splits_for<P>(wkind, kp, C, R, cu));
         xsplits = (gemm::padded(kp) + xpart - 1) / xpart;
@@ -463,14 +641,14 @@ struct Plan {
         const int64_t bm = tile_m<P>(fkind);
         stats = s.take((K + bm - 1) / bm * R * 8);
         parts = 0;
-        for (int64_t r = 0; r < a.N; r += R) parts += ((a.N - r < R ? a.N - r : R) + 63) / 64;
+        for (int64_t r = 0; r < a.N; r += R) parts += lse_blocks(D, a.N - r < R ? a.N - r : R);
         part = s.take(parts * 8);
-        xp = own_x ? s.take(P * R * Cp * 2) : 0;
-        wp = own_w ? s.take(P * K * Cp * 2) : 0;
-        xt = a.grad_w ? s.take(P * C * Rp * 2) : 0;
-        wt = a.grad_x ? s.take(P * C * gemm::padded(K) * 2) : 0;
-        g = a.grad_x ? s.take(P * R * gemm::padded(kp) * 2) : 0;
-        gt = a.grad_w ? s.take(P * kp * Rp * 2) : 0;
+        xp = own_x ? s.take(P * R * Cl * 2) : 0;
+        wp = own_w ? s.take(P * K * Cl * 2) : 0;
+        xt = a.grad_w ? s.take(P * C * Rl * 2) : 0;
+        wt = a.grad_x ? s.take(P * C * gemm::row_length(K) * 2) : 0;
+        g = a.grad_x ? s.take(P * R * gemm::row_length(kp) * 2) : 0;
+        gt = a.grad_w ? s.take(P * kp * Rl * 2) : 0;
         if (a.grad_bias) {
             const int64_t rows = bias_rows<P>(gkind, R);
             pbias = s.take((rows * kp + rowsum::scratch_floats(rows, kp)) * 4);
@@ -501,8 +679,9 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
     const int esz = a.bf16 ? 2 : 4;
     constexpr int BF = P == 1;
 
-    hipLaunchKernelGGL(k_count, dim3(kCounts), dim3(256), 0, st, a.target, a.N, K, a.ignore, ints(p.count), D->status);
-    hipLaunchKernelGGL(k_bias, dim3((unsigned)(p.Kpad / 256)), dim3(256), 0, st, a.bias, K, (int)p.Kpad, f(p.bias));
+    const int first = (int)(a.N < p.R ? a.N : p.R);
+    hipLaunchKernelGGL(k_begin, dim3(kCounts), dim3(256), 0, st, a.target, a.N, first, K, a.ignore, ints(p.count),
+                       D->status, ints(p.label), a.bias, (int)p.Kpad, f(p.bias));
     TRY(hipGetLastError());
     gemm::Operand W = {reinterpret_cast<const uint16_t *>(a.w), a.w_stride, 0, 0, K};
     if (p.own_w || a.grad_x) {
@@ -516,31 +695,40 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
         const int n = (int)(a.N - r0 < p.R ? a.N - r0 : p.R);
         const int64_t np = gemm::padded(n);
         const char *x = reinterpret_cast<const char *>(a.x) + r0 * a.x_stride * esz;
-        hipLaunchKernelGGL(k_rows, dim3((n + 255) / 256), dim3(256), 0, st, a.target + r0, n, K, a.ignore,
-                           ints(p.count), a.mean, ints(p.label), f(p.factor));
-        TRY(hipGetLastError());
+        if (piece > 0) {
+            hipLaunchKernelGGL(k_labels, dim3((n + 255) / 256), dim3(256), 0, st, a.target + r0, n, K, a.ignore,
+                               ints(p.label));
+            TRY(hipGetLastError());
+        }
         gemm::Operand X = {reinterpret_cast<const uint16_t *>(x), a.x_stride, 0, 0, n};
         if (p.own_x || a.grad_w) {
             const planes::Source s = {x, a.x_stride, 0, n, C, ints(p.label), nullptr};
             TRY(planes::launch<P>(st, a.bf16, s, 1, p.own_x ? h(p.xp) : nullptr, a.grad_w ? h(p.xt) : nullptr));
             if (p.own_x) X = planes::operand(h(p.xp), n, C, P);
         }
-        const Stats<P> stats = {f(p.bias), ints(p.label), n, reinterpret_cast<float2 *>(ws + p.stats), f(p.picked)};
+        const Stats<P> stats = {{}, f(p.bias), ints(p.label), n, reinterpret_cast<float2 *>(ws + p.stats), f(p.picked)};
         TRY((product<P>(st, p.fkind, W, X, Cp, Cp, stats)));
         const int tiles = (K + tile_m<P>(p.fkind) - 1) / tile_m<P>(p.fkind);
-        const unsigned lse_grid = (n + 63) / 64;
-        hipLaunchKernelGGL(k_lse, dim3(lse_grid), dim3(256), 0, st, stats.stats, tiles, n, f(p.picked), ints(p.label),
-                           f(p.lse), a.rows ? a.rows + r0 : nullptr, reinterpret_cast<double *>(ws + p.part) + parts);
+        const unsigned lse_grid = (unsigned)lse_blocks(D, n);
+        float *row_loss = a.rows ? a.rows + r0 : nullptr;
+        double *part = reinterpret_cast<double *>(ws + p.part) + parts;
+        if (lse_wide(D, n))
+            hipLaunchKernelGGL(k_lse<64>, dim3(lse_grid), dim3(256), 0, st, stats.stats, tiles, n, f(p.picked),
+                               ints(p.label), f(p.lse), row_loss, part, ints(p.count), a.mean, f(p.factor));
+        else
+            hipLaunchKernelGGL(k_lse<4>, dim3(lse_grid), dim3(256), 0, st, stats.stats, tiles, n, f(p.picked),
+                               ints(p.label), f(p.lse), row_loss, part, ints(p.count), a.mean, f(p.factor));
         TRY(hipGetLastError());
         parts += lse_grid;
         if (!a.any_grad()) continue;
         for (int64_t k0 = 0; k0 < K; k0 += p.KP) {
             const int kn = (int)(K - k0 < p.KP ? K - k0 : p.KP);
-            const int64_t ldg = gemm::padded(kn);
+            const int64_t kp = gemm::padded(kn);
             gemm::Operand Wk = W;
             Wk.p += k0 * W.ld;
             Wk.rows = kn;
-            const Grad<P> grad = {f(p.bias) + k0, {ints(p.label), f(p.lse), n}, (int)k0, kn, (int)ldg, np,
+            const Grad<P> grad = {{}, f(p.bias) + k0, {ints(p.label), f(p.lse), n}, (int)k0, kn, (int)kp, (int)np,
+                                  gemm::row_length(kn), gemm::row_length(n),
                                   a.grad_x ? h(p.g) : nullptr, a.grad_w ? h(p.gt) : nullptr,
                                   a.grad_bias ? f(p.pbias) : nullptr, f(p.factor)};
             TRY((product<P>(st, p.gkind, Wk, X, Cp, Cp, grad)));
@@ -552,18 +740,18 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
             if (a.grad_x) {
                 gemm::Operand Wt = planes::operand(h(p.wt), C, K, P);
                 Wt.p += k0;
-                TRY((product<P>(st, p.xkind, planes::operand(h(p.g), n, kn, P), Wt, ldg, p.xpart,
+                TRY((product<P>(st, p.xkind, planes::operand(h(p.g), n, kn, P), Wt, kp, p.xpart,
                                 Part<P>{f(p.px), n, C, k0 > 0})));
             }
             if (a.grad_w) {
-                float *part = f(p.pw) + k0 * C * p.wsplits;
+                float *sums = f(p.pw) + k0 * C * p.wsplits;
                 TRY((product<P>(st, p.wkind, planes::operand(h(p.gt), kn, n, P), planes::operand(h(p.xt), C, n, P), np,
-                                p.wpart, Part<P>{part, kn, C, r0 > 0})));
+                                p.wpart, Part<P>{sums, kn, C, r0 > 0})));
                 if (r0 + p.R >= a.N) {
                     const int64_t v = (int64_t)kn * C;
                     // a later piece of rows is no longer than the first, and has no more parts
                     const int splits = (int)(piece > 0 ? p.wsplits : (np + p.wpart - 1) / p.wpart);
-                    hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, part,
+                    hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, sums,
                                        splits, v, f(p.factor), reinterpret_cast<char *>(a.grad_w) + k0 * C * esz);
                     TRY(hipGetLastError());
                 }

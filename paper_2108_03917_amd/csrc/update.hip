@@ -105,7 +105,7 @@ __device__ __forceinline__ void store4(uint16_t *p, int64_t plane, const uint16_
 
 // Epilogue of the symmetric products: S = acc, or b S + c acc.
 template <int P>
-struct Symmetric {
+struct Symmetric : gemm::Simple {
     const uint16_t *s;  // S of which b times is added, or null
     uint16_t *out;      // planes [batch][P][m][ld]
     int m;
@@ -113,10 +113,7 @@ struct Symmetric {
     float b, c;
 
     template <class T>
-    static constexpr int lds() { return 0; }
-
-    template <class T>
-    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *) const {
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *, char *) const {
         const int lane = threadIdx.x & 63;
         const int64_t plane = (int64_t)m * ld;
         uint16_t *o = out + at.batch * P * plane;
@@ -161,7 +158,7 @@ struct Symmetric {
 // Epilogue of the step's last product: a X + acc, to both orders of the next X
 // or to the result.
 template <int P>
-struct Next {
+struct Next : gemm::Simple {
     const uint16_t *xt;    // X^T planes [batch][P][n][ldt]
     uint16_t *nr, *nt;     // next X [batch][P][m][ldr] and X^T, or null
     void *out;             // or the result [batch][m][n] ([n][m] if tall)
@@ -171,10 +168,7 @@ struct Next {
     float a;
 
     template <class T>
-    static constexpr int lds() { return 0; }
-
-    template <class T>
-    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *) const {
+    __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *, char *) const {
         const int lane = threadIdx.x & 63;
         const int64_t pt = (int64_t)n * ldt, pr = (int64_t)m * ldr;
 #pragma unroll
@@ -226,7 +220,9 @@ struct Plan {
     int m, n;       // of X: m <= n
     bool tall;
     int P;
-    int64_t ldr, ldt, chunk;  // matrices taken together
+    int64_t ldr, ldt;  // values between rows
+    int64_t kn, km;    // n and m padded
+    int64_t chunk;     // matrices taken together
     int64_t scale, part, xr[2], xt[2], s, q, bytes;
 
     explicit Plan(const UpdateArgs &a) {
@@ -234,8 +230,10 @@ struct Plan {
         m = tall ? a.n : a.m;
         n = tall ? a.m : a.n;
         P = a.out_bf16 ? 2 : 3;
-        ldr = gemm::padded(n);
-        ldt = gemm::padded(m);
+        ldr = gemm::row_length(n);
+        ldt = gemm::row_length(m);
+        kn = gemm::padded(n);
+        km = gemm::padded(m);
         const int64_t each = P * 2 * (2 * (m * ldr + n * ldt) + 2 * m * ldt);
         chunk = kChunkBytes / each;
         chunk = chunk < 1 ? 1 : chunk < a.batch ? chunk : a.batch;
@@ -306,14 +304,14 @@ hipError_t steps(lattice_dense *D, const UpdateArgs &a, const Plan &p) {
             const int now = i & 1, next = now ^ 1;
             const gemm::Operand X = planes::operand(h(p.xr[now]), m, n, P);
             const gemm::Operand Xt = planes::operand(h(p.xt[now]), n, m, P);
-            TRY((product<P>(D, X, X, p.ldr, batch, true, Symmetric<P>{nullptr, h(p.s), m, p.ldt, 0.f, 0.f})));
-            TRY((product<P>(D, S, S, p.ldt, batch, true,
-                            Symmetric<P>{h(p.s), h(p.q), m, p.ldt, a.coef[1], a.coef[2]})));
+            TRY((product<P>(D, X, X, p.kn, batch, true, Symmetric<P>{{}, nullptr, h(p.s), m, p.ldt, 0.f, 0.f})));
+            TRY((product<P>(D, S, S, p.km, batch, true,
+                            Symmetric<P>{{}, h(p.s), h(p.q), m, p.ldt, a.coef[1], a.coef[2]})));
             const bool last = i + 1 == a.steps;
-            const Next<P> e = {h(p.xt[now]), last ? nullptr : h(p.xr[next]), last ? nullptr : h(p.xt[next]),
+            const Next<P> e = {{}, h(p.xt[now]), last ? nullptr : h(p.xr[next]), last ? nullptr : h(p.xt[next]),
                                last ? reinterpret_cast<char *>(a.out) + b0 * a.m * a.n * osz : nullptr,
                                a.out_bf16, p.tall, m, n, p.ldr, p.ldt, a.coef[0]};
-            TRY((product<P>(D, Q, Xt, p.ldt, batch, false, e)));
+            TRY((product<P>(D, Q, Xt, p.km, batch, false, e)));
         }
     }
     return hipSuccess;
