@@ -7,6 +7,13 @@
 
 #include "internal.h"
 
+// In the launchers: pass a failure on.
+#define TRY(expr)                          \
+    do {                                   \
+        const hipError_t e_ = (expr);      \
+        if (e_ != hipSuccess) return e_;   \
+    } while (0)
+
 // Device status bits of a lattice_dense.
 enum : int { DENSE_ST_LABEL = 1 };
 

@@ -320,6 +320,11 @@ inline hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t>
     return e;
 }
 
+inline int64_t tiles_of(int64_t m, int64_t n, int bm, int bn, bool lower) {
+    const int64_t tm = (m + bm - 1) / bm, tn = (n + bn - 1) / bn;
+    return lower ? tm * (tm + 1) / 2 : tm * tn;
+}
+
 template <class T, class Epilogue>
 hipError_t launch(hipStream_t stream, const Operand &A, const Operand &B, int64_t K, int64_t k_split, int64_t batch,
                   bool lower, const Epilogue &epi) {
@@ -330,7 +335,7 @@ hipError_t launch(hipStream_t stream, const Operand &A, const Operand &B, int64_
     s.tiles_m = (A.rows + T::BM - 1) / T::BM;
     s.tiles_n = (B.rows + T::BN - 1) / T::BN;
     s.lower = lower;
-    const int64_t tiles = lower ? (int64_t)s.tiles_m * (s.tiles_m + 1) / 2 : (int64_t)s.tiles_m * s.tiles_n;
+    const int64_t tiles = tiles_of(A.rows, B.rows, T::BM, T::BN, lower);
     const int64_t parts = (K + s.k_split - 1) / s.k_split;
     constexpr int LDS = room<T, Epilogue>() + Epilogue::template extra<T>();
     static_assert(LDS <= 160 * 1024, "LDS");
@@ -346,6 +351,85 @@ hipError_t launch(hipStream_t stream, const Operand &A, const Operand &B, int64_
 
 // The length of a part when a contraction of K is cut into at most `splits`.
 inline int64_t part_length(int64_t K, int64_t splits) { return padded((K + splits - 1) / splits); }
+
+// A product whose contraction is cut into parts: the parts' accumulators, 16
+// bytes a lane, and the launch that adds them and goes on with the epilogue.
+struct Store : Simple {
+    float *out;  // [batch][parts][tiles][accumulators / 4][threads][4]
+    Shape s;
+    int parts;
+
+    Store(float *out, const Shape &s, int parts) : out(out), s(s), parts(parts) {}
+
+    template <class T>
+    __device__ __forceinline__ int64_t place(const Place &at, int part) const {
+        const int64_t tiles = s.lower ? (int64_t)s.tiles_m * (s.tiles_m + 1) / 2 : (int64_t)s.tiles_m * s.tiles_n;
+        const int64_t tile = s.lower ? (int64_t)at.tile_m * (at.tile_m + 1) / 2 + at.tile_n
+                                     : (int64_t)at.tile_m * s.tiles_n + at.tile_n;
+        return (((int64_t)at.batch * parts + part) * tiles + tile) * (T::BM * T::BN) + threadIdx.x * 4;
+    }
+    template <class T>
+    __device__ __forceinline__ void run(f32x16_t (&acc)[T::TM][T::TN], const Place &at, char *, char *) const {
+        float *o = out + place<T>(at, at.split);
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<float4 *>(o + ((i * T::TN + j) * 4 + q) * T::THREADS * 4) =
+                        make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    }
+};
+
+// A workgroup joins one row of 32 x 32 blocks of each wavefront (gridDim.y of
+// them), so that a few large tiles still give many workgroups.
+template <class T, class Epilogue>
+__global__ __launch_bounds__(T::THREADS) void k_gemm_join(Store parts, Epilogue epi) {
+    Place at;
+    tile_of(parts.s, xcd_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
+    at.split = 0;
+    at.batch = blockIdx.z;
+    const int wave = wave_index(), i = blockIdx.y;
+    at.row0 = at.tile_m * T::BM + wave / T::WN * 32 * T::TM + 32 * i;
+    at.col0 = at.tile_n * T::BN + wave % T::WN * 32 * T::TN;
+    f32x16_t acc[1][T::TN];
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[0][j][e] = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < parts.parts; ++k) {
+        const float *from = parts.out + parts.template place<T>(at, k);
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 v = *reinterpret_cast<const float4 *>(from + ((i * T::TN + j) * 4 + q) * T::THREADS * 4);
+                acc[0][j][4 * q] += v.x;
+                acc[0][j][4 * q + 1] += v.y;
+                acc[0][j][4 * q + 2] += v.z;
+                acc[0][j][4 * q + 3] += v.w;
+            }
+    }
+    epi.template direct<1, T::TN>(acc, at);
+}
+
+// The product with its contraction in parts of k_part, by way of `parts`
+// (parts x batch x tiles x BM x BN floats) if there is more than one.
+template <class T, class Epilogue>
+hipError_t launch_parts(hipStream_t stream, const Operand &A, const Operand &B, int64_t K, int64_t k_part,
+                        int64_t batch, bool lower, const Epilogue &epi, float *parts) {
+    const int n = (int)((K + k_part - 1) / k_part);
+    if (n <= 1) return launch<T>(stream, A, B, K, K, batch, lower, epi);
+    const Shape s = {(int)K, (int)k_part, (A.rows + T::BM - 1) / T::BM, (B.rows + T::BN - 1) / T::BN, lower};
+    const Store store(parts, s, n);
+    const hipError_t e = launch<T>(stream, A, B, K, k_part, batch, lower, store);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_gemm_join<T, Epilogue>), dim3((unsigned)tiles_of(A.rows, B.rows, T::BM, T::BN, lower), T::TM, (unsigned)batch),
+                       dim3(T::THREADS), 0, stream, store, epi);
+    return hipGetLastError();
+}
 
 }  // namespace
 }  // namespace gemm

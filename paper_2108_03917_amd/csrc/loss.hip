@@ -248,27 +248,6 @@ __global__ __launch_bounds__(256) void k_total(const double *__restrict__ part, 
     }
 }
 
-// Four lanes hold four 16-bit values each, (a.lo, a.hi, d.lo, d.hi); afterwards
-// lane c holds value c of the four lanes.
-__device__ __forceinline__ void transpose4(uint32_t &a, uint32_t &d) {
-    const int c = threadIdx.x & 3;
-    const uint32_t an = __builtin_amdgcn_mov_dpp(a, 0xB1, 0xF, 0xF, false);  // of lane c ^ 1
-    const uint32_t dn = __builtin_amdgcn_mov_dpp(d, 0xB1, 0xF, 0xF, false);
-    if (c & 1) {
-        a = (an >> 16) | (a & 0xffff0000u);
-        d = (dn >> 16) | (d & 0xffff0000u);
-    } else {
-        a = (a & 0xffffu) | (an << 16);
-        d = (d & 0xffffu) | (dn << 16);
-    }
-    const uint32_t ap = __builtin_amdgcn_mov_dpp(a, 0x4E, 0xF, 0xF, false);  // of lane c ^ 2
-    const uint32_t dp = __builtin_amdgcn_mov_dpp(d, 0x4E, 0xF, 0xF, false);
-    if (c & 2)
-        a = dp;
-    else
-        d = ap;
-}
-
 // The value of lane (this one ^ D).
 template <int D>
 __device__ __forceinline__ float from_lane(float v) {
@@ -400,61 +379,7 @@ struct Grad : gemm::Simple {
                     pbias[((int64_t)at.tile_n * T::WN + wave % T::WN) * K + row] = sum[0] * f;
             }
         }
-        // Both orders go out through LDS, 16 bytes a lane along whole rows of
-        // the tile.
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (g) {
-                constexpr int CH = T::BM / 8;  // 16-byte chunks of a row
-                if (p > 0) __syncthreads();
-#pragma unroll
-                for (int i = 0; i < T::TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < T::TN; ++j)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int c = c0 + 32 * j + (lane & 31), chunk = (r0 + 32 * i + 8 * q) / 8;
-                            *reinterpret_cast<uint2 *>(lds + (c * CH + (chunk ^ (c & (CH - 1)))) * 16 + 8 * (lane >> 5)) =
-                                make_uint2(pk[i][j][q][0][p], pk[i][j][q][1][p]);
-                        }
-                __syncthreads();
-                uint16_t *to = g + ((int64_t)p * n + n0) * ldg + m0;
-                for (int x = threadIdx.x; x < T::BN * CH; x += T::THREADS) {
-                    const int c = x / CH, chunk = x % CH;
-                    if (n0 + c < n && m0 + 8 * chunk < Kp)
-                        *reinterpret_cast<uint4 *>(to + c * ldg + 8 * chunk) =
-                            *reinterpret_cast<const uint4 *>(lds + (c * CH + (chunk ^ (c & (CH - 1)))) * 16);
-                }
-            }
-            if (gt) {
-                constexpr int CH = T::BN / 8;
-                // lanes of a write hold four (eight) rows and four chunks of each
-                auto key = [](int r) { return (r & (CH / 4 - 1)) * 4; };
-                if (p > 0 || g) __syncthreads();
-#pragma unroll
-                for (int i = 0; i < T::TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < T::TN; ++j)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            // lane c of four takes class c of their four rows
-                            uint32_t a = pk[i][j][q][0][p], d = pk[i][j][q][1][p];
-                            transpose4(a, d);
-                            const int r = r0 + 32 * i + 8 * q + 4 * (lane >> 5) + (lane & 3);
-                            const int c = c0 + 32 * j + (lane & 28);
-                            *reinterpret_cast<uint2 *>(lds + (r * CH + ((c / 8) ^ key(r))) * 16 + 2 * (c & 4)) =
-                                make_uint2(a, d);
-                        }
-                __syncthreads();
-                uint16_t *to = gt + ((int64_t)p * K + m0) * ldt + n0;
-                for (int x = threadIdx.x; x < T::BM * CH; x += T::THREADS) {
-                    const int r = x / CH, chunk = x % CH;
-                    if (m0 + r < K && n0 + 8 * chunk < np)
-                        *reinterpret_cast<uint4 *>(to + r * ldt + 8 * chunk) =
-                            *reinterpret_cast<const uint4 *>(lds + (r * CH + (chunk ^ key(r))) * 16);
-                }
-            }
-        }
+        planes::store_both<T, P>(pk, at, lds, g, ldg, (int64_t)n * ldg, n, Kp, gt, ldt, (int64_t)K * ldt, K, np);
     }
 };
 
@@ -659,12 +584,6 @@ struct Plan {
         bytes = s.bytes;
     }
 };
-
-#define TRY(expr)                          \
-    do {                                   \
-        const hipError_t e_ = (expr);      \
-        if (e_ != hipSuccess) return e_;   \
-    } while (0)
 
 template <int P>
 hipError_t run(lattice_dense *D, const LossArgs &a) {

@@ -38,9 +38,99 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t *h) {
     }
 }
 
+// Four lanes hold four 16-bit values each, (a.lo, a.hi, d.lo, d.hi); afterwards
+// lane c holds value c of the four lanes.
+__device__ __forceinline__ void transpose4(uint32_t &a, uint32_t &d) {
+    const int c = threadIdx.x & 3;
+    const uint32_t an = __builtin_amdgcn_mov_dpp(a, 0xB1, 0xF, 0xF, false);  // of lane c ^ 1
+    const uint32_t dn = __builtin_amdgcn_mov_dpp(d, 0xB1, 0xF, 0xF, false);
+    if (c & 1) {
+        a = (an >> 16) | (a & 0xffff0000u);
+        d = (dn >> 16) | (d & 0xffff0000u);
+    } else {
+        a = (a & 0xffffu) | (an << 16);
+        d = (d & 0xffffu) | (dn << 16);
+    }
+    const uint32_t ap = __builtin_amdgcn_mov_dpp(a, 0x4E, 0xF, 0xF, false);  // of lane c ^ 2
+    const uint32_t dp = __builtin_amdgcn_mov_dpp(d, 0x4E, 0xF, 0xF, false);
+    if (c & 2)
+        a = dp;
+    else
+        d = ap;
+}
+
 // What a product of two such operands is multiplied by to be the values' own.
 template <int P>
 constexpr float kBack = P == 3 ? kSplitBack : 1.f;
+
+// A tile's values, packed in pairs of rows as its accumulators lie, to planes in
+// both orders: at[col][row] (columns below `cols`, rows below `row_end`) and
+// at_t[row][col] (rows below `rows`, columns below `col_end`); the ends are
+// multiples of 8, and either matrix may be null.  They go out through LDS (BM x
+// BN values), 16 bytes a lane along whole rows of the tile: stores of 8 bytes
+// straight from the registers, each to another row, took 46 us more for 16384 x
+// 8192 values in both orders.
+template <class T, int P>
+__device__ __forceinline__ void store_both(uint32_t (&pk)[T::TM][T::TN][4][2][P], const gemm::Place &at, char *lds,
+                                           uint16_t *to, int64_t ld, int64_t plane, int cols, int row_end,
+                                           uint16_t *to_t, int64_t ld_t, int64_t plane_t, int rows, int col_end) {
+    const int lane = threadIdx.x & 63;
+    const int m0 = at.tile_m * T::BM, n0 = at.tile_n * T::BN;
+    const int r0 = at.row0 - m0, c0 = at.col0 - n0;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        if (to) {
+            constexpr int CH = T::BM / 8;  // 16-byte chunks of a row
+            if (p > 0) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = c0 + 32 * j + (lane & 31), chunk = (r0 + 32 * i + 8 * q) / 8;
+                        *reinterpret_cast<uint2 *>(lds + (c * CH + (chunk ^ (c & (CH - 1)))) * 16 + 8 * (lane >> 5)) =
+                            make_uint2(pk[i][j][q][0][p], pk[i][j][q][1][p]);
+                    }
+            __syncthreads();
+            uint16_t *o = to + p * plane + n0 * ld + m0;
+            for (int x = threadIdx.x; x < T::BN * CH; x += T::THREADS) {
+                const int c = x / CH, chunk = x % CH;
+                if (n0 + c < cols && m0 + 8 * chunk < row_end)
+                    *reinterpret_cast<uint4 *>(o + c * ld + 8 * chunk) =
+                        *reinterpret_cast<const uint4 *>(lds + (c * CH + (chunk ^ (c & (CH - 1)))) * 16);
+            }
+        }
+        if (to_t) {
+            constexpr int CH = T::BN / 8;
+            // lanes of a write hold four (eight) rows and four chunks of each
+            auto key = [](int r) { return (r & (CH / 4 - 1)) * 4; };
+            if (p > 0 || to) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        // lane c of four takes row c of their four columns
+                        uint32_t a = pk[i][j][q][0][p], d = pk[i][j][q][1][p];
+                        transpose4(a, d);
+                        const int r = r0 + 32 * i + 8 * q + 4 * (lane >> 5) + (lane & 3);
+                        const int c = c0 + 32 * j + (lane & 28);
+                        *reinterpret_cast<uint2 *>(lds + (r * CH + ((c / 8) ^ key(r))) * 16 + 2 * (c & 4)) =
+                            make_uint2(a, d);
+                    }
+            __syncthreads();
+            uint16_t *o = to_t + p * plane_t + m0 * ld_t + n0;
+            for (int x = threadIdx.x; x < T::BM * CH; x += T::THREADS) {
+                const int r = x / CH, chunk = x % CH;
+                if (m0 + r < rows && n0 + 8 * chunk < col_end)
+                    *reinterpret_cast<uint4 *>(o + r * ld_t + 8 * chunk) =
+                        *reinterpret_cast<const uint4 *>(lds + (r * CH + (chunk ^ key(r))) * 16);
+            }
+        }
+    }
+}
 
 struct Source {
     const void *p;
