@@ -31,103 +31,109 @@ __device__ __forceinline__ int64_t row_count(const int32_t *counters, int64_t ro
     return v < rows ? v : rows;
 }
 
-// Sum over the G threads of a row; every one of them gets it.  For G above a
-// wavefront the workgroup's threads all call it: `red` holds one value a wave.
-template <int G>
-__device__ __forceinline__ float row_sum(float v, float *red) {
+// Sums over the G threads of a row; every one of them gets them.  For G above a
+// wavefront all threads of the workgroup call it, with `red` one value for each
+// wave and sum, and with another `red` in the next call: a wavefront that
+// writes one again has passed the barrier of the call in between, which the
+// others reach after reading it.
+template <int G, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float *red) {
 #pragma unroll
-    for (int d = 1; d < (G < 64 ? G : 64); d *= 2) v += __shfl_xor(v, d);
+    for (int d = 1; d < (G < 64 ? G : 64); d *= 2)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], d);
     if constexpr (G > 64) {
         constexpr int W = G / 64;
         const int wave = threadIdx.x >> 6;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) red[wave] = v;
-        __syncthreads();
-        const float *mine = red + wave / W * W;
-        v = 0.f;
+        if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int i = 0; i < W; ++i) v += mine[i];
+            for (int k = 0; k < N; ++k) red[N * wave + k] = v[k];
+        __syncthreads();
+        const float *mine = red + wave / W * W * N;
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += mine[N * i + k];
     }
-    return v;
 }
 
-// Two sums at once.
-template <int G>
-__device__ __forceinline__ void row_sum2(float &a, float &b, float *red) {
-#pragma unroll
-    for (int d = 1; d < (G < 64 ? G : 64); d *= 2) {
-        a += __shfl_xor(a, d);
-        b += __shfl_xor(b, d);
-    }
-    if constexpr (G > 64) {
-        constexpr int W = G / 64;
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) {
-            red[2 * wave] = a;
-            red[2 * wave + 1] = b;
-        }
-        __syncthreads();
-        const float *mine = red + wave / W * W * 2;
-        a = b = 0.f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            a += mine[2 * i];
-            b += mine[2 * i + 1];
-        }
-    }
-}
+// Rows that a thread has in hand at once: two where a row is one load a thread,
+// for the bytes in flight.
+template <int G, int NV>
+constexpr int at_once() { return G <= 64 && NV == 1 ? 2 : 1; }
 
 template <bool XB, bool YB, int G, int NV>
 __global__ __launch_bounds__(G > kForward ? G : kForward) void k_norm(NormArgs a) {
     constexpr int VEC = XB || YB ? 8 : 4;
-    constexpr int RPB = (G > kForward ? G : kForward) / G;
-    __shared__ float red[32];
+    constexpr int RPB = (G > kForward ? G : kForward) / G, U = at_once<G, NV>();
+    __shared__ float red[2][16];
     const int64_t n = row_count(a.counters, a.rows);
     const int j = threadIdx.x % G;
-    const int64_t step = (int64_t)gridDim.x * RPB;
-    // every thread of the workgroup runs the same number of rounds
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < n; r0 += step) {
-        const int64_t r = r0 + threadIdx.x / G;
-        const bool on = r < n;
-        const char *xr = reinterpret_cast<const char *>(a.x) + (on ? r : n - 1) * a.x_stride * (XB ? 2 : 4);
-        float v[NV][VEC];
-        float s = 0.f;
+    float ga[NV][VEC], be[NV][VEC];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) load_row<XB, VEC>(xr, (j + k * G) * VEC, a.C, v[k]);
+    for (int k = 0; k < NV; ++k) {
+        if (a.gamma) load_row<false, VEC>(a.gamma, (j + k * G) * VEC, a.C, ga[k]);
+        if (a.beta) load_row<false, VEC>(a.beta, (j + k * G) * VEC, a.C, be[k]);
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) s += v[k][i];
-        const float mu = row_sum<G>(s, red) / a.C;
-        float q = 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float d = v[k][i] - mu;
-                q += (j + k * G) * VEC + i < a.C ? d * d : 0.f;
-            }
-        const float rs = 1.f / sqrtf(row_sum<G>(q, red) / a.C + a.eps);
-        if (!on) continue;
-        char *yr = reinterpret_cast<char *>(a.y) + r * a.y_stride * (YB ? 2 : 4);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c0 = (j + k * G) * VEC;
-            if (c0 >= a.C) continue;
-            float ga[VEC], be[VEC];
-            if (a.gamma) load_row<false, VEC>(a.gamma, c0, a.C, ga);
-            if (a.beta) load_row<false, VEC>(a.beta, c0, a.C, be);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float h = (v[k][i] - mu) * rs;
-                v[k][i] = (a.gamma ? ga[i] * h : h) + (a.beta ? be[i] : 0.f);
-            }
-            store_row<YB, VEC>(yr, c0, a.C, v[k]);
+        for (int i = 0; i < VEC; ++i) {
+            if (!a.gamma) ga[k][i] = 1.f;
+            if (!a.beta) be[k][i] = 0.f;
         }
-        if (j == 0) {
-            if (a.mean) a.mean[r] = mu;
-            if (a.rstd) a.rstd[r] = rs;
+    }
+    const int64_t step = (int64_t)gridDim.x * RPB * U;
+    // every thread of the workgroup runs the same number of rounds
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB * U; r0 < n; r0 += step) {
+        float v[U][NV][VEC];
+        int64_t row[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            row[u] = r0 + u * RPB + threadIdx.x / G;
+            const char *xr = reinterpret_cast<const char *>(a.x) + (row[u] < n ? row[u] : n - 1) * a.x_stride * (XB ? 2 : 4);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) load_row<XB, VEC>(xr, (j + k * G) * VEC, a.C, v[u][k]);
+        }
+        float s[U], q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            s[u] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) s[u] += v[u][k][i];
+        }
+        row_sums<G, U>(s, red[0]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            s[u] /= a.C;
+            q[u] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float d = v[u][k][i] - s[u];
+                    q[u] += (j + k * G) * VEC + i < a.C ? d * d : 0.f;
+                }
+        }
+        row_sums<G, U>(q, red[1]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (row[u] >= n) continue;
+            const float rs = 1.f / sqrtf(q[u] / a.C + a.eps);
+            char *yr = reinterpret_cast<char *>(a.y) + row[u] * a.y_stride * (YB ? 2 : 4);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c0 = (j + k * G) * VEC;
+                if (c0 >= a.C) continue;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[u][k][i] = ga[k][i] * ((v[u][k][i] - s[u]) * rs) + be[k][i];
+                store_row<YB, VEC>(yr, c0, a.C, v[u][k]);
+            }
+            if (j == 0) {
+                if (a.mean) a.mean[row[u]] = s[u];
+                if (a.rstd) a.rstd[row[u]] = rs;
+            }
         }
     }
 }
@@ -136,26 +142,27 @@ __global__ __launch_bounds__(G > kForward ? G : kForward) void k_norm(NormArgs a
 template <bool XB, bool YB>
 __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
     constexpr int VEC = XB || YB ? 8 : 4;
-    __shared__ float red[32];
+    __shared__ float red[2][16];
     const int64_t n = row_count(a.counters, a.rows);
     for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
         const char *xr = reinterpret_cast<const char *>(a.x) + r * a.x_stride * (XB ? 2 : 4);
         char *yr = reinterpret_cast<char *>(a.y) + r * a.y_stride * (YB ? 2 : 4);
         float v[VEC];
-        float s = 0.f;
+        float s[1] = {0.f}, q[1] = {0.f};
         for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
             load_row<XB, VEC>(xr, c, a.C, v);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s += v[i];
+            for (int i = 0; i < VEC; ++i) s[0] += v[i];
         }
-        const float mu = row_sum<1024>(s, red) / a.C;
-        float q = 0.f;
+        row_sums<1024, 1>(s, red[0]);
+        const float mu = s[0] / a.C;
         for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
             load_row<XB, VEC>(xr, c, a.C, v);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) q += c + i < a.C ? (v[i] - mu) * (v[i] - mu) : 0.f;
+            for (int i = 0; i < VEC; ++i) q[0] += c + i < a.C ? (v[i] - mu) * (v[i] - mu) : 0.f;
         }
-        const float rs = 1.f / sqrtf(row_sum<1024>(q, red) / a.C + a.eps);
+        row_sums<1024, 1>(q, red[1]);
+        const float rs = 1.f / sqrtf(q[0] / a.C + a.eps);
         for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
             load_row<XB, VEC>(xr, c, a.C, v);
             float ga[VEC], be[VEC];
@@ -180,7 +187,8 @@ template <bool XB, bool GB, int G, int NV>
 __global__ __launch_bounds__(kBackward) void k_norm_backward(NormBackwardArgs a, float *part) {
     constexpr int VEC = XB || GB ? 8 : 4;
     constexpr int RPB = kBackward / G;
-    __shared__ float red[64];
+    constexpr int U = at_once<G, NV>();
+    __shared__ float red[2][32];
     extern __shared__ float sums[];  // [RPB][G * NV * VEC]
     const int64_t n = row_count(a.counters, a.rows);
     const int j = threadIdx.x % G;
@@ -194,47 +202,57 @@ __global__ __launch_bounds__(kBackward) void k_norm_backward(NormBackwardArgs a,
             dg[k][i] = db[k][i] = 0.f;
         }
     }
-    const int64_t step = (int64_t)gridDim.x * RPB;
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < n; r0 += step) {
-        const int64_t r = r0 + threadIdx.x / G;
-        const bool on = r < n;
-        const int64_t rr = on ? r : n - 1;
-        const char *gr = reinterpret_cast<const char *>(a.g) + rr * a.g_stride * (GB ? 2 : 4);
-        const char *xr = reinterpret_cast<const char *>(a.x) + rr * a.x_stride * (XB ? 2 : 4);
-        float g[NV][VEC], h[NV][VEC];
+    const int64_t step = (int64_t)gridDim.x * RPB * U;
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB * U; r0 < n; r0 += step, turn ^= 1) {
+        float g[U][NV][VEC], h[U][NV][VEC], mu[U], rs[U], s[2 * U];
+        int64_t row[U];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            load_row<GB, VEC>(gr, (j + k * G) * VEC, a.C, g[k]);
-            load_row<XB, VEC>(xr, (j + k * G) * VEC, a.C, h[k]);
+        for (int u = 0; u < U; ++u) {
+            row[u] = r0 + u * RPB + threadIdx.x / G;
+            const int64_t r = row[u] < n ? row[u] : n - 1;
+            const char *gr = reinterpret_cast<const char *>(a.g) + r * a.g_stride * (GB ? 2 : 4);
+            const char *xr = reinterpret_cast<const char *>(a.x) + r * a.x_stride * (XB ? 2 : 4);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                load_row<GB, VEC>(gr, (j + k * G) * VEC, a.C, g[u][k]);
+                load_row<XB, VEC>(xr, (j + k * G) * VEC, a.C, h[u][k]);
+            }
+            mu[u] = a.mean[r];
+            rs[u] = a.rstd[r];
         }
-        const float mu = a.mean[rr], rs = a.rstd[rr];
-        float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int u = 0; u < U; ++u) {
+            s[2 * u] = s[2 * u + 1] = 0.f;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                h[k][i] = (h[k][i] - mu) * rs;
-                const float u = g[k][i] * ga[k][i];  // 0 past C
-                s1 += u;
-                s2 += u * h[k][i];
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    h[u][k][i] = (h[u][k][i] - mu[u]) * rs[u];
+                    const float t = g[u][k][i] * ga[k][i];  // 0 past C
+                    s[2 * u] += t;
+                    s[2 * u + 1] += t * h[u][k][i];
+                }
+        }
+        row_sums<G, 2 * U>(s, red[turn]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (row[u] >= n) continue;
+            const float s1 = s[2 * u] / a.C, s2 = s[2 * u + 1] / a.C;
+            char *or_ = reinterpret_cast<char *>(a.gx) + row[u] * a.gx_stride * (XB ? 2 : 4);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int c0 = (j + k * G) * VEC;
+                if (c0 >= a.C) continue;
+                float o[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    o[i] = rs[u] * (g[u][k][i] * ga[k][i] - s1 - h[u][k][i] * s2);
+                    dg[k][i] += g[u][k][i] * h[u][k][i];
+                    db[k][i] += g[u][k][i];
+                }
+                if (a.gx) store_row<XB, VEC>(or_, c0, a.C, o);
             }
-        row_sum2<G>(s1, s2, red);
-        if (!on) continue;
-        s1 /= a.C;
-        s2 /= a.C;
-        char *or_ = reinterpret_cast<char *>(a.gx) + r * a.gx_stride * (XB ? 2 : 4);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c0 = (j + k * G) * VEC;
-            if (c0 >= a.C) continue;
-            float o[VEC];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                o[i] = rs * (g[k][i] * ga[k][i] - s1 - h[k][i] * s2);
-                dg[k][i] += g[k][i] * h[k][i];
-                db[k][i] += g[k][i];
-            }
-            if (a.gx) store_row<XB, VEC>(or_, c0, a.C, o);
         }
     }
     if (!part) return;
@@ -261,15 +279,16 @@ __global__ __launch_bounds__(kBackward) void k_norm_backward(NormBackwardArgs a,
 template <bool XB, bool GB>
 __global__ __launch_bounds__(1024) void k_norm_backward_long(NormBackwardArgs a) {
     constexpr int VEC = XB || GB ? 8 : 4;
-    __shared__ float red[64];
+    __shared__ float red[2][32];
     const int64_t n = row_count(a.counters, a.rows);
-    for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < n; r += gridDim.x, turn ^= 1) {
         const char *gr = reinterpret_cast<const char *>(a.g) + r * a.g_stride * (GB ? 2 : 4);
         const char *xr = reinterpret_cast<const char *>(a.x) + r * a.x_stride * (XB ? 2 : 4);
         char *or_ = reinterpret_cast<char *>(a.gx) + r * a.gx_stride * (XB ? 2 : 4);
         const float mu = a.mean[r], rs = a.rstd[r];
         float g[VEC], x[VEC], ga[VEC];
-        float s1 = 0.f, s2 = 0.f;
+        float s[2] = {0.f, 0.f};
         for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
             load_row<GB, VEC>(gr, c, a.C, g);
             load_row<XB, VEC>(xr, c, a.C, x);
@@ -277,13 +296,12 @@ __global__ __launch_bounds__(1024) void k_norm_backward_long(NormBackwardArgs a)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 const float u = a.gamma ? g[i] * ga[i] : g[i];
-                s1 += u;
-                s2 += u * ((x[i] - mu) * rs);
+                s[0] += u;
+                s[1] += u * ((x[i] - mu) * rs);
             }
         }
-        row_sum2<1024>(s1, s2, red);
-        s1 /= a.C;
-        s2 /= a.C;
+        row_sums<1024, 2>(s, red[turn]);
+        const float s1 = s[0] / a.C, s2 = s[1] / a.C;
         for (int c = threadIdx.x * VEC; c < a.C; c += 1024 * VEC) {
             load_row<GB, VEC>(gr, c, a.C, g);
             load_row<XB, VEC>(xr, c, a.C, x);
@@ -355,7 +373,7 @@ hipError_t forward(lattice_dense *D, const NormArgs &a) {
 #define GO(G_, NV_)                                                                                              \
     if (s.G == G_ && s.NV == NV_) {                                                                              \
         constexpr int TB = G_ > kForward ? G_ : kForward;                                                        \
-        hipLaunchKernelGGL((k_norm<XB, YB, G_, NV_>), dim3(grid_for(a.rows, TB / G_, D->cu_count, 2048 / TB)), \
+        hipLaunchKernelGGL((k_norm<XB, YB, G_, NV_>), dim3(grid_for(a.rows, TB / G_ * at_once<G_, NV_>(), D->cu_count, 2048 / TB)), \
                            dim3(TB), 0, D->stream, a);                                                           \
     }
     NORM_SHAPES(GO)
