@@ -120,38 +120,58 @@ hipError_t launch_update(lattice_dense *D, const UpdateArgs &a);
 struct __attribute__((packed, aligned(4))) Words4 { uint32_t v[4]; };
 struct __attribute__((packed, aligned(2))) Halves8 { uint32_t v[4]; };
 
-// Eight or four consecutive channels c0.. of a row of C channels as fp32;
-// those past C are 0.  A row may start at any multiple of its element's size:
-// the vector loads of this chip take any such address.
+// Eight or four consecutive channels of a row as they are stored.
 template <bool BF16, int VEC>
-__device__ __forceinline__ void load_row(const void *row, int c0, int C, float *v) {
-    static_assert(VEC == 4 || VEC == 8, "channels per load");
+struct Raw {
+    static_assert(BF16 ? VEC == 8 : VEC == 4 || VEC == 8, "channels per load");
+    uint32_t w[BF16 ? 4 : VEC];
+};
+
+// Channels c0.. of a row of C channels; those past C are 0.  A row may start at
+// any multiple of its element's size: the vector loads of this chip take any
+// such address.
+template <bool BF16, int VEC>
+__device__ __forceinline__ void load_raw(const void *row, int c0, int C, Raw<BF16, VEC> &u) {
+    constexpr int WORDS = BF16 ? 4 : VEC;
     if (c0 + VEC <= C) {
         if constexpr (BF16) {
-            static_assert(!BF16 || VEC == 8, "16 bytes");
-            const Halves8 u = *reinterpret_cast<const Halves8 *>(reinterpret_cast<const uint16_t *>(row) + c0);
+            const Halves8 t = *reinterpret_cast<const Halves8 *>(reinterpret_cast<const uint16_t *>(row) + c0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = __uint_as_float(u.v[i] << 16);
-                v[2 * i + 1] = __uint_as_float(u.v[i] & 0xffff0000u);
-            }
+            for (int i = 0; i < 4; ++i) u.w[i] = t.v[i];
         } else {
 #pragma unroll
             for (int h = 0; h < VEC / 4; ++h) {
-                const Words4 u = *reinterpret_cast<const Words4 *>(reinterpret_cast<const float *>(row) + c0 + 4 * h);
+                const Words4 t = *reinterpret_cast<const Words4 *>(reinterpret_cast<const float *>(row) + c0 + 4 * h);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[4 * h + i] = __uint_as_float(u.v[i]);
+                for (int i = 0; i < 4; ++i) u.w[4 * h + i] = t.v[i];
             }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            v[i] = 0.f;
-            if (c0 + i < C)
-                v[i] = BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(row)[c0 + i])
-                            : reinterpret_cast<const float *>(row)[c0 + i];
+        for (int i = 0; i < WORDS; ++i) {
+            u.w[i] = 0;
+            if (BF16) {
+                if (c0 + 2 * i < C) u.w[i] = reinterpret_cast<const uint16_t *>(row)[c0 + 2 * i];
+                if (c0 + 2 * i + 1 < C) u.w[i] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[c0 + 2 * i + 1] << 16;
+            } else {
+                if (c0 + i < C) u.w[i] = reinterpret_cast<const uint32_t *>(row)[c0 + i];
+            }
         }
     }
+}
+template <bool BF16, int VEC>
+__device__ __forceinline__ void unpack(const Raw<BF16, VEC> &u, float *v) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+        v[i] = __uint_as_float(!BF16 ? u.w[BF16 ? 0 : i] : (i & 1) ? u.w[i / 2] & 0xffff0000u : u.w[i / 2] << 16);
+}
+
+// The same as fp32.
+template <bool BF16, int VEC>
+__device__ __forceinline__ void load_row(const void *row, int c0, int C, float *v) {
+    Raw<BF16, VEC> u;
+    load_raw<BF16, VEC>(row, c0, C, u);
+    unpack<BF16, VEC>(u, v);
 }
 
 // The reverse: values rounded to nearest even where the row is bf16.

@@ -23,7 +23,10 @@
 namespace {
 
 constexpr int kForward = 256;    // threads of a forward workgroup, at least
-constexpr int kBackward = 1024;  // threads of a backward workgroup
+// Threads of a backward workgroup: two of 512 a CU, each a row of partial sums
+// (16384 x 4096 in bf16: 80 us and 8 for the sums; one of 1024, 89 and 5).
+template <int G>
+constexpr int backward_threads() { return G > 512 ? G : 512; }
 
 __device__ __forceinline__ int64_t row_count(const int32_t *counters, int64_t rows) {
     if (!counters) return rows;
@@ -184,9 +187,9 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
 
 // part: [2][gridDim.x][C] partial dgamma and dbeta, or null without either.
 template <bool XB, bool GB, int G, int NV>
-__global__ __launch_bounds__(kBackward) void k_norm_backward(NormBackwardArgs a, float *part) {
+__global__ __launch_bounds__(backward_threads<G>(), 4) void k_norm_backward(NormBackwardArgs a, float *part) {
     constexpr int VEC = XB || GB ? 8 : 4;
-    constexpr int RPB = kBackward / G;
+    constexpr int THREADS = backward_threads<G>(), RPB = THREADS / G;
     constexpr int U = at_once<G, NV>();
     __shared__ float red[2][32];
     extern __shared__ float sums[];  // [RPB][G * NV * VEC]
@@ -268,7 +271,7 @@ __global__ __launch_bounds__(kBackward) void k_norm_backward(NormBackwardArgs a,
                 sums[(threadIdx.x / G) * WIDE + (j + k * G) * VEC + i] = which ? db[k][i] : dg[k][i];
         __syncthreads();
         float *row = part + ((int64_t)which * gridDim.x + blockIdx.x) * a.C;
-        for (int c = threadIdx.x; c < a.C; c += kBackward) {
+        for (int c = threadIdx.x; c < a.C; c += THREADS) {
             float s = 0.f;
             for (int w = 0; w < RPB; ++w) s += sums[w * WIDE + c];
             row[c] = s;
@@ -381,7 +384,9 @@ hipError_t forward(lattice_dense *D, const NormArgs &a) {
     return hipGetLastError();
 }
 
-unsigned backward_grid(const lattice_dense *D, int64_t rows, int rpb) { return grid_for(rows, rpb, D->cu_count, 1); }
+unsigned backward_grid(const lattice_dense *D, int64_t rows, int rpb, int threads) {
+    return grid_for(rows, rpb, D->cu_count, 1024 / threads);
+}
 
 template <bool XB, bool GB>
 hipError_t backward(lattice_dense *D, const NormBackwardArgs &a) {
@@ -400,12 +405,13 @@ hipError_t backward(lattice_dense *D, const NormBackwardArgs &a) {
         }
     } else {
         const Shape s = shape_of(a.C, VEC);
-        const unsigned grid = backward_grid(D, a.rows, kBackward / s.G);
+        const int threads = s.G > 512 ? s.G : 512;
+        const unsigned grid = backward_grid(D, a.rows, threads / s.G, threads);
         prows = grid;
 #define GO(G_, NV_)                                                                                               \
     if (s.G == G_ && s.NV == NV_)                                                                                 \
-        hipLaunchKernelGGL((k_norm_backward<XB, GB, G_, NV_>), dim3(grid), dim3(kBackward),                       \
-                           params ? kBackward * NV_ * VEC * sizeof(float) : 0, D->stream, a, part);
+        hipLaunchKernelGGL((k_norm_backward<XB, GB, G_, NV_>), dim3(grid), dim3(threads),                       \
+                           params ? threads * NV_ * VEC * sizeof(float) : 0, D->stream, a, part);
         NORM_SHAPES(GO)
 #undef GO
     }
@@ -422,10 +428,10 @@ hipError_t launch_layer_norm(lattice_dense *D, const NormArgs &a) {
     return a.y_bf16 ? forward<false, true>(D, a) : forward<false, false>(D, a);
 }
 
-// The partial rows are at most cu_count (or kLongSplit): one level of rowsum.
+// The partial rows are at most two a CU (or kLongSplit): one level of rowsum.
 int64_t layer_norm_backward_scratch(const lattice_dense *D, const NormBackwardArgs &a) {
     if (!a.grad_gamma && !a.grad_beta) return 0;
-    const int64_t rows = D->cu_count > kLongSplit ? D->cu_count : kLongSplit;
+    const int64_t rows = 2 * D->cu_count > kLongSplit ? 2 * D->cu_count : kLongSplit;
     return 2 * rows * a.C * (int64_t)sizeof(float);
 }
 
