@@ -382,6 +382,51 @@ struct Store : Simple {
     }
 };
 
+// Accumulators that an epilogue stored with Store (in one part), and another
+// epilogue for them.
+template <class T, class Epilogue>
+__global__ __launch_bounds__(T::THREADS) void k_gemm_again(Store stored, Epilogue epi) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Place at;
+    tile_of(stored.s, xcd_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
+    at.split = at.batch = 0;
+    const int wave = wave_index();
+    at.row0 = at.tile_m * T::BM + wave / T::WN * 32 * T::TM;
+    at.col0 = at.tile_n * T::BN + wave % T::WN * 32 * T::TN;
+    constexpr int ROOM = Epilogue::template lds<T>();
+    epi.template begin<T>(at, lds + ROOM);
+    f32x16_t acc[T::TM][T::TN];
+    const float *from = stored.out + stored.template place<T>(at, 0);
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 v = *reinterpret_cast<const float4 *>(from + ((i * T::TN + j) * 4 + q) * T::THREADS * 4);
+                acc[i][j][4 * q] = v.x;
+                acc[i][j][4 * q + 1] = v.y;
+                acc[i][j][4 * q + 2] = v.z;
+                acc[i][j][4 * q + 3] = v.w;
+            }
+    __syncthreads();
+    epi.template run<T>(acc, at, lds, lds + ROOM);
+}
+
+template <class T, class Epilogue>
+hipError_t launch_again(hipStream_t stream, const Store &stored, const Epilogue &epi) {
+    constexpr int LDS = Epilogue::template lds<T>() + Epilogue::template extra<T>();
+    static_assert(LDS <= 160 * 1024, "LDS");
+    if (LDS > 64 * 1024) {
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = allow_lds(reinterpret_cast<const void *>(&k_gemm_again<T, Epilogue>), LDS, done);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((k_gemm_again<T, Epilogue>), dim3((unsigned)(stored.s.tiles_m * stored.s.tiles_n)),
+                       dim3(T::THREADS), LDS, stream, stored, epi);
+    return hipGetLastError();
+}
+
 // A workgroup joins one row of 32 x 32 blocks of each wavefront (gridDim.y of
 // them), so that a few large tiles still give many workgroups.
 template <class T, class Epilogue>

@@ -11,7 +11,9 @@
 // piece of classes, the logits are computed again, G is formed from them in the
 // product's epilogue, in both orders, and multiplied with w and x.  The
 // second product of the logits costs a third more operations than the gradients
-// need; keeping the logits instead would cost rows x classes of memory.
+// need; where it would cost more than writing and reading the logits of a piece
+// of rows (fp32 operands, whose products are six each, from 256 channels on),
+// pieces are cut to a gigabyte of logits and these are kept till G is formed.
 //
 // The products run on the bf16 matrix cores (gemm.h): bf16 operands as they
 // are, fp32 ones as three planes.  G is rounded to bf16 for bf16 gradients (a
@@ -27,6 +29,7 @@ namespace {
 constexpr int kCounts = 256;          // partial counts of rows with a label
 constexpr int64_t kMaxPiece = 65536;  // rows of a piece
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of G in both orders
+constexpr int64_t kKeep = (int64_t)1 << 30;          // of kept logits
 
 __device__ __forceinline__ int label_of(int64_t t, int K, int64_t ignore) {
     return t != ignore && t >= 0 && t < K ? (int)t : -1;
@@ -94,6 +97,7 @@ struct Stats : gemm::Simple {
     int n;
     float2 *stats;      // [tiles of classes][n]
     float *picked;      // [n]
+    gemm::Store kept;   // keeps the accumulators if it has somewhere to
 
     template <class T>
     static constexpr int lds() { return T::WM * T::BN * 8; }
@@ -118,6 +122,7 @@ struct Stats : gemm::Simple {
                                         const char *own) const {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const int wm = wave / T::WN;
+        if (kept.out) kept.template run<T>(acc, at, nullptr, nullptr);
         const float *own_bias = reinterpret_cast<const float *>(own) + at.row0 - at.tile_m * T::BM;
         const int32_t *own_label = reinterpret_cast<const int32_t *>(own) + T::BM + at.col0 - at.tile_n * T::BN;
         float2 *part = reinterpret_cast<float2 *>(lds);
@@ -386,17 +391,20 @@ struct Grad : gemm::Simple {
 // Epilogue of a gradient's product: fp32 partial sums [split][rows][cols],
 // begun, or added to: the accumulators then start as them (reading them at the
 // end, with nothing left to multiply, took 55 of 330 us for 8192 x 1024 sums).
+// A product in one part and one piece gives the gradient itself.
 template <int P>
 struct Part : gemm::Simple {
     float *out;
     int rows, cols;
     bool add;
+    void *result;         // the gradient, or null
+    const float *factor;  // s
 
-    Part(float *out, int rows, int cols, bool add) : out(out), rows(rows), cols(cols), add(add) {}
+    Part(float *out, int rows, int cols, bool add, void *result, const float *factor)
+        : out(out), rows(rows), cols(cols), add(add), result(result), factor(factor) {}
 
     template <class T, class F>
     __device__ __forceinline__ void each(const gemm::Place &at, F &&f) const {
-        float *o = out + (int64_t)at.split * rows * cols;
 #pragma unroll
         for (int i = 0; i < T::TM; ++i)
 #pragma unroll
@@ -404,16 +412,29 @@ struct Part : gemm::Simple {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int row = at.row0 + 32 * i + gemm::acc_row(e), col = at.col0 + 32 * j + (threadIdx.x & 31);
-                    if (row < rows && col < cols) f(o + (int64_t)row * cols + col, i, j, e);
+                    if (row < rows && col < cols) f((int64_t)row * cols + col, i, j, e);
                 }
     }
     template <class T>
     __device__ __forceinline__ void init(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at) const {
-        if (add) each<T>(at, [&](const float *v, int i, int j, int e) { acc[i][j][e] = *v * (1.f / planes::kBack<P>); });
+        const float *o = out + (int64_t)at.split * rows * cols;
+        if (add) each<T>(at, [&](int64_t to, int i, int j, int e) { acc[i][j][e] = o[to] * (1.f / planes::kBack<P>); });
     }
     template <class T>
     __device__ __forceinline__ void run(gemm::f32x16_t (&acc)[T::TM][T::TN], const gemm::Place &at, char *, char *) const {
-        each<T>(at, [&](float *v, int i, int j, int e) { *v = acc[i][j][e] * planes::kBack<P>; });
+        if (result) {
+            const float s = *factor;
+            each<T>(at, [&](int64_t to, int i, int j, int e) {
+                const float v = acc[i][j][e] * planes::kBack<P> * s;
+                if (P == 1)
+                    reinterpret_cast<uint16_t *>(result)[to] = (uint16_t)pack_bf16(v, 0.f);
+                else
+                    reinterpret_cast<float *>(result)[to] = v;
+            });
+            return;
+        }
+        float *o = out + (int64_t)at.split * rows * cols;
+        each<T>(at, [&](int64_t to, int i, int j, int e) { o[to] = acc[i][j][e] * planes::kBack<P>; });
     }
 };
 
@@ -461,30 +482,29 @@ int tile_for(int64_t m, int64_t n, int cu) {
 }
 
 template <int P>
-int64_t tile_count(int kind, int64_t m, int64_t n) {
-    using X = Tiles<P>;
-    const int64_t bm = kind == 0 ? X::Large::BM : kind == 1 ? X::Middle::BM : X::Few::BM;
-    const int64_t bn = kind == 0 ? X::Large::BN : kind == 1 ? X::Middle::BN : X::Few::BN;
-    return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
-}
+int tile_m(int kind) { return kind == 3 ? 256 : kind == 0 ? Tiles<P>::Large::BM : kind == 1 ? Tiles<P>::Middle::BM : Tiles<P>::Few::BM; }
 
 template <int P>
-int tile_m(int kind) { return kind == 0 ? Tiles<P>::Large::BM : kind == 1 ? Tiles<P>::Middle::BM : Tiles<P>::Few::BM; }
+int tile_n(int kind) { return kind == 3 ? 64 : kind == 0 ? Tiles<P>::Large::BN : kind == 1 ? Tiles<P>::Middle::BN : Tiles<P>::Few::BN; }
+
+template <int P>
+int64_t tile_count(int kind, int64_t m, int64_t n) {
+    return (m + tile_m<P>(kind) - 1) / tile_m<P>(kind) * ((n + tile_n<P>(kind) - 1) / tile_n<P>(kind));
+}
 
 // Columns' partial rows of the bias gradient that a product over n rows gives.
 template <int P>
 int64_t bias_rows(int kind, int64_t n) {
     using X = Tiles<P>;
-    const int64_t bn = kind == 0 ? X::Large::BN : kind == 1 ? X::Middle::BN : X::Few::BN;
-    const int64_t wn = kind == 0 ? X::Large::WN : kind == 1 ? X::Middle::WN : X::Few::WN;
-    return (n + bn - 1) / bn * wn;
+    const int64_t wn = kind == 0 ? X::Large::WN : kind == 1 ? X::Middle::WN : 1;
+    return (n + tile_n<P>(kind) - 1) / tile_n<P>(kind) * wn;
 }
 
 // Splits of a contraction of k for m x n tiles that do not fill the chip.
 template <int P>
 int splits_for(int kind, int64_t m, int64_t n, int64_t k, int cu) {
     const int64_t t = tile_count<P>(kind, m, n);
-    int64_t s = (cu + t - 1) / t;
+    int64_t s = cu / t > 1 ? cu / t : 1;  // no more workgroups than CUs: one more takes as long again
     const int64_t most = k / 256 > 0 ? k / 256 : 1;
     s = s < most ? s : most;
     return (int)(s < 16 ? s : 16);
@@ -514,6 +534,114 @@ hipError_t product(hipStream_t st, int kind, const gemm::Operand &A, const gemm:
 bool lse_wide(const lattice_dense *D, int64_t n) { return n < (int64_t)64 * D->cu_count; }
 int64_t lse_blocks(const lattice_dense *D, int64_t n) { return lse_wide(D, n) ? (n + 3) / 4 : (n + 63) / 64; }
 
+// The first pass for at most 64 rows, straight from the caller's w: it is read
+// once, by lanes that each take the 8 channels of a class that their operand of
+// a product holds, and split there; laying it out first would read and write it
+// twice more (18 rows against 61228 x 1209 in fp32: 250 us so).  The rows' planes
+// go through LDS in slices of 64 channels.  Eight wavefronts of 32 classes each.
+struct FewTile {
+    static constexpr int BM = 256, BN = 64, WM = 8, WN = 1, TM = 1, TN = 2, THREADS = 512;
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(512, 4) void k_few(const void *__restrict__ w, int64_t w_stride, int K, int C,
+                                             gemm::Operand X, Stats<BF16 ? 1 : 3> epi) {
+    constexpr int P = BF16 ? 1 : 3, SLICE = P * 64 * 64 * 2;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x & 63, wave = gemm::wave_index();
+    gemm::Place at;
+    at.tile_m = blockIdx.x;
+    at.tile_n = at.split = at.batch = 0;
+    at.row0 = blockIdx.x * 256 + 32 * wave;
+    at.col0 = 0;
+    epi.template begin<FewTile>(at, lds + 2 * SLICE);
+    const int k = at.row0 + (lane & 31);
+    const char *row = reinterpret_cast<const char *>(w) + (int64_t)(k < K ? k : K - 1) * w_stride * (BF16 ? 2 : 4);
+    // a wavefront brings 8 rows of x of each plane: 8 chunks of 16 bytes a row,
+    // swizzled as in gemm.h
+    gemm::rsrc_t from[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) from[p] = gemm::buffer(X.p + p * X.plane);
+    const int xr = 8 * wave + lane / 8;
+    const uint32_t off = (uint32_t)(xr < X.rows ? xr : X.rows - 1) * (uint32_t)(X.ld * 2) + ((lane & 7) ^ ((xr >> 1) & 7)) * 16;
+    auto bring = [&](int buf, int c0) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            gemm::dma16(from[p], off, (uint32_t)c0 * 2, lds + buf * SLICE + p * 8192 + wave * 1024);
+    };
+    Raw<BF16, 8> now[4], next[4];
+    auto read = [&](int c0) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) load_raw<BF16, 8>(row, c0 + 16 * s + 8 * (lane >> 5), C, next[s]);
+    };
+    gemm::f32x16_t acc[1][2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[0][j][e] = 0.f;
+    bring(0, 0);
+    read(0);
+    int buf = 0;
+    for (int c0 = 0; c0 < C; c0 += 64, buf ^= 1) {
+        gemm::wait_and_barrier<0>();  // this slice is there, the other one is read no more
+#pragma unroll
+        for (int s = 0; s < 4; ++s) now[s] = next[s];
+        if (c0 + 64 < C) {
+            bring(buf ^ 1, c0 + 64);
+            read(c0 + 64);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            gemm::bf16x8_t a[P], b[P][2];
+            if constexpr (BF16) {
+                a[0] = __builtin_bit_cast(gemm::bf16x8_t, gemm::u32x4_t{now[s].w[0], now[s].w[1], now[s].w[2], now[s].w[3]});
+            } else {
+                float v[8];
+                unpack<BF16, 8>(now[s], v);
+                uint32_t h[4][P];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) planes::split_pair<P>(v[2 * i], v[2 * i + 1], h[i]);
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    a[p] = __builtin_bit_cast(gemm::bf16x8_t, gemm::u32x4_t{h[0][p], h[1][p], h[2][p], h[3][p]});
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int r = 32 * j + (lane & 31), chunk = 2 * s + (lane >> 5);
+                    b[p][j] = *reinterpret_cast<const gemm::bf16x8_t *>(lds + buf * SLICE + p * 8192 +
+                                                                        (r * 8 + (chunk ^ ((r >> 1) & 7))) * 16);
+                }
+#pragma unroll
+            for (int t = P - 1; t >= 0; --t)  // the smaller products first
+#pragma unroll
+                for (int p = 0; p <= t; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[0][j] = gemm::mfma(a[p], b[t - p][j], acc[0][j]);
+        }
+    }
+    gemm::wait_and_barrier<0>();
+    epi.template run<FewTile>(acc, at, lds, lds + 2 * SLICE);
+}
+
+template <int P>
+hipError_t launch_few(hipStream_t st, const LossArgs &a, const gemm::Operand &X, const Stats<P> &e) {
+    constexpr int LDS = 2 * P * 64 * 64 * 2 + Stats<P>::template extra<FewTile>();
+    static_assert(Stats<P>::template lds<FewTile>() <= 2 * P * 64 * 64 * 2 && LDS <= 64 * 1024, "LDS");
+    hipLaunchKernelGGL((k_few<P == 1>), dim3((a.K + 255) / 256), dim3(512), LDS, st, a.w, a.w_stride, a.K, a.C, X, e);
+    return hipGetLastError();
+}
+
+template <int P, class E>
+hipError_t again(hipStream_t st, int kind, const gemm::Store &kept, const E &e) {
+    using X = Tiles<P>;
+    if (kind == 0) return gemm::launch_again<typename X::Large>(st, kept, e);
+    if (kind == 1) return gemm::launch_again<typename X::Middle>(st, kept, e);
+    if (kind == 2) return gemm::launch_again<typename X::Few>(st, kept, e);
+    return gemm::launch_again<FewTile>(st, kept, e);
+}
+
 // Sizes of the pieces and where everything lies in the scratch.
 template <int P>
 struct Plan {
@@ -525,7 +653,9 @@ struct Plan {
     int64_t xpart, wpart;      // lengths of their contractions' parts
     int64_t xsplits, wsplits;  // and how many there are at most
     bool own_x, own_w;   // operands that have to be laid out first
-    int64_t count, bias, label, factor, lse, picked, stats, part, xp, xt, wp, wt, g, gt, pbias, bias_acc, px, pw, bytes;
+    bool keep;           // the logits of a piece of rows
+    bool one_piece;      // of rows, and of classes
+    int64_t count, bias, label, factor, lse, picked, stats, part, xp, xt, wp, wt, g, gt, pbias, bias_acc, px, pw, kept, bytes;
     int64_t parts;       // partial sums of the loss
 
     Plan(const lattice_dense *D, const LossArgs &a) {
@@ -538,24 +668,29 @@ struct Plan {
         const int64_t most = ((int64_t)1 << 25) / (Kpad / 128);
         if (R > most) R = most < 256 ? 256 : most / 256 * 256;
         if (R < 1) R = 1;
+        keep = P == 3 && C >= 256 && a.any_grad();
+        if (keep && R > 256 && R * Kpad > kKeep / 4) R = kKeep / 4 / Kpad > 256 ? kKeep / 4 / Kpad / 256 * 256 : 256;
         const int64_t Rp = gemm::padded(R), Rl = gemm::row_length(R);
         KP = kPieceBytes / (Rp * P * 2 * 2) / 256 * 256;
         KP = KP < 256 ? 256 : KP;
         KP = KP < Kpad ? KP : Kpad;
         const int64_t kp = KP < K ? KP : K;
-        fkind = tile_for<P>(K, R, cu);
-        gkind = tile_for<P>(kp, R, cu);
+        one_piece = a.N <= R && K <= KP;
+        auto as_is = [&](const void *q, int64_t stride) {
+            return P == 1 && C % gemm::kPad == 0 && stride % 8 == 0 && stride < gemm::kMaxLd && ((uintptr_t)q & 15) == 0;
+        };
+        // few rows: w as it is, if nothing else wants its planes
+        const bool few = a.N <= 64 && (P == 3 ? !a.any_grad() || keep : !a.any_grad() && !as_is(a.w, a.w_stride));
+        fkind = few ? 3 : tile_for<P>(K, R, cu);
+        gkind = keep ? fkind : tile_for<P>(kp, R, cu);
         xkind = split_tile_for<P>(R, C, kp, cu);
         wkind = split_tile_for<P>(kp, C, R, cu);
         xpart = gemm::part_length(gemm::padded(kp), splits_for<P>(xkind, R, C, kp, cu));
         wpart = gemm::part_length(Rp, splits_for<P>(wkind, kp, C, R, cu));
         xsplits = (gemm::padded(kp) + xpart - 1) / xpart;
         wsplits = (Rp + wpart - 1) / wpart;
-        auto as_is = [&](const void *q, int64_t stride) {
-            return P == 1 && C % gemm::kPad == 0 && stride % 8 == 0 && stride < gemm::kMaxLd && ((uintptr_t)q & 15) == 0;
-        };
-        own_x = !as_is(a.x, a.x_stride);
-        own_w = !as_is(a.w, a.w_stride);
+        own_x = few || !as_is(a.x, a.x_stride);
+        own_w = !few && !as_is(a.w, a.w_stride);
         ScratchLayout s;
         count = s.take(kCounts * 4);
         bias = s.take(Kpad * 4);
@@ -579,8 +714,9 @@ struct Plan {
             pbias = s.take((rows * kp + rowsum::scratch_floats(rows, kp)) * 4);
             bias_acc = s.take((a.N + R - 1) / R * K * 4);
         }
-        px = a.grad_x ? s.take(xsplits * R * C * 4) : 0;
-        pw = a.grad_w ? s.take(wsplits * K * C * 4) : 0;
+        px = a.grad_x ? s.take(one_piece && xsplits == 1 ? 0 : xsplits * R * C * 4) : 0;
+        pw = a.grad_w ? s.take(a.N <= R && wsplits == 1 ? 0 : wsplits * K * C * 4) : 0;
+        kept = keep ? s.take(tile_count<P>(fkind, K, R) * tile_m<P>(fkind) * tile_n<P>(fkind) * 4) : 0;
         bytes = s.bytes;
     }
 };
@@ -608,6 +744,8 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
         TRY(planes::launch<P>(st, a.bf16, s, 1, p.own_w ? h(p.wp) : nullptr, a.grad_x ? h(p.wt) : nullptr));
         if (p.own_w) W = planes::operand(h(p.wp), K, C, P);
     }
+    // gradients that their product's epilogue writes as they are
+    const bool x_at_once = p.one_piece && p.xsplits == 1, w_at_once = a.N <= p.R && p.wsplits == 1;
     int64_t parts = 0;
     int piece = 0;
     for (int64_t r0 = 0; r0 < a.N; r0 += p.R, ++piece) {
@@ -625,9 +763,14 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
             TRY(planes::launch<P>(st, a.bf16, s, 1, p.own_x ? h(p.xp) : nullptr, a.grad_w ? h(p.xt) : nullptr));
             if (p.own_x) X = planes::operand(h(p.xp), n, C, P);
         }
-        const Stats<P> stats = {{}, f(p.bias), ints(p.label), n, reinterpret_cast<float2 *>(ws + p.stats), f(p.picked)};
-        TRY((product<P>(st, p.fkind, W, X, Cp, Cp, stats)));
-        const int tiles = (K + tile_m<P>(p.fkind) - 1) / tile_m<P>(p.fkind);
+        const int bm = tile_m<P>(p.fkind), bn = tile_n<P>(p.fkind);
+        const int tiles = (K + bm - 1) / bm, tiles_n = (n + bn - 1) / bn;
+        const gemm::Store kept(p.keep ? f(p.kept) : nullptr, {(int)Cp, (int)Cp, tiles, tiles_n, false}, 1);
+        const Stats<P> stats = {{}, f(p.bias), ints(p.label), n, reinterpret_cast<float2 *>(ws + p.stats), f(p.picked), kept};
+        if (p.fkind == 3)
+            TRY(launch_few<P>(st, a, X, stats));
+        else
+            TRY((product<P>(st, p.fkind, W, X, Cp, Cp, stats)));
         const unsigned lse_grid = (unsigned)lse_blocks(D, n);
         float *row_loss = a.rows ? a.rows + r0 : nullptr;
         double *part = reinterpret_cast<double *>(ws + p.part) + parts;
@@ -650,23 +793,36 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
                                   gemm::row_length(kn), gemm::row_length(n),
                                   a.grad_x ? h(p.g) : nullptr, a.grad_w ? h(p.gt) : nullptr,
                                   a.grad_bias ? f(p.pbias) : nullptr, f(p.factor)};
-            TRY((product<P>(st, p.gkind, Wk, X, Cp, Cp, grad)));
+            bool formed = false;
+            if constexpr (P == 3) {
+                if (p.keep) {
+                    gemm::Store of = kept;  // the piece's tiles
+                    of.out += k0 / bm * tiles_n * (int64_t)bm * bn;
+                    of.s.tiles_m = (kn + bm - 1) / bm;
+                    TRY((again<P>(st, p.gkind, of, grad)));
+                    formed = true;
+                }
+            }
+            if (!formed) TRY((product<P>(st, p.gkind, Wk, X, Cp, Cp, grad)));
             if (a.grad_bias) {
                 const int64_t rows = bias_rows<P>(p.gkind, n);
-                TRY(rowsum::sum(st, f(p.pbias), rows, kn, f(p.pbias) + rows * kn,
-                                f(p.bias_acc) + (int64_t)piece * K + k0));
+                float *to = a.N <= p.R ? a.grad_bias + k0 : f(p.bias_acc) + (int64_t)piece * K + k0;
+                TRY(rowsum::sum(st, f(p.pbias), rows, kn, f(p.pbias) + rows * kn, to));
             }
             if (a.grad_x) {
                 gemm::Operand Wt = planes::operand(h(p.wt), C, K, P);
                 Wt.p += k0;
                 TRY((product<P>(st, p.xkind, planes::operand(h(p.g), n, kn, P), Wt, kp, p.xpart,
-                                Part<P>{f(p.px), n, C, k0 > 0})));
+                                Part<P>{f(p.px), n, C, k0 > 0, x_at_once ? a.grad_x : nullptr, f(p.factor)})));
             }
             if (a.grad_w) {
                 float *sums = f(p.pw) + k0 * C * p.wsplits;
                 TRY((product<P>(st, p.wkind, planes::operand(h(p.gt), kn, n, P), planes::operand(h(p.xt), C, n, P), np,
-                                p.wpart, Part<P>{sums, kn, C, r0 > 0})));
-                if (r0 + p.R >= a.N) {
+                                p.wpart,
+                                Part<P>{sums, kn, C, r0 > 0,
+                                        w_at_once ? reinterpret_cast<char *>(a.grad_w) + k0 * C * esz : nullptr,
+                                        f(p.factor)})));
+                if (r0 + p.R >= a.N && !w_at_once) {
                     const int64_t v = (int64_t)kn * C;
                     // a later piece of rows is no longer than the first, and has no more parts
                     const int splits = (int)(piece > 0 ? p.wsplits : (np + p.wpart - 1) / p.wpart);
@@ -676,7 +832,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
                 }
             }
         }
-        if (a.grad_x) {
+        if (a.grad_x && !x_at_once) {
             const int64_t v = (int64_t)n * C;
             hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, f(p.px),
                                (int)p.xsplits, v, f(p.factor),
@@ -687,7 +843,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
     hipLaunchKernelGGL(k_total, dim3(1), dim3(256), 0, st, reinterpret_cast<const double *>(ws + p.part), parts,
                        ints(p.count), a.mean, a.loss);
     TRY(hipGetLastError());
-    if (a.grad_bias) TRY(rowsum::sum(st, f(p.bias_acc), piece, K, nullptr, a.grad_bias));
+    if (a.grad_bias && piece != 1) TRY(rowsum::sum(st, f(p.bias_acc), piece, K, nullptr, a.grad_bias));
     if (a.N == 0 && a.grad_w) {
         const int64_t v = (int64_t)K * C;
         hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, nullptr, 0, v, nullptr,

@@ -17,6 +17,10 @@ from .lattice import _STORAGE, _TORCH, OK, Lattice, LatticeError, _ptr, load_lib
 
 F32 = torch.float32
 
+# the current stream's handle, without making a Stream object where torch can
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
 
 class Dense:
     """The dense operators on the current device and on one stream (the current
@@ -27,6 +31,7 @@ class Dense:
         self._lib = load_library()
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.device = self.stream.device
+        self._index, self._raw = self.device.index, self.stream.cuda_stream
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             st = self._lib.lattice_dense_create(ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h))
@@ -54,10 +59,10 @@ class Dense:
     def _call(self, fn, what: str, *args):
         if self._h is None:
             raise ValueError("the handle is closed")
-        here = torch.cuda.current_stream(self.device)
-        if here.cuda_stream == self.stream.cuda_stream:
+        if _raw_stream(self._index) == self._raw:
             st = fn(self._h, *args)
         else:
+            here = torch.cuda.current_stream(self.device)
             self.stream.wait_stream(here)
             st = fn(self._h, *args)
             here.wait_stream(self.stream)
@@ -89,6 +94,14 @@ class Dense:
             if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous [{n}]")
 
+    @staticmethod
+    def _like(x: torch.Tensor, dtype: torch.dtype) -> torch.Tensor:
+        """An empty contiguous tensor of x's shape (what empty_like gives for a
+        contiguous x takes the host half as long)."""
+        if dtype == x.dtype and x.is_contiguous():
+            return torch.empty_like(x)
+        return torch.empty(x.shape, dtype=dtype, device=x.device)
+
     # -- layer normalisation ----------------------------------------------
     def layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, out: Optional[torch.Tensor] = None, out_dtype: Optional[str] = None,
@@ -104,13 +117,14 @@ class Dense:
         self._vector(gamma, C, "gamma")
         self._vector(beta, C, "beta")
         if out is None:
-            out = torch.empty((rows, C), dtype=_TORCH[out_dtype] if out_dtype else x.dtype, device=x.device)
-        ys = self._rows(out, "out")
-        if out.shape != x.shape:
-            raise ValueError(f"out must be [{rows}, {C}]")
+            out, ys = self._like(x, _TORCH[out_dtype] if out_dtype else x.dtype), C
+        else:
+            ys = self._rows(out, "out")
+            if out.shape != x.shape:
+                raise ValueError(f"out must be [{rows}, {C}]")
         mean = rstd = None
         if want_stats:
-            mean, rstd = torch.empty((2, rows), dtype=F32, device=x.device)
+            mean, rstd = x.new_empty((2, rows), dtype=F32).unbind()
         if lattice is not None and rows < lattice._rows_needed():
             raise ValueError(f"x needs >= {lattice._rows_needed()} rows")
         self._call(self._lib.lattice_layer_norm, "layer_norm", lattice._h if lattice is not None else None,
@@ -135,15 +149,16 @@ class Dense:
         if lattice is not None and rows < lattice._rows_needed():
             raise ValueError(f"x needs >= {lattice._rows_needed()} rows")
         if grad_x is None and want_input:
-            grad_x = torch.empty((rows, C), dtype=x.dtype, device=x.device)
-        os_ = C
-        if grad_x is not None:
+            grad_x, os_ = self._like(x, x.dtype), C
+        elif grad_x is None:
+            os_ = C
+        else:
             os_ = self._rows(grad_x, "grad_x", (x.dtype,))
             if grad_x.shape != x.shape:
                 raise ValueError(f"grad_x must be [{rows}, {C}]")
         gg = gb = None
         if want_params:
-            gg, gb = torch.empty((2, C), dtype=F32, device=x.device)
+            gg, gb = x.new_empty((2, C), dtype=F32).unbind()
         self._call(self._lib.lattice_layer_norm_backward, "layer_norm_backward",
                    lattice._h if lattice is not None else None, grad_y.data_ptr(), _STORAGE[grad_y.dtype], gs,
                    x.data_ptr(), _STORAGE[x.dtype], xs, rows, C, mean.data_ptr(), rstd.data_ptr(), _ptr(gamma),
@@ -173,16 +188,16 @@ class Dense:
         self._vector(bias, K, "bias")
         if reduction not in ("mean", "sum"):
             raise ValueError("reduction must be 'mean' or 'sum'")
-        loss = torch.empty((), dtype=F32, device=x.device)
-        rows = torch.empty((N,), dtype=F32, device=x.device) if want_rows else None
+        loss = x.new_empty((), dtype=F32)
+        rows = x.new_empty((N,), dtype=F32) if want_rows else None
         gx = gw = gb = None
         if want_grad:
             if want_input:
-                gx = torch.empty((N, C), dtype=x.dtype, device=x.device)
+                gx = self._like(x, x.dtype)
             if want_weight:
-                gw = torch.empty((K, C), dtype=x.dtype, device=x.device)
+                gw = self._like(w, w.dtype)
             if want_bias if want_bias is not None else bias is not None:
-                gb = torch.empty((K,), dtype=F32, device=x.device)
+                gb = torch.empty_like(bias) if bias is not None else x.new_empty((K,), dtype=F32)
         self._call(self._lib.lattice_linear_cross_entropy, "linear_cross_entropy", _STORAGE[x.dtype], x.data_ptr(), xs,
                    N, C, w.data_ptr(), ws, K, _ptr(bias), target.data_ptr(), ignore_index, reduction == "mean",
                    loss.data_ptr(), _ptr(rows), _ptr(gx), _ptr(gw), _ptr(gb))
@@ -206,8 +221,9 @@ class Dense:
         if n > 1 and g.stride(-1) != 1 or m > 1 and rs < n:
             raise ValueError("g: the values of a row must be next to each other, and rows must not overlap")
         if out is None:
-            out = torch.empty(g.shape, dtype=_TORCH[out_dtype] if out_dtype else g.dtype, device=g.device)
-        self._dev(out, "out", _STORAGE)
+            out = self._like(g, _TORCH[out_dtype] if out_dtype else g.dtype)
+        else:
+            self._dev(out, "out", _STORAGE)
         if out.shape != g.shape or not out.is_contiguous():
             raise ValueError(f"out must be a contiguous {list(g.shape)}")
         a, b, c = coefficients
