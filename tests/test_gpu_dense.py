@@ -657,3 +657,19 @@ def test_a_lattice_that_cannot_give_the_rows(ops):
     with pytest.raises(ValueError):
         other.layer_norm(x)
     L.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_training_example(dtype):
+    """The operators together, with the lattice's: a few steps of the example
+    take the loss from that of a guess (log 8 = 2.08) to half of it."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_segmentation.py")
+    spec = importlib.util.spec_from_file_location("train_segmentation", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses = example.train(points=4000, steps=20, dtype=dtype, log=None)
+    assert all(math.isfinite(v) for v in losses)
+    assert losses[-1] < 0.5 * losses[0]
