@@ -127,6 +127,13 @@ struct Place {
 
 __device__ __forceinline__ int acc_row(int e) { return 8 * (e >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (e & 3); }
 
+// Workgroups go round robin to the eight XCDs: those of one XCD take consecutive
+// tiles, also where the tiles are no multiple of eight.
+__device__ __forceinline__ int64_t tile_order(int64_t b, int64_t n) {
+    const int64_t x = b % 8, left = n % 8;
+    return x * (n / 8) + (x < left ? x : left) + b / 8;
+}
+
 // Tile of workgroup b: consecutive workgroups of an XCD take the tiles of a
 // band of 8 tile rows, so that its L2 holds the operands they share.
 __device__ __forceinline__ void tile_of(const Shape &s, int64_t b, int &tm, int &tn) {
@@ -170,7 +177,7 @@ __global__ __launch_bounds__(T::THREADS) void k_gemm(Operand A, Operand B, Shape
     const int lane = threadIdx.x & 63;
     const int wave = wave_index();
     Place at;
-    tile_of(s, xcd_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
+    tile_of(s, tile_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
     at.split = blockIdx.y;
     at.batch = blockIdx.z;
     const int m0 = at.tile_m * T::BM, n0 = at.tile_n * T::BN;
@@ -388,7 +395,7 @@ template <class T, class Epilogue>
 __global__ __launch_bounds__(T::THREADS) void k_gemm_again(Store stored, Epilogue epi) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Place at;
-    tile_of(stored.s, xcd_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
+    tile_of(stored.s, tile_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
     at.split = at.batch = 0;
     const int wave = wave_index();
     at.row0 = at.tile_m * T::BM + wave / T::WN * 32 * T::TM;
@@ -432,7 +439,7 @@ hipError_t launch_again(hipStream_t stream, const Store &stored, const Epilogue 
 template <class T, class Epilogue>
 __global__ __launch_bounds__(T::THREADS) void k_gemm_join(Store parts, Epilogue epi) {
     Place at;
-    tile_of(parts.s, xcd_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
+    tile_of(parts.s, tile_order(blockIdx.x, gridDim.x), at.tile_m, at.tile_n);
     at.split = 0;
     at.batch = blockIdx.z;
     const int wave = wave_index(), i = blockIdx.y;
