@@ -175,10 +175,9 @@ __global__ __launch_bounds__(256) void k_fused_f32(FusedArgs f) {
     float *W = lds, *B = W + KT * 16 * L.ws, *red = B + KT * 16, *X = red + 4 * KT * 16 + 16, *G = X + kRows * L.xs;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int ct = L.cp / 16;
-    for (int e = threadIdx.x; e < KT * 16 * L.cp; e += 256) {
-        const int k = e / L.cp, c = e % L.cp;
-        W[k * L.ws + c] = k < a.K && c < a.C ? reinterpret_cast<const float *>(a.w)[k * a.w_stride + c] : 0.f;
-    }
+    for (int k = wave; k < KT * 16; k += 4)
+        for (int c = lane; c < L.cp; c += 64)
+            W[k * L.ws + c] = k < a.K && c < a.C ? reinterpret_cast<const float *>(a.w)[k * a.w_stride + c] : 0.f;
     for (int k = threadIdx.x; k < KT * 16; k += 256) B[k] = k < a.K ? (a.bias ? a.bias[k] : 0.f) : -INFINITY;
     float factor = 1.f;
     if (a.mean) {
@@ -195,16 +194,23 @@ __global__ __launch_bounds__(256) void k_fused_f32(FusedArgs f) {
     }
     double loss = 0.0;
     bool bad = false;
-    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.N; r0 += (int64_t)gridDim.x * kRows) {
+    // A block's rows are read while the one before it is worked on, into the
+    // registers that its logits have just freed.
+    float x[CT4 * 4][4];
+    int64_t target;
+    auto read = [&](int64_t p) {
+        const float *xr = reinterpret_cast<const float *>(a.x) + (p < a.N ? p : a.N - 1) * a.x_stride;
+#pragma unroll
+        for (int t = 0; t < CT4 * 4; ++t) load_row<false, 4>(xr, 16 * t + 4 * q, a.C, x[t]);
+        target = p < a.N ? a.target[p] : a.ignore;
+    };
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    if ((int64_t)blockIdx.x * kRows < a.N) read((int64_t)blockIdx.x * kRows + 16 * wave + i);
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.N; r0 += step) {
         const int64_t p = r0 + 16 * wave + i;
-        const int64_t target = p < a.N ? a.target[p] : a.ignore;
         const bool has = has_label(target, a.K, a.ignore);
         bad |= !has && target != a.ignore;
         const int label = has ? (int)target : -1;
-        const float *xr = reinterpret_cast<const float *>(a.x) + (p < a.N ? p : a.N - 1) * a.x_stride;
-        float x[CT4 * 4][4];
-#pragma unroll
-        for (int t = 0; t < CT4 * 4; ++t) load_row<false, 4>(xr, 16 * t + 4 * q, a.C, x[t]);
         f32x4_t z[KT];
 #pragma unroll
         for (int t = 0; t < KT; ++t) z[t] = *reinterpret_cast<const f32x4_t *>(B + 16 * t + 4 * q);
@@ -224,6 +230,7 @@ __global__ __launch_bounds__(256) void k_fused_f32(FusedArgs f) {
                 z[k] = mfma4(w.w, v.w, z[k]);
             }
         }
+        if (r0 + step < a.N) read(p + step);
         const float l = softmax<KT>(z, label, has);
         loss += l;
         if (a.rows && q == 0 && p < a.N) a.rows[p] = l;
@@ -289,12 +296,14 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
     float *B = reinterpret_cast<float *>(Xt + (GRAD ? L.cp * L.rs : 0)), *red = B + KT * 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int ct = (a.C + 15) / 16, cs = L.cp / 32;
-    for (int e = threadIdx.x; e < KT * 16 * L.cp; e += 256) {
-        const int k = e / L.cp, c = e % L.cp;
-        const uint16_t v = k < a.K && c < a.C ? reinterpret_cast<const uint16_t *>(a.w)[k * a.w_stride + c] : 0;
-        W[k * L.ws + c] = v;
+    for (int k = wave; k < KT * 16; k += 4) {
         // class 32 u + 16 h + 4 j + r lies at 32 u + 8 j + 4 h + r
-        if (GRAD) V[c * L.vs + (k & ~31) + ((k >> 2) & 3) * 8 + ((k >> 4) & 1) * 4 + (k & 3)] = v;
+        const int at = (k & ~31) + ((k >> 2) & 3) * 8 + ((k >> 4) & 1) * 4 + (k & 3);
+        for (int c = lane; c < L.cp; c += 64) {
+            const uint16_t v = k < a.K && c < a.C ? reinterpret_cast<const uint16_t *>(a.w)[k * a.w_stride + c] : 0;
+            W[k * L.ws + c] = v;
+            if (GRAD) V[c * L.vs + at] = v;
+        }
     }
     for (int k = threadIdx.x; k < KT * 16; k += 256) B[k] = k < a.K ? (a.bias ? a.bias[k] : 0.f) : -INFINITY;
     float factor = 1.f;
@@ -312,42 +321,40 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
     }
     double loss = 0.0;
     bool bad = false;
-    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.N; r0 += (int64_t)gridDim.x * kRows) {
+    // A block's rows are read while the one before it is worked on, into the
+    // registers that its logits have just freed.
+    Raw<true, 8> x[CT4 * 2];
+    int64_t target;
+    auto read = [&](int64_t p) {
+        const uint16_t *xr = reinterpret_cast<const uint16_t *>(a.x) + (p < a.N ? p : a.N - 1) * a.x_stride;
+#pragma unroll
+        for (int t = 0; t < CT4 * 2; ++t) load_raw<true, 8>(xr, 32 * t + 8 * q, a.C, x[t]);
+        target = p < a.N ? a.target[p] : a.ignore;
+    };
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    if ((int64_t)blockIdx.x * kRows < a.N) read((int64_t)blockIdx.x * kRows + 16 * wave + i);
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < a.N; r0 += step) {
         const int64_t p = r0 + 16 * wave + i;
-        const int64_t target = p < a.N ? a.target[p] : a.ignore;
         const bool has = has_label(target, a.K, a.ignore);
         bad |= !has && target != a.ignore;
         const int label = has ? (int)target : -1;
-        const uint16_t *xr = reinterpret_cast<const uint16_t *>(a.x) + (p < a.N ? p : a.N - 1) * a.x_stride;
-        u32x4_t x[CT4 * 2];
-#pragma unroll
-        for (int t = 0; t < CT4 * 2; ++t) {
-            const int c0 = 32 * t + 8 * q;
-            x[t] = u32x4_t{0, 0, 0, 0};
-            if (!has) continue;  // whatever a row without a label holds
-            if (c0 + 8 <= a.C) {
-                const Halves8 u = *reinterpret_cast<const Halves8 *>(xr + c0);
-                x[t] = u32x4_t{u.v[0], u.v[1], u.v[2], u.v[3]};
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c0 + j < a.C) x[t][j >> 1] |= (uint32_t)xr[c0 + j] << (16 * (j & 1));
-            }
-        }
         f32x4_t z[KT];
 #pragma unroll
         for (int t = 0; t < KT; ++t) z[t] = *reinterpret_cast<const f32x4_t *>(B + 16 * t + 4 * q);
 #pragma unroll
         for (int t = 0; t < CT4 * 2; ++t) {
             if (t >= cs) continue;
+            // whatever a row without a label holds
+            const u32x4_t v = has ? u32x4_t{x[t].w[0], x[t].w[1], x[t].w[2], x[t].w[3]} : u32x4_t{0, 0, 0, 0};
             if (GRAD)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    Xt[(32 * t + 8 * q + j) * L.rs + 16 * wave + i] = (uint16_t)(x[t][j >> 1] >> (16 * (j & 1)));
+                    Xt[(32 * t + 8 * q + j) * L.rs + 16 * wave + i] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
 #pragma unroll
             for (int k = 0; k < KT; ++k)
-                z[k] = mfma32(*reinterpret_cast<const u32x4_t *>(W + (16 * k + i) * L.ws + 32 * t + 8 * q), x[t], z[k]);
+                z[k] = mfma32(*reinterpret_cast<const u32x4_t *>(W + (16 * k + i) * L.ws + 32 * t + 8 * q), v, z[k]);
         }
+        if (r0 + step < a.N) read(p + step);
         const float l = softmax<KT>(z, label, has);
         loss += l;
         if (a.rows && q == 0 && p < a.N) a.rows[p] = l;
