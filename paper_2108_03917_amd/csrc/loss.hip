@@ -35,15 +35,33 @@ __device__ __forceinline__ int label_of(int64_t t, int K, int64_t ignore) {
     return t != ignore && t >= 0 && t < K ? (int)t : -1;
 }
 
-// Before the first piece: rows with a label, counted per workgroup (a label
-// that is neither a class nor `ignore` sets the status), the first piece's
-// labels, and the classes' biases, zeros without any and -inf from K on, so
-// that the classes that fill up the last tile have no share.
+// What is laid out before the first piece: of w, and of the piece's rows.
+struct Layout {
+    planes::Source s;
+    uint16_t *dst, *dst_t;
+    int64_t ld, ld_t;
+    int bx, blocks;  // blocks a row of them, and in all
+};
+
+// Everything before the first product, in one launch.  The first kCounts
+// workgroups: rows with a label, counted per workgroup (a label that is neither
+// a class nor `ignore` sets the status), the first piece's labels, and the
+// classes' biases, zeros without any and -inf from K on, so that the classes that
+// fill up the last tile have no share.  The others: the operands' planes.
+template <bool BF16, int P>
 __global__ __launch_bounds__(256) void k_begin(const int64_t *__restrict__ target, int64_t N, int n, int K,
                                                int64_t ignore, int32_t *count, int32_t *status, int32_t *label,
-                                               const float *bias, int Kp, float *padded_bias) {
+                                               const float *bias, int Kp, float *padded_bias, Layout w, Layout x) {
+    __shared__ planes::Block<P> block;
+    int at_ = (int)blockIdx.x - kCounts;
+    if (at_ >= 0) {
+        const Layout &l = at_ < w.blocks ? w : x;
+        at_ -= at_ < w.blocks ? 0 : w.blocks;
+        planes::lay_out<BF16, P>(l.s, at_ % l.bx, at_ / l.bx, 0, l.dst, l.ld, l.dst_t, l.ld_t, block);
+        return;
+    }
     int c = 0, bad = 0;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)kCounts * 256;
     for (int64_t i = at; i < N; i += step) {
         const int64_t t = target[i];
         const int l = label_of(t, K, ignore);
@@ -53,7 +71,7 @@ __global__ __launch_bounds__(256) void k_begin(const int64_t *__restrict__ targe
     }
     for (int64_t k = at; k < Kp; k += step) padded_bias[k] = k < K ? (bias ? bias[k] : 0.f) : -INFINITY;
     if (bad) atomicOr(status, DENSE_ST_LABEL);
-    __shared__ int red[4];
+    int *red = reinterpret_cast<int *>(&block);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) c += __shfl_xor(c, d);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
@@ -463,29 +481,39 @@ struct Tiles<1> {
     using Large = gemm::Tile<256, 256, 4, 2, 64, 1>;
     using Middle = gemm::Tile<128, 128, 2, 2, 64, 1>;
     using Few = gemm::Tile<128, 64, 4, 1, 64, 1>;
+    using Small = gemm::Tile<64, 64, 2, 2, 64, 1>;
 };
 template <>
 struct Tiles<3> {
     using Large = gemm::Tile<256, 128, 4, 2, 32, 3>;
     using Middle = gemm::Tile<128, 128, 2, 2, 32, 3>;
     using Few = gemm::Tile<128, 64, 4, 1, 32, 3>;
+    using Small = gemm::Tile<64, 64, 2, 2, 32, 3>;
 };
 
-// 0: Large, 1: Middle, 2: Few.  The large tile reads the least; it is for
-// products with enough of them to go round, and the last is for few columns.
+enum { LARGE, MIDDLE, FEW, STRAIGHT, SMALL };  // STRAIGHT: FewTile, of k_few
+
+// The large tile reads the least; it is for products with enough of them to go
+// round, and the one of 64 columns for few.
 template <int P>
 int tile_for(int64_t m, int64_t n, int cu) {
     using L = typename Tiles<P>::Large;
-    if (n <= 64) return 2;
+    if (n <= 64) return FEW;
     const int64_t large = (m + L::BM - 1) / L::BM * ((n + L::BN - 1) / L::BN);
-    return large * 4 >= (int64_t)cu * 3 ? 0 : 1;
+    return large * 4 >= (int64_t)cu * 3 ? LARGE : MIDDLE;
 }
 
 template <int P>
-int tile_m(int kind) { return kind == 3 ? 256 : kind == 0 ? Tiles<P>::Large::BM : kind == 1 ? Tiles<P>::Middle::BM : Tiles<P>::Few::BM; }
+int tile_m(int kind) {
+    using X = Tiles<P>;
+    return kind == LARGE ? X::Large::BM : kind == MIDDLE ? X::Middle::BM : kind == FEW ? X::Few::BM : kind == SMALL ? X::Small::BM : 256;
+}
 
 template <int P>
-int tile_n(int kind) { return kind == 3 ? 64 : kind == 0 ? Tiles<P>::Large::BN : kind == 1 ? Tiles<P>::Middle::BN : Tiles<P>::Few::BN; }
+int tile_n(int kind) {
+    using X = Tiles<P>;
+    return kind == LARGE ? X::Large::BN : kind == MIDDLE ? X::Middle::BN : kind == FEW ? X::Few::BN : kind == SMALL ? X::Small::BN : 64;
+}
 
 template <int P>
 int64_t tile_count(int kind, int64_t m, int64_t n) {
@@ -496,7 +524,7 @@ int64_t tile_count(int kind, int64_t m, int64_t n) {
 template <int P>
 int64_t bias_rows(int kind, int64_t n) {
     using X = Tiles<P>;
-    const int64_t wn = kind == 0 ? X::Large::WN : kind == 1 ? X::Middle::WN : 1;
+    const int64_t wn = kind == LARGE ? X::Large::WN : kind == MIDDLE ? X::Middle::WN : kind == SMALL ? X::Small::WN : 1;
     return (n + tile_n<P>(kind) - 1) / tile_n<P>(kind) * wn;
 }
 
@@ -510,22 +538,32 @@ int splits_for(int kind, int64_t m, int64_t n, int64_t k, int cu) {
     return (int)(s < 16 ? s : 16);
 }
 
-// The same for products whose contraction of k may be split: the large tile
-// too where parts of it that fill the chip are long.
+// For products whose contraction of k may be split: the large tile too where
+// parts of it that fill the chip are long.
 template <int P>
 int split_tile_for(int64_t m, int64_t n, int64_t k, int cu) {
     const int kind = tile_for<P>(m, n, cu);
     using L = typename Tiles<P>::Large;
-    if (kind != 1 || m < L::BM || n < L::BN) return kind;
-    return k / splits_for<P>(0, m, n, k, cu) >= 1024 ? 0 : 1;
+    if (kind != MIDDLE || m < L::BM || n < L::BN) return kind;
+    return k / splits_for<P>(LARGE, m, n, k, cu) >= 1024 ? LARGE : MIDDLE;
+}
+
+// For the logits, whose contraction is not split: the smallest tile where the
+// middle one would leave half the CUs idle (1332 x 439 over 1536 channels in
+// bf16: 10.6 us, and 14.4).
+template <int P>
+int logit_tile_for(int64_t m, int64_t n, int cu) {
+    const int kind = tile_for<P>(m, n, cu);
+    return kind == MIDDLE && tile_count<P>(MIDDLE, m, n) * 2 < cu ? SMALL : kind;
 }
 
 template <int P, class E>
 hipError_t product(hipStream_t st, int kind, const gemm::Operand &A, const gemm::Operand &B, int64_t K, int64_t part,
                    const E &e) {
     using X = Tiles<P>;
-    if (kind == 0) return gemm::launch<typename X::Large>(st, A, B, K, part, 1, false, e);
-    if (kind == 1) return gemm::launch<typename X::Middle>(st, A, B, K, part, 1, false, e);
+    if (kind == LARGE) return gemm::launch<typename X::Large>(st, A, B, K, part, 1, false, e);
+    if (kind == MIDDLE) return gemm::launch<typename X::Middle>(st, A, B, K, part, 1, false, e);
+    if (kind == SMALL) return gemm::launch<typename X::Small>(st, A, B, K, part, 1, false, e);
     return gemm::launch<typename X::Few>(st, A, B, K, part, 1, false, e);
 }
 
@@ -636,9 +674,10 @@ hipError_t launch_few(hipStream_t st, const LossArgs &a, const gemm::Operand &X,
 template <int P, class E>
 hipError_t again(hipStream_t st, int kind, const gemm::Store &kept, const E &e) {
     using X = Tiles<P>;
-    if (kind == 0) return gemm::launch_again<typename X::Large>(st, kept, e);
-    if (kind == 1) return gemm::launch_again<typename X::Middle>(st, kept, e);
-    if (kind == 2) return gemm::launch_again<typename X::Few>(st, kept, e);
+    if (kind == LARGE) return gemm::launch_again<typename X::Large>(st, kept, e);
+    if (kind == MIDDLE) return gemm::launch_again<typename X::Middle>(st, kept, e);
+    if (kind == SMALL) return gemm::launch_again<typename X::Small>(st, kept, e);
+    if (kind == FEW) return gemm::launch_again<typename X::Few>(st, kept, e);
     return gemm::launch_again<FewTile>(st, kept, e);
 }
 
@@ -681,8 +720,8 @@ struct Plan {
         };
         // few rows: w as it is, if nothing else wants its planes
         const bool few = a.N <= 64 && (P == 3 ? !a.any_grad() || keep : !a.any_grad() && !as_is(a.w, a.w_stride));
-        fkind = few ? 3 : tile_for<P>(K, R, cu);
-        gkind = keep ? fkind : tile_for<P>(kp, R, cu);
+        fkind = few ? STRAIGHT : logit_tile_for<P>(K, R, cu);
+        gkind = keep ? fkind : logit_tile_for<P>(kp, R, cu);
         xkind = split_tile_for<P>(R, C, kp, cu);
         wkind = split_tile_for<P>(kp, C, R, cu);
         xpart = gemm::part_length(gemm::padded(kp), splits_for<P>(xkind, R, C, kp, cu));
@@ -735,15 +774,20 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
     constexpr int BF = P == 1;
 
     const int first = (int)(a.N < p.R ? a.N : p.R);
-    hipLaunchKernelGGL(k_begin, dim3(kCounts), dim3(256), 0, st, a.target, a.N, first, K, a.ignore, ints(p.count),
-                       D->status, ints(p.label), a.bias, (int)p.Kpad, f(p.bias));
+    auto layout = [&](const void *from, int64_t stride, int64_t rows, bool labelled, uint16_t *to, uint16_t *to_t) {
+        const planes::Source s = {from, stride, 0, (int)rows, C, nullptr, labelled ? a.target : nullptr, K, a.ignore};
+        const int bx = (int)(Cp / 64);
+        return Layout{s, to, to_t, gemm::row_length(C), gemm::row_length(rows), bx,
+                      to || to_t ? bx * (int)(gemm::padded(rows) / 64) : 0};
+    };
+    const Layout lw = layout(a.w, a.w_stride, K, false, p.own_w ? h(p.wp) : nullptr, a.grad_x ? h(p.wt) : nullptr);
+    const Layout lx = layout(a.x, a.x_stride, first, true, p.own_x ? h(p.xp) : nullptr, a.grad_w ? h(p.xt) : nullptr);
+    hipLaunchKernelGGL((k_begin<P == 1, P>), dim3(kCounts + lw.blocks + lx.blocks), dim3(256), 0, st, a.target, a.N,
+                       first, K, a.ignore, ints(p.count), D->status, ints(p.label), a.bias, (int)p.Kpad, f(p.bias), lw,
+                       lx);
     TRY(hipGetLastError());
     gemm::Operand W = {reinterpret_cast<const uint16_t *>(a.w), a.w_stride, 0, 0, K};
-    if (p.own_w || a.grad_x) {
-        const planes::Source s = {a.w, a.w_stride, 0, K, C, nullptr, nullptr};
-        TRY(planes::launch<P>(st, a.bf16, s, 1, p.own_w ? h(p.wp) : nullptr, a.grad_x ? h(p.wt) : nullptr));
-        if (p.own_w) W = planes::operand(h(p.wp), K, C, P);
-    }
+    if (p.own_w) W = planes::operand(h(p.wp), K, C, P);
     // gradients that their product's epilogue writes as they are
     const bool x_at_once = p.one_piece && p.xsplits == 1, w_at_once = a.N <= p.R && p.wsplits == 1;
     int64_t parts = 0;
@@ -758,16 +802,16 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
             TRY(hipGetLastError());
         }
         gemm::Operand X = {reinterpret_cast<const uint16_t *>(x), a.x_stride, 0, 0, n};
-        if (p.own_x || a.grad_w) {
-            const planes::Source s = {x, a.x_stride, 0, n, C, ints(p.label), nullptr};
+        if (piece > 0 && (p.own_x || a.grad_w)) {
+            const planes::Source s = {x, a.x_stride, 0, n, C, nullptr, a.target + r0, K, a.ignore};
             TRY(planes::launch<P>(st, a.bf16, s, 1, p.own_x ? h(p.xp) : nullptr, a.grad_w ? h(p.xt) : nullptr));
-            if (p.own_x) X = planes::operand(h(p.xp), n, C, P);
         }
+        if (p.own_x) X = planes::operand(h(p.xp), n, C, P);
         const int bm = tile_m<P>(p.fkind), bn = tile_n<P>(p.fkind);
         const int tiles = (K + bm - 1) / bm, tiles_n = (n + bn - 1) / bn;
         const gemm::Store kept(p.keep ? f(p.kept) : nullptr, {(int)Cp, (int)Cp, tiles, tiles_n, false}, 1);
         const Stats<P> stats = {{}, f(p.bias), ints(p.label), n, reinterpret_cast<float2 *>(ws + p.stats), f(p.picked), kept};
-        if (p.fkind == 3)
+        if (p.fkind == STRAIGHT)
             TRY(launch_few<P>(st, a, X, stats));
         else
             TRY((product<P>(st, p.fkind, W, X, Cp, Cp, stats)));

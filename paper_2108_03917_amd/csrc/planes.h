@@ -137,28 +137,38 @@ struct Source {
     int64_t stride;   // values between rows
     int64_t batch;    // values between matrices
     int rows, cols;
-    const int32_t *label;      // a row whose label is negative is taken as zeros (whatever it holds), or null
     const double *mat_scale;   // every value of matrix b is multiplied by mat_scale[b] first, or null
+    // rows whose label is no class are taken as zeros, whatever they hold; or null
+    const int64_t *target;
+    int classes;
+    int64_t ignore;
+    __device__ __forceinline__ bool takes(int64_t r) const {
+        return !target || (target[r] != ignore && target[r] >= 0 && target[r] < classes);
+    }
 };
 
 // dst [batch][P][rows][ld] (ld values a row, zeros past cols up to a multiple of
 // kPad) and dst_t [batch][P][cols][ld_t]; either may be null.  A workgroup takes
-// a 64 x 64 block, 16 bytes a lane along rows on both sides, and transposes in
+// the 64 x 64 block (by, bx) of matrix b, 16 bytes a lane along rows on both sides, and transposes in
 // LDS (rows of 33 words: the columns that a wavefront writes at once fall on
 // different banks).  Bound by the bytes.
+template <int P>
+struct Block {
+    uint32_t t[P][64][33];
+};
 template <bool BF16, int P>
-__global__ __launch_bounds__(256) void k_planes(Source s, uint16_t *dst, int64_t ld, uint16_t *dst_t, int64_t ld_t) {
-    __shared__ uint32_t t[P][64][33];
-    const int c0 = blockIdx.x * 64, c = c0 + 8 * (threadIdx.x & 7);
-    const int64_t r0 = (int64_t)blockIdx.y * 64;
-    const int b = blockIdx.z;
+__device__ __forceinline__ void lay_out(const Source &s, int bx, int by, int b, uint16_t *dst, int64_t ld,
+                                        uint16_t *dst_t, int64_t ld_t, Block<P> &block) {
+    auto &t = block.t;
+    const int c0 = bx * 64, c = c0 + 8 * (threadIdx.x & 7);
+    const int64_t r0 = (int64_t)by * 64;
     const double ms = s.mat_scale ? s.mat_scale[b] : 1.0;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int rr = (threadIdx.x >> 3) + 32 * k;
         const int64_t r = r0 + rr;
         float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (r < s.rows && !(s.label && s.label[r] < 0)) {
+        if (r < s.rows && s.takes(r)) {
             const char *row = reinterpret_cast<const char *>(s.p) + (b * s.batch + r * s.stride) * (BF16 ? 2 : 4);
             load_row<BF16, 8>(row, c, s.cols, x);
             if (s.mat_scale)
@@ -191,6 +201,12 @@ __global__ __launch_bounds__(256) void k_planes(Source s, uint16_t *dst, int64_t
             *reinterpret_cast<uint4 *>(dst_t + ((int64_t)(b * P + p) * s.cols + c0 + cc) * ld_t + r0 + 2 * q) =
                 make_uint4(t[p][cc][q], t[p][cc][q + 1], t[p][cc][q + 2], t[p][cc][q + 3]);
     }
+}
+
+template <bool BF16, int P>
+__global__ __launch_bounds__(256) void k_planes(Source s, uint16_t *dst, int64_t ld, uint16_t *dst_t, int64_t ld_t) {
+    __shared__ Block<P> block;
+    lay_out<BF16, P>(s, blockIdx.x, blockIdx.y, blockIdx.z, dst, ld, dst_t, ld_t, block);
 }
 
 template <int P>

@@ -405,8 +405,8 @@ hipError_t steps(lattice_dense *D, const UpdateArgs &a, const Plan &p) {
     for (int64_t b0 = 0; b0 < a.batch; b0 += p.chunk) {
         const int64_t batch = a.batch - b0 < p.chunk ? a.batch - b0 : p.chunk;
         const planes::Source src = {reinterpret_cast<const char *>(a.g) + b0 * a.batch_stride * esz, a.row_stride,
-                                    a.batch_stride, a.m, a.n, nullptr,
-                                    reinterpret_cast<const double *>(ws + p.scale) + b0};
+                                    a.batch_stride, a.m, a.n,
+                                    reinterpret_cast<const double *>(ws + p.scale) + b0, nullptr, 0, 0};
         TRY(planes::launch<P>(st, a.g_bf16, src, batch, h(p.tall ? p.xt[0] : p.xr[0]), h(p.tall ? p.xr[0] : p.xt[0])));
         const gemm::Operand S = planes::operand(h(p.s), m, m, P), Q = planes::operand(h(p.q), m, m, P);
         for (int i = 0; i < a.steps; ++i) {
