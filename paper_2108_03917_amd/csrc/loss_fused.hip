@@ -175,9 +175,14 @@ __global__ __launch_bounds__(256) void k_fused_f32(FusedArgs f) {
     float *W = lds, *B = W + KT * 16 * L.ws, *red = B + KT * 16, *X = red + 4 * KT * 16 + 16, *G = X + kRows * L.xs;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int ct = L.cp / 16;
-    for (int k = wave; k < KT * 16; k += 4)
-        for (int c = lane; c < L.cp; c += 64)
-            W[k * L.ws + c] = k < a.K && c < a.C ? reinterpret_cast<const float *>(a.w)[k * a.w_stride + c] : 0.f;
+    {
+        // a row of w by as many threads as it has values, up to 64
+        const int wide = L.cp < 64 ? (L.cp <= 16 ? 16 : 32) : 64, c0 = threadIdx.x & (wide - 1);
+        for (int c = c0; c < L.cp; c += wide)
+#pragma unroll 4
+            for (int k = threadIdx.x / wide; k < KT * 16; k += 256 / wide)
+                W[k * L.ws + c] = k < a.K && c < a.C ? reinterpret_cast<const float *>(a.w)[k * a.w_stride + c] : 0.f;
+    }
     for (int k = threadIdx.x; k < KT * 16; k += 256) B[k] = k < a.K ? (a.bias ? a.bias[k] : 0.f) : -INFINITY;
     float factor = 1.f;
     if (a.mean) {
@@ -296,14 +301,16 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
     float *B = reinterpret_cast<float *>(Xt + (GRAD ? L.cp * L.rs : 0)), *red = B + KT * 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int ct = (a.C + 15) / 16, cs = L.cp / 32;
-    for (int k = wave; k < KT * 16; k += 4) {
-        // class 32 u + 16 h + 4 j + r lies at 32 u + 8 j + 4 h + r
-        const int at = (k & ~31) + ((k >> 2) & 3) * 8 + ((k >> 4) & 1) * 4 + (k & 3);
-        for (int c = lane; c < L.cp; c += 64) {
-            const uint16_t v = k < a.K && c < a.C ? reinterpret_cast<const uint16_t *>(a.w)[k * a.w_stride + c] : 0;
-            W[k * L.ws + c] = v;
-            if (GRAD) V[c * L.vs + at] = v;
-        }
+    {
+        const int wide = L.cp < 64 ? 32 : 64, c0 = threadIdx.x & (wide - 1);
+        for (int c = c0; c < L.cp; c += wide)
+#pragma unroll 4
+            for (int k = threadIdx.x / wide; k < KT * 16; k += 256 / wide) {
+                const uint16_t v = k < a.K && c < a.C ? reinterpret_cast<const uint16_t *>(a.w)[k * a.w_stride + c] : 0;
+                W[k * L.ws + c] = v;
+                // class 32 u + 16 h + 4 j + r lies at 32 u + 8 j + 4 h + r
+                if (GRAD) V[c * L.vs + (k & ~31) + ((k >> 2) & 3) * 8 + ((k >> 4) & 1) * 4 + (k & 3)] = v;
+            }
     }
     for (int k = threadIdx.x; k < KT * 16; k += 256) B[k] = k < a.K ? (a.bias ? a.bias[k] : 0.f) : -INFINITY;
     float factor = 1.f;
