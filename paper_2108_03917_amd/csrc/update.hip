@@ -280,18 +280,25 @@ struct Next : gemm::Simple {
     }
 };
 
-// Tiles, the largest first (square ones for the symmetric products).
+// Tiles, the largest first (square ones for the symmetric products).  Slices
+// of 64 values are read in whole 128-byte lines, but of three planes they leave
+// a CU room for one workgroup: Small is for products with a tile a CU at most
+// (640 x 1536 over 704 in 24 bits: 14.1 us, and 18.0 in slices of 32), Between
+// for a few more (704 x 1536: 16.5 us in 144 tiles of 128 x 64, 19.2 in 264 of
+// 64 x 64 in slices of 32).
 template <int P, bool LOWER>
 struct Tiles {
     using Large = gemm::Tile<256, 256, 2, 4, 32, 2>;
     using Middle = gemm::Tile<128, 128, 2, 2, 32, 2, 4>;
-    using Small = gemm::Tile<64, 64, 2, 2, 32, 2>;
+    using Between = gemm::Tile<64, 64, 2, 2, 32, 2>;
+    using Small = gemm::Tile<64, 64, 2, 2, 64, 2>;
 };
 template <bool LOWER>
 struct Tiles<3, LOWER> {
-    using Large = typename std::conditional<LOWER, gemm::Tile<128, 128, 2, 2, 32, 3>, gemm::Tile<256, 128, 4, 2, 32, 3>>::type;
     using Middle = gemm::Tile<128, 128, 2, 2, 32, 3>;
-    using Small = gemm::Tile<64, 64, 2, 2, 32, 3>;
+    using Large = typename std::conditional<LOWER, Middle, gemm::Tile<256, 128, 4, 2, 32, 3>>::type;
+    using Between = typename std::conditional<LOWER, gemm::Tile<64, 64, 2, 2, 32, 3>, gemm::Tile<128, 64, 4, 2, 64, 3>>::type;
+    using Small = gemm::Tile<64, 64, 2, 2, 64, 3>;
 };
 
 // Which tile a product takes and the length of its contraction's parts.  The
@@ -299,8 +306,10 @@ struct Tiles<3, LOWER> {
 // where parts of a long contraction give enough and each is still long (S of a
 // 2048 x 8192 matrix in 16 bits: 106 us in 7 parts, 182 in 128 x 128 tiles).
 // Else the largest tile that keeps half the CUs busy (its square: 42 us in 136
-// tiles of 128 x 128, 49 in 528 of 64 x 64), or the smallest, in parts if need
-// be (S of a 700 x 1531 matrix in 24 bits: 16 us in 4 parts, 31 in one).
+// tiles of 128 x 128, 49 in 528 of 64 x 64), or the smallest, in parts if the
+// contraction is long enough to pay for the launch that joins them, 7 us (S of
+// a 700 x 1531 matrix in 24 bits: 20 us in 3 parts, 25 in one; its square, over
+// 704: 14.6 in 3 parts, 11.5 in one).
 struct Choice {
     int kind;
     int64_t part, parts;
@@ -310,7 +319,8 @@ template <int P, bool LOWER>
 Choice choose(const lattice_dense *D, int64_t m, int64_t n, int64_t K, int64_t batch) {
     using X = Tiles<P, LOWER>;
     const int64_t cu = D->cu_count;
-    const int bm[3] = {X::Large::BM, X::Middle::BM, X::Small::BM}, bn[3] = {X::Large::BN, X::Middle::BN, X::Small::BN};
+    const int bm[4] = {X::Large::BM, X::Middle::BM, X::Between::BM, X::Small::BM};
+    const int bn[4] = {X::Large::BN, X::Middle::BN, X::Between::BN, X::Small::BN};
     auto tiles = [&](int k) { return batch * gemm::tiles_of(m, n, bm[k], bn[k], LOWER); };
     auto with = [&](int kind, int64_t splits) {
         const int64_t part = gemm::part_length(K, splits), parts = (K + part - 1) / part;
@@ -320,9 +330,10 @@ Choice choose(const lattice_dense *D, int64_t m, int64_t n, int64_t K, int64_t b
     const int64_t s = cu / tiles(0);
     if (K / s >= 1024) return with(0, s);
     if (tiles(1) * 2 >= cu) return with(1, 1);
-    if (tiles(2) * 2 >= cu) return with(2, 1);
-    const int64_t most = K / 192 > 1 ? K / 192 : 1, fill = cu / tiles(2);
-    return with(2, fill < most ? fill : most);
+    if (tiles(3) > cu) return with(2, 1);
+    if (tiles(3) * 2 >= cu || K < 1024) return with(3, 1);
+    const int64_t most = K / 256, fill = cu / tiles(3);
+    return with(3, fill < most ? fill : most);
 }
 
 template <int P, bool LOWER, class E>
@@ -332,6 +343,7 @@ hipError_t product(const lattice_dense *D, const gemm::Operand &A, const gemm::O
     const Choice c = choose<P, LOWER>(D, A.rows, B.rows, K, batch);
     if (c.kind == 0) return gemm::launch_parts<typename X::Large>(D->stream, A, B, K, c.part, batch, LOWER, e, parts);
     if (c.kind == 1) return gemm::launch_parts<typename X::Middle>(D->stream, A, B, K, c.part, batch, LOWER, e, parts);
+    if (c.kind == 2) return gemm::launch_parts<typename X::Between>(D->stream, A, B, K, c.part, batch, LOWER, e, parts);
     return gemm::launch_parts<typename X::Small>(D->stream, A, B, K, c.part, batch, LOWER, e, parts);
 }
 
