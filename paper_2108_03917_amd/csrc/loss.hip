@@ -463,7 +463,15 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, in
     const float f = splits > 0 ? *factor : 0.f;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         float s = 0.f;  // without any part, zeros
-        for (int k = 0; k < splits; ++k) s += part[k * n + i];
+        int k = 0;
+        for (; k + 8 <= splits; k += 8) {
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = part[(k + u) * n + i];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += x[u];
+        }
+        for (; k < splits; ++k) s += part[k * n + i];
         s *= f;
         if (BF16)
             reinterpret_cast<uint16_t *>(out)[i] = (uint16_t)pack_bf16(s, 0.f);
@@ -471,6 +479,10 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, in
             reinterpret_cast<float *>(out)[i] = s;
     }
 }
+
+struct FewTile {
+    static constexpr int BM = 256, BN = 64, WM = 8, WN = 1, TM = 1, TN = 2, THREADS = 512;
+};
 
 // Tiles: classes x rows for the logits, rows x channels and classes x channels
 // for the gradients.
@@ -482,6 +494,7 @@ struct Tiles<1> {
     using Middle = gemm::Tile<128, 128, 2, 2, 64, 1>;
     using Few = gemm::Tile<128, 64, 4, 1, 64, 1>;
     using Small = gemm::Tile<64, 64, 2, 2, 64, 1>;
+    using Thin = Small;
 };
 template <>
 struct Tiles<3> {
@@ -489,9 +502,10 @@ struct Tiles<3> {
     using Middle = gemm::Tile<128, 128, 2, 2, 32, 3>;
     using Few = gemm::Tile<128, 64, 4, 1, 32, 3>;
     using Small = gemm::Tile<64, 64, 2, 2, 32, 3>;
+    using Thin = gemm::Tile<64, 64, 2, 2, 64, 3>;
 };
 
-enum { LARGE, MIDDLE, FEW, STRAIGHT, SMALL };  // STRAIGHT: FewTile, of k_few
+enum { LARGE, MIDDLE, FEW, STRAIGHT, SMALL, THIN };  // STRAIGHT: FewTile, of k_few
 
 // The large tile reads the least; it is for products with enough of them to go
 // round, and the one of 64 columns for few.
@@ -506,13 +520,15 @@ int tile_for(int64_t m, int64_t n, int cu) {
 template <int P>
 int tile_m(int kind) {
     using X = Tiles<P>;
-    return kind == LARGE ? X::Large::BM : kind == MIDDLE ? X::Middle::BM : kind == FEW ? X::Few::BM : kind == SMALL ? X::Small::BM : 256;
+    const int of[] = {X::Large::BM, X::Middle::BM, X::Few::BM, FewTile::BM, X::Small::BM, X::Thin::BM};
+    return of[kind];
 }
 
 template <int P>
 int tile_n(int kind) {
     using X = Tiles<P>;
-    return kind == LARGE ? X::Large::BN : kind == MIDDLE ? X::Middle::BN : kind == FEW ? X::Few::BN : kind == SMALL ? X::Small::BN : 64;
+    const int of[] = {X::Large::BN, X::Middle::BN, X::Few::BN, FewTile::BN, X::Small::BN, X::Thin::BN};
+    return of[kind];
 }
 
 template <int P>
@@ -528,20 +544,29 @@ int64_t bias_rows(int kind, int64_t n) {
     return (n + tile_n<P>(kind) - 1) / tile_n<P>(kind) * wn;
 }
 
-// Splits of a contraction of k for m x n tiles that do not fill the chip.
+// Splits of a contraction of k for m x n tiles that do not fill the chip, each of
+// 256 values at least (100 x 256 over 50000 rows in fp32: 38 us in 112 parts and
+// 7 to join them, 146 and 17 in 16).
 template <int P>
 int splits_for(int kind, int64_t m, int64_t n, int64_t k, int cu) {
     const int64_t t = tile_count<P>(kind, m, n);
     int64_t s = cu / t > 1 ? cu / t : 1;  // no more workgroups than CUs: one more takes as long again
     const int64_t most = k / 256 > 0 ? k / 256 : 1;
     s = s < most ? s : most;
-    return (int)(s < 16 ? s : 16);
+    return (int)(s < 128 ? s : 128);
 }
 
-// For products whose contraction of k may be split: the large tile too where
-// parts of it that fill the chip are long.
+// For products whose contraction of k may be split.  Short contractions are
+// bound by what they write, and many small workgroups on a CU write while others
+// load (21384 x 472 over 43 rows in fp32: 24 us, 31 in large tiles; over 120
+// rows 33 and 38, in bf16 17 and 23; 50000 x 256 over 100 classes 42 and 43, in
+// bf16 20 and 25).  Few rows leave most of a tile of 128 empty (43 x 472 over
+// 21384: 19 us, 46 in 128 x 128).  Else the large tile too where parts of it
+// that fill the chip are long.
 template <int P>
 int split_tile_for(int64_t m, int64_t n, int64_t k, int cu) {
+    if (k <= 128) return SMALL;
+    if (m <= 64) return THIN;
     const int kind = tile_for<P>(m, n, cu);
     using L = typename Tiles<P>::Large;
     if (kind != MIDDLE || m < L::BM || n < L::BN) return kind;
@@ -564,6 +589,7 @@ hipError_t product(hipStream_t st, int kind, const gemm::Operand &A, const gemm:
     if (kind == LARGE) return gemm::launch<typename X::Large>(st, A, B, K, part, 1, false, e);
     if (kind == MIDDLE) return gemm::launch<typename X::Middle>(st, A, B, K, part, 1, false, e);
     if (kind == SMALL) return gemm::launch<typename X::Small>(st, A, B, K, part, 1, false, e);
+    if (kind == THIN) return gemm::launch<typename X::Thin>(st, A, B, K, part, 1, false, e);
     return gemm::launch<typename X::Few>(st, A, B, K, part, 1, false, e);
 }
 
@@ -575,14 +601,12 @@ int64_t lse_blocks(const lattice_dense *D, int64_t n) { return lse_wide(D, n) ? 
 // The first pass for at most 64 rows, straight from the caller's w: it is read
 // once, by lanes that each take the 8 channels of a class that their operand of
 // a product holds, and split there; laying it out first would read and write it
-// twice more (18 rows against 61228 x 1209 in fp32: 250 us so).  The rows' planes
-// go through LDS in slices of 64 channels.  Eight wavefronts of 32 classes each.
-struct FewTile {
-    static constexpr int BM = 256, BN = 64, WM = 8, WN = 1, TM = 1, TN = 2, THREADS = 512;
-};
-
+// twice more (18 rows against 61228 x 1209 in fp32: 250 us so, and 83, 3.6 TB/s
+// of w, straight).  The rows' planes go through LDS in slices of 64 channels.
+// Eight wavefronts of 32 classes each; one workgroup a CU for fp32, whose
+// registers spill otherwise (90 us).
 template <bool BF16>
-__global__ __launch_bounds__(512, 4) void k_few(const void *__restrict__ w, int64_t w_stride, int K, int C,
+__global__ __launch_bounds__(512, BF16 ? 4 : 2) void k_few(const void *__restrict__ w, int64_t w_stride, int K, int C,
                                              gemm::Operand X, Stats<BF16 ? 1 : 3> epi) {
     constexpr int P = BF16 ? 1 : 3, SLICE = P * 64 * 64 * 2;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -590,7 +614,7 @@ __global__ __launch_bounds__(512, 4) void k_few(const void *__restrict__ w, int6
     gemm::Place at;
     at.tile_m = blockIdx.x;
     at.tile_n = at.split = at.batch = 0;
-    at.row0 = blockIdx.x * 256 + 32 * wave;
+    at.row0 = blockIdx.x * FewTile::BM + 32 * wave;
     at.col0 = 0;
     epi.template begin<FewTile>(at, lds + 2 * SLICE);
     const int k = at.row0 + (lane & 31);
@@ -602,15 +626,22 @@ __global__ __launch_bounds__(512, 4) void k_few(const void *__restrict__ w, int6
     for (int p = 0; p < P; ++p) from[p] = gemm::buffer(X.p + p * X.plane);
     const int xr = 8 * wave + lane / 8;
     const uint32_t off = (uint32_t)(xr < X.rows ? xr : X.rows - 1) * (uint32_t)(X.ld * 2) + ((lane & 7) ^ ((xr >> 1) & 7)) * 16;
+    const bool both = X.rows > 32;  // halves of the tile's columns
     auto bring = [&](int buf, int c0) {
+        if (wave >= 4 && !both) return;
 #pragma unroll
         for (int p = 0; p < P; ++p)
             gemm::dma16(from[p], off, (uint32_t)c0 * 2, lds + buf * SLICE + p * 8192 + wave * 1024);
     };
     Raw<BF16, 8> now[4], next[4];
     auto read = [&](int c0) {
+        if (c0 + 64 <= C) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) load_raw<BF16, 8>(row, c0 + 16 * s + 8 * (lane >> 5), C, next[s]);
+            for (int s = 0; s < 4; ++s) load_raw<BF16, 8>(row, c0 + 16 * s + 8 * (lane >> 5), 1 << 30, next[s]);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) load_raw<BF16, 8>(row, c0 + 16 * s + 8 * (lane >> 5), C, next[s]);
+        }
     };
     gemm::f32x16_t acc[1][2];
 #pragma unroll
@@ -647,6 +678,7 @@ __global__ __launch_bounds__(512, 4) void k_few(const void *__restrict__ w, int6
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    if (j > 0 && !both) continue;
                     const int r = 32 * j + (lane & 31), chunk = 2 * s + (lane >> 5);
                     b[p][j] = *reinterpret_cast<const gemm::bf16x8_t *>(lds + buf * SLICE + p * 8192 +
                                                                         (r * 8 + (chunk ^ ((r >> 1) & 7))) * 16);
@@ -656,7 +688,8 @@ __global__ __launch_bounds__(512, 4) void k_few(const void *__restrict__ w, int6
 #pragma unroll
                 for (int p = 0; p <= t; ++p)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[0][j] = gemm::mfma(a[p], b[t - p][j], acc[0][j]);
+                    for (int j = 0; j < 2; ++j)
+                        if (j == 0 || both) acc[0][j] = gemm::mfma(a[p], b[t - p][j], acc[0][j]);
         }
     }
     gemm::wait_and_barrier<0>();
@@ -667,7 +700,7 @@ template <int P>
 hipError_t launch_few(hipStream_t st, const LossArgs &a, const gemm::Operand &X, const Stats<P> &e) {
     constexpr int LDS = 2 * P * 64 * 64 * 2 + Stats<P>::template extra<FewTile>();
     static_assert(Stats<P>::template lds<FewTile>() <= 2 * P * 64 * 64 * 2 && LDS <= 64 * 1024, "LDS");
-    hipLaunchKernelGGL((k_few<P == 1>), dim3((a.K + 255) / 256), dim3(512), LDS, st, a.w, a.w_stride, a.K, a.C, X, e);
+    hipLaunchKernelGGL((k_few<P == 1>), dim3((a.K + FewTile::BM - 1) / FewTile::BM), dim3(FewTile::THREADS), LDS, st, a.w, a.w_stride, a.K, a.C, X, e);
     return hipGetLastError();
 }
 
@@ -870,7 +903,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
                     const int64_t v = (int64_t)kn * C;
                     // a later piece of rows is no longer than the first, and has no more parts
                     const int splits = (int)(piece > 0 ? p.wsplits : (np + p.wpart - 1) / p.wpart);
-                    hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, sums,
+                    hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 256, D->cu_count)), dim3(256), 0, st, sums,
                                        splits, v, f(p.factor), reinterpret_cast<char *>(a.grad_w) + k0 * C * esz);
                     TRY(hipGetLastError());
                 }
@@ -878,7 +911,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
         }
         if (a.grad_x && !x_at_once) {
             const int64_t v = (int64_t)n * C;
-            hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, f(p.px),
+            hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 256, D->cu_count)), dim3(256), 0, st, f(p.px),
                                (int)p.xsplits, v, f(p.factor),
                                reinterpret_cast<char *>(a.grad_x) + r0 * C * esz);
             TRY(hipGetLastError());
@@ -890,7 +923,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
     if (a.grad_bias && piece != 1) TRY(rowsum::sum(st, f(p.bias_acc), piece, K, nullptr, a.grad_bias));
     if (a.N == 0 && a.grad_w) {
         const int64_t v = (int64_t)K * C;
-        hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 1024, D->cu_count)), dim3(256), 0, st, nullptr, 0, v, nullptr,
+        hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 256, D->cu_count)), dim3(256), 0, st, nullptr, 0, v, nullptr,
                            a.grad_w);
         TRY(hipGetLastError());
     }
