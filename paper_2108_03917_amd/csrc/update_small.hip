@@ -12,6 +12,10 @@
 //
 // Products as in gemm.h: operands in LDS as bf16 planes, two for a bf16 result
 // and three for an fp32 one, v_mfma_f32_32x32x16_bf16, fp32 sums.
+//
+// Bound by the chain of a step's three products in one workgroup: 64 x 576 in
+// fp32 takes 9 us a step (9 workgroups), twelve of 128 x 1152 take 19 (216 of
+// them) and 4.7 for the sums of the parts.
 #include "planes.h"
 #include "update.h"
 
