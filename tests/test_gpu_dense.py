@@ -413,6 +413,19 @@ def test_loss_in_pieces(ops, N, C, K, dtype):
     check_loss(got, loss_ref(x, w, t, bias, True), dtype)
 
 
+# Few rows (32 and 64 to a tile), few classes of many channels, and a long
+# contraction of few results: each takes tiles and parts of its own.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C,K", [(1, 1132, 645), (32, 320, 5000), (33, 472, 2100), (64, 301, 9000), (65, 90, 3000),
+                                   (128, 260, 1000), (3000, 260, 100), (20000, 300, 9)])
+def test_loss_few_rows_or_classes(ops, N, C, K, dtype):
+    x, w, t = rand(1, N, C, dtype=dtype), rand(2, K, C, dtype=dtype) * 0.1, labels(3, N, K)
+    bias = rand(4, K)
+    ref = loss_ref(x, w, t, bias, True)
+    check_loss(ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True), ref, dtype)
+    check(ops.linear_cross_entropy(x, w, t, bias), *ref["loss"], REL_F32, "loss alone")
+
+
 @pytest.mark.parametrize("K", [6, 200])
 def test_loss_gradient_against_differences(ops, K):
     N, C, d = 5, 12, 1e-2
@@ -472,6 +485,17 @@ def test_update(ops, m, n, gt, ot):
     assert got.dtype == T[ot]
     check_update(got, update_ref(g))
     assert torch.equal(got, ops.orthogonalize(g, out_dtype=ot))
+
+
+# Products of one tile a CU and of a few more, in one part and in several.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(640, 1536), (704, 1536), (1531, 700), (1030, 1030), (1500, 1510), (2048, 2100),
+                                 (300, 5000)])
+def test_update_of_larger_matrices(ops, m, n, dtype):
+    g = rand(1, m, n, dtype=dtype)
+    got = ops.orthogonalize(g)
+    check_update(got, update_ref(g))
+    assert torch.equal(got, ops.orthogonalize(g))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
