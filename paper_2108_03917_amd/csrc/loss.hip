@@ -486,7 +486,7 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, in
 }
 
 struct FewTile {
-    static constexpr int BM = 256, BN = 64, WM = 8, WN = 1, TM = 1, TN = 2, THREADS = 512;
+    static constexpr int BM = 128, BN = 64, WM = 4, WN = 1, TM = 1, TN = 2, THREADS = 256;
 };
 
 // Tiles: classes x rows for the logits, rows x channels and classes x channels
@@ -606,13 +606,15 @@ int64_t lse_blocks(const lattice_dense *D, int64_t n) { return lse_wide(D, n) ? 
 // The first pass for at most 64 rows, straight from the caller's w: it is read
 // once, by lanes that each take the 8 channels of a class that their operand of
 // a product holds, and split there; laying it out first would read and write it
-// twice more (18 rows against 61228 x 1209 in fp32: 250 us so, and 83, 3.6 TB/s
-// of w, straight).  The rows' planes go through LDS in slices of 64 channels.
-// Eight wavefronts of 32 classes each; one workgroup a CU for fp32, whose
-// registers spill otherwise (90 us).
+// twice more (18 rows against 61228 x 1209 in fp32: 250 us so, and 79, 3.7 TB/s
+// of w, straight).  The rows' planes go through LDS in slices of 64 channels, of
+// 32 rows only where there are no more.  Four wavefronts of 32 classes each: what
+// a CU's wavefronts read of scattered rows of w adds up, so that fewer to a CU
+// are faster where there are CUs left (5 rows against 6450 x 1132: 34 us, 51 with
+// eight), and with two the rows' planes are read too often (97 of 79 us above).
 template <bool BF16>
-__global__ __launch_bounds__(512, BF16 ? 4 : 2) void k_few(const void *__restrict__ w, int64_t w_stride, int K, int C,
-                                             gemm::Operand X, Stats<BF16 ? 1 : 3> epi) {
+__global__ __launch_bounds__(256, BF16 ? 4 : 2) void k_few(const void *__restrict__ w, int64_t w_stride, int K, int C,
+                                                                   gemm::Operand X, Stats<BF16 ? 1 : 3> epi) {
     constexpr int P = BF16 ? 1 : 3, SLICE = P * 64 * 64 * 2;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = gemm::wave_index();
@@ -624,19 +626,26 @@ __global__ __launch_bounds__(512, BF16 ? 4 : 2) void k_few(const void *__restric
     epi.template begin<FewTile>(at, lds + 2 * SLICE);
     const int k = at.row0 + (lane & 31);
     const char *row = reinterpret_cast<const char *>(w) + (int64_t)(k < K ? k : K - 1) * w_stride * (BF16 ? 2 : 4);
-    // a wavefront brings 8 rows of x of each plane: 8 chunks of 16 bytes a row,
+    // a wavefront's load brings 8 rows of a plane of x: 8 chunks of 16 bytes a row,
     // swizzled as in gemm.h
     gemm::rsrc_t from[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) from[p] = gemm::buffer(X.p + p * X.plane);
-    const int xr = 8 * wave + lane / 8;
-    const uint32_t off = (uint32_t)(xr < X.rows ? xr : X.rows - 1) * (uint32_t)(X.ld * 2) + ((lane & 7) ^ ((xr >> 1) & 7)) * 16;
+    constexpr int NW = FewTile::WM, U = 8 / NW;
+    uint32_t off[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int xr = 8 * (NW * u + wave) + lane / 8;
+        off[u] = (uint32_t)(xr < X.rows ? xr : X.rows - 1) * (uint32_t)(X.ld * 2) + ((lane & 7) ^ ((xr >> 1) & 7)) * 16;
+    }
     const bool both = X.rows > 32;  // halves of the tile's columns
     auto bring = [&](int buf, int c0) {
-        if (wave >= 4 && !both) return;
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-            gemm::dma16(from[p], off, (uint32_t)c0 * 2, lds + buf * SLICE + p * 8192 + wave * 1024);
+        for (int u = 0; u < U; ++u)
+            if (u < U / 2 || both)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    gemm::dma16(from[p], off[u], (uint32_t)c0 * 2, lds + buf * SLICE + p * 8192 + (NW * u + wave) * 1024);
     };
     Raw<BF16, 8> now[4], next[4];
     auto read = [&](int c0) {
