@@ -12,8 +12,10 @@
 // product's epilogue, in both orders, and multiplied with w and x.  The
 // second product of the logits costs a third more operations than the gradients
 // need; where it would cost more than writing and reading the logits of a piece
-// of rows (fp32 operands, whose products are six each, from 256 channels on),
-// pieces are cut to a gigabyte of logits and these are kept till G is formed.
+// of rows (fp32 operands, whose products are six each, from 192 channels on),
+// pieces are cut to a gigabyte of logits and these are kept till G is formed
+// (both passes over 1848 x 18928 logits of 245 channels: 265 us kept, 308 again;
+// of 192 channels 229 and 248, of 128 200 and 207).
 //
 // The products run on the bf16 matrix cores (gemm.h): bf16 operands as they
 // are, fp32 ones as three planes.  G is rounded to bf16 for bf16 gradients (a
@@ -754,7 +756,7 @@ struct Plan {
         const int64_t most = ((int64_t)1 << 25) / (Kpad / 128);
         if (R > most) R = most < 256 ? 256 : most / 256 * 256;
         if (R < 1) R = 1;
-        keep = P == 3 && C >= 256 && a.any_grad();
+        keep = P == 3 && C >= 192 && a.any_grad();
         if (keep && R > 256 && R * Kpad > kKeep / 4) R = kKeep / 4 / Kpad > 256 ? kKeep / 4 / Kpad / 256 * 256 : 256;
         const int64_t Rp = gemm::padded(R), Rl = gemm::row_length(R);
         KP = kPieceBytes / (Rp * P * 2 * 2) / 256 * 256;
