@@ -37,6 +37,10 @@ constexpr int kCounts = 256;          // partial counts of rows with a label
 constexpr int64_t kMaxPiece = 65536;  // rows of a piece
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;  // of G in both orders
 constexpr int64_t kKeep = (int64_t)1 << 30;          // of kept logits
+// Pieces of rows whose bias gradients are held apart before they are added up
+// (each time rounded to fp32 once): with room for all of them the scratch would
+// grow with the rows.
+constexpr int64_t kHeld = 64;
 
 __device__ __forceinline__ int label_of(int64_t t, int K, int64_t ignore) {
     return t != ignore && t >= 0 && t < K ? (int)t : -1;
@@ -800,7 +804,8 @@ struct Plan {
         if (a.grad_bias) {
             const int64_t rows = bias_rows<P>(gkind, R);
             pbias = s.take((rows * kp + rowsum::scratch_floats(rows, kp)) * 4);
-            bias_acc = s.take((a.N + R - 1) / R * K * 4);
+            const int64_t pieces = (a.N + R - 1) / R;
+            bias_acc = s.take((pieces < kHeld ? pieces : kHeld) * K * 4);
         }
         px = a.grad_x ? s.take(one_piece && xsplits == 1 ? 0 : xsplits * R * C * 4) : 0;
         pw = a.grad_w ? s.take(a.N <= R && wsplits == 1 ? 0 : wsplits * K * C * 4) : 0;
@@ -840,8 +845,13 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
     // gradients that their product's epilogue writes as they are
     const bool x_at_once = p.one_piece && p.xsplits == 1, w_at_once = a.N <= p.R && p.wsplits == 1;
     int64_t parts = 0;
-    int piece = 0;
+    int piece = 0, held = 0;  // pieces, and rows of bias_acc that wait to be added
     for (int64_t r0 = 0; r0 < a.N; r0 += p.R, ++piece) {
+        if (a.grad_bias && held == kHeld) {
+            // into the first of them: a workgroup reads all of its columns before it writes them
+            TRY(rowsum::sum(st, f(p.bias_acc), held, K, nullptr, f(p.bias_acc)));
+            held = 1;
+        }
         const int n = (int)(a.N - r0 < p.R ? a.N - r0 : p.R);
         const int64_t np = gemm::padded(n);
         const char *x = reinterpret_cast<const char *>(a.x) + r0 * a.x_stride * esz;
@@ -899,7 +909,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
             if (!formed) TRY((product<P>(st, p.gkind, Wk, X, Cp, Cp, grad)));
             if (a.grad_bias) {
                 const int64_t rows = bias_rows<P>(p.gkind, n);
-                float *to = a.N <= p.R ? a.grad_bias + k0 : f(p.bias_acc) + (int64_t)piece * K + k0;
+                float *to = a.N <= p.R ? a.grad_bias + k0 : f(p.bias_acc) + (int64_t)held * K + k0;
                 TRY(rowsum::sum(st, f(p.pbias), rows, kn, f(p.pbias) + rows * kn, to));
             }
             if (a.grad_x) {
@@ -925,6 +935,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
                 }
             }
         }
+        ++held;
         if (a.grad_x && !x_at_once) {
             const int64_t v = (int64_t)n * C;
             hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 256, D->cu_count)), dim3(256), 0, st, f(p.px),
@@ -936,7 +947,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
     hipLaunchKernelGGL(k_total, dim3(1), dim3(256), 0, st, reinterpret_cast<const double *>(ws + p.part), parts,
                        ints(p.count), a.mean, a.loss);
     TRY(hipGetLastError());
-    if (a.grad_bias && piece != 1) TRY(rowsum::sum(st, f(p.bias_acc), piece, K, nullptr, a.grad_bias));
+    if (a.grad_bias && piece != 1) TRY(rowsum::sum(st, f(p.bias_acc), held, K, nullptr, a.grad_bias));
     if (a.N == 0 && a.grad_w) {
         const int64_t v = (int64_t)K * C;
         hipLaunchKernelGGL((k_join<BF>), dim3(grid_for(v, 256, D->cu_count)), dim3(256), 0, st, nullptr, 0, v, nullptr,

@@ -107,9 +107,11 @@ inline hipError_t launch_level(hipStream_t stream, const Job *job, int count, in
 }
 
 // out[0..n) = column sums of part [rows][n]; `tmp` holds scratch_floats(rows,
-// n) floats (the levels' chunk sums).  rows = 0 writes zeros.
+// n) floats (the levels' chunk sums; null is an error where it is any).  rows = 0
+// writes zeros.
 inline hipError_t sum(hipStream_t stream, const float *part, int64_t rows, int64_t n, float *tmp, float *out) {
     if (n <= 0) return hipSuccess;
+    if (rows > kRsChunk && !tmp) return hipErrorInvalidValue;
     while (rows > kRsChunk) {
         const int64_t chunks = (rows + kRsChunk - 1) / kRsChunk;
         const Job job = {part, tmp, rows, n};

@@ -1,0 +1,218 @@
+// The dense operators' host side without a GPU: this program is linked with
+// the library and defines the HIP calls that it makes, so that what a call
+// allocates, frees and launches, with which arguments and on which device, can
+// be looked at.  No kernel runs, and no address that hipMalloc gives is read or
+// written: they only stand for device memory.
+//
+//   host_driver CHECK      prints "ok", or what is wrong and exits with 1
+#include <hip/hip_runtime_api.h>
+
+#include <cstdarg>
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <map>
+#include <string>
+#include <vector>
+
+#include "lattice.h"
+
+namespace {
+
+[[noreturn]] void fail(const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    std::vprintf(fmt, ap);
+    va_end(ap);
+    std::printf("\n");
+    std::exit(1);
+}
+
+struct Launch {
+    std::string name;
+    dim3 grid;
+    int device;
+    void **args;
+};
+
+int device = 0;                           // current
+hipError_t last = hipSuccess;
+std::map<uintptr_t, size_t> blocks;       // live, by address
+uintptr_t next_address = (uintptr_t)1 << 44;
+int64_t launches = 0;
+int alloc_device = -1;                    // that the last block was made on
+void (*on_launch)(const Launch &) = nullptr;
+dim3 pushed_grid, pushed_block;
+size_t pushed_lds;
+hipStream_t pushed_stream;
+
+std::map<const void *, std::string> &names() {
+    static std::map<const void *, std::string> all;   // filled before main
+    return all;
+}
+
+// The live block that holds [p, p + bytes), or 0.
+uintptr_t block_of(const void *p, int64_t bytes) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    auto it = blocks.upper_bound(a);
+    if (it == blocks.begin()) return 0;
+    --it;
+    return bytes >= 0 && a + (uintptr_t)bytes <= it->first + it->second ? it->first : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+void **__hipRegisterFatBinary(const void *) {
+    static void *module;
+    return &module;
+}
+void __hipUnregisterFatBinary(void **) {}
+void __hipRegisterVar(void **, void *, char *, char *, int, size_t, int, int) {}
+void __hipRegisterFunction(void **, const void *host, char *, const char *name, unsigned, void *, void *, void *, void *,
+                           int *) {
+    names()[host] = name;
+}
+hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t lds, hipStream_t stream) {
+    pushed_grid = grid;
+    pushed_block = block;
+    pushed_lds = lds;
+    pushed_stream = stream;
+    return hipSuccess;
+}
+hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *lds, hipStream_t *stream) {
+    *grid = pushed_grid;
+    *block = pushed_block;
+    *lds = pushed_lds;
+    *stream = pushed_stream;
+    return hipSuccess;
+}
+hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, size_t lds, hipStream_t) {
+    if (!grid.x || !grid.y || !grid.z || !block.x || !block.y || !block.z || block.x * block.y * block.z > 1024 ||
+        lds > 160 * 1024)
+        return last = hipErrorInvalidConfiguration;
+    ++launches;
+    if (on_launch) on_launch({names()[fn], grid, device, args});
+    return hipSuccess;
+}
+hipError_t hipGetLastError(void) {
+    const hipError_t e = last;
+    last = hipSuccess;
+    return e;
+}
+const char *hipGetErrorString(hipError_t e) { return e == hipSuccess ? "no error" : "an error"; }
+hipError_t hipGetDevice(int *d) {
+    *d = device;
+    return hipSuccess;
+}
+hipError_t hipSetDevice(int d) {
+    device = d;
+    return hipSuccess;
+}
+hipError_t hipDeviceGetAttribute(int *v, hipDeviceAttribute_t, int) {
+    *v = 256;
+    return hipSuccess;
+}
+hipError_t hipFuncSetAttribute(const void *, hipFuncAttribute, int) { return hipSuccess; }
+hipError_t hipMalloc(void **p, size_t n) {
+    *p = reinterpret_cast<void *>(next_address);
+    blocks[next_address] = n;
+    next_address += (n + 8191) / 4096 * 4096;   // a gap after each
+    alloc_device = device;
+    return hipSuccess;
+}
+hipError_t hipFree(void *p) {
+    if (p && !blocks.erase(reinterpret_cast<uintptr_t>(p))) fail("hipFree of %p, which is no block", p);
+    return hipSuccess;
+}
+hipError_t hipHostMalloc(void **p, size_t n, unsigned) {
+    *p = std::calloc(1, n);
+    return hipSuccess;
+}
+hipError_t hipHostFree(void *p) {
+    std::free(p);
+    return hipSuccess;
+}
+hipError_t hipMemset(void *, int, size_t) { return hipSuccess; }
+hipError_t hipMemsetAsync(void *, int, size_t, hipStream_t) { return hipSuccess; }
+hipError_t hipMemcpyAsync(void *to, const void *, size_t n, hipMemcpyKind, hipStream_t) {
+    std::memset(to, 0, n);
+    return hipSuccess;
+}
+hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+
+}  // extern "C"
+
+namespace {
+
+template <class T>
+T *buffer(int64_t values) {
+    void *p = nullptr;
+    (void)hipMalloc(&p, values > 0 ? (size_t)values * sizeof(T) : 1);
+    return static_cast<T *>(p);
+}
+
+lattice_dense *handle() {
+    lattice_dense *D = nullptr;
+    if (lattice_dense_create(nullptr, &D) != LATTICE_OK) fail("lattice_dense_create failed");
+    return D;
+}
+
+void expect(const char *what, lattice_dense *D, lattice_status got, lattice_status want) {
+    if (got != want) fail("%s: status %d, not %d (%s)", what, (int)got, (int)want, lattice_dense_last_error(D));
+}
+
+// -- rowsum ------------------------------------------------------------------
+
+struct RowsumJobs {   // the kernel's first argument
+    struct {
+        const float *part;
+        float *out;
+        int64_t rows, n;
+    } j[4];
+    int64_t first[5];
+};
+
+// Every sum over partial rows reads and writes inside blocks that are there.
+void look_at_rowsum(const Launch &l) {
+    if (l.name.find("k_rowsum") == std::string::npos) return;
+    const RowsumJobs &jobs = *static_cast<const RowsumJobs *>(l.args[0]);
+    const int count = *static_cast<const int *>(l.args[1]);
+    for (int i = 0; i < count; ++i) {
+        const auto &j = jobs.j[i];
+        if (j.rows > 0 && !block_of(j.part, j.rows * j.n * 4))
+            fail("a sum reads %lld rows of %lld from %p, outside every block", (long long)j.rows, (long long)j.n,
+                 (const void *)j.part);
+        if (!block_of(j.out, (int64_t)l.grid.y * j.n * 4)) fail("a sum writes to %p, outside every block", (void *)j.out);
+    }
+}
+
+// The bias gradient of more pieces of rows than one sum adds up: kept logits
+// (fp32, 192 channels) of the most classes come in pieces of 256 rows.
+void many_pieces() {
+    on_launch = look_at_rowsum;
+    const int64_t N = (int64_t)256 * 8193 - 100;
+    const int C = 192, K = LATTICE_LOSS_MAX_CLASSES;
+    const float *x = buffer<float>(N * C), *w = buffer<float>((int64_t)K * C), *bias = buffer<float>(K);
+    const int64_t *target = buffer<int64_t>(N);
+    float *loss = buffer<float>(1), *grad_bias = buffer<float>(K);
+    lattice_dense *D = handle();
+    expect("linear_cross_entropy", D,
+           lattice_linear_cross_entropy(D, LATTICE_F32, x, C, N, C, w, C, K, bias, target, -100, 1, loss, nullptr, nullptr,
+                                        nullptr, grad_bias),
+           LATTICE_OK);
+    lattice_dense_destroy(D);
+}
+
+}  // namespace
+
+int main(int argc, char **argv) {
+    const std::map<std::string, void (*)()> checks = {{"many_pieces", many_pieces}};
+    const auto it = checks.find(argc > 1 ? argv[1] : "");
+    if (it == checks.end()) fail("which check?");
+    it->second();
+    std::printf("ok\n");
+    return 0;
+}

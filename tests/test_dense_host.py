@@ -1,0 +1,34 @@
+"""The dense operators' host side (sizes of the scratch, arguments of the
+launches, errors) without a GPU: tests/native/host_driver.cpp, linked with the
+built library, stands in for the HIP runtime."""
+import os
+import subprocess
+
+import pytest
+
+from paper_2108_03917_amd.lattice import LIB_PATH
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("native") / "host_driver")
+    libdir = os.path.dirname(LIB_PATH)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROCM, "include"),
+                    "-I", os.path.join(ROOT, "include"), os.path.join(HERE, "native", "host_driver.cpp"),
+                    LIB_PATH, "-rdynamic", f"-Wl,-rpath,{libdir}", "-Wl,--allow-shlib-undefined", "-o", exe],
+                   check=True, timeout=120)
+    return exe
+
+
+def run(driver, check):
+    r = subprocess.run([driver, check], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", (r.returncode, r.stdout, r.stderr)
+
+
+def test_bias_gradient_of_many_pieces_of_rows(driver):
+    """More pieces than one sum takes: no level of it reads outside the scratch."""
+    run(driver, "many_pieces")
