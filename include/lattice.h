@@ -642,7 +642,11 @@ lattice_status lattice_get_timing(lattice *L, double *ms, int64_t *count);
  * enqueued on the stream given at creation, and no call but
  * lattice_dense_get_status and lattice_dense_destroy synchronises with the
  * host.  A call that needs more scratch than any before it allocates device
- * memory (make one such call before capturing the call into a HIP graph).
+ * memory; while the stream is being captured into a HIP graph it is refused
+ * instead (LATTICE_E_STATE: make the call once before the capture).  A graph
+ * goes on using the scratch that its calls were captured with, which is kept
+ * until the handle is destroyed whatever later calls need: destroy it after the
+ * graph, and order replays with the handle's other calls.
  * Arguments are checked synchronously; on an error nothing is enqueued and
  * lattice_dense_last_error holds a message.  A handle is not thread safe.
  *

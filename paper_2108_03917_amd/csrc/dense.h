@@ -17,12 +17,20 @@
 // Device status bits of a lattice_dense.
 enum : int { DENSE_ST_LABEL = 1 };
 
+// Scratch that a larger one has replaced while a graph may still use it.
+struct KeptScratch {
+    void *p;
+    KeptScratch *next;
+};
+
 struct lattice_dense {
     int device = 0;
     hipStream_t stream = nullptr;
     int cu_count = 256;
     void *ws = nullptr;  // scratch of the operators, grown on demand
     int64_t ws_bytes = 0;
+    bool ws_captured = false;     // a call with this scratch was captured
+    KeptScratch *kept = nullptr;  // freed with the handle
     int32_t *status = nullptr;       // device
     int32_t *host_status = nullptr;  // pinned
     char err[512] = {0};

@@ -23,16 +23,49 @@ lattice_status hip_fail(lattice_dense *D, hipError_t e, const char *what) {
     return e == hipErrorOutOfMemory ? LATTICE_E_NOMEM : LATTICE_E_HIP;
 }
 
+// Whether calls on the handle's stream are being captured (the null stream is
+// never).
+bool capturing(const lattice_dense *D) {
+    if (!D->stream) return false;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(D->stream, &status) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    return status != hipStreamCaptureStatusNone;
+}
+
 // Grow the scratch to at least `need` bytes (a device allocation, only when it
-// is too small; freeing the old one waits for the work that uses it).
+// is too small; freeing the old one waits for the work that uses it).  A graph
+// goes on using the scratch that its calls were captured with: that one is
+// kept until the handle is destroyed.
 lattice_status grow(lattice_dense *D, int64_t need, const char *what) {
-    if (need <= D->ws_bytes) return LATTICE_OK;
-    if (D->ws) {
+    if (need <= 0) return LATTICE_OK;
+    const bool now = capturing(D);
+    if (need <= D->ws_bytes) {
+        D->ws_captured |= now;
+        return LATTICE_OK;
+    }
+    if (now) {
+        set_err(D, "%s: the stream is being captured and %lld bytes of scratch are needed, of which there are %lld "
+                   "(make the call once before the capture)",
+                what, (long long)need, (long long)D->ws_bytes);
+        return LATTICE_E_STATE;
+    }
+    if (D->ws && D->ws_captured) {
+        KeptScratch *k = new (std::nothrow) KeptScratch{D->ws, D->kept};
+        if (!k) {
+            set_err(D, "%s: out of host memory", what);
+            return LATTICE_E_NOMEM;
+        }
+        D->kept = k;
+    } else if (D->ws) {
         const hipError_t e = hipFree(D->ws);
         if (e != hipSuccess) return hip_fail(D, e, what);
     }
     D->ws = nullptr;
     D->ws_bytes = 0;
+    D->ws_captured = false;
     if (hipMalloc(&D->ws, need) != hipSuccess) {
         (void)hipGetLastError();
         D->ws = nullptr;
@@ -112,6 +145,12 @@ void lattice_dense_destroy(lattice_dense *D) {
     if (!D) return;
     (void)hipStreamSynchronize(D->stream);
     (void)hipFree(D->ws);
+    while (D->kept) {
+        KeptScratch *k = D->kept;
+        D->kept = k->next;
+        (void)hipFree(k->p);
+        delete k;
+    }
     (void)hipFree(D->status);
     (void)hipHostFree(D->host_status);
     delete D;

@@ -46,6 +46,7 @@ void (*on_launch)(const Launch &) = nullptr;
 dim3 pushed_grid, pushed_block;
 size_t pushed_lds;
 hipStream_t pushed_stream;
+bool capturing = false;
 
 std::map<const void *, std::string> &names() {
     static std::map<const void *, std::string> all;   // filled before main
@@ -142,6 +143,10 @@ hipError_t hipMemcpyAsync(void *to, const void *, size_t n, hipMemcpyKind, hipSt
     return hipSuccess;
 }
 hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *s) {
+    *s = capturing ? hipStreamCaptureStatusActive : hipStreamCaptureStatusNone;
+    return hipSuccess;
+}
 
 }  // extern "C"
 
@@ -154,9 +159,9 @@ T *buffer(int64_t values) {
     return static_cast<T *>(p);
 }
 
-lattice_dense *handle() {
+lattice_dense *handle(void *stream = nullptr) {
     lattice_dense *D = nullptr;
-    if (lattice_dense_create(nullptr, &D) != LATTICE_OK) fail("lattice_dense_create failed");
+    if (lattice_dense_create(stream, &D) != LATTICE_OK) fail("lattice_dense_create failed");
     return D;
 }
 
@@ -206,10 +211,45 @@ void many_pieces() {
     lattice_dense_destroy(D);
 }
 
+// -- scratch -----------------------------------------------------------------
+
+// The scratch that a call was captured with outlives every larger call.
+void captured_scratch() {
+    int stream_of_its_own = 0;
+    const float *g = buffer<float>(300 * 4096);
+    float *out = buffer<float>(300 * 4096);
+    const float ns[3] = {3.4445f, -4.7750f, 2.0315f};
+    const size_t callers = blocks.size();
+    lattice_dense *D = handle(&stream_of_its_own);
+    const size_t without = blocks.size();
+    auto update = [&](int n, lattice_status want) {
+        expect("orthogonalize", D,
+               lattice_orthogonalize(D, g, LATTICE_F32, 1, 64, n, 0, n, 5, ns, 1e-7f, out, LATTICE_F32), want);
+    };
+    update(128, LATTICE_OK);
+    if (blocks.size() != without + 1) fail("no scratch after a call");
+    update(256, LATTICE_OK);
+    if (blocks.size() != without + 1) fail("scratch that no graph uses was not freed");
+    const uintptr_t scratch = blocks.rbegin()->first;
+    capturing = true;
+    update(256, LATTICE_OK);
+    const int64_t before = launches;
+    update(512, LATTICE_E_STATE);   // would have to allocate
+    if (launches != before || blocks.size() != without + 1 || !blocks.count(scratch))
+        fail("a call that was refused launched, allocated or freed something");
+    capturing = false;
+    for (int n : {512, 1024, 2048}) update(n, LATTICE_OK);
+    if (!blocks.count(scratch)) fail("the scratch of a captured call was freed by a larger one");
+    if (blocks.size() != without + 2) fail("%zu blocks of scratch, not 2", blocks.size() - without);
+    lattice_dense_destroy(D);
+    if (blocks.size() != callers) fail("%zu blocks left by the handle", blocks.size() - callers);
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
-    const std::map<std::string, void (*)()> checks = {{"many_pieces", many_pieces}};
+    const std::map<std::string, void (*)()> checks = {{"many_pieces", many_pieces},
+                                                         {"captured_scratch", captured_scratch}};
     const auto it = checks.find(argc > 1 ? argv[1] : "");
     if (it == checks.end()) fail("which check?");
     it->second();

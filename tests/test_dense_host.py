@@ -32,3 +32,9 @@ def run(driver, check):
 def test_bias_gradient_of_many_pieces_of_rows(driver):
     """More pieces than one sum takes: no level of it reads outside the scratch."""
     run(driver, "many_pieces")
+
+
+def test_scratch_of_a_captured_call_is_kept(driver):
+    """A larger call frees the scratch only if no graph may use it, and is
+    refused, with nothing done, while its stream is being captured."""
+    run(driver, "captured_scratch")
