@@ -639,9 +639,9 @@ lattice_status lattice_get_timing(lattice *L, double *ms, int64_t *count);
  * orthogonalised form of a weight gradient.  They work on plain row-major
  * matrices and need no lattice: a lattice_dense is their handle.  It owns
  * scratch that grows on demand and a device status word; all its work is
- * enqueued on the stream given at creation, and no call but
- * lattice_dense_get_status and lattice_dense_destroy synchronises with the
- * host.  A call that needs more scratch than any before it allocates device
+ * enqueued on the stream given at creation, on the device that was current
+ * then, whichever is at the call, and no call but lattice_dense_get_status and
+ * lattice_dense_destroy synchronises with the host.  A call that needs more scratch than any before it allocates device
  * memory; while the stream is being captured into a HIP graph it is refused
  * instead (LATTICE_E_STATE: make the call once before the capture).  A graph
  * goes on using the scratch that its calls were captured with, which is kept

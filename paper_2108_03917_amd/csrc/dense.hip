@@ -76,6 +76,25 @@ lattice_status grow(lattice_dense *D, int64_t need, const char *what) {
     return LATTICE_OK;
 }
 
+// Makes the handle's device the current one for a call, whichever the caller's is:
+// allocations and launches go to the current device, the null stream's too.
+struct OnDevice {
+    int before = -1;
+    hipError_t error;
+    explicit OnDevice(const lattice_dense *D) {
+        int now = 0;
+        error = hipGetDevice(&now);
+        if (error != hipSuccess || now == D->device) return;
+        error = hipSetDevice(D->device);
+        if (error == hipSuccess) before = now;
+    }
+    ~OnDevice() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+    OnDevice(const OnDevice &) = delete;
+    OnDevice &operator=(const OnDevice &) = delete;
+};
+
 bool is_storage(lattice_dtype t) { return t == LATTICE_F32 || t == LATTICE_BF16; }
 
 // Bytes of rows x C values at `stride` values a row (0 for no rows).
@@ -143,16 +162,19 @@ lattice_status lattice_dense_create(void *stream, lattice_dense **out) {
 
 void lattice_dense_destroy(lattice_dense *D) {
     if (!D) return;
-    (void)hipStreamSynchronize(D->stream);
-    (void)hipFree(D->ws);
-    while (D->kept) {
-        KeptScratch *k = D->kept;
-        D->kept = k->next;
-        (void)hipFree(k->p);
-        delete k;
+    {
+        const OnDevice on(D);
+        (void)hipStreamSynchronize(D->stream);
+        (void)hipFree(D->ws);
+        while (D->kept) {
+            KeptScratch *k = D->kept;
+            D->kept = k->next;
+            (void)hipFree(k->p);
+            delete k;
+        }
+        (void)hipFree(D->status);
+        (void)hipHostFree(D->host_status);
     }
-    (void)hipFree(D->status);
-    (void)hipHostFree(D->host_status);
     delete D;
 }
 
@@ -160,6 +182,8 @@ const char *lattice_dense_last_error(const lattice_dense *D) { return D ? D->err
 
 lattice_status lattice_dense_get_status(lattice_dense *D) {
     if (!D) return LATTICE_E_ARG;
+    const OnDevice on(D);
+    if (on.error != hipSuccess) return hip_fail(D, on.error, "get_status");
     hipError_t e = hipMemcpyAsync(D->host_status, D->status, sizeof(int32_t), hipMemcpyDeviceToHost, D->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(D->stream);
     if (e != hipSuccess) return hip_fail(D, e, "get_status");
@@ -189,6 +213,8 @@ lattice_status lattice_layer_norm(lattice_dense *D, const lattice *rows_of, cons
         return LATTICE_E_ARG;
     }
     if (rows == 0) return LATTICE_OK;
+    const OnDevice on(D);
+    if (on.error != hipSuccess) return hip_fail(D, on.error, "layer_norm");
     NormArgs a = {rows_of ? rows_of->counters : nullptr, rows, C, eps, x, x_stride, x_dtype == LATTICE_BF16, gamma,
                   beta, y, y_stride, y_dtype == LATTICE_BF16, mean, rstd};
     const hipError_t e = launch_layer_norm(D, a);
@@ -219,6 +245,8 @@ lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows
         set_err(D, "layer_norm_backward: grad_x overlaps x or grad_y");
         return LATTICE_E_ARG;
     }
+    const OnDevice on(D);
+    if (on.error != hipSuccess) return hip_fail(D, on.error, "layer_norm_backward");
     NormBackwardArgs a = {rows_of ? rows_of->counters : nullptr, rows, C, grad_y, g_stride, g_dtype == LATTICE_BF16, x,
                           x_stride, x_dtype == LATTICE_BF16, mean, rstd, gamma, grad_x, grad_x_stride, grad_gamma,
                           grad_beta};
@@ -251,6 +279,8 @@ lattice_status lattice_linear_cross_entropy(lattice_dense *D, lattice_dtype dtyp
         set_err(D, "linear_cross_entropy: a gradient overlaps x or w");
         return LATTICE_E_ARG;
     }
+    const OnDevice on(D);
+    if (on.error != hipSuccess) return hip_fail(D, on.error, "linear_cross_entropy");
     LossArgs a = {dtype == LATTICE_BF16, N, C, x, x_stride, w, K, w_stride, bias, target, ignore_index, mean != 0, loss,
                   row_loss, grad_x, grad_w, grad_bias};
     const lattice_status s = grow(D, loss_scratch(D, a), "linear_cross_entropy");
@@ -287,6 +317,8 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
         return LATTICE_E_ARG;
     }
     if (batch == 0) return LATTICE_OK;
+    const OnDevice on(D);
+    if (on.error != hipSuccess) return hip_fail(D, on.error, "orthogonalize");
     UpdateArgs a = {g, g_dtype == LATTICE_BF16, batch, m, n, batch_stride, row_stride, steps,
                     {coefficients[0], coefficients[1], coefficients[2]}, eps, out, out_dtype == LATTICE_BF16};
     const lattice_status s = grow(D, update_scratch(D, a), "orthogonalize");

@@ -41,12 +41,16 @@ hipError_t last = hipSuccess;
 std::map<uintptr_t, size_t> blocks;       // live, by address
 uintptr_t next_address = (uintptr_t)1 << 44;
 int64_t launches = 0;
-int alloc_device = -1;                    // that the last block was made on
+int want_device = -1;                     // on which all work has to be, or any
 void (*on_launch)(const Launch &) = nullptr;
 dim3 pushed_grid, pushed_block;
 size_t pushed_lds;
 hipStream_t pushed_stream;
 bool capturing = false;
+
+void here(const char *what) {
+    if (want_device >= 0 && device != want_device) fail("%s on device %d, not %d", what, device, want_device);
+}
 
 std::map<const void *, std::string> &names() {
     static std::map<const void *, std::string> all;   // filled before main
@@ -94,6 +98,7 @@ hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, s
     if (!grid.x || !grid.y || !grid.z || !block.x || !block.y || !block.z || block.x * block.y * block.z > 1024 ||
         lds > 160 * 1024)
         return last = hipErrorInvalidConfiguration;
+    here("a launch");
     ++launches;
     if (on_launch) on_launch({names()[fn], grid, device, args});
     return hipSuccess;
@@ -121,10 +126,11 @@ hipError_t hipMalloc(void **p, size_t n) {
     *p = reinterpret_cast<void *>(next_address);
     blocks[next_address] = n;
     next_address += (n + 8191) / 4096 * 4096;   // a gap after each
-    alloc_device = device;
+    here("an allocation");
     return hipSuccess;
 }
 hipError_t hipFree(void *p) {
+    here("hipFree");
     if (p && !blocks.erase(reinterpret_cast<uintptr_t>(p))) fail("hipFree of %p, which is no block", p);
     return hipSuccess;
 }
@@ -136,13 +142,23 @@ hipError_t hipHostFree(void *p) {
     std::free(p);
     return hipSuccess;
 }
-hipError_t hipMemset(void *, int, size_t) { return hipSuccess; }
-hipError_t hipMemsetAsync(void *, int, size_t, hipStream_t) { return hipSuccess; }
+hipError_t hipMemset(void *, int, size_t) {
+    here("hipMemset");
+    return hipSuccess;
+}
+hipError_t hipMemsetAsync(void *, int, size_t, hipStream_t) {
+    here("hipMemsetAsync");
+    return hipSuccess;
+}
 hipError_t hipMemcpyAsync(void *to, const void *, size_t n, hipMemcpyKind, hipStream_t) {
+    here("a copy");
     std::memset(to, 0, n);
     return hipSuccess;
 }
-hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+hipError_t hipStreamSynchronize(hipStream_t) {
+    here("hipStreamSynchronize");
+    return hipSuccess;
+}
 hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *s) {
     *s = capturing ? hipStreamCaptureStatusActive : hipStreamCaptureStatusNone;
     return hipSuccess;
@@ -245,11 +261,43 @@ void captured_scratch() {
     if (blocks.size() != callers) fail("%zu blocks left by the handle", blocks.size() - callers);
 }
 
+// -- device ------------------------------------------------------------------
+
+// A handle's work is on its device, whichever is current at the call.
+void another_current_device() {
+    device = 1;
+    lattice_dense *D = handle();
+    const int64_t rows = 3000;
+    const int C = 64, K = 20;
+    float *x = buffer<float>(rows * C), *y = buffer<float>(rows * C), *v = buffer<float>(4 * rows), *w = buffer<float>(K * C);
+    int64_t *target = buffer<int64_t>(rows);
+    const float ns[3] = {1.5f, -0.5f, 0.f};
+    auto after = [&](const char *what, lattice_status got) {
+        expect(what, D, got, LATTICE_OK);
+        if (device != 0) fail("%s left device %d current", what, device);
+    };
+    want_device = 1;
+    device = 0;
+    after("layer_norm", lattice_layer_norm(D, nullptr, x, LATTICE_F32, C, rows, C, nullptr, nullptr, 0.f, y, LATTICE_F32, C,
+                                           v, v + rows));
+    after("layer_norm_backward",
+          lattice_layer_norm_backward(D, nullptr, y, LATTICE_F32, C, x, LATTICE_F32, C, rows, C, v, v + rows, nullptr,
+                                      nullptr, C, v + 2 * rows, v + 3 * rows));
+    after("linear_cross_entropy",
+          lattice_linear_cross_entropy(D, LATTICE_F32, x, C, rows, C, w, C, K, nullptr, target, -100, 1, v, nullptr, y,
+                                       nullptr, nullptr));
+    after("orthogonalize", lattice_orthogonalize(D, x, LATTICE_F32, 1, C, (int)rows, 0, rows, 5, ns, 0.f, y, LATTICE_F32));
+    after("get_status", lattice_dense_get_status(D));
+    lattice_dense_destroy(D);
+    if (device != 0) fail("destroy left device %d current", device);
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
     const std::map<std::string, void (*)()> checks = {{"many_pieces", many_pieces},
-                                                         {"captured_scratch", captured_scratch}};
+                                                         {"captured_scratch", captured_scratch},
+                                                         {"another_current_device", another_current_device}};
     const auto it = checks.find(argc > 1 ? argv[1] : "");
     if (it == checks.end()) fail("which check?");
     it->second();

@@ -38,3 +38,9 @@ def test_scratch_of_a_captured_call_is_kept(driver):
     """A larger call frees the scratch only if no graph may use it, and is
     refused, with nothing done, while its stream is being captured."""
     run(driver, "captured_scratch")
+
+
+def test_work_is_on_the_handles_device(driver):
+    """Allocations, launches and waits, with another device current, which is
+    current again after each call."""
+    run(driver, "another_current_device")
