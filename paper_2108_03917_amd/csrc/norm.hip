@@ -400,7 +400,8 @@ hipError_t backward(lattice_dense *D, const NormBackwardArgs &a) {
         if (a.gx)
             hipLaunchKernelGGL((k_norm_backward_long<XB, GB>), dim3(grid_for(a.rows, 1, D->cu_count, 2)), dim3(1024),
                                0, D->stream, a);
-        if (params) {
+        // without rows there is no partial row, and the sums are zeros
+        if (params && a.rows > 0) {
             prows = a.rows < kLongSplit ? a.rows : kLongSplit;
             hipLaunchKernelGGL((k_norm_params_long<XB, GB>), dim3((a.C + 255) / 256, (unsigned)prows), dim3(256), 0,
                                D->stream, a, part);

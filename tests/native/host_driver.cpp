@@ -292,12 +292,30 @@ void another_current_device() {
     if (device != 0) fail("destroy left device %d current", device);
 }
 
+// -- empty inputs ------------------------------------------------------------
+
+// No rows: every width and output is taken, and no launch is malformed.
+void no_rows() {
+    const int most = 1 << 20;
+    lattice_dense *D = handle();
+    float *grad = buffer<float>(2 * most);
+    for (const int C : {32, 9000, 17000, most})
+        for (const lattice_dtype t : {LATTICE_F32, LATTICE_BF16})
+            for (int wanted = 1; wanted < 4; ++wanted)
+                expect("layer_norm_backward", D,
+                       lattice_layer_norm_backward(D, nullptr, nullptr, t, C, nullptr, t, C, 0, C, nullptr, nullptr, nullptr,
+                                                   nullptr, C, wanted & 1 ? grad : nullptr, wanted & 2 ? grad + C : nullptr),
+                       LATTICE_OK);
+    lattice_dense_destroy(D);
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
     const std::map<std::string, void (*)()> checks = {{"many_pieces", many_pieces},
                                                          {"captured_scratch", captured_scratch},
-                                                         {"another_current_device", another_current_device}};
+                                                         {"another_current_device", another_current_device},
+                                                         {"no_rows", no_rows}};
     const auto it = checks.find(argc > 1 ? argv[1] : "");
     if (it == checks.end()) fail("which check?");
     it->second();

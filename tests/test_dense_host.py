@@ -44,3 +44,8 @@ def test_work_is_on_the_handles_device(driver):
     """Allocations, launches and waits, with another device current, which is
     current again after each call."""
     run(driver, "another_current_device")
+
+
+def test_layer_norm_backward_without_rows(driver):
+    """Short and long rows, any of the sums."""
+    run(driver, "no_rows")

@@ -49,3 +49,16 @@ def test_graph_replays_after_larger_calls(_gpu):  # noqa: F811
             s.synchronize()
             assert all(torch.equal(a, c) for a, c in zip(out, eager)), i
         own.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [32, 9000, 17000])
+def test_layer_norm_without_rows(ops, C, dtype):  # noqa: F811
+    x = rand(1, 0, C, dtype=dtype)
+    y, mean, rstd = ops.layer_norm(x, want_stats=True)
+    assert y.shape == (0, C) and mean.shape == rstd.shape == (0,)
+    gx, gg, gb = ops.layer_norm_backward(x, x, mean, rstd)
+    assert gx.shape == (0, C) and gx.dtype == x.dtype
+    assert gg.shape == gb.shape == (C,) and torch.all(gg == 0) and torch.all(gb == 0)
+    gx, gg, gb = ops.layer_norm_backward(x, x, mean, rstd, want_input=False)
+    assert gx is None and torch.all(gg == 0) and torch.all(gb == 0)
