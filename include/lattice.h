@@ -704,7 +704,7 @@ lattice_status lattice_layer_norm(lattice_dense *D, const lattice *rows_of, cons
  *   grad_x        dev [rows][C] stored as x_dtype, or NULL; may be grad_y (of
  *                 the same type) or x itself for C up to 8192.
  *   grad_gamma, grad_beta   dev fp32 [C], or NULL.  Zero without rows.
- * At least one of the three.  The sums over rows are fp32 in a thread and fp64
+ * At least one of the three, if there are rows.  The sums over rows are fp32 in a thread and fp64
  * between workgroups, in a fixed order.
  */
 lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows_of, const void *grad_y,

@@ -231,10 +231,11 @@ lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows
     if (s) return s;
     if (!is_storage(x_dtype) || !is_storage(g_dtype) || x_stride < C || g_stride < C || x_stride > kMaxStride ||
         g_stride > kMaxStride || (grad_x && (grad_x_stride < C || grad_x_stride > kMaxStride)) ||
-        (!grad_x && !grad_gamma && !grad_beta) || (rows > 0 && (!grad_y || !x || !mean || !rstd))) {
+        (rows > 0 && (!grad_y || !x || !mean || !rstd || (!grad_x && !grad_gamma && !grad_beta)))) {
         set_err(D, "layer_norm_backward: bad pointer, type or stride (C = %d)", C);
         return LATTICE_E_ARG;
     }
+    if (rows == 0 && !grad_gamma && !grad_beta) return LATTICE_OK;  // a grad_x without rows may have no address
     const int64_t nx = span(rows, C, x_stride, x_dtype), ng = span(rows, C, g_stride, g_dtype);
     const int64_t no = grad_x ? span(rows, C, grad_x_stride, x_dtype) : 0;
     const bool on_x = grad_x == x && grad_x_stride == x_stride;

@@ -47,5 +47,5 @@ def test_work_is_on_the_handles_device(driver):
 
 
 def test_layer_norm_backward_without_rows(driver):
-    """Short and long rows, any of the sums."""
+    """Short and long rows, any of the outputs, or none that has an address."""
     run(driver, "no_rows")

@@ -60,5 +60,7 @@ def test_layer_norm_without_rows(ops, C, dtype):  # noqa: F811
     gx, gg, gb = ops.layer_norm_backward(x, x, mean, rstd)
     assert gx.shape == (0, C) and gx.dtype == x.dtype
     assert gg.shape == gb.shape == (C,) and torch.all(gg == 0) and torch.all(gb == 0)
+    gx, gg, gb = ops.layer_norm_backward(x, x, mean, rstd, want_params=False)
+    assert gx.shape == (0, C) and gg is None and gb is None
     gx, gg, gb = ops.layer_norm_backward(x, x, mean, rstd, want_input=False)
     assert gx is None and torch.all(gg == 0) and torch.all(gb == 0)
