@@ -760,7 +760,7 @@ lattice_status lattice_linear_cross_entropy(lattice_dense *D, lattice_dtype dtyp
  *   steps         0 .. 64.     coefficients  host: a, b, c.     eps  >= 0.
  *   out           dev [batch][m][n] stored as out_dtype; no overlap with g.
  * For an fp32 result X and S carry 24 bits between the products, for a bf16
- * one 16.  A matrix of zeros gives zeros.
+ * one 16.  A matrix of zeros gives zeros, also with eps = 0.
  */
 #define LATTICE_UPDATE_MAX_BATCH 65535
 #define LATTICE_UPDATE_MAX_SIDE 65536

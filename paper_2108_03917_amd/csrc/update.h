@@ -14,7 +14,8 @@ inline int square_parts(const UpdateArgs &a) {
 hipError_t launch_squares(hipStream_t stream, const UpdateArgs &a, double *part);
 
 // 1 / (norm + eps) for every thread of the workgroup, from its threads' sums of
-// squares, or from the partial sums of launch_squares.
+// squares, or from the partial sums of launch_squares.  0 for zeros without eps,
+// so that they stay zeros; a norm that is NaN stays one.
 template <int THREADS>
 __device__ __forceinline__ double inverse_norm(double s, float eps, double *red) {
 #pragma unroll
@@ -24,7 +25,8 @@ __device__ __forceinline__ double inverse_norm(double s, float eps, double *red)
     s = 0.0;
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) s += red[w];
-    return 1.0 / (sqrt(s) + (double)eps);
+    const double d = sqrt(s) + (double)eps;
+    return d == 0.0 ? 0.0 : 1.0 / d;
 }
 template <int THREADS>
 __device__ __forceinline__ double inverse_norm(const double *part, int parts, float eps, double *red) {

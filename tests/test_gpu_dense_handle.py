@@ -64,3 +64,16 @@ def test_layer_norm_without_rows(ops, C, dtype):  # noqa: F811
     assert gx.shape == (0, C) and gg is None and gb is None
     gx, gg, gb = ops.layer_norm_backward(x, x, mean, rstd, want_input=False)
     assert gx is None and torch.all(gg == 0) and torch.all(gb == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(30, 64), (64, 3000), (150, 170)])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+def test_update_of_zeros_without_eps(ops, m, n, steps, dtype):  # noqa: F811
+    """Zeros stay zeros where nothing is added to their norm; a NaN stays one."""
+    g = rand(1, 3, m, n, dtype=dtype)
+    g[1] = 0
+    g[2, 1, 2] = float("nan")
+    got = ops.orthogonalize(g, steps=steps, eps=0.0)
+    assert torch.all(got[1] == 0) and torch.isfinite(got[0]).all() and torch.isnan(got[2]).any()
+    assert torch.equal(got[0], ops.orthogonalize(g[0], steps=steps, eps=0.0))
