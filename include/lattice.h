@@ -724,8 +724,10 @@ lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows
  *   grad_x, grad_w, grad_bias = the gradients of `loss`.
  *   dtype         storage of x, w, grad_x and grad_w.  Products of fp32
  *                 operands are as in LATTICE_F32; of bf16 ones they are exact,
- *                 and d loss / dz is rounded to bf16 before the products that
- *                 give grad_x and grad_w (not for grad_bias).
+ *                 and d loss / dz is rounded before the products that give
+ *                 grad_x and grad_w (not for grad_bias): to 16 bits where one
+ *                 workgroup holds w (up to 128 classes and 256 channels, not
+ *                 both), else to bf16.
  *   x             dev [N][C], x_stride values a row; N 0 .. 2^28, C 1 .. 2^14.
  *   w             dev [K][C], w_stride values a row; K 1 .. 2^20.
  *   bias          dev fp32 [K], or NULL.  -inf takes a class out.

@@ -17,14 +17,18 @@
 // sums, and k_fused_join adds the rows in a fixed order in fp64.
 //
 // fp32 operands are multiplied on the fp32 matrix cores (16x16x4: exact
-// products), bf16 ones on the bf16 ones (16x16x32), where G is rounded to bf16.
+// products), bf16 ones on the bf16 ones (16x16x32), where a value of G is the sum
+// of two bf16 (16 bits): rounded to one, the gradients' error against 64 bits was
+// 2.1e-3, of which the rounding of the stored result alone makes 1.7e-3.  The
+// second one costs 2% (103889 x 128 with 20 classes: 30.6 and 31.3 us a call) to 13%
+// (100000 x 128 with 100: 77 and 87).
 //
 // 537211 x 64 with 20 classes in fp32: 91 us (3.0 TB/s of x and dx; the fp32
 // matrix cores, half busy, and the exponentials do not hide all of it).
 // 103889 x 128 with 20 classes in bf16: 24 us (2.2 TB/s), two wavefronts a SIMD
 // for the registers of dw.  The next block's rows are read while a block is
 // multiplied.
-#include "dense.h"
+#include "planes.h"
 
 namespace {
 
@@ -34,6 +38,11 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kRows = 64;           // rows of a block
 constexpr int kCounts = 256;        // partial counts of rows with a label
+constexpr int kParts = 2;           // bf16 that a value of G is the sum of
+// Those of them whose transposed matrices are in LDS at a time: one after the
+// other where room for both would leave a CU one workgroup instead of two (100000
+// x 256 with 20 classes in bf16: 49 us, 56 at once).
+__host__ __device__ constexpr int parts_at_once(int KT, int CT4) { return KT == 2 && CT4 == 4 ? 1 : kParts; }
 constexpr int64_t kCountHere = 8192;  // up to so many rows every workgroup counts them itself
 
 __device__ __forceinline__ f32x4_t mfma4(float a, float b, f32x4_t c) {
@@ -292,8 +301,9 @@ struct Lds16 {
     static constexpr int rs = kRows + 8;
     __host__ __device__ Lds16(int C, int KT) : cp((C + 31) / 32 * 32), ws(cp + 8), vs(KT * 16 + 8) {}
     // in bytes: w, V, G^T and x^T, biases and the sums
-    __host__ __device__ int bytes(int KT, bool grad) const {
-        return 2 * KT * 16 * ws + (grad ? 2 * cp * vs + 2 * (KT * 16 + cp) * rs : 0) + 4 * (5 * KT * 16 + 16);
+    __host__ __device__ int bytes(int KT, int CT4, bool grad) const {
+        return 2 * KT * 16 * ws + (grad ? 2 * cp * vs + 2 * (parts_at_once(KT, CT4) * KT * 16 + cp) * rs : 0) +
+               4 * (5 * KT * 16 + 16);
     }
 };
 
@@ -302,8 +312,9 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
     extern __shared__ __attribute__((aligned(16))) uint16_t lds16[];
     const LossArgs &a = f.a;
     const Lds16 L(a.C, KT);
+    constexpr int HELD = parts_at_once(KT, CT4);
     uint16_t *W = lds16, *V = W + KT * 16 * L.ws;
-    uint16_t *Gt = V + (GRAD ? L.cp * L.vs : 0), *Xt = Gt + (GRAD ? KT * 16 * L.rs : 0);
+    uint16_t *Gt = V + (GRAD ? L.cp * L.vs : 0), *Xt = Gt + (GRAD ? HELD * KT * 16 * L.rs : 0);
     float *B = reinterpret_cast<float *>(Xt + (GRAD ? L.cp * L.rs : 0)), *red = B + KT * 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int ct = (a.C + 15) / 16, cs = L.cp / 32;
@@ -372,17 +383,31 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
         loss += l;
         if (a.rows && q == 0 && p < a.N) a.rows[p] = l;
         if (!GRAD) continue;
-        u32x4_t g[KT / 2];
+        u32x4_t g[kParts][KT / 2];
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
             db[k] += z[k];
-            g[k / 2][2 * (k & 1)] = pack_bf16(z[k][0], z[k][1]);
-            g[k / 2][2 * (k & 1) + 1] = pack_bf16(z[k][2], z[k][3]);
+            uint32_t lo[kParts], hi[kParts];
+            planes::split_pair<kParts>(z[k][0], z[k][1], lo);
+            planes::split_pair<kParts>(z[k][2], z[k][3], hi);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                Gt[(16 * k + 4 * q + r) * L.rs + 16 * wave + i] =
-                    (uint16_t)(g[k / 2][2 * (k & 1) + (r >> 1)] >> (16 * (r & 1)));
+            for (int p = 0; p < kParts; ++p) {
+                g[p][k / 2][2 * (k & 1)] = lo[p];
+                g[p][k / 2][2 * (k & 1) + 1] = hi[p];
+            }
         }
+        // parts `first` on of G^T
+        auto transposed = [&](int first) {
+#pragma unroll
+            for (int p = 0; p < HELD; ++p)
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        Gt[(16 * (KT * p + k) + 4 * q + r) * L.rs + 16 * wave + i] =
+                            (uint16_t)(g[first + p][k / 2][2 * (k & 1) + (r >> 1)] >> (16 * (r & 1)));
+        };
+        if (a.grad_w) transposed(kParts - HELD);
         if (a.grad_x) {
             uint16_t *gr = reinterpret_cast<uint16_t *>(a.grad_x) + p * a.C;
 #pragma unroll
@@ -390,8 +415,11 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
                 if (c >= ct) continue;
                 f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int u = 0; u < KT / 2; ++u)
-                    o = mfma32(*reinterpret_cast<const u32x4_t *>(V + (16 * c + i) * L.vs + 32 * u + 8 * q), g[u], o);
+                for (int u = 0; u < KT / 2; ++u) {
+                    const u32x4_t v = *reinterpret_cast<const u32x4_t *>(V + (16 * c + i) * L.vs + 32 * u + 8 * q);
+#pragma unroll
+                    for (int p = kParts - 1; p >= 0; --p) o = mfma32(v, g[p][u], o);
+                }
                 const int c0 = 16 * c + 4 * q;
                 if (p >= a.N) continue;
                 const uint32_t lo = pack_bf16(o[0] * factor, o[1] * factor), hi = pack_bf16(o[2] * factor, o[3] * factor);
@@ -406,19 +434,28 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
             }
         }
         if (!a.grad_w) continue;
-        __syncthreads();
 #pragma unroll
-        for (int c = 0; c < CT4; ++c) {
-            if (wave + 4 * c >= ct) continue;
+        for (int first = kParts - HELD; first >= 0; first -= HELD) {  // the smaller parts first
+            if (first != kParts - HELD) transposed(first);
+            __syncthreads();
 #pragma unroll
-            for (int s = 0; s < kRows / 32; ++s) {
-                const u32x4_t v = *reinterpret_cast<const u32x4_t *>(Xt + (16 * (wave + 4 * c) + i) * L.rs + 32 * s + 8 * q);
+            for (int c = 0; c < CT4; ++c) {
+                if (wave + 4 * c >= ct) continue;
 #pragma unroll
-                for (int k = 0; k < KT; ++k)
-                    dw[c][k] = mfma32(*reinterpret_cast<const u32x4_t *>(Gt + (16 * k + i) * L.rs + 32 * s + 8 * q), v, dw[c][k]);
+                for (int s = 0; s < kRows / 32; ++s) {
+                    const u32x4_t v =
+                        *reinterpret_cast<const u32x4_t *>(Xt + (16 * (wave + 4 * c) + i) * L.rs + 32 * s + 8 * q);
+#pragma unroll
+                    for (int k = 0; k < KT; ++k)
+#pragma unroll
+                        for (int p = HELD - 1; p >= 0; --p)
+                            dw[c][k] = mfma32(
+                                *reinterpret_cast<const u32x4_t *>(Gt + (16 * (KT * p + k) + i) * L.rs + 32 * s + 8 * q), v,
+                                dw[c][k]);
+                }
             }
+            __syncthreads();
         }
-        __syncthreads();
     }
     if (bad) atomicOr(f.status, DENSE_ST_LABEL);
     write_part<KT, CT4, GRAD>(f, dw, db, loss, factor, red);
@@ -476,7 +513,7 @@ int channel_groups(int C) { return C <= 64 ? 1 : C <= 128 ? 2 : 4; }
 
 int lds_bytes(const LossArgs &a) {
     const int KT = class_tiles(a.bf16, a.K);
-    return a.bf16 ? Lds16(a.C, KT).bytes(KT, a.any_grad()) : Lds32(a.C, KT).floats(KT, a.any_grad()) * 4;
+    return a.bf16 ? Lds16(a.C, KT).bytes(KT, channel_groups(a.C), a.any_grad()) : Lds32(a.C, KT).floats(KT, a.any_grad()) * 4;
 }
 
 unsigned fused_grid(const lattice_dense *D, const LossArgs &a) {

@@ -88,3 +88,16 @@ def test_update_in_chunks_of_a_batch(ops, batch, m, n, dtype):  # noqa: F811
     # each as alone, up to the parts that its sums are made of
     for b in (0, batch - 1):
         check_update(ops.orthogonalize(g[b]), got[b].double(), b)
+
+
+FEW = [(5000, 64, 20), (3000, 128, 20), (700, 96, 50), (257, 33, 3), (2000, 128, 100), (900, 256, 40)]
+
+
+@pytest.mark.parametrize("N,C,K", FEW)
+def test_gradients_of_few_classes_in_bf16(ops, N, C, K):  # noqa: F811
+    """d loss / dz keeps 16 bits in the products that give the gradients."""
+    x, w, t, bias = rand(1, N, C, dtype="bf16"), (rand(2, K, C) * 0.3).bfloat16(), labels(3, N, K), rand(4, K)
+    got = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    terms, ref = loss_terms(x, w, t, bias)
+    check_loss(got, ref, "bf16")
+    check_gradients(got[2:4], terms, 16)
