@@ -670,6 +670,12 @@ void lattice_dense_destroy(lattice_dense *D);
  */
 lattice_status lattice_dense_get_status(lattice_dense *D);
 const char *lattice_dense_last_error(const lattice_dense *D);
+/*
+ * Significant bits of d loss / dz in the products with which later calls of
+ * lattice_linear_cross_entropy make grad_x and grad_w of bf16 operands: 8 (one
+ * bf16, the default) or 16 (the sum of two: those products are two each).
+ */
+lattice_status lattice_dense_set_gradient_bits(lattice_dense *D, int bits);
 
 /*
  * lattice_layer_norm -- normalise each row over its channels:
@@ -727,7 +733,7 @@ lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows
  *                 and d loss / dz is rounded before the products that give
  *                 grad_x and grad_w (not for grad_bias): to 16 bits where one
  *                 workgroup holds w (up to 128 classes and 256 channels, not
- *                 both), else to bf16.
+ *                 both), else as lattice_dense_set_gradient_bits says.
  *   x             dev [N][C], x_stride values a row; N 0 .. 2^28, C 1 .. 2^14.
  *   w             dev [K][C], w_stride values a row; K 1 .. 2^20.
  *   bias          dev fp32 [K], or NULL.  -inf takes a class out.

@@ -29,6 +29,7 @@ struct lattice_dense {
     int cu_count = 256;
     void *ws = nullptr;  // scratch of the operators, grown on demand
     int64_t ws_bytes = 0;
+    bool split_gradients = false;  // d loss / dz of bf16 operands in 16 bits
     bool ws_captured = false;     // a call with this scratch was captured
     KeptScratch *kept = nullptr;  // freed with the handle
     int32_t *status = nullptr;       // device
@@ -98,6 +99,7 @@ struct LossArgs {
     float *loss, *rows;
     void *grad_x, *grad_w;
     float *grad_bias;
+    bool split;  // bf16: G in two planes, where it is not anyway
     bool any_grad() const { return grad_x || grad_w || grad_bias; }
 };
 int64_t loss_scratch(const lattice_dense *D, const LossArgs &a);

@@ -194,6 +194,16 @@ lattice_status lattice_dense_get_status(lattice_dense *D) {
     return LATTICE_E_RANGE;
 }
 
+lattice_status lattice_dense_set_gradient_bits(lattice_dense *D, int bits) {
+    if (!D) return LATTICE_E_ARG;
+    if (bits != 8 && bits != 16) {
+        set_err(D, "set_gradient_bits: bits = %d is neither 8 nor 16", bits);
+        return LATTICE_E_ARG;
+    }
+    D->split_gradients = bits == 16;
+    return LATTICE_OK;
+}
+
 lattice_status lattice_layer_norm(lattice_dense *D, const lattice *rows_of, const void *x, lattice_dtype x_dtype,
                                   int64_t x_stride, int64_t rows, int C, const float *gamma, const float *beta,
                                   float eps, void *y, lattice_dtype y_dtype, int64_t y_stride, float *mean,
@@ -283,7 +293,7 @@ lattice_status lattice_linear_cross_entropy(lattice_dense *D, lattice_dtype dtyp
     const OnDevice on(D);
     if (on.error != hipSuccess) return hip_fail(D, on.error, "linear_cross_entropy");
     LossArgs a = {dtype == LATTICE_BF16, N, C, x, x_stride, w, K, w_stride, bias, target, ignore_index, mean != 0, loss,
-                  row_loss, grad_x, grad_w, grad_bias};
+                  row_loss, grad_x, grad_w, grad_bias, D->split_gradients};
     const lattice_status s = grow(D, loss_scratch(D, a), "linear_cross_entropy");
     if (s) return s;
     const hipError_t err = launch_loss(D, a);

@@ -18,11 +18,16 @@
 // of 192 channels 229 and 248, of 128 200 and 207).
 //
 // The products run on the bf16 matrix cores (gemm.h): bf16 operands as they
-// are, fp32 ones as three planes.  G is rounded to bf16 for bf16 gradients (a
+// are, fp32 ones as three planes.  For bf16 gradients G is rounded to bf16 (a
 // relative 2^-8 of each term at most, random in sign, as the gradients' own
 // rounding is; s is left out of it, or the entries near -s of all rows would be off by
-// the same part), and kept in three planes for fp32 ones.  The bias gradient is
-// summed from G before that rounding.  Sums are fp32, joined in a fixed order.
+// the same part), or held in two planes if the caller asks for that: dx and dw are
+// then two products each.  dx against 64 bits, and the time of a call, with one
+// plane and with two, where the rounding of the stored dx alone makes 1.66e-3:
+// 8192 x 1024 x 65536 1.66e-3 and 1.66e-3, 4.5 and 7.7 ms; 2048 x 512 x 5000
+// 1.69e-3 and 1.65e-3, 122 and 188 us; 100000 x 64 x 200 1.90e-3 and 1.66e-3, 150
+// and 212 us.  For fp32 gradients G is in three planes.  The bias gradient is
+// summed from G before any rounding.  Sums are fp32, joined in a fixed order.
 //
 // With gradients the matrix cores bound it: 8192 rows, 65536 classes of 1024
 // channels in bf16 take 4.4 ms (1.0 PFLOP/s of 8 N C K operations): the first
@@ -317,17 +322,17 @@ __device__ __forceinline__ int sum32(float (&sum)[16]) {
     return which;
 }
 
-// Epilogue of the second pass over a piece of classes: G in both orders, and
-// partial sums of its columns.
-template <int P>
+// Epilogue of the second pass over a piece of classes: G in both orders, in PG
+// planes, and partial sums of its columns.
+template <int P, int PG>
 struct Grad : gemm::Simple {
     const float *bias;  // padded, of the piece's first class on
     Rows rows;
     int class0;         // of the piece
     int K, Kp, np;      // classes of the piece, classes and rows padded
     int64_t ldg, ldt;   // values between the rows of g and of gt
-    uint16_t *g;        // [P][n][ldg], classes up to Kp written, or null
-    uint16_t *gt;       // [P][K][ldt], rows up to np written, or null
+    uint16_t *g;        // [PG][n][ldg], classes up to Kp written, or null
+    uint16_t *gt;       // [PG][K][ldt], rows up to np written, or null
     float *pbias;       // [tiles of rows * WN][K], or null
     const float *factor;
 
@@ -376,7 +381,7 @@ struct Grad : gemm::Simple {
         }
         const bool labels = __any(here);  // few wavefronts hold a row's label
         const float f = pbias ? *factor : 0.f;
-        uint32_t pk[T::TM][T::TN][4][2][P];  // four classes of a row, twice two
+        uint32_t pk[T::TM][T::TN][4][2][PG];  // four classes of a row, twice two
 #pragma unroll
         for (int i = 0; i < T::TM; ++i) {
             float sum[16];
@@ -401,8 +406,8 @@ struct Grad : gemm::Simple {
                             if (row + r == t[j]) v[r] -= 1.f;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) sum[4 * q + r] += v[r];
-                    planes::split_pair<P>(v[0], v[1], pk[i][j][q][0]);
-                    planes::split_pair<P>(v[2], v[3], pk[i][j][q][1]);
+                    planes::split_pair<PG>(v[0], v[1], pk[i][j][q][0]);
+                    planes::split_pair<PG>(v[2], v[3], pk[i][j][q][1]);
                 }
             if (pbias) {
                 // over the 32 lanes: halves of the values are exchanged, so that
@@ -413,7 +418,7 @@ struct Grad : gemm::Simple {
                     pbias[((int64_t)at.tile_n * T::WN + wave % T::WN) * K + row] = sum[0] * f;
             }
         }
-        planes::store_both<T, P>(pk, at, lds, g, ldg, (int64_t)n * ldg, n, Kp, gt, ldt, (int64_t)K * ldt, K, np);
+        planes::store_both<T, PG>(pk, at, lds, g, ldg, (int64_t)n * ldg, n, Kp, gt, ldt, (int64_t)K * ldt, K, np);
     }
 };
 
@@ -734,8 +739,8 @@ hipError_t again(hipStream_t st, int kind, const gemm::Store &kept, const E &e) 
     return gemm::launch_again<FewTile>(st, kept, e);
 }
 
-// Sizes of the pieces and where everything lies in the scratch.
-template <int P>
+// Sizes of the pieces and where everything lies in the scratch.  PG: planes of G.
+template <int P, int PG>
 struct Plan {
     int64_t R;           // rows of a piece
     int64_t Kpad;        // classes in whole tiles
@@ -763,7 +768,7 @@ struct Plan {
         keep = P == 3 && C >= 192 && a.any_grad();
         if (keep && R > 256 && R * Kpad > kKeep / 4) R = kKeep / 4 / Kpad > 256 ? kKeep / 4 / Kpad / 256 * 256 : 256;
         const int64_t Rp = gemm::padded(R), Rl = gemm::row_length(R);
-        KP = kPieceBytes / (Rp * P * 2 * 2) / 256 * 256;
+        KP = kPieceBytes / (Rp * PG * 2 * 2) / 256 * 256;
         KP = KP < 256 ? 256 : KP;
         KP = KP < Kpad ? KP : Kpad;
         const int64_t kp = KP < K ? KP : K;
@@ -775,6 +780,7 @@ struct Plan {
         const bool few = a.N <= 64 && (P == 3 ? !a.any_grad() || keep : !a.any_grad() && !as_is(a.w, a.w_stride));
         fkind = few ? STRAIGHT : logit_tile_for<P>(K, R, cu);
         gkind = keep ? fkind : logit_tile_for<P>(kp, R, cu);
+        if (PG != P && gkind == LARGE) gkind = MIDDLE;  // two planes beside the large tile's sums do not fit the registers
         xkind = split_tile_for<P>(R, C, kp, cu);
         wkind = split_tile_for<P>(kp, C, R, cu);
         xpart = gemm::part_length(gemm::padded(kp), splits_for<P>(xkind, R, C, kp, cu));
@@ -799,24 +805,24 @@ struct Plan {
         wp = own_w ? s.take(P * K * Cl * 2) : 0;
         xt = a.grad_w ? s.take(P * C * Rl * 2) : 0;
         wt = a.grad_x ? s.take(P * C * gemm::row_length(K) * 2) : 0;
-        g = a.grad_x ? s.take(P * R * gemm::row_length(kp) * 2) : 0;
-        gt = a.grad_w ? s.take(P * kp * Rl * 2) : 0;
+        g = a.grad_x ? s.take(PG * R * gemm::row_length(kp) * 2) : 0;
+        gt = a.grad_w ? s.take(PG * kp * Rl * 2) : 0;
         if (a.grad_bias) {
             const int64_t rows = bias_rows<P>(gkind, R);
             pbias = s.take((rows * kp + rowsum::scratch_floats(rows, kp)) * 4);
             const int64_t pieces = (a.N + R - 1) / R;
             bias_acc = s.take((pieces < kHeld ? pieces : kHeld) * K * 4);
         }
-        px = a.grad_x ? s.take(one_piece && xsplits == 1 ? 0 : xsplits * R * C * 4) : 0;
-        pw = a.grad_w ? s.take(a.N <= R && wsplits == 1 ? 0 : wsplits * K * C * 4) : 0;
+        px = a.grad_x ? s.take(PG == P && one_piece && xsplits == 1 ? 0 : xsplits * R * C * 4) : 0;
+        pw = a.grad_w ? s.take(PG == P && a.N <= R && wsplits == 1 ? 0 : wsplits * K * C * 4) : 0;
         kept = keep ? s.take(tile_count<P>(fkind, K, R) * tile_m<P>(fkind) * tile_n<P>(fkind) * 4) : 0;
         bytes = s.bytes;
     }
 };
 
-template <int P>
+template <int P, int PG>
 hipError_t run(lattice_dense *D, const LossArgs &a) {
-    const Plan<P> p(D, a);
+    const Plan<P, PG> p(D, a);
     char *ws = reinterpret_cast<char *>(D->ws);
     hipStream_t st = D->stream;
     auto f = [&](int64_t at) { return reinterpret_cast<float *>(ws + at); };
@@ -843,7 +849,9 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
     gemm::Operand W = {reinterpret_cast<const uint16_t *>(a.w), a.w_stride, 0, 0, K};
     if (p.own_w) W = planes::operand(h(p.wp), K, C, P);
     // gradients that their product's epilogue writes as they are
-    const bool x_at_once = p.one_piece && p.xsplits == 1, w_at_once = a.N <= p.R && p.wsplits == 1;
+    const bool x_at_once = PG == P && p.one_piece && p.xsplits == 1;
+    const bool w_at_once = PG == P && a.N <= p.R && p.wsplits == 1;
+    constexpr int MORE = PG - P;  // planes of G that are multiplied apart: the smaller ones, first
     int64_t parts = 0;
     int piece = 0, held = 0;  // pieces, and rows of bias_acc that wait to be added
     for (int64_t r0 = 0; r0 < a.N; r0 += p.R, ++piece) {
@@ -892,7 +900,7 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
             gemm::Operand Wk = W;
             Wk.p += k0 * W.ld;
             Wk.rows = kn;
-            const Grad<P> grad = {{}, f(p.bias) + k0, {ints(p.label), f(p.lse), n}, (int)k0, kn, (int)kp, (int)np,
+            const Grad<P, PG> grad = {{}, f(p.bias) + k0, {ints(p.label), f(p.lse), n}, (int)k0, kn, (int)kp, (int)np,
                                   gemm::row_length(kn), gemm::row_length(n),
                                   a.grad_x ? h(p.g) : nullptr, a.grad_w ? h(p.gt) : nullptr,
                                   a.grad_bias ? f(p.pbias) : nullptr, f(p.factor)};
@@ -915,16 +923,21 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
             if (a.grad_x) {
                 gemm::Operand Wt = planes::operand(h(p.wt), C, K, P);
                 Wt.p += k0;
-                TRY((product<P>(st, p.xkind, planes::operand(h(p.g), n, kn, P), Wt, kp, p.xpart,
-                                Part<P>{f(p.px), n, C, k0 > 0, x_at_once ? a.grad_x : nullptr, f(p.factor)})));
+                for (int q = MORE; q >= 0; --q)
+                    TRY((product<P>(st, p.xkind,
+                                    planes::operand(h(p.g) + q * n * gemm::row_length(kn), n, kn, P), Wt, kp, p.xpart,
+                                    Part<P>{f(p.px), n, C, k0 > 0 || q < MORE, x_at_once ? a.grad_x : nullptr,
+                                            f(p.factor)})));
             }
             if (a.grad_w) {
                 float *sums = f(p.pw) + k0 * C * p.wsplits;
-                TRY((product<P>(st, p.wkind, planes::operand(h(p.gt), kn, n, P), planes::operand(h(p.xt), C, n, P), np,
-                                p.wpart,
-                                Part<P>{sums, kn, C, r0 > 0,
-                                        w_at_once ? reinterpret_cast<char *>(a.grad_w) + k0 * C * esz : nullptr,
-                                        f(p.factor)})));
+                for (int q = MORE; q >= 0; --q)
+                    TRY((product<P>(st, p.wkind,
+                                    planes::operand(h(p.gt) + q * kn * gemm::row_length(n), kn, n, P),
+                                    planes::operand(h(p.xt), C, n, P), np, p.wpart,
+                                    Part<P>{sums, kn, C, r0 > 0 || q < MORE,
+                                            w_at_once ? reinterpret_cast<char *>(a.grad_w) + k0 * C * esz : nullptr,
+                                            f(p.factor)})));
                 if (r0 + p.R >= a.N && !w_at_once) {
                     const int64_t v = (int64_t)kn * C;
                     // a later piece of rows is no longer than the first, and has no more parts
@@ -961,10 +974,12 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
 
 int64_t loss_scratch(const lattice_dense *D, const LossArgs &a) {
     if (loss_fused_covers(a)) return loss_fused_scratch(D, a);
-    return a.bf16 ? Plan<1>(D, a).bytes : Plan<3>(D, a).bytes;
+    if (!a.bf16) return Plan<3, 3>(D, a).bytes;
+    return a.split && a.any_grad() ? Plan<1, 2>(D, a).bytes : Plan<1, 1>(D, a).bytes;
 }
 
 hipError_t launch_loss(lattice_dense *D, const LossArgs &a) {
     if (loss_fused_covers(a)) return launch_loss_fused(D, a);
-    return a.bf16 ? run<1>(D, a) : run<3>(D, a);
+    if (!a.bf16) return run<3, 3>(D, a);
+    return a.split && a.any_grad() ? run<1, 2>(D, a) : run<1, 1>(D, a);
 }

@@ -25,9 +25,12 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 class Dense:
     """The dense operators on the current device and on one stream (the current
     one unless given).  Called while another stream is current, an operator
-    waits for that stream's work so far, and that stream for the operator."""
+    waits for that stream's work so far, and that stream for the operator.
+    ``gradient_bits`` (8 or 16) are those of d loss / dz in the products that
+    give ``linear_cross_entropy``'s gradients of bf16 operands; few classes of
+    few channels have 16 in any case.  No operator records an autograd graph."""
 
-    def __init__(self, stream: Optional[torch.cuda.Stream] = None):
+    def __init__(self, stream: Optional[torch.cuda.Stream] = None, gradient_bits: int = 8):
         self._lib = load_library()
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self.device = self.stream.device
@@ -38,6 +41,10 @@ class Dense:
         if st != OK:
             raise LatticeError(st, f"lattice_dense_create: {self._lib.lattice_status_string(st).decode()}")
         self._h = h
+        st = self._lib.lattice_dense_set_gradient_bits(h, gradient_bits)
+        if st != OK:
+            self.close()
+            raise ValueError(f"gradient_bits must be 8 or 16, got {gradient_bits}")
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:

@@ -34,6 +34,7 @@ EXPORTS = (
     "lattice_distribute_pointnet", "lattice_conv_backward_noalloc", "lattice_downsample_backward",
     "lattice_upsample_backward", "lattice_deform_slice_backward", "lattice_distribute_pointnet_backward",
     "lattice_dense_create", "lattice_dense_destroy", "lattice_dense_get_status", "lattice_dense_last_error",
+    "lattice_dense_set_gradient_bits",
     "lattice_layer_norm", "lattice_layer_norm_backward", "lattice_linear_cross_entropy", "lattice_orthogonalize",
 )
 
@@ -94,6 +95,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "lattice_dense_destroy": (None, [P]),
         "lattice_dense_get_status": (St, [P]),
         "lattice_dense_last_error": (ctypes.c_char_p, [P]),
+        "lattice_dense_set_gradient_bits": (St, [P, I]),
         "lattice_layer_norm": (St, [P, P, P, I, I64, I64, I, P, P, F, P, I, I64, P, P]),
         "lattice_layer_norm_backward": (St, [P, P, P, I, I64, P, I, I64, I64, I, P, P, P, P, I64, P, P]),
         "lattice_linear_cross_entropy": (St, [P, I, P, I64, I64, I, P, I64, I, P, P, I64, I, P, P, P, P, P]),

@@ -49,3 +49,9 @@ def test_work_is_on_the_handles_device(driver):
 def test_layer_norm_backward_without_rows(driver):
     """Short and long rows, any of the outputs, or none that has an address."""
     run(driver, "no_rows")
+
+
+def test_gradient_bits_of_no_handle():
+    from paper_2108_03917_amd import lattice as B
+
+    assert B.load_library().lattice_dense_set_gradient_bits(None, 8) == B.E_ARG

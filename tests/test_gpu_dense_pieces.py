@@ -101,3 +101,39 @@ def test_gradients_of_few_classes_in_bf16(ops, N, C, K):  # noqa: F811
     terms, ref = loss_terms(x, w, t, bias)
     check_loss(got, ref, "bf16")
     check_gradients(got[2:4], terms, 16)
+
+
+MANY = [(1000, 64, 200), (513, 100, 777), (300, 130, 129), (128, 260, 1000), (2048, 512, 3000), (40, 64, 1000),
+        (3000, 260, 100), (105536, 64, 2500), (70000, 48, 200)]
+
+
+@pytest.mark.parametrize("N,C,K", MANY)
+def test_gradients_of_many_classes_in_16_bits(ops, N, C, K):  # noqa: F811
+    """A handle that asks for them, on every tile, in one piece and in several;
+    what the bits do not enter is the same, bit for bit."""
+    from paper_2108_03917_amd import Dense
+
+    x, w, t, bias = rand(1, N, C, dtype="bf16"), (rand(2, K, C) * 0.3).bfloat16(), labels(3, N, K), rand(4, K)
+    own = Dense(gradient_bits=16)
+    got = own.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    terms, ref = loss_terms(x, w, t, bias)
+    check_loss(got, ref, "bf16")
+    check_gradients(got[2:4], terms, 16)
+    again = own.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    only = [own.linear_cross_entropy(x, w, t, bias, want_grad=True, want_input=i == 0, want_weight=i == 1,
+                                     want_bias=False)[1 + i] for i in range(2)]
+    assert torch.equal(only[0], got[2]) and torch.equal(only[1], got[3])
+    eight = ops.linear_cross_entropy(x, w, t, bias, want_rows=True, want_grad=True)
+    assert torch.equal(eight[0], got[0]) and torch.equal(eight[1], got[1])
+    check(got[4], eight[4].double(), ref["grad_bias"][1], REL_F32, "grad_bias")
+    torch.cuda.synchronize()
+    own.close()
+
+
+def test_gradient_bits_that_are_neither(ops):  # noqa: F811
+    from paper_2108_03917_amd import Dense
+
+    for bits in (0, 7, 24):
+        with pytest.raises(ValueError):
+            Dense(gradient_bits=bits)
