@@ -602,7 +602,8 @@ template <int P, class E>
 hipError_t product(hipStream_t st, int kind, const gemm::Operand &A, const gemm::Operand &B, int64_t K, int64_t part,
                    const E &e) {
     using X = Tiles<P>;
-    if (kind == LARGE) return gemm::launch<typename X::Large>(st, A, B, K, part, 1, false, e);
+    if constexpr (!std::is_same<E, Grad<1, 2>>::value)  // the plan has no large tile for it
+        if (kind == LARGE) return gemm::launch<typename X::Large>(st, A, B, K, part, 1, false, e);
     if (kind == MIDDLE) return gemm::launch<typename X::Middle>(st, A, B, K, part, 1, false, e);
     if (kind == SMALL) return gemm::launch<typename X::Small>(st, A, B, K, part, 1, false, e);
     if (kind == THIN) return gemm::launch<typename X::Thin>(st, A, B, K, part, 1, false, e);
