@@ -722,7 +722,9 @@ lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows
 /*
  * lattice_linear_cross_entropy -- a linear classifier with its softmax cross
  * entropy, and in the same call its gradients, without the N x K logits in
- * memory:
+ * memory, but for those of a piece of rows where computing them twice would cost
+ * more (gradients of fp32 operands of 192 channels or more: scratch of up to 1 GiB,
+ * or for 256 rows if these need more; a problem that fits keeps all of them):
  *   z_ik = x_i . w_k + bias_k,   lse_i = log sum_k exp z_ik
  *   row_loss_i = lse_i - z_it, t = target_i (0 for a row without a label)
  *   loss = sum of the row losses; with mean, over the rows that have a label
@@ -744,8 +746,8 @@ lattice_status lattice_layer_norm_backward(lattice_dense *D, const lattice *rows
  *   grad_x        dev [N][C], or NULL; zero for rows without a label.
  *   grad_w        dev [K][C], or NULL.    grad_bias dev fp32 [K], or NULL.
  * What a row without a label holds (NaN, infinities) reaches no result.  fp32
- * operands of 2^104 or more in magnitude give NaN.  The gradients overlap
- * neither x nor w.
+ * operands of 2^104 or more in magnitude, and infinities, give NaN where one
+ * workgroup does not hold w.  The gradients overlap neither x nor w.
  */
 #define LATTICE_LOSS_MAX_ROWS ((int64_t)1 << 28)
 #define LATTICE_LOSS_MAX_CHANNELS (1 << 14)

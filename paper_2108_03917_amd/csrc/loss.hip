@@ -1,5 +1,5 @@
-// The linear classifier with softmax cross entropy, and its gradients, without
-// the logits in memory.
+// The linear classifier with softmax cross entropy, and its gradients, with no
+// more than a piece of the logits in memory at a time.
 //
 //   z_ik = x_i . w_k + b_k,   lse_i = log sum_k exp z_ik,   l_i = lse_i - z_it (t = target_i)
 //   L = sum_i s l_i,  s = 1, or 1 / (rows with a label);  rows without a label count for nothing
@@ -13,8 +13,9 @@
 // second product of the logits costs a third more operations than the gradients
 // need; where it would cost more than writing and reading the logits of a piece
 // of rows (fp32 operands, whose products are six each, from 192 channels on),
-// pieces are cut to a gigabyte of logits and these are kept till G is formed
-// (both passes over 1848 x 18928 logits of 245 channels: 265 us kept, 308 again;
+// pieces are cut to a gigabyte of logits, or to 256 rows if these have more, and
+// they are kept till G is formed (so a small problem's logits are all in memory;
+// both passes over 1848 x 18928 logits of 245 channels: 265 us kept, 308 again;
 // of 192 channels 229 and 248, of 128 200 and 207).
 //
 // The products run on the bf16 matrix cores (gemm.h): bf16 operands as they

@@ -22,7 +22,8 @@
 // Large matrices are bound by the matrix cores: a step of 2048 x 8192 with a
 // bf16 result takes 375 us (190 for Q X, at 1.1 PFLOP/s of bf16 products, 103
 // and 21 for S and the join of its parts, 62 for S S), of 210 at the rate of a
-// large library product.  Small ones by the latency of a slice on a chip that
+// large library product.  Q X holds its packed result beside the sums: 256
+// registers a lane and 17 more in memory.  Small ones by the latency of a slice on a chip that
 // they do not fill: 700 x 1531 in fp32, 52 us a step of 10.
 #include "planes.h"
 #include "update.h"
@@ -311,12 +312,13 @@ struct Tiles<3, LOWER> {
 // Which tile a product takes and the length of its contraction's parts.  The
 // large tile reads the least: it is taken where there are enough of them, or
 // where parts of a long contraction give enough and each is still long (S of a
-// 2048 x 8192 matrix in 16 bits: 106 us in 7 parts, 182 in 128 x 128 tiles).
-// Else the largest tile that keeps half the CUs busy (its square: 42 us in 136
-// tiles of 128 x 128, 49 in 528 of 64 x 64), or the smallest, in parts if the
-// contraction is long enough to pay for the launch that joins them, 6 us (S of
-// a 700 x 1531 matrix in 24 bits: 16 us in 3 parts, 25 in one; its square, over
-// 704: 15 either way).
+// 2048 x 8192 matrix in 16 bits: 98 us in 7 parts and 20 to join them, 182 in 128 x
+// 128 tiles).  Else the largest tile that keeps half the CUs busy (its square, in
+// a step: 58 us in 136 tiles of 128 x 128, 66 in 528 of 64 x 64; both slower than
+// alone, since the product before it has filled the caches), or the smallest, in
+// parts if the contraction is long enough to pay for the launch that joins them,
+// 6 us (S of a 700 x 1531 matrix in 24 bits: 16 us in 3 parts, 25 in one; its
+// square, over 704: 15 either way).
 struct Choice {
     int kind;
     int64_t part, parts;
