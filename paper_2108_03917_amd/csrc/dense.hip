@@ -148,7 +148,7 @@ lattice_status lattice_dense_create(void *stream, lattice_dense **out) {
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, D->device) == hipSuccess && cus > 0)
         D->cu_count = cus;
     const bool ok = hipMalloc(&D->status, sizeof(int32_t)) == hipSuccess &&
-                    hipMemset(D->status, 0, sizeof(int32_t)) == hipSuccess &&
+                    hipMemsetAsync(D->status, 0, sizeof(int32_t), D->stream) == hipSuccess &&
                     hipHostMalloc(&D->host_status, sizeof(int32_t), hipHostMallocDefault) == hipSuccess;
     if (!ok) {
         (void)hipGetLastError();

@@ -42,6 +42,7 @@ std::map<uintptr_t, size_t> blocks;       // live, by address
 uintptr_t next_address = (uintptr_t)1 << 44;
 int64_t launches = 0;
 int want_device = -1;                     // on which all work has to be, or any
+hipStream_t want_stream = nullptr;        // likewise
 void (*on_launch)(const Launch &) = nullptr;
 dim3 pushed_grid, pushed_block;
 size_t pushed_lds;
@@ -50,6 +51,10 @@ bool capturing = false;
 
 void here(const char *what) {
     if (want_device >= 0 && device != want_device) fail("%s on device %d, not %d", what, device, want_device);
+}
+
+void on(const char *what, hipStream_t s) {
+    if (want_stream && s != want_stream) fail("%s on another stream than the handle's", what);
 }
 
 std::map<const void *, std::string> &names() {
@@ -94,11 +99,12 @@ hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *lds, hipSt
     *stream = pushed_stream;
     return hipSuccess;
 }
-hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, size_t lds, hipStream_t) {
+hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, size_t lds, hipStream_t stream) {
     if (!grid.x || !grid.y || !grid.z || !block.x || !block.y || !block.z || block.x * block.y * block.z > 1024 ||
         lds > 160 * 1024)
         return last = hipErrorInvalidConfiguration;
     here("a launch");
+    on("a launch", stream);
     ++launches;
     if (on_launch) on_launch({names()[fn], grid, device, args});
     return hipSuccess;
@@ -144,14 +150,17 @@ hipError_t hipHostFree(void *p) {
 }
 hipError_t hipMemset(void *, int, size_t) {
     here("hipMemset");
+    on("hipMemset", nullptr);
     return hipSuccess;
 }
-hipError_t hipMemsetAsync(void *, int, size_t, hipStream_t) {
+hipError_t hipMemsetAsync(void *, int, size_t, hipStream_t stream) {
     here("hipMemsetAsync");
+    on("hipMemsetAsync", stream);
     return hipSuccess;
 }
-hipError_t hipMemcpyAsync(void *to, const void *, size_t n, hipMemcpyKind, hipStream_t) {
+hipError_t hipMemcpyAsync(void *to, const void *, size_t n, hipMemcpyKind, hipStream_t stream) {
     here("a copy");
+    on("a copy", stream);
     std::memset(to, 0, n);
     return hipSuccess;
 }
@@ -292,6 +301,38 @@ void another_current_device() {
     if (device != 0) fail("destroy left device %d current", device);
 }
 
+// -- stream ------------------------------------------------------------------
+
+// Everything a handle does from its making on is in the order of its stream,
+// which need not wait for the null stream.
+void the_handles_stream() {
+    int stream_of_its_own = 0;
+    const int64_t rows = 70000;
+    const int C = 200, K = 300;
+    float *x = buffer<float>(rows * C), *y = buffer<float>(rows * C), *v = buffer<float>(4 * rows), *w = buffer<float>(K * C);
+    int64_t *target = buffer<int64_t>(rows);
+    const float ns[3] = {1.5f, -0.5f, 0.f};
+    want_stream = reinterpret_cast<hipStream_t>(&stream_of_its_own);
+    lattice_dense *D = handle(want_stream);
+    for (const lattice_dtype t : {LATTICE_F32, LATTICE_BF16}) {
+        expect("layer_norm", D, lattice_layer_norm(D, nullptr, x, t, C, rows, C, nullptr, nullptr, 0.f, y, t, C, v, v + rows),
+               LATTICE_OK);
+        expect("layer_norm_backward", D,
+               lattice_layer_norm_backward(D, nullptr, y, t, C, x, t, C, rows, C, v, v + rows, nullptr, nullptr, C,
+                                           v + 2 * rows, v + 3 * rows),
+               LATTICE_OK);
+        for (const int k : {20, K})
+            expect("linear_cross_entropy", D,
+                   lattice_linear_cross_entropy(D, t, x, C, rows, C, w, C, k, nullptr, target, -100, 1, v, v + 1, y, nullptr,
+                                                v + 2 * rows),
+                   LATTICE_OK);
+        for (const int n : {100, 400})
+            expect("orthogonalize", D, lattice_orthogonalize(D, x, t, 2, n, n, n * n, n, 5, ns, 0.f, y, t), LATTICE_OK);
+    }
+    expect("get_status", D, lattice_dense_get_status(D), LATTICE_OK);
+    lattice_dense_destroy(D);
+}
+
 // -- empty inputs ------------------------------------------------------------
 
 // No rows: every width and output is taken, and no launch is malformed.
@@ -315,6 +356,7 @@ int main(int argc, char **argv) {
     const std::map<std::string, void (*)()> checks = {{"many_pieces", many_pieces},
                                                          {"captured_scratch", captured_scratch},
                                                          {"another_current_device", another_current_device},
+                                                         {"the_handles_stream", the_handles_stream},
                                                          {"no_rows", no_rows}};
     const auto it = checks.find(argc > 1 ? argv[1] : "");
     if (it == checks.end()) fail("which check?");

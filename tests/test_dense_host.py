@@ -55,3 +55,9 @@ def test_gradient_bits_of_no_handle():
     from paper_2108_03917_amd import lattice as B
 
     assert B.load_library().lattice_dense_set_gradient_bits(None, 8) == B.E_ARG
+
+
+def test_work_is_in_the_order_of_the_handles_stream(driver):
+    """From the clearing of its status word on: its stream need not wait for the
+    null stream."""
+    run(driver, "the_handles_stream")
