@@ -5,14 +5,17 @@
 // written: they only stand for device memory.
 //
 //   host_driver CHECK      prints "ok", or what is wrong and exits with 1
+#include <cxxabi.h>
 #include <hip/hip_runtime_api.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <random>
 #include <string>
 #include <vector>
 
@@ -236,6 +239,95 @@ void many_pieces() {
     lattice_dense_destroy(D);
 }
 
+// -- products ----------------------------------------------------------------
+
+// The arguments of k_gemm<Tile<BM, BN, WM, WN, BK, P, STAGES>, ..>.
+struct Operand {
+    const uint16_t *p;
+    int64_t ld, plane, batch;
+    int rows;
+};
+struct Shape {
+    int K, k_split, tiles_m, tiles_n;
+    bool lower;
+};
+
+std::string demangled(const std::string &name) {
+    int status = 0;
+    char *d = abi::__cxa_demangle(name.c_str(), nullptr, nullptr, &status);
+    std::string s = d ? d : name;
+    std::free(d);
+    return s;
+}
+
+// What a product's direct loads read of an operand: 16-byte pieces of all its
+// rows and planes, for every matrix of a batch, up to the contraction's end.
+void look_at_products(const Launch &l) {
+    look_at_rowsum(l);
+    if (l.name.find("6k_gemmI") == std::string::npos) return;
+    static std::map<std::string, int> planes_of;
+    auto it = planes_of.find(l.name);
+    if (it == planes_of.end()) {
+        const std::string s = demangled(l.name);
+        int t[7];
+        const size_t at = s.find("Tile<");
+        if (at == std::string::npos || std::sscanf(s.c_str() + at, "Tile<%d, %d, %d, %d, %d, %d, %d", t, t + 1, t + 2, t + 3,
+                                                   t + 4, t + 5, t + 6) != 7)
+            fail("a product without a tile: %s", s.c_str());
+        it = planes_of.emplace(l.name, t[5]).first;
+    }
+    const Shape &s = *static_cast<const Shape *>(l.args[2]);
+    if (s.K < 64 || s.K % 64 || s.k_split < 64 || s.k_split % 64 || (int64_t)(l.grid.y - 1) * s.k_split >= s.K)
+        fail("a contraction of %d in %u parts of %d", s.K, l.grid.y, s.k_split);
+    for (int i = 0; i < 2; ++i) {
+        const Operand &o = *static_cast<const Operand *>(l.args[i]);
+        if (o.rows < 1 || o.ld < s.K || o.ld >= (int64_t)1 << 22 || o.ld % 8 || (reinterpret_cast<uintptr_t>(o.p) & 15))
+            fail("operand %d: %d rows of %lld at %p over %d", i, o.rows, (long long)o.ld, (const void *)o.p, s.K);
+        const int64_t values = (int64_t)(l.grid.z - 1) * o.batch + (it->second - 1) * o.plane + (o.rows - 1) * o.ld + s.K;
+        if (!block_of(o.p, values * 2))
+            fail("operand %d: %lld values from %p leave their block", i, (long long)values, (const void *)o.p);
+    }
+}
+
+// Losses and updates of many sizes, most of them odd, up to pieces of rows and
+// classes and chunks of a batch.
+void products_stay_inside() {
+    on_launch = look_at_products;
+    std::mt19937 rng(5);
+    auto size = [&](double lo, double hi) {
+        return (int64_t)std::exp(std::uniform_real_distribution<double>(std::log(lo), std::log(hi))(rng));
+    };
+    const float ns[3] = {3.4445f, -4.7750f, 2.0315f};
+    for (int i = 0; i < 3000; ++i) {
+        const std::map<uintptr_t, size_t> none;
+        blocks = none;
+        lattice_dense *D = handle();
+        const lattice_dtype t = rng() % 2 ? LATTICE_F32 : LATTICE_BF16;
+        const int64_t e = t == LATTICE_F32 ? 4 : 2;
+        lattice_status got;
+        if (rng() % 3) {
+            const int64_t N = size(1, rng() % 4 ? 9000 : 1e6);
+            const int C = (int)(rng() % 3 ? size(1, 3000) : 64 * (1 + rng() % 32)), K = (int)size(1, rng() % 4 ? 70000 : 1 << 20);
+            const int64_t xs = C + (rng() % 2 ? 0 : (rng() % 2 ? 8 : rng() % 9)), ws = C + (rng() % 2 ? 0 : 8);
+            const int want = rng() % 8;
+            lattice_dense_set_gradient_bits(D, rng() % 2 ? 8 : 16);
+            got = lattice_linear_cross_entropy(
+                D, t, buffer<char>(((N - 1) * xs + C) * e), xs, N, C, buffer<char>(((K - 1) * ws + C) * e), ws, K,
+                rng() % 2 ? buffer<float>(K) : nullptr, buffer<int64_t>(N), -100, 1, buffer<float>(1), buffer<float>(N),
+                want & 1 ? buffer<char>(N * C * e) : nullptr, want & 2 ? buffer<char>((int64_t)K * C * e) : nullptr,
+                want & 4 ? buffer<float>(K) : nullptr);
+        } else {
+            const int64_t batch = size(1, 300), m = size(1, 3000), n = size(1, 9000);
+            const lattice_dtype o = rng() % 2 ? LATTICE_F32 : LATTICE_BF16;
+            got = lattice_orthogonalize(D, buffer<char>(batch * m * n * e), t, batch, (int)m, (int)n, m * n, n, 2, ns, 1e-7f,
+                                        buffer<char>(batch * m * n * 4), o);
+        }
+        expect("a call", D, got, LATTICE_OK);
+        lattice_dense_destroy(D);
+    }
+    if (launches < 20000) fail("only %lld launches", (long long)launches);
+}
+
 // -- scratch -----------------------------------------------------------------
 
 // The scratch that a call was captured with outlives every larger call.
@@ -357,7 +449,8 @@ int main(int argc, char **argv) {
                                                          {"captured_scratch", captured_scratch},
                                                          {"another_current_device", another_current_device},
                                                          {"the_handles_stream", the_handles_stream},
-                                                         {"no_rows", no_rows}};
+                                                         {"no_rows", no_rows},
+                                                         {"products_stay_inside", products_stay_inside}};
     const auto it = checks.find(argc > 1 ? argv[1] : "");
     if (it == checks.end()) fail("which check?");
     it->second();

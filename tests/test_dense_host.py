@@ -61,3 +61,9 @@ def test_work_is_in_the_order_of_the_handles_stream(driver):
     """From the clearing of its status word on: its stream need not wait for the
     null stream."""
     run(driver, "the_handles_stream")
+
+
+def test_products_read_inside_their_operands(driver):
+    """Operands of every product of 3000 losses and updates of random sizes lie
+    inside the callers' buffers or the scratch, padding and planes included."""
+    run(driver, "products_stay_inside")
