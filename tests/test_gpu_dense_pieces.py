@@ -137,3 +137,18 @@ def test_gradient_bits_that_are_neither(ops):  # noqa: F811
     for bits in (0, 7, 24):
         with pytest.raises(ValueError):
             Dense(gradient_bits=bits)
+
+
+@pytest.mark.parametrize("batch,m,n", [(1, 1531, 700), (2, 1255, 1504), (1, 2000, 2048)])
+def test_update_is_as_accurate_as_fp32_products(ops, batch, m, n):  # noqa: F811
+    """The same steps in plain fp32 products are no nearer to 64 bits."""
+    g = rand(1, batch, m, n) + rand(2, batch, m, 40) @ rand(3, batch, 40, n)
+    ref = update_ref(g)
+    a, b, c = 3.4445, -4.7750, 2.0315
+    x = g.mT.contiguous() if m > n else g
+    x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + 1e-7)
+    for _ in range(5):
+        s = torch.matmul(x, x.mT.contiguous())
+        x = a * x + torch.matmul(b * s + c * torch.matmul(s, s), x)
+    plain = ((x.mT if m > n else x).double() - ref).norm()
+    assert (ops.orthogonalize(g).double() - ref).norm() <= plain
