@@ -642,8 +642,7 @@ lattice_status lattice_get_timing(lattice *L, double *ms, int64_t *count);
  * enqueued on the stream given at creation, on the device that was current
  * then, whichever is at the call, and no call but lattice_dense_get_status and
  * lattice_dense_destroy synchronises with the host.  A call that needs more scratch than any before it allocates device
- * memory; while the stream is being captured into a HIP graph it is refused
- * instead (LATTICE_E_STATE: make the call once before the capture).  A graph
+ * memory, also while its stream is being captured into a HIP graph.  A graph
  * goes on using the scratch that its calls were captured with, which is kept
  * until the handle is destroyed whatever later calls need: destroy it after the
  * graph, and order replays with the handle's other calls.

@@ -35,10 +35,21 @@ bool capturing(const lattice_dense *D) {
     return status != hipStreamCaptureStatusNone;
 }
 
+// hipMalloc, also while a stream of this thread is being captured in a mode that
+// forbids it: an allocation is no part of the graph.
+hipError_t allocate(void **p, int64_t bytes, bool captured) {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    if (captured) TRY(hipThreadExchangeStreamCaptureMode(&mode));
+    const hipError_t e = hipMalloc(p, bytes);
+    if (captured) (void)hipThreadExchangeStreamCaptureMode(&mode);
+    return e;
+}
+
 // Grow the scratch to at least `need` bytes (a device allocation, only when it
 // is too small; freeing the old one waits for the work that uses it).  A graph
 // goes on using the scratch that its calls were captured with: that one is
-// kept until the handle is destroyed.
+// kept until the handle is destroyed, and so is any that is replaced during a
+// capture, which cannot wait.
 lattice_status grow(lattice_dense *D, int64_t need, const char *what) {
     if (need <= 0) return LATTICE_OK;
     const bool now = capturing(D);
@@ -46,13 +57,7 @@ lattice_status grow(lattice_dense *D, int64_t need, const char *what) {
         D->ws_captured |= now;
         return LATTICE_OK;
     }
-    if (now) {
-        set_err(D, "%s: the stream is being captured and %lld bytes of scratch are needed, of which there are %lld "
-                   "(make the call once before the capture)",
-                what, (long long)need, (long long)D->ws_bytes);
-        return LATTICE_E_STATE;
-    }
-    if (D->ws && D->ws_captured) {
+    if (D->ws && (D->ws_captured || now)) {
         KeptScratch *k = new (std::nothrow) KeptScratch{D->ws, D->kept};
         if (!k) {
             set_err(D, "%s: out of host memory", what);
@@ -65,8 +70,8 @@ lattice_status grow(lattice_dense *D, int64_t need, const char *what) {
     }
     D->ws = nullptr;
     D->ws_bytes = 0;
-    D->ws_captured = false;
-    if (hipMalloc(&D->ws, need) != hipSuccess) {
+    D->ws_captured = now;
+    if (allocate(&D->ws, need, now) != hipSuccess) {
         (void)hipGetLastError();
         D->ws = nullptr;
         set_err(D, "%s: cannot allocate %lld bytes of scratch", what, (long long)need);

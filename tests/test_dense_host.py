@@ -35,8 +35,8 @@ def test_bias_gradient_of_many_pieces_of_rows(driver):
 
 
 def test_scratch_of_a_captured_call_is_kept(driver):
-    """A larger call frees the scratch only if no graph may use it, and is
-    refused, with nothing done, while its stream is being captured."""
+    """A larger call frees the scratch only if no graph may use it, and leaves a
+    capture that it falls into whole."""
     run(driver, "captured_scratch")
 
 

@@ -8,10 +8,9 @@ pytestmark = pytest.mark.gpu
 
 
 def test_graph_replays_after_larger_calls(_gpu):  # noqa: F811
-    """What a graph uses stays when later calls need more scratch; a call that
-    would need more during the capture is refused and leaves the capture whole."""
-    from paper_2108_03917_amd import Dense, LatticeError
-    from paper_2108_03917_amd.lattice import E_STATE
+    """What a graph uses stays when later calls need more scratch, those in the
+    capture itself among them."""
+    from paper_2108_03917_amd import Dense
 
     s = torch.cuda.Stream()
     torch.cuda.synchronize()
@@ -32,20 +31,20 @@ def test_graph_replays_after_larger_calls(_gpu):  # noqa: F811
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=s):
             out = all_of()
-            with pytest.raises(LatticeError) as e:
-                own.linear_cross_entropy(large, w, tl, b, want_grad=True)
-            assert e.value.status == E_STATE
+            out += own.linear_cross_entropy(large[:1500], w, tl[:1500], b, want_grad=True)
+            out += all_of()
         for i in range(4):
             x.copy_(rand(10 + i, 300, 64))
             g.copy_(rand(20 + i, 200, 250))
-            # more scratch each time but the last, then something in the place
-            # of what they might have freed
-            if i < 3:
-                own.linear_cross_entropy(large[: 1500 * (i + 1)], w, tl[: 1500 * (i + 1)], b, want_grad=True)
+            # more scratch each time but the last
+            n = min(2000 + 1500 * i, 5000)
+            own.linear_cross_entropy(large[:n], w, tl[:n], b, want_grad=True)
             own.orthogonalize(wide)
             graph.replay()
             s.synchronize()
             eager = all_of()
+            eager += own.linear_cross_entropy(large[:1500], w, tl[:1500], b, want_grad=True)
+            eager += all_of()
             s.synchronize()
             assert all(torch.equal(a, c) for a, c in zip(out, eager)), i
         own.close()
