@@ -782,7 +782,8 @@ struct Plan {
         const bool few = a.N <= 64 && (P == 3 ? !a.any_grad() || keep : !a.any_grad() && !as_is(a.w, a.w_stride));
         fkind = few ? STRAIGHT : logit_tile_for<P>(K, R, cu);
         gkind = keep ? fkind : logit_tile_for<P>(kp, R, cu);
-        if (PG != P && gkind == LARGE) gkind = MIDDLE;  // two planes beside the large tile's sums do not fit the registers
+        // two planes beside the large tile's sums do not fit the registers
+        if (PG != P && gkind == LARGE) gkind = MIDDLE;
         xkind = split_tile_for<P>(R, C, kp, cu);
         wkind = split_tile_for<P>(kp, C, R, cu);
         xpart = gemm::part_length(gemm::padded(kp), splits_for<P>(xkind, R, C, kp, cu));
@@ -903,9 +904,9 @@ hipError_t run(lattice_dense *D, const LossArgs &a) {
             Wk.p += k0 * W.ld;
             Wk.rows = kn;
             const Grad<P, PG> grad = {{}, f(p.bias) + k0, {ints(p.label), f(p.lse), n}, (int)k0, kn, (int)kp, (int)np,
-                                  gemm::row_length(kn), gemm::row_length(n),
-                                  a.grad_x ? h(p.g) : nullptr, a.grad_w ? h(p.gt) : nullptr,
-                                  a.grad_bias ? f(p.pbias) : nullptr, f(p.factor)};
+                                      gemm::row_length(kn), gemm::row_length(n),
+                                      a.grad_x ? h(p.g) : nullptr, a.grad_w ? h(p.gt) : nullptr,
+                                      a.grad_bias ? f(p.pbias) : nullptr, f(p.factor)};
             bool formed = false;
             if constexpr (P == 3) {
                 if (p.keep) {

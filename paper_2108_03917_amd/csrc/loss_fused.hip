@@ -450,9 +450,9 @@ __global__ __launch_bounds__(256) void k_fused_bf16(FusedArgs f) {
                     for (int k = 0; k < KT; ++k)
 #pragma unroll
                         for (int p = HELD - 1; p >= 0; --p)
-                            dw[c][k] = mfma32(
-                                *reinterpret_cast<const u32x4_t *>(Gt + (16 * (KT * p + k) + i) * L.rs + 32 * s + 8 * q), v,
-                                dw[c][k]);
+                            dw[c][k] = mfma32(*reinterpret_cast<const u32x4_t *>(
+                                                  Gt + (16 * (KT * p + k) + i) * L.rs + 32 * s + 8 * q),
+                                              v, dw[c][k]);
                 }
             }
             __syncthreads();
@@ -514,7 +514,8 @@ int channel_groups(int C) { return C <= 64 ? 1 : C <= 128 ? 2 : 4; }
 
 int lds_bytes(const LossArgs &a) {
     const int KT = class_tiles(a.bf16, a.K);
-    return a.bf16 ? Lds16(a.C, KT).bytes(KT, channel_groups(a.C), a.any_grad()) : Lds32(a.C, KT).floats(KT, a.any_grad()) * 4;
+    return a.bf16 ? Lds16(a.C, KT).bytes(KT, channel_groups(a.C), a.any_grad())
+                  : Lds32(a.C, KT).floats(KT, a.any_grad()) * 4;
 }
 
 unsigned fused_grid(const lattice_dense *D, const LossArgs &a) {
