@@ -635,9 +635,10 @@ lattice_status lattice_get_timing(lattice *L, double *ms, int64_t *count);
 
 /*
  * Dense operators of a training step around the lattice: the normalisation of
- * vertex or point rows, the classifier's loss with its gradients, and the
- * orthogonalised form of a weight gradient.  They work on plain row-major
- * matrices and need no lattice: a lattice_dense is their handle.  It owns
+ * vertex or point rows, the classifier's loss with its gradients, the
+ * orthogonalised form of a weight gradient, attention between points with the
+ * rotation of its queries and keys, and the clipping of gradients by their
+ * norm.  They work on plain tensors and need no lattice: a lattice_dense is their handle.  It owns
  * scratch that grows on demand and a device status word; all its work is
  * enqueued on the stream given at creation, on the device that was current
  * then, whichever is at the call, and no call but lattice_dense_get_status and
@@ -665,7 +666,8 @@ void lattice_dense_destroy(lattice_dense *D);
 /*
  * Synchronise and return the device status since the last call of this
  * function, clearing it: LATTICE_E_RANGE if a lattice_linear_cross_entropy met
- * a label that is neither a class nor ignore_index.
+ * a label that is neither a class nor ignore_index, or an attention starts or
+ * lengths that do not fit its rows.
  */
 lattice_status lattice_dense_get_status(lattice_dense *D);
 const char *lattice_dense_last_error(const lattice_dense *D);
@@ -776,6 +778,149 @@ lattice_status lattice_linear_cross_entropy(lattice_dense *D, lattice_dtype dtyp
 lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dtype g_dtype, int64_t batch, int m,
                                      int n, int64_t batch_stride, int64_t row_stride, int steps,
                                      const float *coefficients, float eps, void *out, lattice_dtype out_dtype);
+
+/*
+ * Attention between the rows of packed sequences, and what stands around it.
+ * A tensor of heads [rows][heads][C] is given with the values from a row to the
+ * next and from a head to the next (any that are >= 0 for what is read, so that
+ * heads next to heads of another kind, heads before rows and repeated heads are
+ * views; what is written must not overlap itself or what is read); a head's C
+ * values are next to each other.  Tensors may start at any multiple of an
+ * element's size.
+ */
+
+/*
+ * lattice_attention -- softmax attention, a key head shared by heads / kv_heads
+ * query heads next to each other:
+ *   s_ij = scale q_i . k_j,  lse_i = log sum_j exp s_ij,
+ *   out_i = sum_j exp(s_ij - lse_i) v_j
+ * over the keys j that row i of a sequence sees: all of the sequence's, and if
+ * causal those with j <= i + (its keys) - (its rows), i and j from 0 in it.
+ *   dtype         storage of q, k, v and out.
+ *   q_rows, kv_rows   rows of q and out, and of k and v; 0 .. 2^31 - 1.
+ *   heads, kv_heads   1 .. 65536, kv_heads a divisor of heads.   C  1 .. 128.
+ *   q_starts      dev int32 [sequences + 1]: sequence b has rows q_starts[b] ..
+ *                 q_starts[b + 1] - 1.  NULL: one sequence of all rows
+ *                 (sequences = 1, kv_starts NULL).
+ *   kv_starts     dev int32 [sequences + 1], the same for k and v, or NULL for
+ *                 q_starts.
+ *   kv_lengths    dev int32 [sequences]: the keys that count of each sequence's
+ *                 rows of k and v, the first ones (a cache that is filled in
+ *                 part), or NULL for all.
+ *   sequences     0 .. 2^24.
+ *   scale         > 0.
+ *   zero_rest     rows of no sequence: non-zero makes their out 0 and their lse
+ *                 -inf, 0 leaves both as they are.
+ *   out           dev [q_rows][heads][C].   lse  dev fp32 [heads][q_rows], or NULL.
+ * A row that sees no key gets 0 and an lse of -inf.  Starts that go back or lie
+ * outside the rows, and lengths outside their sequence, are clamped to what there
+ * is, and reported by lattice_dense_get_status (LATTICE_E_RANGE).
+ * Products of fp32 are fp32 ones; of bf16 values they are exact, and exp(..) is
+ * rounded to bf16 before the product with v.  Sums are fp32.
+ * Rows of k and v that belong to no sequence or do not count are not used,
+ * whatever they hold.  A value that is not finite in a sequence's own keys or
+ * values may reach all of its rows, also those that a causal mask keeps from it.
+ */
+#define LATTICE_ATTENTION_MAX_ROWS (((int64_t)1 << 31) - 1)
+#define LATTICE_ATTENTION_MAX_HEADS 65536
+#define LATTICE_ATTENTION_MAX_CHANNELS 128
+#define LATTICE_ATTENTION_MAX_SEQUENCES ((int64_t)1 << 24)
+lattice_status lattice_attention(lattice_dense *D, lattice_dtype dtype, int64_t q_rows, int64_t kv_rows, int heads,
+                                 int kv_heads, int C, const void *q, int64_t q_row, int64_t q_head, const void *k,
+                                 int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
+                                 const int32_t *q_starts, const int32_t *kv_starts, const int32_t *kv_lengths,
+                                 int64_t sequences, int causal, float scale, int zero_rest, void *out, int64_t out_row,
+                                 int64_t out_head, float *lse);
+
+/*
+ * lattice_attention_backward -- its gradients, given g = dL/dout, with
+ * p_ij = exp(s_ij - lse_i) and t_ij = p_ij (g_i . v_j - g_i . out_i):
+ *   dq_i = scale sum_j t_ij k_j,  dk_j = scale sum_i t_ij q_i,  dv_j = sum_i p_ij g_i,
+ * the sums over i over all rows and query heads that see key j.
+ *   out, lse      of the forward call with these arguments.
+ *   grad_q        dev [q_rows][heads][C],  grad_k, grad_v  dev [kv_rows][kv_heads][C],
+ *                 without gaps, stored as dtype.
+ *   zero_rest     rows of no sequence, and keys that do not count: non-zero makes
+ *                 their gradients 0, 0 leaves them as they are.
+ * The rest as in the forward call; p and t are rounded to bf16 before their
+ * products with bf16 values.
+ */
+lattice_status lattice_attention_backward(lattice_dense *D, lattice_dtype dtype, int64_t q_rows, int64_t kv_rows,
+                                          int heads, int kv_heads, int C, const void *grad_out, int64_t grad_row,
+                                          int64_t grad_head, const void *q, int64_t q_row, int64_t q_head,
+                                          const void *k, int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                                          int64_t v_head, const void *out, int64_t out_row, int64_t out_head,
+                                          const float *lse, const int32_t *q_starts, const int32_t *kv_starts,
+                                          const int32_t *kv_lengths, int64_t sequences, int causal, float scale,
+                                          int zero_rest, void *grad_q, void *grad_k, void *grad_v);
+
+/*
+ * lattice_rotate_heads -- the norm of each head's row and the rotation of its
+ * channels by the row's position, for queries and keys:
+ *   w_c = gain_c x_c / sqrt(mean_c x_c^2 + eps)      (w = x without norm)
+ *   y_a = w_a cos t - w_b sin t,  y_b = w_b cos t + w_a sin t,
+ *   t = position_axis freq_pair, for each pair (a, b) of channels.
+ * There are sections[0] pairs that turn with axis 0, then sections[1] with axis
+ * 1, and so on, P in all; pair p is (p, p + P), or (2 p, 2 p + 1) if interleaved.
+ * Channels from 2 P on do not turn.
+ *   q, k          dev [rows][heads][C] and [rows][kv_heads][C] stored as dtype;
+ *                 kv_heads may be 0 (no keys).   C  1 .. 256.
+ *   positions     dev [rows][axes], position_stride values a row: fp32, or int32
+ *                 if integers.    axes  1 .. 8.   sections  host [axes], >= 0.
+ *   freq          dev fp32 [P]: radians for a unit of the position.  Angles are
+ *                 products in fp64.
+ *   norm          0: rotation alone (no gains).
+ *   gain_q, gain_k   dev fp32 [C], or NULL for ones.     eps  >= 0.
+ *   out_q, out_k  as q and k; may be these themselves (the same strides).
+ */
+#define LATTICE_ROTATE_MAX_CHANNELS 256
+#define LATTICE_ROTATE_MAX_AXES 8
+lattice_status lattice_rotate_heads(lattice_dense *D, lattice_dtype dtype, int64_t rows, int heads, int kv_heads, int C,
+                                    const void *q, int64_t q_row, int64_t q_head, const void *k, int64_t k_row,
+                                    int64_t k_head, const void *positions, int integers, int64_t position_stride,
+                                    int axes, const int *sections, const float *freq, int norm, const float *gain_q,
+                                    const float *gain_k, float eps, int interleaved, void *out_q, int64_t out_q_row,
+                                    int64_t out_q_head, void *out_k, int64_t out_k_row, int64_t out_k_head);
+
+/*
+ * lattice_rotate_heads_backward -- its gradients: with u the gradient of y turned
+ * back, n_c = x_c / sqrt(mean_c x_c^2 + eps) and v_c = gain_c u_c,
+ *   dx_c = (v_c - n_c mean_c(v n)) / sqrt(mean_c x_c^2 + eps)    (u without norm)
+ *   dgain_c = sum over rows and heads of u_c n_c.
+ *   grad_out_q, grad_out_k   dL/dy.      q, k   the forward call's inputs.
+ *   grad_q, grad_k           as q and k; may be grad_out_q and grad_out_k.
+ *   grad_gain_q, grad_gain_k dev fp32 [C], or NULL.  Zero without rows.
+ * The sums over rows are fp32 in a workgroup and fp64 between workgroups.
+ */
+lattice_status lattice_rotate_heads_backward(lattice_dense *D, lattice_dtype dtype, int64_t rows, int heads,
+                                             int kv_heads, int C, const void *grad_out_q, int64_t grad_out_q_row,
+                                             int64_t grad_out_q_head, const void *grad_out_k, int64_t grad_out_k_row,
+                                             int64_t grad_out_k_head, const void *q, int64_t q_row, int64_t q_head,
+                                             const void *k, int64_t k_row, int64_t k_head, const void *positions,
+                                             int integers, int64_t position_stride, int axes, const int *sections,
+                                             const float *freq, int norm, const float *gain_q, const float *gain_k,
+                                             float eps, int interleaved, void *grad_q, int64_t grad_q_row,
+                                             int64_t grad_q_head, void *grad_k, int64_t grad_k_row, int64_t grad_k_head,
+                                             float *grad_gain_q, float *grad_gain_k);
+
+/*
+ * lattice_clip_gradients -- the norm over all values of all tensors, and the
+ * tensors scaled so that it is at most max_norm:
+ *   norm = sqrt(sum x^2),   out = x min(1, max_norm / (norm + eps)).
+ *   count         tensors, 0 .. 2^16.
+ *   in, out       host arrays of dev addresses; values  host: of each tensor.
+ *                 An output may be its own input (of the same type), otherwise
+ *                 none overlaps another output or an input.
+ *   in_dtype, out_dtype   host: storage of each.
+ *   max_norm      >= 0, also infinity (the norm alone, and copies).     eps  >= 0.
+ *   norm          dev fp32 [1].
+ * The sum is fp64.  A norm that is not finite scales by what the formula gives:
+ * NaN for NaN, and 0 for infinity (with NaN for infinite values).
+ */
+#define LATTICE_CLIP_MAX_TENSORS 65536
+lattice_status lattice_clip_gradients(lattice_dense *D, int count, const void *const *in, const lattice_dtype *in_dtype,
+                                      void *const *out, const lattice_dtype *out_dtype, const int64_t *values,
+                                      float max_norm, float eps, float *norm);
 
 /* Query the hash capacity and dimension of L. */
 int64_t lattice_hash_capacity(const lattice *L);

@@ -23,7 +23,7 @@ ARCH = "gfx950"
 
 SOURCES = ["lattice.hip", "splat.hip", "neighbors.hip", "conv.hip", "conv_seg.hip", "slice.hip", "deform.hip", "deform_bwd.hip",
            "backward.hip", "distribute.hip", "dense.hip", "norm.hip", "loss.hip", "loss_fused.hip",
-           "update.hip", "update_small.hip"]
+           "update.hip", "update_small.hip", "attention.hip", "attention_bwd.hip", "rotate.hip", "clip.hip"]
 EXTRA = {"splat.hip": ["-ffp-contract=off"]}
 PEAKS_SRC = "peaks.hip"
 PEAKS = os.path.join(LIBDIR, "peaks")

@@ -1,0 +1,430 @@
+// Softmax attention over packed sequences: what the forward pass (attention.hip)
+// and the backward pass (attention_bwd.hip) share.
+//
+//   s_ij = scale q_i . k_j  for the keys j that row i may see,
+//   p_ij = exp(s_ij - lse_i),  lse_i = log sum_j exp s_ij,  o_i = sum_j p_ij v_j.
+//
+// Products run on the matrix cores in 32 x 32 blocks, v_mfma_f32_32x32x16_bf16
+// for bf16 and v_mfma_f32_32x32x2_f32 for fp32 storage.  An accumulator holds a
+// block transposed to what the next product wants as its right operand: lane l
+// has column l % 32 and rows 8 (e / 4) + 4 (l / 32) + e % 4 of it.  Scores are
+// made as k q^T, so that a query's scores lie in the registers of two lanes
+// (maxima and sums need one exchange between them) and the probabilities are,
+// without a move, the right operand of v^T p^T: the order of the contraction's
+// index is free as long as the left operand has the same one.  The left one, 4
+// keys next to each other for each channel, comes out of LDS by the transposing
+// read (ds_read_b64_tr_b16) for bf16 and lane by lane for fp32.
+#pragma once
+
+#include "dense.h"
+#include "gemm.h"
+
+namespace attend {
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+using gemm::bf16x8_t;
+using gemm::f32x16_t;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kJoinRows = 16;  // of a workgroup that joins splits
+
+// A tensor [rows][heads][D]: values between rows and between heads.
+struct View {
+    const void *p;
+    int64_t row, head;
+};
+
+// Where the rows of packed sequences lie, and the tiles that a launch cuts the
+// rows of one side into.
+struct Packing {
+    int64_t q_rows, kv_rows;
+    const int32_t *q_starts, *kv_starts, *kv_lengths;  // device, or null
+    int sequences;
+    bool causal;
+};
+
+// One sequence as the kernels see it.
+struct Sequence {
+    int64_t q0, k0;  // its first rows
+    int q_len, keys, kv_len;  // kv_len: rows of keys, of which `keys` count
+    bool real;       // otherwise rows of no sequence
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// Rows are cut into tiles of R that lie in one sequence each.  Sequence i of a
+// list of starts s_0 = 0 <= s_1 <= .. gets the slots from s_i / R + i on: at
+// least as many as it has tiles, and no sum over the sequences before it is
+// needed to find them.  The list is the caller's with the rows before its first
+// and behind its last start as sequences of their own; `find` returns the place
+// in it of the slot's sequence, searching 64 places at a time.
+__device__ __forceinline__ int64_t start_of(const int32_t *starts, int sequences, int64_t rows, int i) {
+    if (i <= 0) return 0;
+    if (i >= sequences + 2) return rows;
+    return clamp64(starts[i - 1], 0, rows);
+}
+__device__ __forceinline__ int find(const int32_t *starts, int sequences, int64_t rows, int R, int slot) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, len = sequences + 2;
+    while (len > 1) {
+        const int step = (len + 63) >> 6, i = lane * step;
+        const bool here = i < len && start_of(starts, sequences, rows, lo + i) / R + lo + i <= slot;
+        int n = __popcll(__ballot(here));
+        n = n < 1 ? 1 : n;
+        const int skip = (n - 1) * step;
+        lo += skip;
+        len = len - skip < step ? len - skip : step;
+    }
+    return uniform(lo);
+}
+
+// The sequence of a slot, and the slot's first row in it (>= its length: none).
+// `by_keys`: the slots are tiles of the keys' rows.  Starts that go back or lie
+// outside the rows are clamped, and noted in *status.
+__device__ __forceinline__ Sequence locate(const Packing &p, int R, int slot, bool by_keys, int &first, int32_t *status) {
+    Sequence s;
+    const int32_t *ks = p.kv_starts ? p.kv_starts : p.q_starts;
+    int b = 0, tile = slot;
+    s.real = true;
+    if (!p.q_starts) {
+        s.q0 = s.k0 = 0;
+        s.q_len = (int)p.q_rows;
+        s.kv_len = (int)p.kv_rows;
+    } else {
+        const int32_t *starts = by_keys ? ks : p.q_starts;
+        const int64_t rows = by_keys ? p.kv_rows : p.q_rows;
+        const int i = find(starts, p.sequences, rows, R, slot);
+        const int64_t from = start_of(starts, p.sequences, rows, i);
+        int64_t to = start_of(starts, p.sequences, rows, i + 1);
+        to = to < from ? from : to;
+        tile = slot - (int)(from / R) - i;
+        s.real = i > 0 && i <= p.sequences;
+        b = s.real ? i - 1 : 0;
+        if (!s.real) {
+            s.q0 = s.k0 = from;
+            s.q_len = s.kv_len = (int)(to - from);
+            s.keys = 0;
+            first = tile * R;
+            return s;
+        }
+        const int q_a = p.q_starts[b], q_b = p.q_starts[b + 1], k_a = ks[b], k_b = ks[b + 1];
+        s.q0 = clamp64(q_a, 0, p.q_rows);
+        s.q_len = (int)(clamp64(q_b, s.q0, p.q_rows) - s.q0);
+        s.k0 = clamp64(k_a, 0, p.kv_rows);
+        s.kv_len = (int)(clamp64(k_b, s.k0, p.kv_rows) - s.k0);
+        if (q_a != s.q0 || q_b != s.q0 + s.q_len || k_a != s.k0 || k_b != s.k0 + s.kv_len)
+            if (threadIdx.x == 0) atomicOr(status, DENSE_ST_STARTS);
+    }
+    s.keys = s.kv_len;
+    if (p.kv_lengths) {
+        const int n = p.kv_lengths[b];
+        s.keys = n < 0 ? 0 : n > s.kv_len ? s.kv_len : n;
+        if (s.keys != n && threadIdx.x == 0) atomicOr(status, DENSE_ST_STARTS);
+    }
+    s.q0 = (int64_t)uniform((int)s.q0);
+    s.k0 = (int64_t)uniform((int)s.k0);
+    s.q_len = uniform(s.q_len);
+    s.kv_len = uniform(s.kv_len);
+    s.keys = uniform(s.keys);
+    first = uniform(tile) * R;
+    return s;
+}
+
+// The keys that row r of a sequence sees: [0, keys_seen).
+__device__ __forceinline__ int keys_seen(const Sequence &s, bool causal, int r) {
+    if (!causal) return s.keys;
+    const int n = r + 1 + s.keys - s.q_len;
+    return n < 0 ? 0 : n > s.keys ? s.keys : n;
+}
+
+// Workgroup b of `units` (heads) x n (slots): the slots of a unit go to as few
+// XCDs as can be, since they read the same rows, but in turns, since with causal
+// masks the later ones of a sequence have more keys (or the earlier ones more
+// rows): those first.
+__device__ __forceinline__ bool unit_of(int64_t b, int units, int n, bool later_first, int &unit, int &slot) {
+    const int x = (int)(b & 7), i = (int)(b >> 3);
+    if (units % 8 == 0) {
+        unit = x + 8 * (i / n);
+        slot = i % n;
+    } else if (8 % units == 0) {
+        unit = x % units;
+        slot = i * (8 / units) + x / units;
+    } else {
+        unit = (int)(b % units);
+        slot = (int)(b / units);
+    }
+    if (later_first) slot = n - 1 - slot;
+    return slot >= 0 && slot < n && unit < units;
+}
+inline int64_t unit_grid(int units, int64_t n) {
+    if (units % 8 && 8 % units == 0) return (n + 8 / units - 1) / (8 / units) * 8;
+    return units * n;
+}
+
+// Rows of DP values in LDS, in chunks of 16 bytes: chunk c of row r lies at
+// place c ^ key(r) of the row.  The keys are such that reading one chunk of 16
+// rows, and 4 chunks of each of 4 rows (the transposing read), meets every one
+// of the 64 banks once.
+template <bool BF16, int DP>
+struct Rows {
+    static constexpr int E = BF16 ? 2 : 4, BYTES = DP * E, CHUNKS = BYTES / 16;
+    static constexpr int VEC = BF16 ? 8 : 4;     // values of a chunk
+    static constexpr int STEPS = CHUNKS / 2;     // products over a row's channels
+    static_assert(CHUNKS >= 4, "head dimension");
+    __device__ static __forceinline__ int key(int row) {
+        if (CHUNKS == 4) return (row >> 2) & 3;
+        if (CHUNKS == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
+        if (BF16) return ((row & 3) << 2) | ((row >> 2) & 3);
+        return ((row & 4) << 1) | ((row & 8) >> 1) | (row & 3);
+    }
+    __device__ static __forceinline__ int at(int row, int chunk) { return row * BYTES + ((chunk ^ key(row)) << 4); }
+};
+
+// acc += a b over 2 x 16 bytes of each row.
+template <bool BF16>
+__device__ __forceinline__ void mma(const u32x4_t &a, const u32x4_t &b, f32x16_t &acc) {
+    if constexpr (BF16) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b),
+                                                      acc, 0, 0, 0);
+    } else {
+        const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], acc, 0, 0, 0);
+    }
+}
+
+__device__ __forceinline__ void clear(f32x16_t &a) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) a[e] = 0.f;
+}
+
+// acc = (rows row0.. of the tile) (fragments b)^T.
+template <bool BF16, int DP>
+__device__ __forceinline__ void rows_times(const char *tile, int row0, const u32x4_t (&b)[Rows<BF16, DP>::STEPS],
+                                           f32x16_t &acc) {
+    using L = Rows<BF16, DP>;
+    const int lane = threadIdx.x & 63, row = row0 + (lane & 31), h = lane >> 5;
+#pragma unroll
+    for (int t = 0; t < L::STEPS; ++t)
+        mma<BF16>(*reinterpret_cast<const u32x4_t *>(tile + L::at(row, 2 * t + h)), b[t], acc);
+}
+
+// The right operand made of an accumulator's block: 4 values a register group.
+template <bool BF16>
+struct Right {
+    u32x4_t v[BF16 ? 2 : 4];
+    __device__ __forceinline__ void set(const f32x16_t &p) {
+        if constexpr (BF16) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[s][i] = pack_bf16(p[8 * s + 2 * i], p[8 * s + 2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[g][i] = __float_as_uint(p[4 * g + i]);
+        }
+    }
+};
+
+// acc[d] += (channels of the tile's rows row0 .. row0 + 31)^T p, for 32 channels
+// a block d.
+template <bool BF16, int DP>
+__device__ __forceinline__ void columns_times(const char *tile, int row0, const Right<BF16> &p,
+                                              f32x16_t (&acc)[DP / 32]) {
+    using L = Rows<BF16, DP>;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    if constexpr (BF16) {
+        typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+        const int j = lane & 15, wide = (lane >> 4) & 1;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                const int chunk = 4 * d + 2 * wide + ((j & 3) >> 1);
+                s16x4_t a[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int row = row0 + 16 * s + 8 * u + 4 * h + (j >> 2);
+                    a[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_s16x4 *)(tile + L::at(row, chunk) + 8 * (j & 1)));
+                }
+                typedef short s16x8_t __attribute__((ext_vector_type(8)));
+                const s16x8_t both = __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                mma<true>(__builtin_bit_cast(u32x4_t, both), p.v[s], acc[d]);
+            }
+    } else {
+        const int c = lane & 31;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row0 + 8 * g + 4 * h + i;
+                    const float x = *reinterpret_cast<const float *>(tile + L::at(row, 8 * d + (c >> 2)) + 4 * (c & 3));
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p.v[g][i]), acc[d], 0, 0, 0);
+                }
+    }
+}
+
+// Fragments of a row of a tensor: this lane's chunks 2 t + lane / 32, zeros past
+// the row's D channels.
+template <bool BF16, int DP>
+__device__ __forceinline__ void load_fragments(const View &x, int64_t row, int head, int D,
+                                               u32x4_t (&f)[Rows<BF16, DP>::STEPS]) {
+    using L = Rows<BF16, DP>;
+    const int h = (threadIdx.x & 63) >> 5;
+    const char *p = reinterpret_cast<const char *>(x.p) + (row * x.row + head * x.head) * L::E;
+#pragma unroll
+    for (int t = 0; t < L::STEPS; ++t) {
+        Raw<BF16, L::VEC> u;
+        load_raw<BF16, L::VEC>(p, (2 * t + h) * L::VEC, D, u);
+        f[t] = u32x4_t{u.w[0], u.w[1], u.w[2], u.w[3]};
+    }
+}
+
+// Bring ROWS rows of a tensor into LDS with WAVES wavefronts (this one is number
+// `wave` of them): straight (DMA; rows start at multiples of 16 bytes and are
+// whole chunks long) or through registers.  Rows past the last one and chunks
+// past a row's last stand in for those that are not there: their scores are
+// masked, their channels not stored.
+template <bool BF16, int DP, int ROWS, int WAVES, bool DMA>
+struct Loader {
+    using L = Rows<BF16, DP>;
+    static constexpr int ALL = ROWS * L::CHUNKS / 64;  // 1 KB each; small tiles leave wavefronts without one
+    static constexpr int N = (ALL + WAVES - 1) / WAVES;
+    static_assert(ROWS * L::CHUNKS % 64 == 0 && (ALL < WAVES || ALL % WAVES == 0), "loads of a tile");
+    const char *base;
+    int64_t stride;  // bytes
+    int D, wave;
+    u32x4_t r[DMA ? 1 : N];
+
+    __device__ __forceinline__ Loader(const View &x, int64_t row0, int head, int D, int wave)
+        : base(reinterpret_cast<const char *>(x.p) + (row0 * x.row + head * x.head) * L::E), stride(x.row * L::E), D(D),
+          wave(wave) {}
+    // Rows first .. of which the tensor has `rows` (more than first).
+    __device__ __forceinline__ void fetch(char *tile, int first, int rows) {
+        if (ALL < WAVES && wave >= ALL) return;
+        const int lane = threadIdx.x & 63, last = rows - 1 - first;
+        const char *from = base + first * stride;
+        if constexpr (DMA) {
+            const gemm::rsrc_t src = gemm::buffer(from);
+            const int end = D * L::E / 16 - 1;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int id = (n * WAVES + wave) * 64 + lane, row = id / L::CHUNKS;
+                int chunk = (id % L::CHUNKS) ^ L::key(row);
+                chunk = chunk < end ? chunk : end;
+                gemm::dma16(src, (uint32_t)(row < last ? row : last) * (uint32_t)stride + chunk * 16, 0,
+                            tile + (n * WAVES + wave) * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int id = (n * WAVES + wave) * 64 + lane, row = id / L::CHUNKS;
+                const int chunk = (id % L::CHUNKS) ^ L::key(row);
+                Raw<BF16, L::VEC> u;
+                load_raw<BF16, L::VEC>(from + (int64_t)(row < last ? row : last) * stride, chunk * L::VEC, D, u);
+                r[n] = u32x4_t{u.w[0], u.w[1], u.w[2], u.w[3]};
+            }
+        }
+    }
+    // What fetch() holds in registers goes to the tile.
+    __device__ __forceinline__ void commit(char *tile) const {
+        if constexpr (!DMA) {
+            if (ALL < WAVES && wave >= ALL) return;
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                *reinterpret_cast<u32x4_t *>(tile + ((n * WAVES + wave) * 64 + lane) * 16) = r[n];
+        }
+    }
+};
+
+// The maximum, or the sum, of a value and that of the lane 32 further (or before).
+__device__ __forceinline__ float pair_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Row of an accumulator's value e in this lane.
+__device__ __forceinline__ int acc_row(int e) { return gemm::acc_row(e); }
+
+// Store 4 channels c0 .. of a row of D of them.
+template <bool BF16>
+__device__ __forceinline__ void store4(void *row, int c0, int D, const float *v) {
+    if (c0 + 4 <= D) {
+        if constexpr (BF16) {
+            struct __attribute__((packed, aligned(2))) Two { uint32_t v[2]; };
+            *reinterpret_cast<Two *>(reinterpret_cast<uint16_t *>(row) + c0) = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        } else {
+            *reinterpret_cast<Words4 *>(reinterpret_cast<float *>(row) + c0) =
+                {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c0 + i < D) {
+                if (BF16)
+                    reinterpret_cast<uint16_t *>(row)[c0 + i] = (uint16_t)pack_bf16(v[i], 0.f);
+                else
+                    reinterpret_cast<float *>(row)[c0 + i] = v[i];
+            }
+    }
+}
+
+// D values of zero.
+template <bool BF16>
+__device__ __forceinline__ void zero_row(void *row, int D, int lane, int lanes) {
+    for (int c = lane; c < D; c += lanes) {
+        if (BF16)
+            reinterpret_cast<uint16_t *>(row)[c] = 0;
+        else
+            reinterpret_cast<float *>(row)[c] = 0.f;
+    }
+}
+
+// -- host side --
+
+// Whether a tensor's rows can go to LDS straight.
+inline bool straight(const View &x, int D, int E) {
+    return (D * E) % 16 == 0 && (x.row * E) % 16 == 0 && (x.head * E) % 16 == 0 &&
+           reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.row * E < ((int64_t)1 << 25);
+}
+inline int padded_dim(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
+// Slots of tiles of R rows, see find().
+inline int64_t slots_of(const int32_t *starts, int64_t sequences, int64_t rows, int R) {
+    return starts ? rows / R + sequences + 2 : (rows + R - 1) / R;
+}
+// How the query heads of a key head and the rows of a sequence share the columns
+// of a tile.
+struct Columns {
+    int parts, heads, R;  // parts of the group, query heads of one, rows
+    Columns(int group, int columns) {
+        parts = (group + columns - 1) / columns;
+        heads = (group + parts - 1) / parts;
+        parts = (group + heads - 1) / heads;
+        R = columns / heads;
+    }
+};
+inline Packing packing_of(const AttendArgs &a) {
+    return {a.q_rows, a.kv_rows, a.q_starts, a.kv_starts, a.kv_lengths, (int)a.sequences, a.causal};
+}
+// As many splits as give `want` workgroups, of `least` rows each at least.
+inline int splits_of(int64_t tiles, int64_t rows, int64_t want, int64_t least) {
+    int64_t n = want / (tiles > 0 ? tiles : 1);
+    n = n < rows / least ? n : rows / least;
+    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+}  // namespace attend

@@ -1,0 +1,523 @@
+// Softmax attention, forward:  o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i),
+// s_ij = scale q_i . k_j.
+//
+// A tile is a number of columns, each one row of one query head; the heads that
+// share a key head lie next to each other, so that a tile's keys and values are
+// read once for all of them.  The keys of its sequence go by in blocks, and a
+// column's maximum, sum and output are kept in registers (the output rescaled only when
+// the maximum has grown by more than 2^8, which the last division makes good).
+//
+// Many rows: four wavefronts have 32 or 64 columns each, and share blocks of keys in
+// LDS that are loaded one ahead.  Few rows (single tokens against a cache): one
+// tile of 32 columns, whose keys the wavefronts of a workgroup take in turns,
+// each with blocks of its own, so that they never wait for each other; their
+// results are joined in LDS.
+// Where that leaves CUs without work, the keys of a tile are split among
+// workgroups, whose results a second launch joins in a fixed order.
+#include "attention.h"
+
+namespace {
+
+using namespace attend;
+
+struct Params {
+    Packing pack;
+    View q, k, v, o;
+    float *lse;         // [heads][rows], or null
+    int heads, units;   // units: (key head, part of its query heads)
+    int D;
+    int group;          // query heads of a key head
+    int parts, tile_heads;  // parts that a group is cut into, query heads of one
+    int R, slots, splits;   // rows of a tile
+    float c;            // scale, for powers of 2
+    bool zero_rest;
+    float *part_o, *part_lse;  // of the splits: [splits][rows][heads][D], [splits][heads][rows]
+    int32_t *status;
+};
+
+// One workgroup's tile.
+struct Tile {
+    Sequence s;
+    int first, rows;      // its rows of the sequence
+    int head0, heads;     // its query heads
+    int kv_head, split;
+    int t0, t1;           // blocks of keys of this split
+    int least, most;      // keys that its first and its last row see
+};
+
+// The workgroup's tile; false where there is nothing to compute (then rows of no
+// sequence, or without keys, have been seen to).
+template <bool BF16, int KT>
+__device__ __forceinline__ bool tile_of(const Params &a, Tile &t) {
+    int unit, slot;
+    t.split = blockIdx.y;
+    if (!unit_of(blockIdx.x, a.units, a.slots, true, unit, slot)) return false;
+    const int part = unit % a.parts;
+    t.kv_head = unit / a.parts;
+    t.head0 = t.kv_head * a.group + part * a.tile_heads;
+    const int left = a.group - part * a.tile_heads;
+    t.heads = left < a.tile_heads ? left : a.tile_heads;
+    t.s = locate(a.pack, a.R, slot, false, t.first, a.status);
+    if (t.first >= t.s.q_len || t.heads <= 0) return false;
+    t.rows = t.s.q_len - t.first < a.R ? t.s.q_len - t.first : a.R;
+    if (!t.s.real) {
+        if (t.split == 0 && a.zero_rest)
+            for (int r = 0; r < t.rows; ++r)
+                for (int h = 0; h < t.heads; ++h) {
+                    const int64_t row = t.s.q0 + t.first + r;
+                    const int head = t.head0 + h;
+                    zero_row<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) +
+                                       (row * a.o.row + head * a.o.head) * (BF16 ? 2 : 4),
+                                   a.D, threadIdx.x, blockDim.x);
+                    if (a.lse && threadIdx.x == 0) a.lse[head * a.pack.q_rows + row] = -INFINITY;
+                }
+        return false;
+    }
+    t.least = keys_seen(t.s, a.pack.causal, t.first);
+    t.most = keys_seen(t.s, a.pack.causal, t.first + t.rows - 1);
+    const int n = (t.most + KT - 1) / KT;
+    t.t0 = (int)((int64_t)n * t.split / a.splits);
+    t.t1 = (int)((int64_t)n * (t.split + 1) / a.splits);
+    return true;
+}
+
+// A column's state: its maximum (of the scores as they are), the sum of
+// this lane's share of the exponentials, and the output's channels.
+template <int DP>
+struct Column {
+    float top = -INFINITY, sum = 0.f;
+    f32x16_t o[DP / 32];
+};
+
+// Take in a block of KB x 32 scores of a column.
+template <bool BF16, int DP, int KB>
+__device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, float c, Right<BF16> (&p)[KB]) {
+    float m = s[0][0];
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, s[b][e]);
+    m = fmaxf(pair_max(m), col.top);
+    // grown too far: (m - top) c > 8; a first maximum always (top is -inf)
+    if (__any((m - col.top) * c > 8.f)) {
+        const float f = m == -INFINITY ? 1.f : exp2_((col.top - m) * c);
+        col.top = m;
+        col.sum *= f;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) col.o[d][e] *= f;
+    }
+    const float mc = col.top == -INFINITY ? 0.f : col.top * c;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[b][e] = exp2_(fmaf(s[b][e], c, -mc));
+            col.sum += s[b][e];
+        }
+        p[b].set(s[b]);
+    }
+}
+
+// Scores of keys from `seen` on (of the block from key0 on) count for nothing.
+__device__ __forceinline__ void mask(f32x16_t &s, int key0, int seen) {
+    const int n = seen - key0 - 4 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (8 * (e >> 2) + (e & 3) >= n) s[e] = -INFINITY;
+}
+
+// Write a column: 4 channels at a time, by f.
+template <bool BF16, int DP>
+__device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t row, int head, Column<DP> &col) {
+    const float sum = pair_sum(col.sum);
+    const float f = col.top == -INFINITY ? 0.f : 1.f / sum;
+    const float lse2 = col.top == -INFINITY ? -INFINITY : fmaf(col.top, a.c, 0.f) + log2f(sum);
+    const int h = (threadIdx.x & 63) >> 5;
+    const bool part = a.splits > 1;
+    if (h == 0) {
+        if (part)
+            a.part_lse[((int64_t)t.split * a.heads + head) * a.pack.q_rows + row] = lse2;
+        else if (a.lse)
+            a.lse[head * a.pack.q_rows + row] = lse2 * kLn2;
+    }
+    char *o = const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + head * a.o.head) * (BF16 ? 2 : 4);
+    float *po = a.part_o + (((int64_t)t.split * a.pack.q_rows + row) * a.heads + head) * a.D;
+    if (part && col.top == -INFINITY) return;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c0 = 32 * d + 8 * g + 4 * h;
+            if (c0 >= a.D) continue;
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = col.top == -INFINITY ? 0.f : col.o[d][4 * g + i] * f;
+            if (part)
+                store4<false>(po, c0, a.D, v);
+            else
+                store4<BF16>(o, c0, a.D, v);
+        }
+}
+
+// Many rows: 4 wavefronts x NQ blocks of 32 columns.  Keys of a block:
+template <bool BF16, int DP>
+constexpr int keys_of_block() { return BF16 ? 64 : 32; }
+
+template <bool BF16, int DP, int NQ, bool DMA>
+__global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(Params a) {
+    using L = Rows<BF16, DP>;
+    constexpr int KT = keys_of_block<BF16, DP>(), KB = KT / 32;
+    constexpr int HALF = KT * L::BYTES, STAGE = 2 * HALF;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Tile t;
+    if (!tile_of<BF16, KT>(a, t)) return;
+    const int lane = threadIdx.x & 63, wave = gemm::wave_index();
+
+    int seen[NQ];
+    int64_t row[NQ];
+    int head[NQ];
+    bool mine[NQ];
+    u32x4_t q[NQ][L::STEPS];
+    Column<DP> col[NQ];
+    int wave_most = 0;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int c = (wave * NQ + n) * 32 + (lane & 31);
+        int r = c / t.heads;
+        const int h = c - r * t.heads;
+        mine[n] = r < t.rows;
+        r = mine[n] ? r : t.rows - 1;
+        row[n] = t.s.q0 + t.first + r;
+        head[n] = t.head0 + h;
+        seen[n] = keys_seen(t.s, a.pack.causal, t.first + r);
+        int last = ((wave * NQ + n) * 32 + 31) / t.heads;
+        last = last < t.rows ? last : t.rows - 1;
+        wave_most = uniform(keys_seen(t.s, a.pack.causal, t.first + last));
+        load_fragments<BF16, DP>(a.q, row[n], head[n], a.D, q[n]);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) clear(col[n].o[d]);
+    }
+
+    Loader<BF16, DP, KT, 4, DMA> lk(a.k, t.s.k0, t.kv_head, a.D, wave), lv(a.v, t.s.k0, t.kv_head, a.D, wave);
+    if (t.t0 < t.t1) {
+        lk.fetch(lds, t.t0 * KT, t.s.keys);
+        lv.fetch(lds + HALF, t.t0 * KT, t.s.keys);
+        lk.commit(lds);
+        lv.commit(lds + HALF);
+    }
+    int stage = 0;
+    for (int i = t.t0; i < t.t1; ++i) {
+        char *now = lds + stage * STAGE, *next = lds + (stage ^ 1) * STAGE;
+        gemm::wait_and_barrier<0>();
+        const bool more = i + 1 < t.t1;
+        if (more) {
+            lk.fetch(next, (i + 1) * KT, t.s.keys);
+            lv.fetch(next + HALF, (i + 1) * KT, t.s.keys);
+        }
+        if (i * KT < wave_most) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                f32x16_t s[KB];
+#pragma unroll
+                for (int b = 0; b < KB; ++b) {
+                    clear(s[b]);
+                    rows_times<BF16, DP>(now, 32 * b, q[n], s[b]);
+                }
+                if ((i + 1) * KT > t.least)
+#pragma unroll
+                    for (int b = 0; b < KB; ++b) mask(s[b], i * KT + 32 * b, seen[n]);
+                Right<BF16> p[KB];
+                softmax<BF16, DP, KB>(s, col[n], a.c, p);
+#pragma unroll
+                for (int b = 0; b < KB; ++b) columns_times<BF16, DP>(now + HALF, 32 * b, p[b], col[n].o);
+            }
+        }
+        if (more) {
+            lk.commit(next);
+            lv.commit(next + HALF);
+        }
+        stage ^= 1;
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)  // a column's two lanes go the same way
+        if (mine[n]) finish<BF16, DP>(a, t, row[n], head[n], col[n]);
+}
+
+// Few rows: one tile of 32 columns, WAVES wavefronts with their own keys.
+template <bool BF16, int DP>
+constexpr int few_waves() { return Rows<BF16, DP>::BYTES <= 256 ? 4 : 2; }
+
+template <bool BF16, int DP, bool DMA>
+__global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Params a) {
+    using L = Rows<BF16, DP>;
+    constexpr int KT = 32, WAVES = few_waves<BF16, DP>();
+    constexpr int HALF = KT * L::BYTES, STAGE = 2 * HALF;
+    constexpr int LOADS = 2 * KT * L::CHUNKS / 64;
+    constexpr int PITCH = DP + 4;  // floats of a column's output in LDS
+    static_assert(32 * PITCH * 4 <= 2 * STAGE && LOADS < 64, "LDS");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float tops[WAVES][32], sums[WAVES][32];
+    Tile t;
+    if (!tile_of<BF16, KT>(a, t)) return;
+    const int lane = threadIdx.x & 63, wave = gemm::wave_index();
+    char *own = lds + wave * 2 * STAGE;
+
+    const int c = lane & 31;
+    int r = c / t.heads;
+    const int h = c - r * t.heads;
+    r = r < t.rows ? r : t.rows - 1;
+    const int seen = keys_seen(t.s, a.pack.causal, t.first + r);
+    u32x4_t q[L::STEPS];
+    Column<DP> col;
+    load_fragments<BF16, DP>(a.q, t.s.q0 + t.first + r, t.head0 + h, a.D, q);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) clear(col.o[d]);
+
+    Loader<BF16, DP, KT, 1, DMA> lk(a.k, t.s.k0, t.kv_head, a.D, 0), lv(a.v, t.s.k0, t.kv_head, a.D, 0);
+    int i = t.t0 + wave;
+    if (i < t.t1) {
+        lk.fetch(own, i * KT, t.s.keys);
+        lv.fetch(own + HALF, i * KT, t.s.keys);
+        lk.commit(own);
+        lv.commit(own + HALF);
+    }
+    int stage = 0;
+    for (; i < t.t1; i += WAVES) {
+        char *now = own + stage * STAGE, *next = own + (stage ^ 1) * STAGE;
+        const bool more = i + WAVES < t.t1;
+        // what lies in `next` has been read: its products are done
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) {
+            lk.fetch(next, (i + WAVES) * KT, t.s.keys);
+            lv.fetch(next + HALF, (i + WAVES) * KT, t.s.keys);
+        }
+        if (DMA) {
+            if (more)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        f32x16_t s[1];
+        clear(s[0]);
+        rows_times<BF16, DP>(now, 0, q, s[0]);
+        if ((i + 1) * KT > t.least) mask(s[0], i * KT, seen);
+        Right<BF16> p[1];
+        softmax<BF16, DP, 1>(s, col, a.c, p);
+        columns_times<BF16, DP>(now + HALF, 0, p[0], col.o);
+        if (more) {
+            lk.commit(next);
+            lv.commit(next + HALF);
+        }
+        stage ^= 1;
+    }
+    // join: every wavefront's columns to LDS (its own part, whose blocks are done with)
+    const float sum = pair_sum(col.sum);
+    const int half = lane >> 5;
+    float *out = reinterpret_cast<float *>(own) + c * PITCH;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<float4 *>(out + 32 * d + 8 * g + 4 * half) =
+                make_float4(col.o[d][4 * g], col.o[d][4 * g + 1], col.o[d][4 * g + 2], col.o[d][4 * g + 3]);
+    if (half == 0) {
+        tops[wave][c] = col.top;
+        sums[wave][c] = sum;
+    }
+    __syncthreads();
+    const int columns = t.rows * t.heads;
+    for (int id = threadIdx.x; id < columns * (DP / 4); id += 64 * WAVES) {
+        const int cc = id / (DP / 4), c0 = id % (DP / 4) * 4;
+        float m = tops[0][cc];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w][cc]);
+        float all = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (tops[w][cc] == -INFINITY) continue;
+            const float f = exp2_((tops[w][cc] - m) * a.c);
+            all += f * sums[w][cc];
+            const float *x = reinterpret_cast<const float *>(lds + w * 2 * STAGE) + cc * PITCH + c0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += f * x[k];
+        }
+        const bool none = m == -INFINITY;
+        const float inv = none ? 0.f : 1.f / all;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = none ? 0.f : v[k] * inv;
+        const int rr = cc / t.heads, hh = t.head0 + cc - rr * t.heads;
+        const int64_t row = t.s.q0 + t.first + rr;
+        if (c0 == 0) {
+            const float lse2 = none ? -INFINITY : m * a.c + log2f(all);
+            if (a.splits > 1)
+                a.part_lse[((int64_t)t.split * a.heads + hh) * a.pack.q_rows + row] = lse2;
+            else if (a.lse)
+                a.lse[hh * a.pack.q_rows + row] = lse2 * kLn2;
+        }
+        if (c0 >= a.D) continue;
+        if (a.splits > 1) {
+            if (!none) store4<false>(a.part_o + (((int64_t)t.split * a.pack.q_rows + row) * a.heads + hh) * a.D, c0, a.D, v);
+        } else {
+            store4<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + hh * a.o.head) * L::E,
+                         c0, a.D, v);
+        }
+    }
+}
+
+// The splits' results of kJoinRows rows: weights 2^(lse - their common lse), a
+// wavefront for each row and head.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_join(Params a) {
+    int first;
+    const Sequence s = locate(a.pack, kJoinRows, blockIdx.x, false, first, a.status);
+    if (!s.real || first >= s.q_len) return;
+    const int rows = s.q_len - first < kJoinRows ? s.q_len - first : kJoinRows;
+    const int lane = threadIdx.x & 63;
+    const int64_t next = a.pack.q_rows * a.heads;
+    for (int i = threadIdx.x >> 6; i < rows * a.heads; i += 4) {
+        const int64_t row = s.q0 + first + i / a.heads;
+        const int head = i % a.heads;
+        const float *lse = a.part_lse + head * a.pack.q_rows + row;
+        float m = -INFINITY, sum = 0.f;
+        bool nan = false;
+        for (int n = 0; n < a.splits; ++n) {
+            const float x = lse[n * next];
+            nan |= x != x;
+            const float top = fmaxf(m, x);
+            if (top == -INFINITY) continue;
+            sum = sum * exp2_(m - top) + exp2_(x - top);
+            m = top;
+        }
+        const float all = nan ? NAN : m == -INFINITY ? m : m + log2f(sum);
+        if (a.lse && lane == 0) a.lse[head * a.pack.q_rows + row] = all * kLn2;
+        const int c0 = lane * 4;
+        if (c0 >= a.D) continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < a.splits; ++n) {
+            const float x = lse[n * next];
+            if (x == -INFINITY) continue;
+            const float f = exp2_(x - all);
+            const float *p = a.part_o + (n * next + row * a.heads + head) * a.D + c0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c0 + k < a.D) v[k] += f * p[k];
+        }
+        store4<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) +
+                         (row * a.o.row + head * a.o.head) * (BF16 ? 2 : 4),
+                     c0, a.D, v);
+    }
+}
+
+// What a call does.
+struct Plan {
+    Params p;
+    bool few, dma;
+    int nq;
+    int64_t grid, part_o, part_lse;  // grid.x; floats of scratch
+};
+
+Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
+    Plan r = {};
+    Params &p = r.p;
+    p.pack = packing_of(a);
+    p.q = {a.q, a.q_row, a.q_head};
+    p.k = {a.k, a.k_row, a.k_head};
+    p.v = {a.v, a.v_row, a.v_head};
+    p.o = {a.out, a.o_row, a.o_head};
+    p.lse = a.lse;
+    p.heads = a.heads;
+    p.D = a.D;
+    p.group = a.heads / a.kv_heads;
+    p.c = a.scale * kLog2e;
+    p.zero_rest = a.zero_rest;
+    p.status = D->status;
+    const int E = a.bf16 ? 2 : 4;
+    r.dma = straight(p.k, a.D, E) && straight(p.v, a.D, E);
+    const int64_t sequences = a.sequences > 0 ? a.sequences : 1;
+    const int64_t rows = (a.q_rows + sequences - 1) / sequences, keys = (a.kv_rows + sequences - 1) / sequences;
+    r.few = rows * p.group <= 64;
+    r.nq = !r.few && a.D <= 64 && a.q_rows * a.heads >= (int64_t)256 * 2 * D->cu_count ? 2 : 1;
+    const Columns c(p.group, r.few ? 32 : 128 * r.nq);
+    p.parts = c.parts;
+    p.tile_heads = c.heads;
+    p.R = c.R;
+    p.units = a.kv_heads * p.parts;
+    const int64_t slots = slots_of(a.q_starts, sequences, a.q_rows, p.R);
+    p.slots = (int)slots;
+    r.grid = unit_grid(p.units, slots);
+    const int64_t tiles = (a.q_rows + p.R - 1) / p.R;
+    p.splits = splits_of(p.units * (tiles > sequences ? tiles : sequences), keys, 2 * D->cu_count, 256);
+    if (p.splits > 1) {
+        r.part_o = (int64_t)p.splits * a.q_rows * a.heads * a.D;
+        r.part_lse = (int64_t)p.splits * a.q_rows * a.heads;
+    }
+    return r;
+}
+
+template <bool BF16, int DP, bool DMA>
+hipError_t launch_as(lattice_dense *D, const Plan &r) {
+    using L = Rows<BF16, DP>;
+    const dim3 grid((unsigned)r.grid, (unsigned)r.p.splits);
+    if (r.few) {
+        constexpr int W = few_waves<BF16, DP>(), LDS = W * 2 * 2 * 32 * L::BYTES;
+        static std::atomic<uint64_t> done{0};
+        if (LDS + 1024 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend_few<BF16, DP, DMA>), LDS, done));
+        hipLaunchKernelGGL((k_attend_few<BF16, DP, DMA>), grid, dim3(64 * W), LDS, D->stream, r.p);
+        return hipGetLastError();
+    }
+    constexpr int LDS = 2 * 2 * keys_of_block<BF16, DP>() * L::BYTES;
+    if constexpr (DP <= 64) {
+        if (r.nq == 2) {
+            hipLaunchKernelGGL((k_attend<BF16, DP, 2, DMA>), grid, dim3(256), LDS, D->stream, r.p);
+            return hipGetLastError();
+        }
+    }
+    static std::atomic<uint64_t> done{0};
+    if (LDS > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend<BF16, DP, 1, DMA>), LDS, done));
+    hipLaunchKernelGGL((k_attend<BF16, DP, 1, DMA>), grid, dim3(256), LDS, D->stream, r.p);
+    return hipGetLastError();
+}
+
+template <bool BF16, int DP>
+hipError_t launch_dim(lattice_dense *D, const Plan &r) {
+    return r.dma ? launch_as<BF16, DP, true>(D, r) : launch_as<BF16, DP, false>(D, r);
+}
+
+template <bool BF16>
+hipError_t launch_type(lattice_dense *D, const Plan &r) {
+    switch (padded_dim(r.p.D)) {
+        case 32: TRY((launch_dim<BF16, 32>(D, r))); break;
+        case 64: TRY((launch_dim<BF16, 64>(D, r))); break;
+        default: TRY((launch_dim<BF16, 128>(D, r))); break;
+    }
+    if (r.p.splits == 1) return hipSuccess;
+    const int64_t n = slots_of(r.p.pack.q_starts, r.p.pack.sequences, r.p.pack.q_rows, kJoinRows);
+    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)n), dim3(256), 0, D->stream, r.p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t attention_scratch(const lattice_dense *D, const AttendArgs &a) {
+    const Plan r = plan_of(D, a);
+    ScratchLayout s;
+    s.take(r.part_o * 4);
+    s.take(r.part_lse * 4);
+    return s.bytes;
+}
+
+bool attention_fits(const lattice_dense *D, const AttendArgs &a) {
+    return plan_of(D, a).grid < ((int64_t)1 << 31);
+}
+
+hipError_t launch_attention(lattice_dense *D, const AttendArgs &a) {
+    Plan r = plan_of(D, a);
+    ScratchLayout s;
+    char *ws = static_cast<char *>(D->ws);
+    r.p.part_o = reinterpret_cast<float *>(ws + s.take(r.part_o * 4));
+    r.p.part_lse = reinterpret_cast<float *>(ws + s.take(r.part_lse * 4));
+    return a.bf16 ? launch_type<true>(D, r) : launch_type<false>(D, r);
+}

@@ -1,0 +1,453 @@
+// Softmax attention, backward.  With g = dL/do, delta_i = g_i . o_i and
+// p_ij = exp(s_ij - lse_i) made again from the scores,
+//   t_ij = p_ij (g_i . v_j - delta_i)          (dL/ds_ij)
+//   dq_i = scale sum_j t_ij k_j,  dk_j = scale sum_i t_ij q_i,  dv_j = sum_i p_ij g_i.
+//
+// Two launches, each with sums of its own in registers, so that no float is added
+// by atomics and two calls give the same bits, at the price of making p and g . v
+// twice (seven products in place of five):
+//   by queries   tiles of columns as in the forward pass, the keys go by; makes
+//                delta on the way and dq.
+//   by keys      each wavefront has 32 keys of a key head; the rows of all its
+//                query heads go by; makes dk and dv, so that heads which share
+//                keys are added here.
+// p and t are rounded to bf16 for the products with bf16 tensors (a relative 2^-9
+// of each term), all sums are fp32.
+#include "attention.h"
+
+namespace {
+
+using namespace attend;
+
+struct Params {
+    Packing pack;
+    View q, k, v, o, g;
+    void *dq, *dk, *dv;       // without gaps
+    const float *lse;         // [heads][rows]
+    float *delta;             // the same
+    int heads, kv_heads, D, group;
+    int parts, tile_heads;    // by queries, as in the forward pass
+    int units, R, slots, splits;
+    float c, scale;
+    bool zero_rest;
+    float *part;              // of the splits, without gaps, one after another
+    int32_t *status;
+};
+
+template <bool BF16>
+__device__ __forceinline__ float dot(const u32x4_t &a, const u32x4_t &b) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (BF16) {
+            s = fmaf(__uint_as_float(a[i] << 16), __uint_as_float(b[i] << 16), s);
+            s = fmaf(__uint_as_float(a[i] & 0xffff0000u), __uint_as_float(b[i] & 0xffff0000u), s);
+        } else {
+            s = fmaf(__uint_as_float(a[i]), __uint_as_float(b[i]), s);
+        }
+    }
+    return s;
+}
+
+// Store a column's channels times f: row `at` of D values, at its type or, of a
+// split, in fp32.
+template <bool BF16, int DP>
+__device__ __forceinline__ void store_column(void *out, float *part, int64_t at, int D, const f32x16_t (&x)[DP / 32],
+                                             float f) {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int c0 = 32 * d + 8 * g + 4 * h;
+            if (c0 >= D) continue;
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = x[d][4 * g + i] * f;
+            if (part)
+                store4<false>(part + at * D, c0, D, v);
+            else
+                store4<BF16>(reinterpret_cast<char *>(out) + at * D * (BF16 ? 2 : 4), c0, D, v);
+        }
+}
+
+// By queries: 4 wavefronts of 32 columns.
+template <bool BF16, int DP, bool DMA>
+__global__ __launch_bounds__(256) void k_by_queries(Params a) {
+    using L = Rows<BF16, DP>;
+    constexpr int KT = 32, HALF = KT * L::BYTES, STAGE = 2 * HALF;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    int unit, slot, first;
+    if (!unit_of(blockIdx.x, a.units, a.slots, true, unit, slot)) return;
+    const int kv_head = unit / a.parts, part = unit % a.parts, head0 = kv_head * a.group + part * a.tile_heads;
+    const int left = a.group - part * a.tile_heads, heads = left < a.tile_heads ? left : a.tile_heads;
+    const Sequence s = locate(a.pack, a.R, slot, false, first, a.status);
+    if (first >= s.q_len || heads <= 0) return;
+    const int rows = s.q_len - first < a.R ? s.q_len - first : a.R;
+    const int split = blockIdx.y;
+    float *mine_part = a.splits > 1 ? a.part + (int64_t)split * a.pack.q_rows * a.heads * a.D : nullptr;
+    if (!s.real) {
+        if (a.zero_rest && split == 0)
+            for (int r = 0; r < rows; ++r)
+                for (int h = 0; h < heads; ++h)
+                    zero_row<BF16>(reinterpret_cast<char *>(a.dq) +
+                                       ((s.q0 + first + r) * a.heads + head0 + h) * a.D * L::E,
+                                   a.D, threadIdx.x, 256);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = gemm::wave_index();
+    const int column = wave * 32 + (lane & 31);
+    int r = column / heads;
+    const int head = head0 + column - r * heads;
+    const bool mine = r < rows;
+    r = mine ? r : rows - 1;
+    const int64_t row = s.q0 + first + r;
+    const int seen = keys_seen(s, a.pack.causal, first + r);
+    const int least = keys_seen(s, a.pack.causal, first), most = keys_seen(s, a.pack.causal, first + rows - 1);
+    int last = (wave * 32 + 31) / heads;
+    last = last < rows ? last : rows - 1;
+    const int wave_most = uniform(keys_seen(s, a.pack.causal, first + last));
+
+    u32x4_t q[L::STEPS], g[L::STEPS];
+    float delta = 0.f;
+    {
+        u32x4_t o[L::STEPS];
+        load_fragments<BF16, DP>(a.g, row, head, a.D, g);
+        load_fragments<BF16, DP>(a.o, row, head, a.D, o);
+#pragma unroll
+        for (int t = 0; t < L::STEPS; ++t) delta += dot<BF16>(g[t], o[t]);
+        delta = pair_sum(delta);
+    }
+    load_fragments<BF16, DP>(a.q, row, head, a.D, q);
+    const float lse = a.lse[head * a.pack.q_rows + row];
+    const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    if (mine && lane < 32 && split == 0) a.delta[head * a.pack.q_rows + row] = delta;
+
+    f32x16_t dq[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) clear(dq[d]);
+    const int n = (most + KT - 1) / KT;
+    const int t0 = (int)((int64_t)n * split / a.splits), t1 = (int)((int64_t)n * (split + 1) / a.splits);
+    Loader<BF16, DP, KT, 4, DMA> lk(a.k, s.k0, kv_head, a.D, wave), lv(a.v, s.k0, kv_head, a.D, wave);
+    if (t0 < t1) {
+        lk.fetch(lds, t0 * KT, s.keys);
+        lv.fetch(lds + HALF, t0 * KT, s.keys);
+        lk.commit(lds);
+        lv.commit(lds + HALF);
+    }
+    int stage = 0;
+    for (int i = t0; i < t1; ++i) {
+        char *now = lds + stage * STAGE, *next = lds + (stage ^ 1) * STAGE;
+        gemm::wait_and_barrier<0>();
+        const bool more = i + 1 < t1;
+        if (more) {
+            lk.fetch(next, (i + 1) * KT, s.keys);
+            lv.fetch(next + HALF, (i + 1) * KT, s.keys);
+        }
+        if (i * KT < wave_most) {
+            f32x16_t x, y;
+            clear(x);
+            clear(y);
+            rows_times<BF16, DP>(now, 0, q, x);
+            rows_times<BF16, DP>(now + HALF, 0, g, y);
+            const int left_keys = (i + 1) * KT > least ? seen - i * KT - 4 * (lane >> 5) : KT;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float p = 8 * (e >> 2) + (e & 3) < left_keys ? exp2_(fmaf(x[e], a.c, -lse2)) : 0.f;
+                x[e] = p * (y[e] - delta);
+            }
+            Right<BF16> t;
+            t.set(x);
+            columns_times<BF16, DP>(now, 0, t, dq);
+        }
+        if (more) {
+            lk.commit(next);
+            lv.commit(next + HALF);
+        }
+        stage ^= 1;
+    }
+    if (mine) store_column<BF16, DP>(a.dq, mine_part, row * a.heads + head, a.D, dq, a.scale);
+}
+
+// By keys: 4 wavefronts of 32 keys.
+template <bool BF16, int DP, bool DMA>
+__global__ __launch_bounds__(256) void k_by_keys(Params a) {
+    using L = Rows<BF16, DP>;
+    constexpr int QT = 32, HALF = QT * L::BYTES, STAGE = 2 * HALF;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ __attribute__((aligned(16))) float stats[2][2][QT];  // lse (of 2) and delta of the block's rows
+    int kv_head, slot, first;
+    if (!unit_of(blockIdx.x, a.kv_heads, a.slots, false, kv_head, slot)) return;
+    const Sequence s = locate(a.pack, a.R, slot, true, first, a.status);
+    if (first >= s.kv_len) return;
+    const int split = blockIdx.y;
+    const int lane = threadIdx.x & 63, wave = gemm::wave_index(), h = lane >> 5;
+    const int64_t size = a.pack.kv_rows * a.kv_heads * a.D;
+    const int key = first + wave * 32 + (lane & 31);
+    // rows that no key of the tile counts in
+    if (!s.real || first >= s.keys) {
+        const int end = s.kv_len - first < a.R ? s.kv_len : first + a.R;
+        if (a.zero_rest && split == 0)
+            for (int j = first; j < end; ++j) {
+                const int64_t at = ((s.k0 + j) * a.kv_heads + kv_head) * a.D * L::E;
+                zero_row<BF16>(reinterpret_cast<char *>(a.dk) + at, a.D, threadIdx.x, 256);
+                zero_row<BF16>(reinterpret_cast<char *>(a.dv) + at, a.D, threadIdx.x, 256);
+            }
+        return;
+    }
+    const bool counts = key < s.keys;
+    const int64_t row = s.k0 + (counts ? key : s.keys - 1);
+    u32x4_t k[L::STEPS], v[L::STEPS];
+    load_fragments<BF16, DP>(a.k, row, kv_head, a.D, k);
+    load_fragments<BF16, DP>(a.v, row, kv_head, a.D, v);
+    f32x16_t dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+        clear(dk[d]);
+        clear(dv[d]);
+    }
+    // rows from r0 on see the tile's first key; this lane's key is seen from `from` on
+    const int shift = a.pack.causal ? s.q_len - s.keys : -(1 << 30);
+    int r0 = a.pack.causal ? first + shift : 0;
+    r0 = (r0 < 0 ? 0 : r0) / QT * QT;
+    const int from = !counts ? 0x7fffffff : a.pack.causal ? key + shift : 0;
+    const int per = r0 < s.q_len ? (s.q_len - r0 + QT - 1) / QT : 0;  // blocks of a head
+    // rows that see all keys of the tile
+    const int all_see = first + a.R <= s.keys ? (a.pack.causal ? first + a.R - 1 + shift : 0) : 0x7fffffff;
+    const int64_t blocks = (int64_t)per * a.group;
+    int64_t i = blocks * split / a.splits;
+    const int64_t end = blocks * (split + 1) / a.splits;
+    int head = per > 0 ? (int)(i / per) : 0, at = per > 0 ? (int)(i % per) : 0;
+
+    float stat = 0.f;  // lanes 0 .. 31 of the first wavefront: lse, the others delta
+    Loader<BF16, DP, QT, 4, DMA> lq(a.q, s.q0, kv_head * a.group, a.D, wave), lg(a.g, s.q0, kv_head * a.group, a.D, wave);
+    const int64_t q_step = a.q.head * L::E, g_step = a.g.head * L::E;
+    const char *q_base = lq.base, *g_base = lg.base;
+    auto fetch = [&](char *to, int head, int at) {
+        lq.base = q_base + head * q_step;
+        lg.base = g_base + head * g_step;
+        const int r = r0 + at * QT;
+        lq.fetch(to, r, s.q_len);
+        lg.fetch(to + HALF, r, s.q_len);
+        if (wave == 0) {
+            const int rr = r + (lane & 31);
+            const int64_t where = (kv_head * a.group + head) * a.pack.q_rows + s.q0 + (rr < s.q_len ? rr : s.q_len - 1);
+            const float x = h == 0 ? a.lse[where] : a.delta[where];
+            stat = h == 0 ? (rr < s.q_len && x != -INFINITY ? x * kLog2e : INFINITY) : (rr < s.q_len ? x : 0.f);
+        }
+    };
+    auto commit = [&](char *to, int stage) {
+        lq.commit(to);
+        lg.commit(to + HALF);
+        if (wave == 0) stats[stage][h][lane & 31] = stat;
+    };
+    if (i < end) {
+        fetch(lds, head, at);
+        commit(lds, 0);
+    }
+    int stage = 0;
+    for (; i < end; ++i) {
+        char *now = lds + stage * STAGE, *next = lds + (stage ^ 1) * STAGE;
+        gemm::wait_and_barrier<0>();
+        const int r = r0 + at * QT;
+        if (++at == per) {
+            at = 0;
+            ++head;
+        }
+        const bool more = i + 1 < end;
+        if (more) fetch(next, head, at);
+        f32x16_t x, y;
+        clear(x);
+        clear(y);
+        rows_times<BF16, DP>(now, 0, k, x);
+        rows_times<BF16, DP>(now + HALF, 0, v, y);
+        const int hidden = r >= all_see ? -1 : from - r - 4 * h;  // rows before it do not see this lane's key
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const float4 l = *reinterpret_cast<const float4 *>(&stats[stage][0][8 * b + 4 * h]);
+            const float4 d = *reinterpret_cast<const float4 *>(&stats[stage][1][8 * b + 4 * h]);
+            const float ls[4] = {l.x, l.y, l.z, l.w}, ds[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+            for (int k4 = 0; k4 < 4; ++k4) {
+                const int e = 4 * b + k4;
+                const float p = 8 * b + k4 >= hidden ? exp2_(fmaf(x[e], a.c, -ls[k4])) : 0.f;
+                x[e] = p;
+                y[e] = p * (y[e] - ds[k4]);
+            }
+        }
+        Right<BF16> p;
+        p.set(x);
+        columns_times<BF16, DP>(now + HALF, 0, p, dv);
+        p.set(y);
+        columns_times<BF16, DP>(now, 0, p, dk);
+        if (more) commit(next, stage ^ 1);
+        stage ^= 1;
+    }
+    const int64_t at_row = (s.k0 + key) * a.kv_heads + kv_head;
+    if (counts) {
+        float *pk = a.splits > 1 ? a.part + split * 2 * size : nullptr, *pv = pk ? pk + size : nullptr;
+        store_column<BF16, DP>(a.dk, pk, at_row, a.D, dk, a.scale);
+        store_column<BF16, DP>(a.dv, pv, at_row, a.D, dv, 1.f);
+    } else if (a.zero_rest && split == 0 && key < s.kv_len && key < first + a.R) {
+        zero_row<BF16>(reinterpret_cast<char *>(a.dk) + at_row * a.D * L::E, a.D, h, 2);
+        zero_row<BF16>(reinterpret_cast<char *>(a.dv) + at_row * a.D * L::E, a.D, h, 2);
+    }
+}
+
+// Sums of the splits' values in their order, of kJoinRows rows a workgroup:
+// those of a sequence, or of its keys that count.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_join(Params a, bool by_keys) {
+    int first;
+    const Sequence s = locate(a.pack, kJoinRows, blockIdx.x, by_keys, first, a.status);
+    const int all = by_keys ? s.keys : s.q_len;
+    if (!s.real || first >= all) return;
+    const int rows = all - first < kJoinRows ? all - first : kJoinRows;
+    const int64_t width = (int64_t)(by_keys ? a.kv_heads : a.heads) * a.D;
+    const int64_t size = (by_keys ? a.pack.kv_rows : a.pack.q_rows) * width;
+    const int64_t from = ((by_keys ? s.k0 : s.q0) + first) * width;
+    void *out = !by_keys ? a.dq : blockIdx.y == 0 ? a.dk : a.dv;
+    const float *part = a.part + blockIdx.y * size + from;
+    const int64_t step = (by_keys ? 2 : 1) * size;
+    for (int64_t i = threadIdx.x; i < rows * width; i += 256) {
+        float x = 0.f;
+        for (int n = 0; n < a.splits; ++n) x += part[n * step + i];
+        if (BF16)
+            reinterpret_cast<uint16_t *>(out)[from + i] = (uint16_t)pack_bf16(x, 0.f);
+        else
+            reinterpret_cast<float *>(out)[from + i] = x;
+    }
+}
+
+// The two launches of a call, with their joins.
+struct Plan {
+    Params by_queries, by_keys;
+    bool dma_queries, dma_keys;
+    int64_t grid_queries, grid_keys, part;  // floats that the larger of the joins needs
+};
+
+Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
+    Plan r = {};
+    Params &p = r.by_queries;
+    p.pack = packing_of(a);
+    p.q = {a.q, a.q_row, a.q_head};
+    p.k = {a.k, a.k_row, a.k_head};
+    p.v = {a.v, a.v_row, a.v_head};
+    p.o = {a.out, a.o_row, a.o_head};
+    p.g = {a.grad, a.g_row, a.g_head};
+    p.dq = a.grad_q;
+    p.dk = a.grad_k;
+    p.dv = a.grad_v;
+    p.lse = a.lse;
+    p.heads = a.heads;
+    p.kv_heads = a.kv_heads;
+    p.D = a.D;
+    p.group = a.heads / a.kv_heads;
+    p.c = a.scale * kLog2e;
+    p.scale = a.scale;
+    p.zero_rest = a.zero_rest;
+    p.status = D->status;
+    r.by_keys = p;
+    const int E = a.bf16 ? 2 : 4;
+    r.dma_queries = straight(p.k, a.D, E) && straight(p.v, a.D, E);
+    r.dma_keys = straight(p.q, a.D, E) && straight(p.g, a.D, E);
+    const int64_t sequences = a.sequences > 0 ? a.sequences : 1;
+    const int64_t rows = (a.q_rows + sequences - 1) / sequences, keys = (a.kv_rows + sequences - 1) / sequences;
+    {
+        const Columns c(p.group, 128);
+        p.parts = c.parts;
+        p.tile_heads = c.heads;
+        p.R = c.R;
+        p.units = a.kv_heads * p.parts;
+        const int64_t slots = slots_of(a.q_starts, sequences, a.q_rows, p.R), tiles = (a.q_rows + p.R - 1) / p.R;
+        p.slots = (int)slots;
+        r.grid_queries = unit_grid(p.units, slots);
+        p.splits = splits_of(p.units * (tiles > sequences ? tiles : sequences), keys, 2 * D->cu_count, 256);
+        if (p.splits > 1) r.part = (int64_t)p.splits * a.q_rows * a.heads * a.D;
+    }
+    Params &b = r.by_keys;
+    b.R = 128;
+    const int32_t *starts = !a.q_starts ? nullptr : a.kv_starts ? a.kv_starts : a.q_starts;
+    const int64_t slots = slots_of(starts, sequences, a.kv_rows, b.R), tiles = (a.kv_rows + b.R - 1) / b.R;
+    b.slots = (int)slots;
+    r.grid_keys = unit_grid(a.kv_heads, slots);
+    b.splits = splits_of(a.kv_heads * (tiles > sequences ? tiles : sequences), rows * p.group, 2 * D->cu_count, 256);
+    if (b.splits > 1) {
+        const int64_t n = (int64_t)b.splits * 2 * a.kv_rows * a.kv_heads * a.D;
+        r.part = r.part > n ? r.part : n;
+    }
+    return r;
+}
+
+template <bool BF16, int DP, bool DMA>
+hipError_t by_queries(lattice_dense *D, const Plan &r) {
+    constexpr int LDS = 2 * 2 * 32 * Rows<BF16, DP>::BYTES;
+    static_assert(LDS <= 64 * 1024, "LDS");
+    hipLaunchKernelGGL((k_by_queries<BF16, DP, DMA>), dim3((unsigned)r.grid_queries, (unsigned)r.by_queries.splits),
+                       dim3(256), LDS, D->stream, r.by_queries);
+    return hipGetLastError();
+}
+
+template <bool BF16, int DP, bool DMA>
+hipError_t by_keys(lattice_dense *D, const Plan &r) {
+    constexpr int LDS = 2 * 2 * 32 * Rows<BF16, DP>::BYTES;
+    static std::atomic<uint64_t> done{0};
+    if (LDS + 1024 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_by_keys<BF16, DP, DMA>), LDS, done));
+    hipLaunchKernelGGL((k_by_keys<BF16, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.splits), dim3(256), LDS,
+                       D->stream, r.by_keys);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t join(lattice_dense *D, const Params &p, bool keys) {
+    if (p.splits == 1) return hipSuccess;
+    const int64_t n = slots_of(p.pack.q_starts, p.pack.sequences, keys ? p.pack.kv_rows : p.pack.q_rows, kJoinRows);
+    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)n, keys ? 2 : 1), dim3(256), 0, D->stream, p, keys);
+    return hipGetLastError();
+}
+
+template <bool BF16, int DP>
+hipError_t launch_dim(lattice_dense *D, const Plan &r) {
+    if (r.by_queries.pack.q_rows > 0) {
+        TRY(r.dma_queries ? (by_queries<BF16, DP, true>(D, r)) : (by_queries<BF16, DP, false>(D, r)));
+        TRY(join<BF16>(D, r.by_queries, false));
+    }
+    if (r.by_queries.pack.kv_rows > 0) {
+        TRY(r.dma_keys ? (by_keys<BF16, DP, true>(D, r)) : (by_keys<BF16, DP, false>(D, r)));
+        TRY(join<BF16>(D, r.by_keys, true));
+    }
+    return hipSuccess;
+}
+
+template <bool BF16>
+hipError_t launch_type(lattice_dense *D, const Plan &r) {
+    switch (padded_dim(r.by_queries.D)) {
+        case 32: return launch_dim<BF16, 32>(D, r);
+        case 64: return launch_dim<BF16, 64>(D, r);
+        default: return launch_dim<BF16, 128>(D, r);
+    }
+}
+
+}  // namespace
+
+int64_t attention_backward_scratch(const lattice_dense *D, const AttendArgs &a) {
+    const Plan r = plan_of(D, a);
+    ScratchLayout s;
+    s.take(a.q_rows * a.heads * 4);
+    s.take(r.part * 4);
+    return s.bytes;
+}
+
+bool attention_backward_fits(const lattice_dense *D, const AttendArgs &a) {
+    const Plan r = plan_of(D, a);
+    return r.grid_queries < ((int64_t)1 << 31) && r.grid_keys < ((int64_t)1 << 31);
+}
+
+hipError_t launch_attention_backward(lattice_dense *D, const AttendArgs &a) {
+    Plan r = plan_of(D, a);
+    ScratchLayout s;
+    char *ws = static_cast<char *>(D->ws);
+    r.by_queries.delta = r.by_keys.delta = reinterpret_cast<float *>(ws + s.take(a.q_rows * a.heads * 4));
+    r.by_queries.part = r.by_keys.part = reinterpret_cast<float *>(ws + s.take(r.part * 4));
+    return a.bf16 ? launch_type<true>(D, r) : launch_type<false>(D, r);
+}

@@ -1,5 +1,6 @@
 // Declarations shared by the dense operators (dense.hip: the host side;
-// norm.hip, loss.hip, update.hip: the kernels).
+// norm.hip, loss.hip, update.hip, attention.hip, attention_bwd.hip, rotate.hip,
+// clip.hip: the kernels).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -15,7 +16,7 @@
     } while (0)
 
 // Device status bits of a lattice_dense.
-enum : int { DENSE_ST_LABEL = 1 };
+enum : int { DENSE_ST_LABEL = 1, DENSE_ST_STARTS = 2 };
 
 // Scratch that a larger one has replaced while a graph may still use it.
 struct KeptScratch {
@@ -125,6 +126,78 @@ struct UpdateArgs {
 };
 int64_t update_scratch(const lattice_dense *D, const UpdateArgs &a);
 hipError_t launch_update(lattice_dense *D, const UpdateArgs &a);
+
+// attention.hip, attention_bwd.hip
+struct AttendArgs {
+    bool bf16;  // storage of all tensors but lse
+    int64_t q_rows, kv_rows;
+    int heads, kv_heads, D;
+    // values from row to row and from head to head
+    const void *q;
+    int64_t q_row, q_head;
+    const void *k;
+    int64_t k_row, k_head;
+    const void *v;
+    int64_t v_row, v_head;
+    const int32_t *q_starts, *kv_starts, *kv_lengths;
+    int64_t sequences;
+    bool causal;
+    float scale;
+    bool zero_rest;  // rows of no sequence become zeros
+    void *out;
+    int64_t o_row, o_head;
+    float *lse;
+    // the backward pass only
+    const void *grad;
+    int64_t g_row, g_head;
+    void *grad_q, *grad_k, *grad_v;  // [rows][heads][D], without gaps
+};
+int64_t attention_scratch(const lattice_dense *D, const AttendArgs &a);
+bool attention_fits(const lattice_dense *D, const AttendArgs &a);
+hipError_t launch_attention(lattice_dense *D, const AttendArgs &a);
+int64_t attention_backward_scratch(const lattice_dense *D, const AttendArgs &a);
+bool attention_backward_fits(const lattice_dense *D, const AttendArgs &a);
+hipError_t launch_attention_backward(lattice_dense *D, const AttendArgs &a);
+
+// rotate.hip
+struct RotateArgs {
+    bool bf16;
+    int64_t rows;
+    int heads, kv_heads, D;
+    // values from row to row and from head to head
+    const void *q, *k;
+    int64_t q_row, q_head, k_row, k_head;
+    const void *pos;
+    bool integers;
+    int64_t pos_stride;
+    int axes;
+    const int *sections;  // host
+    const float *freq, *gain_q, *gain_k;
+    bool norm, interleaved;
+    float eps;
+    void *out_q, *out_k;  // the rotated heads, or the gradients of q and k
+    int64_t oq_row, oq_head, ok_row, ok_head;
+    // the backward pass only
+    const void *grad_q, *grad_k;
+    int64_t gq_row, gq_head, gk_row, gk_head;
+    float *grad_gain_q, *grad_gain_k;
+};
+hipError_t launch_rotate(lattice_dense *D, const RotateArgs &a);
+int64_t rotate_backward_scratch(const lattice_dense *D, const RotateArgs &a);
+hipError_t launch_rotate_backward(lattice_dense *D, const RotateArgs &a);
+
+// clip.hip
+struct ClipArgs {
+    int count;
+    const void *const *in;  // host arrays of device addresses
+    void *const *out;
+    const int64_t *n;
+    const lattice_dtype *in_type, *out_type;
+    float most, eps;
+    float *norm;
+};
+int64_t clip_scratch(const lattice_dense *D, const ClipArgs &a);
+hipError_t launch_clip(lattice_dense *D, const ClipArgs &a);
 
 // Sixteen or fewer bytes of consecutive values, at the alignment of one value.
 struct __attribute__((packed, aligned(4))) Words4 { uint32_t v[4]; };

@@ -1,6 +1,8 @@
 """ctypes binding of the dense operators of include/lattice.h: layer
-normalisation, the linear classifier with its softmax cross entropy, and the
-orthogonalised form of a weight gradient.
+normalisation, the linear classifier with its softmax cross entropy, the
+orthogonalised form of a weight gradient, attention over packed sequences with the
+norm and rotation of its queries and keys, and clipping by the norm of all
+gradients.
 
 Argument marshalling only, as in ``lattice``: tensors are passed as raw device
 pointers, outputs are allocated with torch, and every step runs in the
@@ -9,6 +11,7 @@ library's HIP kernels.
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Optional, Sequence
 
 import torch
@@ -59,7 +62,8 @@ class Dense:
 
     def status(self) -> int:
         """Synchronise; the device status since the last such call (0 is ok,
-        E_RANGE after a label that is neither a class nor ``ignore_index``)."""
+        E_RANGE after a label that is neither a class nor ``ignore_index``, or
+        after starts or lengths of an attention that do not fit its rows)."""
         return int(self._lib.lattice_dense_get_status(self._h))
 
     # -- marshalling ------------------------------------------------------
@@ -238,3 +242,207 @@ class Dense:
                    g.stride(0) if g.dim() == 3 else 0, rs if rs > n else n, steps, (ctypes.c_float * 3)(a, b, c), eps,
                    out.data_ptr(), _STORAGE[out.dtype])
         return out
+
+    # -- attention -----------------------------------------------------------
+    def _heads(self, t: torch.Tensor, name: str, shape=None, dtype=None):
+        """Check a [rows, heads, C] tensor whose heads' values are next to each
+        other; (address, values from row to row, from head to head)."""
+        if t.dtype not in _STORAGE or dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype or ' or '.join(map(str, _STORAGE))}, got {t.dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}, is on {t.device}")
+        if t.dim() != 3 or shape is not None and t.shape != shape:
+            raise ValueError(f"{name} must be {list(shape) if shape is not None else '[rows, heads, channels]'}, "
+                             f"is {list(t.shape)}")
+        row, head, one = t.stride()
+        if one != 1 and t.shape[2] > 1:
+            raise ValueError(f"{name}: the values of a head must be next to each other")
+        return t.data_ptr(), row, head
+
+    def _starts(self, t: Optional[torch.Tensor], n: int, name: str):
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 [{n}] on {self.device}")
+        return t.data_ptr()
+
+    def _attention(self, q, k, v, q_starts, kv_starts, kv_lengths, scale):
+        """Check what both passes take: (dtype .. C, q, k, v), (starts .. sequences), scale."""
+        qv = self._heads(q, "q")
+        kv = self._heads(k, "k", dtype=q.dtype)
+        vv = self._heads(v, "v", k.shape, q.dtype)
+        rows, heads, C = q.shape
+        kv_rows, kv_heads, kC = k.shape
+        if kC != C or kv_heads == 0 or heads % kv_heads:
+            raise ValueError(f"k must have heads of {C} channels, as many as divide q's {heads}, is {list(k.shape)}")
+        n = 1
+        if q_starts is not None:
+            n = q_starts.shape[0] - 1 if q_starts.dim() == 1 else -1
+            if n < 0:
+                raise ValueError("q_starts must be [sequences + 1]")
+        elif kv_starts is not None:
+            raise ValueError("kv_starts without q_starts")
+        packing = (self._starts(q_starts, n + 1, "q_starts"), self._starts(kv_starts, n + 1, "kv_starts"),
+                   self._starts(kv_lengths, n, "kv_lengths"), n)
+        scale = 1 / math.sqrt(C) if scale is None and C else scale
+        return (_STORAGE[q.dtype], rows, kv_rows, heads, kv_heads, C), (*qv, *kv, *vv), packing, scale
+
+    def attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: Optional[torch.Tensor] = None,
+                  kv_starts: Optional[torch.Tensor] = None, kv_lengths: Optional[torch.Tensor] = None,
+                  causal: bool = False, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                  want_lse: bool = False):
+        """Softmax attention of ``q`` [rows, heads, C] over ``k`` and ``v``
+        [kv_rows, kv_heads, C] (all fp32 or all bf16, any strides but along C; C
+        up to 128), a key head for ``heads // kv_heads`` query heads next to each
+        other.  ``q_starts`` (int32 [sequences + 1]) packs sequences one behind
+        the other; keys have the same starts unless ``kv_starts`` gives theirs, of
+        which ``kv_lengths`` (int32 [sequences]) says how many count.  Without
+        starts there is one sequence.  With ``causal`` row i of a sequence of n
+        sees the keys up to i + (its keys) - n.  ``scale`` is 1 / sqrt(C) unless
+        given.  A row that sees no key gets zeros; rows of no sequence are left
+        alone in a given ``out``, else zeros.  Returns out, with ``want_lse`` also
+        the log of each row's sum of exponentials (fp32 [heads, rows]), which the
+        backward pass takes."""
+        sizes, tensors, packing, scale = self._attention(q, k, v, q_starts, kv_starts, kv_lengths, scale)
+        rest = out is None
+        if rest:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ov = self._heads(out, "out", q.shape, q.dtype)
+        lse = torch.empty((q.shape[1], q.shape[0]), dtype=F32, device=q.device) if want_lse else None
+        if want_lse and not rest:
+            lse.fill_(-math.inf)
+        self._call(self._lib.lattice_attention, "attention", *sizes, *tensors, *packing, causal, scale, rest, *ov, _ptr(lse))
+        return (out, lse) if want_lse else out
+
+    def attention_backward(self, grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                           out: torch.Tensor, lse: torch.Tensor, q_starts: Optional[torch.Tensor] = None,
+                           kv_starts: Optional[torch.Tensor] = None, kv_lengths: Optional[torch.Tensor] = None,
+                           causal: bool = False, scale: Optional[float] = None):
+        """Gradients of ``attention`` with the same arguments, given ``grad_out``
+        and the forward's ``out`` and ``lse``: (grad_q, grad_k, grad_v), contiguous
+        and stored as their inputs, zeros for rows of no sequence and for keys that
+        do not count."""
+        sizes, tensors, packing, scale = self._attention(q, k, v, q_starts, kv_starts, kv_lengths, scale)
+        gv = self._heads(grad_out, "grad_out", q.shape, q.dtype)
+        ov = self._heads(out, "out", q.shape, q.dtype)
+        self._dev(lse, "lse", (F32,))
+        if lse.shape != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
+            raise ValueError(f"lse must be a contiguous [{q.shape[1]}, {q.shape[0]}]")
+        gq, gk, gvv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        self._call(self._lib.lattice_attention_backward, "attention_backward", *sizes, *gv, *tensors, *ov, lse.data_ptr(),
+                   *packing, causal, scale, True, gq.data_ptr(), gk.data_ptr(), gvv.data_ptr())
+        return gq, gk, gvv
+
+    # -- norm and rotation of heads ------------------------------------------
+    def _rotation(self, q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved):
+        rows, heads, C = q.shape
+        if positions.dtype not in (F32, torch.int32) or positions.device != self.device:
+            raise ValueError(f"positions must be float32 or int32 on {self.device}")
+        if positions.dim() == 1:
+            positions = positions[:, None]
+        if positions.dim() != 2 or positions.shape[0] != rows or positions.shape[1] > 1 and positions.stride(1) != 1:
+            raise ValueError(f"positions must be [{rows}, axes], the axes next to each other")
+        axes = positions.shape[1]
+        sections = [freq.shape[0]] if sections is None and freq.dim() == 1 else sections
+        if sections is None or len(sections) != axes:
+            raise ValueError(f"sections must hold the pairs of each of {axes} axes")
+        self._vector(freq, sum(sections), "freq")
+        self._vector(gain_q, C, "gain_q")
+        self._vector(gain_k, C, "gain_k")
+        return (positions.data_ptr(), positions.dtype == torch.int32, positions.stride(0) if rows > 1 else axes, axes,
+                (ctypes.c_int * axes)(*sections), freq.data_ptr(), norm, _ptr(gain_q), _ptr(gain_k), eps, interleaved)
+
+    def rotate_heads(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, freq: torch.Tensor,
+                     sections: Optional[Sequence[int]] = None, gain_q: Optional[torch.Tensor] = None,
+                     gain_k: Optional[torch.Tensor] = None, norm: bool = True, eps: float = 1e-6,
+                     interleaved: bool = False, out_q: Optional[torch.Tensor] = None,
+                     out_k: Optional[torch.Tensor] = None):
+        """Divide each head's row of ``q`` [rows, heads, C] and ``k`` [rows,
+        kv_heads, C] (or None; both fp32 or both bf16, any strides but along C; C
+        up to 256) by the root of its mean square (and ``eps``), multiply by the
+        gains (fp32 [C] or None), and turn its pairs of channels by the row's
+        ``positions`` [rows, axes] (fp32 or int32; [rows] for one axis) times
+        ``freq`` (fp32, one for each pair, radians): ``sections[a]`` pairs with
+        axis a, one behind the other, all with a single axis unless given.  Of P
+        pairs, pair p is the channels p and p + P, or 2 p and 2 p + 1 if
+        ``interleaved``; channels from 2 P on do not turn.  Without ``norm`` only
+        the rotation.  Returns (out_q, out_k); the outputs may be the inputs."""
+        qv = self._heads(q, "q")
+        kv = self._heads(k, "k", (q.shape[0], k.shape[1], q.shape[2]) if k.dim() == 3 else None, q.dtype) if k is not None \
+            else (None, 0, 0)
+        rotation = self._rotation(q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved)
+        if out_q is None:
+            out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        oq = self._heads(out_q, "out_q", q.shape, q.dtype)
+        if k is None:
+            out_k, ok = None, (None, 0, 0)
+        else:
+            if out_k is None:
+                out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            ok = self._heads(out_k, "out_k", k.shape, k.dtype)
+        self._call(self._lib.lattice_rotate_heads, "rotate_heads", _STORAGE[q.dtype], q.shape[0], q.shape[1],
+                   k.shape[1] if k is not None else 0, q.shape[2], *qv, *kv, *rotation, *oq, *ok)
+        return out_q, out_k
+
+    def rotate_heads_backward(self, grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: torch.Tensor,
+                              k: Optional[torch.Tensor], positions: torch.Tensor, freq: torch.Tensor,
+                              sections: Optional[Sequence[int]] = None, gain_q: Optional[torch.Tensor] = None,
+                              gain_k: Optional[torch.Tensor] = None, norm: bool = True, eps: float = 1e-6,
+                              interleaved: bool = False, want_gains: Optional[bool] = None):
+        """Gradients of ``rotate_heads`` with the same arguments, given those of
+        its results: (of q, of k, of gain_q, of gain_k), the first two contiguous
+        and stored as their inputs, the last two fp32 [C], or None with
+        ``want_gains`` False (which is so without the norm unless given).
+        Positions and frequencies get none."""
+        qv = self._heads(q, "q")
+        gq = self._heads(grad_q, "grad_q", q.shape, q.dtype)
+        if (k is None) != (grad_k is None):
+            raise ValueError("k and grad_k go together")
+        kv = gk = ok = (None, 0, 0)
+        out_k = None
+        if k is not None:
+            kv = self._heads(k, "k", (q.shape[0], k.shape[1], q.shape[2]) if k.dim() == 3 else None, q.dtype)
+            gk = self._heads(grad_k, "grad_k", k.shape, k.dtype)
+            out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            ok = (out_k.data_ptr(), k.shape[1] * k.shape[2], k.shape[2])
+        rotation = self._rotation(q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved)
+        out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        oq = (out_q.data_ptr(), q.shape[1] * q.shape[2], q.shape[2])
+        gg = [None, None]
+        if norm if want_gains is None else want_gains:
+            both = torch.empty((2, q.shape[2]), dtype=F32, device=q.device)
+            gg = [both[0], both[1] if k is not None else None]
+        self._call(self._lib.lattice_rotate_heads_backward, "rotate_heads_backward", _STORAGE[q.dtype], q.shape[0],
+                   q.shape[1], k.shape[1] if k is not None else 0, q.shape[2], *gq, *gk, *qv, *kv, *rotation, *oq, *ok,
+                   _ptr(gg[0]), _ptr(gg[1]))
+        return out_q, out_k, gg[0], gg[1]
+
+    # -- clipping ------------------------------------------------------------
+    def clip_gradients(self, grads: Sequence[torch.Tensor], max_norm: float, eps: float = 1e-6,
+                       out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+        """Scale ``grads`` (fp32 or bf16, contiguous, of any shapes) by
+        min(1, max_norm / (norm + eps)), where norm is that over all their values,
+        in place or into ``out`` (fp32 or bf16, the same shapes).  Returns the norm
+        before, an fp32 scalar.  A norm that is not finite is not refused: NaN
+        makes every value NaN, infinity makes finite ones 0."""
+        n = len(grads)
+        to = grads if out is None else out
+        if len(to) != n:
+            raise ValueError(f"out must hold {n} tensors")
+        device, types = self.device, _STORAGE
+        for name, ts in (("grads", grads),) if out is None else (("grads", grads), ("out", to)):
+            for i, t in enumerate(ts):
+                if t.dtype not in types or t.device != device or not t.is_contiguous():
+                    raise ValueError(f"{name}[{i}] must be contiguous, fp32 or bf16, and on {device}")
+        if out is not None:
+            for i, (a, b) in enumerate(zip(grads, to)):
+                if a.shape != b.shape:
+                    raise ValueError(f"out[{i}] must be {list(a.shape)}")
+        norm = torch.empty((), dtype=F32, device=device)
+        pointers, kinds = ctypes.c_void_p * n, ctypes.c_int * n
+        src, src_t = pointers(*[t.data_ptr() for t in grads]), kinds(*[types[t.dtype] for t in grads])
+        dst, dst_t = (src, src_t) if out is None else (pointers(*[t.data_ptr() for t in to]),
+                                                       kinds(*[types[t.dtype] for t in to]))
+        self._call(self._lib.lattice_clip_gradients, "clip_gradients", n, src, src_t, dst, dst_t,
+                   (ctypes.c_int64 * n)(*[t.numel() for t in grads]), max_norm, eps, norm.data_ptr())
+        return norm

@@ -36,6 +36,8 @@ EXPORTS = (
     "lattice_dense_create", "lattice_dense_destroy", "lattice_dense_get_status", "lattice_dense_last_error",
     "lattice_dense_set_gradient_bits",
     "lattice_layer_norm", "lattice_layer_norm_backward", "lattice_linear_cross_entropy", "lattice_orthogonalize",
+    "lattice_attention", "lattice_attention_backward", "lattice_rotate_heads", "lattice_rotate_heads_backward",
+    "lattice_clip_gradients",
 )
 
 _lib = None
@@ -100,6 +102,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "lattice_layer_norm_backward": (St, [P, P, P, I, I64, P, I, I64, I64, I, P, P, P, P, I64, P, P]),
         "lattice_linear_cross_entropy": (St, [P, I, P, I64, I64, I, P, I64, I, P, P, I64, I, P, P, P, P, P]),
         "lattice_orthogonalize": (St, [P, P, I, I64, I, I, I64, I64, I, P, F, P, I]),
+        "lattice_attention": (St, [P, I, I64, I64, I, I, I] + [P, I64, I64] * 3 + [P, P, P, I64, I, F, I, P, I64, I64, P]),
+        "lattice_attention_backward": (St, [P, I, I64, I64, I, I, I] + [P, I64, I64] * 5 +
+                                       [P, P, P, P, I64, I, F, I, P, P, P]),
+        "lattice_rotate_heads": (St, [P, I, I64, I, I, I] + [P, I64, I64] * 2 + [P, I, I64, I, P, P, I, P, P, F, I] +
+                                 [P, I64, I64] * 2),
+        "lattice_rotate_heads_backward": (St, [P, I, I64, I, I, I] + [P, I64, I64] * 4 +
+                                          [P, I, I64, I, P, P, I, P, P, F, I] + [P, I64, I64] * 2 + [P, P]),
+        "lattice_clip_gradients": (St, [P, I, P, P, P, P, P, F, F, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

@@ -1,0 +1,242 @@
+"""The norm and rotation of queries' and keys' heads, forward and backward, against
+a plain 64-bit implementation.
+
+Tolerances, fixed from the arithmetic, u = 2^-24 being half a step of fp32.  A
+normalised value is off by (C / 2 + 8) u of itself (a sum of C squares under a
+root, a division, two products), an angle's sine and cosine by 4 u (two for the
+part of a turn, 2 pi 2^-25 for its rounding among them), a turned value so by
+e = (C / 2 + 16) u of |w_a| + |w_b|; gradients of x by 2 e of what they add up, the
+mean's sum among it; a gain's gradient by e and, of n rows and heads, n u of the
+sum of its terms.  bf16 results by 2^-8 of themselves more.
+"""
+import math
+
+import pytest
+import torch
+
+from tests.test_gpu_attention import U, within
+from tests.test_gpu_dense import DEV, HALF, T, _gpu, ops, rand  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def pairs_of(C, P, interleaved):
+    p = torch.arange(P, device=DEV)
+    return (2 * p, 2 * p + 1) if interleaved else (p, p + P)
+
+
+def angles(pos, freq, sections):
+    axis = torch.repeat_interleave(torch.arange(len(sections)), torch.tensor(sections)).to(DEV)
+    return pos.double()[:, axis] * freq.double()
+
+
+def turn(x, t, a, b):
+    """Pairs (a, b) of x [rows, heads, C] by angles t [rows, P], and the sizes of what
+    is added up."""
+    c, s = torch.cos(t)[:, None], torch.sin(t)[:, None]
+    y, m = x.clone(), x.abs()
+    y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., b] * c + x[..., a] * s
+    both = x[..., a].abs() + x[..., b].abs()
+    m[..., a], m[..., b] = both, both
+    return y, m
+
+
+def rotate_ref(x, pos, freq, sections, gain, norm, eps, interleaved, g=None):
+    half = HALF if x.dtype == torch.bfloat16 else 0.0
+    x = x.double()
+    rows, heads, C = x.shape
+    a, b = pairs_of(C, sum(sections), interleaved)
+    t = angles(pos, freq, sections)
+    e = (C / 2 + 16) * U
+    ga = torch.ones(C, device=DEV).double() if gain is None else gain.double()
+    r = 1 / (x.square().mean(-1, keepdim=True) + eps).sqrt() if norm else torch.ones(rows, heads, 1, device=DEV).double()
+    n = x * r
+    y, m = turn(n * ga, t, a, b)
+    if g is None:
+        return y, e * m + half * y.abs()
+    u, um = turn(g.double(), -t, a, b)
+    v, vm = u * ga, um * ga.abs()
+    if norm:
+        gx = r * (v - n * (v * n).mean(-1, keepdim=True))
+        gm = r * (vm + n.abs() * (vm * n.abs()).mean(-1, keepdim=True))
+    else:
+        gx, gm = u, um
+    gg, ggm = (u * n).sum((0, 1)), (um * n.abs()).sum((0, 1))
+    return (gx, 2 * e * gm + half * gx.abs()), (gg, (e + U * min(rows * heads, 1 << 14)) * ggm)
+
+
+def check(ops, q, k, pos, freq, sections, gains=(None, None), norm=True, eps=1e-6, interleaved=False):  # noqa: F811
+    args = (q, k, pos, freq, sections, *gains)
+    kw = dict(norm=norm, eps=eps, interleaved=interleaved)
+    got = ops.rotate_heads(*args, **kw)
+    gq = rand(91, *q.shape).to(q.dtype)
+    gk = rand(92, *k.shape).to(q.dtype) if k is not None else None
+    back = ops.rotate_heads_backward(gq, gk, *args, **kw)
+    pos2 = pos if pos.dim() == 2 else pos[:, None]
+    sections = sections or [freq.shape[0]]
+    for x, y, g, gx, gg, gain in ((q, got[0], gq, back[0], back[2], gains[0]), (k, got[1], gk, back[1], back[3], gains[1])):
+        if x is None:
+            assert y is None and gx is None and gg is None
+            continue
+        within(y, *rotate_ref(x, pos2, freq, sections, gain, norm, eps, interleaved), "out")
+        (r, e), (rg, eg) = rotate_ref(x, pos2, freq, sections, gain, norm, eps, interleaved, g)
+        within(gx, r, e, "grad")
+        if norm:
+            within(gg, rg, eg, "grad_gain")
+        else:
+            assert gg is None
+    return got
+
+
+def frequencies(P):
+    return (10000.0 ** (-torch.arange(P, device=DEV).double() / max(P, 1))).float()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,sections", [(1, [0]), (2, [1]), (7, [3]), (20, [3, 3, 3]), (32, [16]), (36, [4, 4, 4, 4]),
+                                        (64, [8, 24]), (100, [50]), (100, [10, 0, 33]), (128, [16, 24, 24]), (128, [0, 1]),
+                                        (200, [100]), (256, [1, 2, 3, 4, 5, 6, 7, 100])])
+def test_head_sizes(ops, C, sections, dtype, interleaved):  # noqa: F811
+    q, k = rand(1, 37, 4, C, dtype=dtype) * 2, rand(2, 37, 2, C, dtype=dtype)
+    pos = 30 * rand(3, 37, len(sections))
+    gains = 1 + 0.3 * rand(4, C), rand(5, C)
+    check(ops, q, k, pos, frequencies(sum(sections)), sections, gains, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,heads,kv_heads", [(1, 1, 1), (1, 32, 8), (2, 3, 5), (5, 1, 0), (4000, 1, 1), (1300, 12, 4),
+                                                 (20000, 2, 1)])
+def test_rows_and_heads(ops, rows, heads, kv_heads, dtype):  # noqa: F811
+    q = rand(1, rows, heads, 48, dtype=dtype)
+    k = rand(2, rows, kv_heads, 48, dtype=dtype) if kv_heads else None
+    check(ops, q, k, 5 * rand(3, rows, 3), frequencies(24), [8, 8, 8], (1 + 0.3 * rand(4, 48), None))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rotation_alone_and_one_axis(ops, dtype):  # noqa: F811
+    q, k = rand(1, 50, 4, 64, dtype=dtype), rand(2, 50, 4, 64, dtype=dtype)
+    got = check(ops, q, k, torch.arange(50, device=DEV, dtype=torch.int32), frequencies(32), None, norm=False)
+    assert torch.equal(got[0][0], q[0])              # position 0 turns nothing
+
+
+def test_far_positions(ops):  # noqa: F811
+    """Positions whose angles have millions of turns, as fp32 and as int32."""
+    q, k = rand(1, 6, 2, 32), rand(2, 6, 2, 32)
+    far = torch.tensor([0, 1, 99999, 16777215, 2 ** 31 - 1, -(2 ** 31)], device=DEV)
+    check(ops, q, k, far.int(), frequencies(16), None)
+    check(ops, q, k, far.float(), frequencies(16), None)
+
+
+def test_a_position_that_is_no_number_turns_no_other_channel(ops):  # noqa: F811
+    q = rand(1, 3, 1, 40)
+    pos = torch.zeros(3, 2, device=DEV)
+    pos[1, 1] = float("nan")
+    y, _ = ops.rotate_heads(q, None, pos, frequencies(16), [8, 8])
+    bad = torch.isnan(y)
+    assert not bad[0].any() and not bad[2].any()
+    assert bad[1, 0, 8:16].all() and bad[1, 0, 24:32].all() and bad.sum() == 16
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,offset", [(32, 0), (32, 3), (36, 1)])
+def test_strides_and_in_place(ops, C, offset, dtype):  # noqa: F811
+    n = 70
+    flat = rand(1, n * 7 * C + offset, dtype=dtype)[offset:].view(n, 7, C)
+    q, k, v = flat[:, :4], flat[:, 4:6], flat[:, 6:].clone()
+    pos = rand(3, n, 5)[:, 1:4]
+    gains = rand(4, C), rand(5, C)
+    want = [x.clone() for x in check(ops, q, k, pos, frequencies(C // 2), [C // 2 - 2, 1, 1], gains)]
+    heads_first = rand(7, 4, n, C, dtype=dtype).transpose(0, 1)
+    check(ops, heads_first, heads_first[:, :1].expand(n, 3, C), pos, frequencies(3), [1, 1, 1], gains)
+    got = ops.rotate_heads(q, k, pos, frequencies(C // 2), [C // 2 - 2, 1, 1], *gains, out_q=q, out_k=k)
+    assert torch.equal(got[0], want[0]) and torch.equal(flat[:, 4:6], want[1]) and torch.equal(flat[:, 6:], v)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_zeros(ops, dtype):  # noqa: F811
+    q = torch.zeros(5, 2, 16, device=DEV, dtype=T[dtype])
+    y, _ = ops.rotate_heads(q, None, rand(1, 5, 1), frequencies(8))
+    assert torch.all(y == 0)
+    gx, _, gg, _ = ops.rotate_heads_backward(rand(2, 5, 2, 16, dtype=dtype), None, q, None, rand(1, 5, 1), frequencies(8))
+    assert torch.isfinite(gx).all() and torch.all(gg == 0)
+
+
+def test_no_rows(ops):  # noqa: F811
+    q, k, pos = rand(1, 0, 2, 16), rand(2, 0, 1, 16), rand(3, 0, 2)
+    assert ops.rotate_heads(q, k, pos, frequencies(8), [4, 4])[0].shape == q.shape
+    gq, gk, ggq, ggk = ops.rotate_heads_backward(q, k, q, k, pos, frequencies(8), [4, 4])
+    assert gq.shape == q.shape and gk.shape == k.shape and torch.all(ggq == 0) and torch.all(ggk == 0)
+
+
+def test_gradients_against_differences(ops):  # noqa: F811
+    n, C = 30, 24
+    q, k, pos, gq, gk = rand(1, n, 3, C), rand(2, n, 2, C), rand(3, n, 2), rand(4, n, 3, C), rand(5, n, 2, C)
+    x = [q, k, 1 + 0.2 * rand(6, C), 1 + 0.2 * rand(7, C)]
+
+    def loss(q, k, a, b):
+        y, z = ops.rotate_heads(q, k, pos, frequencies(10), [5, 5], a, b)
+        return ((y.double() * gq.double()).sum() + (z.double() * gk.double()).sum()).item()
+
+    grads = ops.rotate_heads_backward(gq, gk, q, k, pos, frequencies(10), [5, 5], *x[2:])
+    for i in range(4):
+        d, h = rand(20 + i, *x[i].shape), 1e-2
+        step = [y + h * d if j == i else y for j, y in enumerate(x)]
+        back = [y - h * d if j == i else y for j, y in enumerate(x)]
+        slope = (grads[i].double() * d.double()).sum().item()
+        # 3600 results off by 1e-6, over 2 h; the third derivative's share 1e-4
+        assert abs((loss(*step) - loss(*back)) / (2 * h) - slope) <= 2e-3 * max(1.0, abs(slope))
+
+
+def test_same_bits_and_graph(_gpu):  # noqa: F811
+    from paper_2108_03917_amd import Dense
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    own = Dense(side)
+    q, k, pos = rand(1, 5000, 4, 64, dtype="bf16"), rand(2, 5000, 2, 64, dtype="bf16"), 10 * rand(3, 5000, 3)
+    gain, f = 1 + 0.1 * rand(4, 64), frequencies(30)
+
+    def all_of():
+        y = own.rotate_heads(q, k, pos, f, [10, 10, 10], gain, gain)
+        return [*y, *own.rotate_heads_backward(*y, q, k, pos, f, [10, 10, 10], gain, gain)]
+
+    first = all_of()
+    assert all(torch.equal(a, b) for a, b in zip(first, all_of()))
+    with torch.cuda.stream(side):
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = all_of()
+        for i in range(3):
+            q.copy_(rand(10 + i, 5000, 4, 64, dtype="bf16"))
+            graph.replay()
+            side.synchronize()
+            want = all_of()
+            side.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+    own.close()
+
+
+def test_refusals(ops):  # noqa: F811
+    from paper_2108_03917_amd import LatticeError
+
+    q, k, pos, f, g = rand(1, 10, 4, 16), rand(2, 10, 2, 16), rand(3, 10, 2), frequencies(8), rand(4, 16)
+    for bad in (lambda: ops.rotate_heads(q, k[:5], pos, f, [4, 4]), lambda: ops.rotate_heads(q, k.bfloat16(), pos, f, [4, 4]),
+                lambda: ops.rotate_heads(q, k, pos, f), lambda: ops.rotate_heads(q, k, pos, f, [8]),
+                lambda: ops.rotate_heads(q, k, pos, f[:7], [4, 4]), lambda: ops.rotate_heads(q, k, pos.double(), f, [4, 4]),
+                lambda: ops.rotate_heads(q, k, pos[:9], f, [4, 4]), lambda: ops.rotate_heads(q, k, pos, f, [4, 4], g[:8]),
+                lambda: ops.rotate_heads(q.half(), None, pos, f, [4, 4]), lambda: ops.rotate_heads(q[..., ::2], None, pos, f, [4, 4]),
+                lambda: ops.rotate_heads(q, k, pos, f, [4, 4], out_q=k),
+                lambda: ops.rotate_heads_backward(q, None, q, k, pos, f, [4, 4])):
+        with pytest.raises(ValueError):
+            bad()
+    long = frequencies(9)
+    wide = rand(1, 10, 1, 257)
+    for bad in (lambda: ops.rotate_heads(q, k, pos, long, [4, 5]), lambda: ops.rotate_heads(q, k, pos, f, [9, -1]),
+                lambda: ops.rotate_heads(q, k, pos, f, [4, 4], eps=-1.0), lambda: ops.rotate_heads(q, k, pos, f, [4, 4], g, norm=False),
+                lambda: ops.rotate_heads(wide, None, pos, f, [4, 4]), lambda: ops.rotate_heads(q, k, pos, f, [4, 4], out_k=q[:, 1:3]),
+                lambda: ops.rotate_heads(q, k, pos, f, [4, 4], out_q=rand(1, 10, 1, 16).expand(10, 4, 16)),
+                lambda: ops.rotate_heads(q, k, rand(1, 10, 9), f, [8] + [0] * 8)):
+        with pytest.raises(LatticeError):
+            bad()
