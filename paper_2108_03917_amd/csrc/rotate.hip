@@ -8,12 +8,20 @@
 // (= dL/dw),  dgain_c = sum over rows of u_c n_c,  and with v_c = u_c gain_c
 //   dx_c = r (v_c - n_c mean(v n)).
 //
-// Channels go in units of two: a pair that turns, or two of those that stay.  A
-// lane has 4 units of a head, the same ones for each row it takes, so that their
-// gain and frequency stay in registers; a group of 4 to 32 lanes has a head, and
-// takes one row's heads after another, so that angles are made once a row.  An angle is
+// A lane has 4 pairs, or 8 of the channels that stay, the same ones for each row it
+// takes, so that their gain and frequency stay in registers; a group of 4 to 64 lanes
+// has a head, and takes one row's heads after another, so that angles are made once
+// a row.  An angle is
 // reduced to a part of a turn in 64 bits: a position of 1e5 has 1.6e4 turns, of
-// which 24 bits would leave 1e-3 of one.  Everything is bound by the bytes.
+// which 24 bits would leave 1e-3 of one.
+//
+// Everything is bound by the bytes: 16384 rows of 32 + 8 heads of 128 in bf16, 67 us
+// forward (335 MB, 5.0 TB/s; a large copy 5.6) and 110 backward (503 MB, 4.6 TB/s);
+// 82411 rows of 4 + 4 heads of 36 in fp32, 47 and 98 (4.1 and 2.9 TB/s: 5 of a
+// group's 8 lanes have channels).  What got them there from 113 and 364 us: loads without
+// a branch around them, of 4 (backward 2) heads at a time; sums by moves between lanes
+// in place of LDS; addresses made for each head, which leaves room for 5 (4)
+// wavefronts a SIMD.
 //
 // dgain: each lane adds up its channels in fp32, a workgroup its groups in LDS,
 // and rowsum.h the workgroups in fp64, in a fixed order.
@@ -34,7 +42,7 @@ struct Side {  // queries or keys
 struct Params {
     Side side[2];
     int64_t rows;
-    int D, pairs, units;
+    int D, pairs;
     const void *pos;
     int64_t pos_stride;
     int integers;   // positions are int32
@@ -42,220 +50,323 @@ struct Params {
     const float *freq;
     int norm;
     float eps;
-    int share;      // groups that share a row
+    int share, log_share;  // groups that share a row: a power of 2
     int64_t items;  // rows x share
 };
 
-// Channels of unit u: (a, b), -1 for none.
-template <bool INTER>
-__device__ __forceinline__ void channels(const Params &p, int u, int &a, int &b) {
-    const int rest = p.D - 2 * p.pairs, half = (rest + 1) / 2;
-    if (u < p.pairs) {
-        a = INTER ? 2 * u : u;
-        b = INTER ? 2 * u + 1 : u + p.pairs;
-    } else {
-        a = 2 * p.pairs + u - p.pairs;
-        b = a + half;
-        if (u >= p.units) a = b = -1;
-        else if (b >= p.D) b = -1;
-    }
+// How a kernel's lanes take their values, four at a time: all there are (WHOLE), the
+// last ones of a row fewer (TAILS), or one by one (ONES, rows of fewer than four).
+enum Mode { WHOLE, TAILS, ONES };
+
+// Addresses are kept as numbers, hidden from the compiler when they are made: it would
+// otherwise keep one for each of a lane's values from head to head, in 100 registers.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2), aligned(2)));
+template <class T>
+using global = __attribute__((address_space(1))) T;
+__device__ __forceinline__ uint64_t address(const void *p, int64_t bytes) {
+    uint64_t a = reinterpret_cast<uint64_t>(p) + (uint64_t)bytes;
+    asm("" : "+v"(a));
+    return a;
 }
 
+// Values c .. c + n - 1 of a row of D as they are stored, with zeros after them.
 template <bool BF16>
-__device__ __forceinline__ float load1(const void *row, int c) {
-    if (c < 0) return 0.f;
-    return BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(row)[c]) : reinterpret_cast<const float *>(row)[c];
-}
-template <bool BF16>
-__device__ __forceinline__ void store1(void *row, int c, float v) {
-    if (c < 0) return;
-    if (BF16)
-        reinterpret_cast<uint16_t *>(row)[c] = (uint16_t)pack_bf16(v, 0.f);
-    else
-        reinterpret_cast<float *>(row)[c] = v;
-}
-
-// Four values next to each other, at the alignment of one.
-template <bool BF16>
-__device__ __forceinline__ void load4(const void *row, int c, float *v) {
-    if constexpr (BF16) {
-        struct __attribute__((packed, aligned(2))) Two { uint32_t v[2]; };
-        const Two t = *reinterpret_cast<const Two *>(reinterpret_cast<const uint16_t *>(row) + c);
+struct Four {
+    uint32_t w[BF16 ? 2 : 4];
+};
+template <bool BF16, Mode MODE>
+__device__ __forceinline__ Four<BF16> load4(uint64_t row, int c, int n, int D) {
+    Four<BF16> r;
+    if constexpr (MODE == ONES) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            v[2 * i] = __uint_as_float(t.v[i] << 16);
-            v[2 * i + 1] = __uint_as_float(t.v[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < (BF16 ? 2 : 4); ++i) r.w[i] = 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) {
+                if (BF16)
+                    r.w[i / 2] |= (uint32_t) * (const global<uint16_t> *)(row + (c + i) * 2) << (16 * (i & 1));
+                else
+                    r.w[i] = *(const global<uint32_t> *)(row + (c + i) * 4);
+            }
+        return r;
     } else {
-        const Words4 t = *reinterpret_cast<const Words4 *>(reinterpret_cast<const float *>(row) + c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(t.v[i]);
-    }
-}
-template <bool BF16>
-__device__ __forceinline__ void store4(void *row, int c, const float *v) {
-    if constexpr (BF16) {
-        struct __attribute__((packed, aligned(2))) Two { uint32_t v[2]; };
-        *reinterpret_cast<Two *>(reinterpret_cast<uint16_t *>(row) + c) = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    } else {
-        *reinterpret_cast<Words4 *>(reinterpret_cast<float *>(row) + c) = {__float_as_uint(v[0]), __float_as_uint(v[1]),
-                                                                            __float_as_uint(v[2]), __float_as_uint(v[3])};
-    }
-}
-
-// A lane's four units of a row: first channels in v[0..3], second in v[4..7].
-template <bool BF16, bool INTER>
-__device__ __forceinline__ void load_units(const Params &p, const void *row, int u0, float *v) {
-    if (u0 + 4 <= p.pairs) {
-        if (INTER) {
-            float t[8];
-            load4<BF16>(row, 2 * u0, t);
-            load4<BF16>(row, 2 * u0 + 4, t + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = t[2 * i];
-                v[4 + i] = t[2 * i + 1];
+        // four that lie in the row, moved to their places; no branch, so that the loads of all
+        // heads are under way before the first is waited for
+        const int from = MODE == WHOLE || c <= D - 4 ? c : D - 4, k = c - from;
+        if constexpr (BF16) {
+            const u32x2_t t = *(const global<u32x2_t> *)(row + (uint32_t)from * 2);
+            if (MODE == WHOLE) {
+                r.w[0] = t.x, r.w[1] = t.y;
+            } else {
+                uint64_t x = (uint64_t)t.y << 32 | t.x;
+                x = n <= 0 ? 0 : (x >> (16 * (k & 3))) & (~(uint64_t)0 >> (64 - 16 * n));
+                r.w[0] = (uint32_t)x, r.w[1] = (uint32_t)(x >> 32);
             }
         } else {
-            load4<BF16>(row, u0, v);
-            load4<BF16>(row, u0 + p.pairs, v + 4);
-        }
-    } else {
+            u32x4_t t = *(const global<u32x4_t> *)(row + (uint32_t)from * 4);
+            if (MODE == TAILS) {
+                if (k & 1) t = u32x4_t{t.y, t.z, t.w, 0};
+                if (k & 2) t = u32x4_t{t.z, t.w, 0, 0};
+            }
+            r.w[0] = t.x, r.w[1] = t.y, r.w[2] = t.z, r.w[3] = t.w;
+            if (MODE == TAILS)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            int a, b;
-            channels<INTER>(p, u0 + i, a, b);
-            v[i] = load1<BF16>(row, a);
-            v[4 + i] = load1<BF16>(row, b);
+                for (int i = 0; i < 4; ++i)
+                    if (i >= n) r.w[i] = 0;
         }
+        return r;
     }
 }
-template <bool BF16, bool INTER>
-__device__ __forceinline__ void store_units(const Params &p, void *row, int u0, const float *v) {
-    if (u0 + 4 <= p.pairs) {
-        if (INTER) {
-            const float t[8] = {v[0], v[4], v[1], v[5], v[2], v[6], v[3], v[7]};
-            store4<BF16>(row, 2 * u0, t);
-            store4<BF16>(row, 2 * u0 + 4, t + 4);
-        } else {
-            store4<BF16>(row, u0, v);
-            store4<BF16>(row, u0 + p.pairs, v + 4);
-        }
+template <bool BF16>
+__device__ __forceinline__ void widen(const Four<BF16> &r, float *v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = __uint_as_float(!BF16 ? r.w[BF16 ? 0 : i] : (i & 1) ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
+}
+template <bool BF16, Mode MODE>
+__device__ __forceinline__ void store4(uint64_t row, int c, int n, const float *v) {
+    if (MODE == WHOLE || (MODE == TAILS && n == 4)) {
+        if constexpr (BF16)
+            *(global<u32x2_t> *)(row + (uint32_t)c * 2) = u32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        else
+            *(global<u32x4_t> *)(row + (uint32_t)c * 4) = u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]),
+                                                                  __float_as_uint(v[2]), __float_as_uint(v[3])};
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            int a, b;
-            channels<INTER>(p, u0 + i, a, b);
-            store1<BF16>(row, a, v[i]);
-            store1<BF16>(row, b, v[4 + i]);
-        }
+        for (int i = 0; i < 3; ++i)
+            if (i < n) {
+                if (BF16)
+                    *(global<uint16_t> *)(row + (uint32_t)(c + i) * 2) = (uint16_t)pack_bf16(v[i], 0.f);
+                else
+                    *(global<float> *)(row + (uint32_t)(c + i) * 4) = v[i];
+            }
     }
 }
 
+// What a lane has of a row: n[0] channels from c[0] and n[1] from c[1] on, up to 4
+// each.  Lanes with pairs come first (four pairs each), then those with channels
+// that stay.
+struct Share {
+    int c[2], n[2];
+    int pair0, pairs;
+};
+template <bool INTER>
+__device__ __forceinline__ Share share_of(const Params &p, int lane) {
+    const int turning = (p.pairs + 3) / 4;
+    Share s;
+    int left[2];
+    if (lane < turning) {
+        s.pair0 = 4 * lane;
+        s.pairs = p.pairs - s.pair0 < 4 ? p.pairs - s.pair0 : 4;
+        s.c[0] = INTER ? 2 * s.pair0 : s.pair0;
+        s.c[1] = INTER ? 2 * s.pair0 + 4 : s.pair0 + p.pairs;
+        left[0] = INTER ? 2 * s.pairs : s.pairs;
+        left[1] = INTER ? 2 * s.pairs - 4 : s.pairs;
+    } else {
+        s.pair0 = s.pairs = 0;
+        s.c[0] = 2 * p.pairs + 8 * (lane - turning);
+        s.c[1] = s.c[0] + 4;
+        left[0] = p.D - s.c[0];
+        left[1] = p.D - s.c[1];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) s.n[i] = left[i] < 0 ? 0 : left[i] > 4 ? 4 : left[i];
+    return s;
+}
+
+// Turn the pairs of x by the angles, or back.
+template <bool INTER, bool BACK>
+__device__ __forceinline__ void turn(const float (&x)[8], const float (&cs)[4], const float (&sn)[4], float (&y)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int a = INTER ? 2 * i : i, b = INTER ? 2 * i + 1 : 4 + i;
+        const float s = BACK ? -sn[i] : sn[i];
+        y[a] = x[a] * cs[i] - x[b] * s;
+        y[b] = x[b] * cs[i] + x[a] * s;
+    }
+}
+
+// Sum over the G lanes of a group, the same in each: lanes 1, 2 away, then mirrored
+// in 8 and 16, then 16 and 32 away.  Moves between lanes of a row of 16 are part of
+// the addition; through LDS (shuffles) a sum took 8 round trips of it.
+template <int CTRL>
+__device__ __forceinline__ float plus_moved(float x) {
+    return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
 template <int G>
 __device__ __forceinline__ float group_sum(float x) {
-#pragma unroll
-    for (int d = 1; d < G; d *= 2) x += __shfl_xor(x, d);
+    x = plus_moved<0xb1>(x);   // quad_perm 1 0 3 2
+    x = plus_moved<0x4e>(x);   // quad_perm 2 3 0 1
+    if (G > 4) x = plus_moved<0x141>(x);   // row_half_mirror
+    if (G > 8) x = plus_moved<0x140>(x);   // row_mirror
+    if (G > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (G > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
     return x;
+}
+
+// 1 / sqrt(x): the hardware's, which is off by a unit in the last place and takes no
+// subnormal x, and a Newton step; infinity for 0 and 0 for infinity, as they come.
+__device__ __forceinline__ float inverse_root(float x) {
+    const bool small = x < 1e-30f;
+    const float y = small ? x * 1.2676506e30f : x;  // 2^100
+    const float r = __builtin_amdgcn_rsqf(y), e = fmaf(-y * r, r, 1.f);
+    const float z = e == e ? fmaf(0.5f * r, e, r) : r;
+    return small ? z * 1.1258999e15f : z;           // 2^50
+}
+
+// Sine and cosine of `turns` whole turns: the part of a turn (exact in 64 bits),
+// its nearest quarter, and in the eighth of a turn about that the Taylor series
+// about 0, whose first terms left out are below 2^-27.
+__device__ __forceinline__ void sin_cos(double turns, float &sn, float &cs) {
+    const float t = (float)(turns - rint(turns));
+    const float quarter = rintf(4.f * t), y = fmaf(quarter, -0.25f, t) * 6.283185307179586f, z = y * y;
+    const float s = y * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -0.16666667f), 1.f);
+    const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
+    const int q = (int)quarter;
+    const float a = q & 1 ? c : s, b = q & 1 ? s : c;
+    sn = q & 2 ? -a : a;
+    cs = (q + 1) & 2 ? -b : b;
+    if (t != t) sn = cs = t;
 }
 
 constexpr int kThreads = 256;
 constexpr double kTurns = 0.15915494309189535;  // 1 / (2 pi)
 
-template <bool BF16, bool INTER, int G, bool BACKWARD>
-__global__ __launch_bounds__(kThreads) void k_rotate(Params p) {
+template <bool BF16, bool INTER, int G, Mode MODE, bool BACKWARD>
+__global__ __launch_bounds__(kThreads, 4) void k_rotate(Params p) {
     constexpr int E = BF16 ? 2 : 4, GROUPS = kThreads / G;
-    const int lane = threadIdx.x % G, group = threadIdx.x / G, u0 = 4 * lane;
-    // this lane's units: what they turn with
-    double turns[4];
-    int axis[4];
+    // what a lane's pairs turn with, and the gains of its channels in the order of its
+    // values (registers are few)
+    __shared__ double turns[4 * G];
+    __shared__ int axes[4 * G];
+    __shared__ __attribute__((aligned(16))) float gains[2][8 * G];
+    const int lane = threadIdx.x % G, group = threadIdx.x / G;
+    const Share own = share_of<INTER>(p, lane);
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t item = (int64_t)blockIdx.x * GROUPS + group;
+
+    // U heads' values at a time, so that enough loads are under way
+    constexpr int U = BACKWARD ? 2 : 4;
+    Four<BF16> xs[U][2], gs[BACKWARD ? U : 1][2];
+    auto fetch = [&](int s, int64_t row, int h) {
+        const Side &d = p.side[s];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int u = u0 + i;
-        turns[i] = u < p.pairs ? (double)p.freq[u] * kTurns : 0.0;
-        axis[i] = 0;
-        for (int j = 0; j + 1 < p.axes; ++j)
-            if (u < p.pairs && u >= p.end[j]) axis[i] = j + 1;
+        for (int k = 0; k < U; ++k) {
+            const int at = h + k * p.share < d.heads ? h + k * p.share : h;
+            const uint64_t xr = address(d.x, (row * d.x_row + at * d.x_head) * E);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) xs[k][i] = load4<BF16, MODE>(xr, own.c[i], own.n[i], p.D);
+            if (BACKWARD) {
+                const uint64_t gr = address(d.g, (row * d.g_row + at * d.g_head) * E);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) gs[k][i] = load4<BF16, MODE>(gr, own.c[i], own.n[i], p.D);
+            }
+        }
+    };
+
+    if (group == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int pair = own.pair0 + i;
+            int axis = 0;
+            for (int j = 0; j + 1 < p.axes; ++j)
+                if (i < own.pairs && pair >= p.end[j]) axis = j + 1;
+            turns[4 * lane + i] = i < own.pairs ? (double)p.freq[pair] * kTurns : 0.0;
+            axes[4 * lane + i] = axis;
+        }
+    if (group < 2) {
+        const float *gain = p.side[group].gain;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            gains[group][8 * lane + i] = gain && (i & 3) < own.n[i / 4] ? gain[own.c[i / 4] + (i & 3)] : 1.f;
     }
-    float gain[2][8], sums[2][8];
+    __syncthreads();
+    float sums[2][8];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            int a, b;
-            channels<INTER>(p, u0 + i, a, b);
-            gain[s][i] = p.side[s].gain && a >= 0 ? p.side[s].gain[a] : 1.f;
-            gain[s][4 + i] = p.side[s].gain && b >= 0 ? p.side[s].gain[b] : 1.f;
-            sums[s][i] = sums[s][4 + i] = 0.f;
-        }
-    for (int64_t item = (int64_t)blockIdx.x * GROUPS + group; item < p.items; item += (int64_t)gridDim.x * GROUPS) {
-        const int64_t row = p.share == 1 ? item : item / p.share;
-        const int mine = (int)(item - row * p.share);
+        for (int i = 0; i < 8; ++i) sums[s][i] = 0.f;
+    const float of_all = 1.f / (float)p.D;
+    for (; item < p.items; item += step) {
+        const int64_t row = item >> p.log_share;
+        const int mine = (int)item & (p.share - 1);
+        fetch(0, row, mine);  // every share has one of the queries' heads
         float cs[4], sn[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t at = row * p.pos_stride + axis[i];
-            const double x = p.integers ? (double)reinterpret_cast<const int32_t *>(p.pos)[at]
-                                        : (double)reinterpret_cast<const float *>(p.pos)[at];
-            const double t = x * turns[i];
-            sincospif((float)(2.0 * (t - rint(t))), &sn[i], &cs[i]);
-            if (u0 + i >= p.pairs) {  // also where the position is no number
-                cs[i] = 1.f;
-                sn[i] = 0.f;
+            cs[i] = 1.f;
+            sn[i] = 0.f;
+            if (i < own.pairs) {
+                const int64_t at = row * p.pos_stride + axes[4 * lane + i];
+                const double x = p.integers ? (double)reinterpret_cast<const int32_t *>(p.pos)[at]
+                                            : (double)reinterpret_cast<const float *>(p.pos)[at];
+                sin_cos(x * turns[4 * lane + i], sn[i], cs[i]);
             }
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const Side &d = p.side[s];
-            for (int h = mine; h < d.heads; h += p.share) {
-                const char *xr = reinterpret_cast<const char *>(d.x) + (row * d.x_row + h * d.x_head) * E;
-                float x[8], y[8];
-                load_units<BF16, INTER>(p, xr, u0, x);
-                if (!BACKWARD) {
-                    float r = 1.f;
-                    if (p.norm) {
-                        float ss = 0.f;
+#pragma unroll 1
+            for (int h0 = mine; h0 < d.heads; h0 += U * p.share) {
+                if (s > 0 || h0 > mine) fetch(s, row, h0);
+                float gain[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 t = *reinterpret_cast<const float4 *>(&gains[s][8 * lane + i]);
+                    gain[i] = t.x, gain[i + 1] = t.y, gain[i + 2] = t.z, gain[i + 3] = t.w;
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int h = h0 + k * p.share;
+                    if (h >= d.heads) break;
+                    float x[8], y[8];
+                    widen<BF16>(xs[k][0], x);
+                    widen<BF16>(xs[k][1], x + 4);
+                    if (!BACKWARD) {
+                        float ss = 0.f, w[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-                        r = 1.f / sqrtf(group_sum<G>(ss) / (float)p.D + p.eps);
-                    }
+                        const float r = p.norm ? inverse_root(group_sum<G>(ss) * of_all + p.eps) : 1.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float a = x[i] * r * gain[s][i], b = x[4 + i] * r * gain[s][4 + i];
-                        y[i] = a * cs[i] - b * sn[i];
-                        y[4 + i] = b * cs[i] + a * sn[i];
-                    }
-                } else {
-                    float g[8], u[8];
-                    load_units<BF16, INTER>(p, reinterpret_cast<const char *>(d.g) + (row * d.g_row + h * d.g_head) * E, u0,
-                                            g);
-                    float ss = 0.f, vx = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        u[i] = g[i] * cs[i] + g[4 + i] * sn[i];
-                        u[4 + i] = g[4 + i] * cs[i] - g[i] * sn[i];
-                    }
-                    if (p.norm) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            ss = fmaf(x[i], x[i], ss);
-                            vx = fmaf(u[i] * gain[s][i], x[i], vx);
-                        }
-                        ss = group_sum<G>(ss);
-                        vx = group_sum<G>(vx);
-                        const float r = 1.f / sqrtf(ss / (float)p.D + p.eps), m = vx * r / (float)p.D;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float n = x[i] * r;
-                            y[i] = r * (u[i] * gain[s][i] - n * m);
-                            sums[s][i] = fmaf(u[i], n, sums[s][i]);
-                        }
+                        for (int i = 0; i < 8; ++i) w[i] = x[i] * r * gain[i];
+                        turn<INTER, false>(w, cs, sn, y);
                     } else {
+                        float g[8], u[8];
+                        widen<BF16>(gs[k][0], g);
+                        widen<BF16>(gs[k][1], g + 4);
+                        turn<INTER, true>(g, cs, sn, u);
+                        if (p.norm) {
+                            float ss = 0.f, vx = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = u[i];
+                            for (int i = 0; i < 8; ++i) {
+                                ss = fmaf(x[i], x[i], ss);
+                                vx = fmaf(u[i] * gain[i], x[i], vx);
+                            }
+                            ss = group_sum<G>(ss);
+                            vx = group_sum<G>(vx);
+                            const float r = inverse_root(ss * of_all + p.eps), m = vx * r * of_all;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float n = x[i] * r;
+                                y[i] = r * (u[i] * gain[i] - n * m);
+                                sums[s][i] = fmaf(u[i], n, sums[s][i]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) y[i] = u[i];
+                        }
                     }
+                    const uint64_t to = address(d.out, (row * d.out_row + h * d.out_head) * E);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) store4<BF16, MODE>(to, own.c[i], own.n[i], y + 4 * i);
                 }
-                store_units<BF16, INTER>(p, reinterpret_cast<char *>(d.out) + (row * d.out_row + h * d.out_head) * E, u0, y);
             }
         }
     }
@@ -269,18 +380,20 @@ __global__ __launch_bounds__(kThreads) void k_rotate(Params p) {
         __syncthreads();
         for (int id = threadIdx.x; id < 2 * 8 * G; id += kThreads) {
             const int s = id / (8 * G), at = id % (8 * G), i = at & 7;
-            int c[2];
-            channels<INTER>(p, 4 * (at >> 3) + (i & 3), c[0], c[1]);
-            const int to = i < 4 ? c[0] : c[1];
-            if (to < 0 || !p.side[s].part) continue;
+            const Share of = share_of<INTER>(p, at >> 3);
+            if ((i & 3) >= of.n[i / 4] || !p.side[s].part) continue;
             float x = 0.f;
             for (int g = 0; g < GROUPS; ++g) x += all[s][g][at];
-            p.side[s].part[(int64_t)blockIdx.x * p.D + to] = x;
+            p.side[s].part[(int64_t)blockIdx.x * p.D + of.c[i / 4] + (i & 3)] = x;
         }
     }
 }
 
-int group_of(int D) { return D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32; }
+// Lanes of a head's row.
+int group_of(int D, int pairs) {
+    const int lanes = (pairs + 3) / 4 + (D - 2 * pairs + 7) / 8;
+    return lanes <= 4 ? 4 : lanes <= 8 ? 8 : lanes <= 16 ? 16 : lanes <= 32 ? 32 : 64;
+}
 
 Params params_of(const lattice_dense *D, const RotateArgs &a, bool backward, unsigned &grid) {
     Params p = {};
@@ -293,35 +406,53 @@ Params params_of(const lattice_dense *D, const RotateArgs &a, bool backward, uns
     p.integers = a.integers;
     p.axes = a.axes;
     for (int i = 0; i < a.axes; ++i) p.end[i] = p.pairs += a.sections[i];
-    p.units = p.pairs + (a.D - 2 * p.pairs + 1) / 2;
     p.freq = a.freq;
     p.norm = a.norm;
     p.eps = a.eps;
-    // groups share a row where the rows alone are few
-    const int groups = kThreads / group_of(a.D), heads = a.heads > a.kv_heads ? a.heads : a.kv_heads;
-    const int64_t enough = (int64_t)4 * D->cu_count * groups;
+    // Groups share a row, of which each makes the angles, where the rows alone are few
+    // for the 4 workgroups of a CU, but one row and head each; every share has a query.
+    const int groups = kThreads / group_of(a.D, p.pairs);
+    const int64_t resident = (int64_t)4 * D->cu_count * groups;
     p.share = 1;
-    while (p.share < heads && a.rows * p.share < enough) p.share *= 2;
+    while (2 * p.share <= a.heads && (a.rows * p.share < resident || (a.rows * p.share < 4 * resident && a.heads >= 8 * p.share)))
+        p.share = 1 << ++p.log_share;
     p.items = a.rows * p.share;
-    grid = grid_for(p.items, groups, D->cu_count, backward ? 4 : 8);
+    grid = grid_for(p.items, groups, D->cu_count, backward ? 4 : 1 << 16);
     return p;
 }
 
-template <bool BF16, bool INTER, bool BACKWARD>
+template <bool BF16, bool INTER, bool BACKWARD, Mode MODE>
 hipError_t launch_as(lattice_dense *D, const Params &p, unsigned grid) {
-    switch (group_of(p.D)) {
-        case 4: hipLaunchKernelGGL((k_rotate<BF16, INTER, 4, BACKWARD>), dim3(grid), dim3(kThreads), 0, D->stream, p); break;
-        case 8: hipLaunchKernelGGL((k_rotate<BF16, INTER, 8, BACKWARD>), dim3(grid), dim3(kThreads), 0, D->stream, p); break;
-        case 16: hipLaunchKernelGGL((k_rotate<BF16, INTER, 16, BACKWARD>), dim3(grid), dim3(kThreads), 0, D->stream, p); break;
-        default: hipLaunchKernelGGL((k_rotate<BF16, INTER, 32, BACKWARD>), dim3(grid), dim3(kThreads), 0, D->stream, p); break;
+    const int g = MODE == ONES ? 4 : group_of(p.D, p.pairs);  // a row of three has two lanes at most
+    const dim3 blocks(grid), threads(kThreads);
+    if (g == 4) {
+        hipLaunchKernelGGL((k_rotate<BF16, INTER, 4, MODE, BACKWARD>), blocks, threads, 0, D->stream, p);
+    } else if constexpr (MODE != ONES) {
+        if (g == 8)
+            hipLaunchKernelGGL((k_rotate<BF16, INTER, 8, MODE, BACKWARD>), blocks, threads, 0, D->stream, p);
+        else if (g == 16)
+            hipLaunchKernelGGL((k_rotate<BF16, INTER, 16, MODE, BACKWARD>), blocks, threads, 0, D->stream, p);
+        else if (g == 32)
+            hipLaunchKernelGGL((k_rotate<BF16, INTER, 32, MODE, BACKWARD>), blocks, threads, 0, D->stream, p);
+        else if constexpr (MODE == TAILS)
+            hipLaunchKernelGGL((k_rotate<BF16, INTER, 64, MODE, BACKWARD>), blocks, threads, 0, D->stream, p);
     }
     return hipGetLastError();
 }
 
+template <bool BF16, bool INTER, bool BACKWARD>
+hipError_t launch_mode(lattice_dense *D, const Params &p, unsigned grid) {
+    if (p.D < 4) return launch_as<BF16, INTER, BACKWARD, ONES>(D, p, grid);
+    // every lane of a group has eight values: no lane past them, no row's end inside
+    if (p.pairs % 4 == 0 && (p.D - 2 * p.pairs) % 8 == 0 && p.D == 8 * group_of(p.D, p.pairs))
+        return launch_as<BF16, INTER, BACKWARD, WHOLE>(D, p, grid);
+    return launch_as<BF16, INTER, BACKWARD, TAILS>(D, p, grid);
+}
+
 template <bool BACKWARD>
 hipError_t launch(lattice_dense *D, const RotateArgs &a, const Params &p, unsigned grid) {
-    if (a.bf16) return a.interleaved ? launch_as<true, true, BACKWARD>(D, p, grid) : launch_as<true, false, BACKWARD>(D, p, grid);
-    return a.interleaved ? launch_as<false, true, BACKWARD>(D, p, grid) : launch_as<false, false, BACKWARD>(D, p, grid);
+    if (a.bf16) return a.interleaved ? launch_mode<true, true, BACKWARD>(D, p, grid) : launch_mode<true, false, BACKWARD>(D, p, grid);
+    return a.interleaved ? launch_mode<false, true, BACKWARD>(D, p, grid) : launch_mode<false, false, BACKWARD>(D, p, grid);
 }
 
 }  // namespace
