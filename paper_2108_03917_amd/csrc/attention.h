@@ -53,6 +53,13 @@ struct Sequence {
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// The same for an address (otherwise each direct load becomes a loop over the lanes'
+// descriptors).
+__device__ __forceinline__ const char *uniform(const char *p) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return reinterpret_cast<const char *>((uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
 // Rows are cut into tiles of R that lie in one sequence each.  Sequence i of a
@@ -201,6 +208,21 @@ __device__ __forceinline__ void clear(f32x16_t &a) {
     for (int e = 0; e < 16; ++e) a[e] = 0.f;
 }
 
+// Order of what lies between two sched_barriers: AHEAD reads of LDS, then a product and
+// a read in turns (left alone, the compiler waits for each read before its product).
+template <int PRODUCTS, int READS, int AHEAD, int I = 0>
+__device__ __forceinline__ void read_ahead() {
+    if constexpr (I == 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD < READS ? AHEAD : READS, 0);
+    if constexpr (I < PRODUCTS) {
+        // as many a product as keep the distance
+        constexpr int PER = (READS + PRODUCTS - 1) / PRODUCTS, DONE = AHEAD + I * PER;
+        constexpr int r = DONE >= READS ? 0 : READS - DONE < PER ? READS - DONE : PER;
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+        read_ahead<PRODUCTS, READS, AHEAD, I + 1>();
+    }
+}
+
 // acc = (rows row0.. of the tile) (fragments b)^T.
 template <bool BF16, int DP>
 __device__ __forceinline__ void rows_times(const char *tile, int row0, const u32x4_t (&b)[Rows<BF16, DP>::STEPS],
@@ -302,28 +324,37 @@ struct Loader {
     const char *base;
     int64_t stride;  // bytes
     int D, wave;
+    uint32_t offset[DMA ? N : 1];  // of this lane's loads from the first row's start
     u32x4_t r[DMA ? 1 : N];
 
     __device__ __forceinline__ Loader(const View &x, int64_t row0, int head, int D, int wave)
         : base(reinterpret_cast<const char *>(x.p) + (row0 * x.row + head * x.head) * L::E), stride(x.row * L::E), D(D),
-          wave(wave) {}
+          wave(wave) {
+        if constexpr (DMA)
+#pragma unroll
+            for (int n = 0; n < N; ++n) offset[n] = offset_of(n, ROWS - 1);
+    }
+    __device__ __forceinline__ uint32_t offset_of(int n, int last) const {
+        const int id = (n * WAVES + wave) * 64 + (threadIdx.x & 63), row = id / L::CHUNKS, end = D * L::E / 16 - 1;
+        const int chunk = (id % L::CHUNKS) ^ L::key(row);
+        return (uint32_t)(row < last ? row : last) * (uint32_t)stride + (chunk < end ? chunk : end) * 16;
+    }
     // Rows first .. of which the tensor has `rows` (more than first).
     __device__ __forceinline__ void fetch(char *tile, int first, int rows) {
         if (ALL < WAVES && wave >= ALL) return;
-        const int lane = threadIdx.x & 63, last = rows - 1 - first;
+        const int last = rows - 1 - first;
         const char *from = base + first * stride;
         if constexpr (DMA) {
-            const gemm::rsrc_t src = gemm::buffer(from);
-            const int end = D * L::E / 16 - 1;
+            const gemm::rsrc_t src = gemm::buffer(uniform(from));
+            if (last >= ROWS - 1) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int id = (n * WAVES + wave) * 64 + lane, row = id / L::CHUNKS;
-                int chunk = (id % L::CHUNKS) ^ L::key(row);
-                chunk = chunk < end ? chunk : end;
-                gemm::dma16(src, (uint32_t)(row < last ? row : last) * (uint32_t)stride + chunk * 16, 0,
-                            tile + (n * WAVES + wave) * 1024);
+                for (int n = 0; n < N; ++n) gemm::dma16(src, offset[n], 0, tile + (n * WAVES + wave) * 1024);
+            } else {
+#pragma unroll
+                for (int n = 0; n < N; ++n) gemm::dma16(src, offset_of(n, last), 0, tile + (n * WAVES + wave) * 1024);
             }
         } else {
+            const int lane = threadIdx.x & 63;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int id = (n * WAVES + wave) * 64 + lane, row = id / L::CHUNKS;
@@ -346,6 +377,10 @@ struct Loader {
     }
 };
 
+// In a branch that few blocks take: keeps the compiler from making selects of it, which all
+// blocks would go through.
+__device__ __forceinline__ void seldom() { asm volatile(""); }
+
 // The maximum, or the sum, of a value and that of the lane 32 further (or before).
 __device__ __forceinline__ float pair_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -359,6 +394,14 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 
 // Row of an accumulator's value e in this lane.
 __device__ __forceinline__ int acc_row(int e) { return gemm::acc_row(e); }
+
+// Scores of keys from `seen` on (of the block from key0 on) count for nothing.
+__device__ __forceinline__ void mask(f32x16_t &s, int key0, int seen) {
+    const int n = seen - key0 - 4 * ((threadIdx.x & 63) >> 5);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (8 * (e >> 2) + (e & 3) >= n) s[e] = -INFINITY;
+}
 
 // Store 4 channels c0 .. of a row of D of them.
 template <bool BF16>

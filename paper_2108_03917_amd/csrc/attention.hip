@@ -120,14 +120,6 @@ __device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, floa
     }
 }
 
-// Scores of keys from `seen` on (of the block from key0 on) count for nothing.
-__device__ __forceinline__ void mask(f32x16_t &s, int key0, int seen) {
-    const int n = seen - key0 - 4 * ((threadIdx.x & 63) >> 5);
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-        if (8 * (e >> 2) + (e & 3) >= n) s[e] = -INFINITY;
-}
-
 // Write a column: 4 channels at a time, by f.
 template <bool BF16, int DP>
 __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t row, int head, Column<DP> &col) {
@@ -207,9 +199,10 @@ __global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(P
         lk.commit(lds);
         lv.commit(lds + HALF);
     }
-    int stage = 0;
-    for (int i = t.t0; i < t.t1; ++i) {
-        char *now = lds + stage * STAGE, *next = lds + (stage ^ 1) * STAGE;
+    // the stage is a constant, so that addresses in LDS are
+    // (and the two stages' addresses are told to be apart: reads of one need not wait for
+    // what is on its way to the other)
+    auto block = [&](int i, const char *__restrict now, char *__restrict next) {
         gemm::wait_and_barrier<0>();
         const bool more = i + 1 < t.t1;
         if (more) {
@@ -220,14 +213,19 @@ __global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(P
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 f32x16_t s[KB];
+                gemm::sched_barrier();
 #pragma unroll
                 for (int b = 0; b < KB; ++b) {
                     clear(s[b]);
                     rows_times<BF16, DP>(now, 32 * b, q[n], s[b]);
                 }
-                if ((i + 1) * KT > t.least)
+                if (BF16) read_ahead<KB * L::STEPS, KB * L::STEPS, 6>();
+                gemm::sched_barrier();
+                if ((i + 1) * KT > t.least) {
+                    seldom();
 #pragma unroll
                     for (int b = 0; b < KB; ++b) mask(s[b], i * KT + 32 * b, seen[n]);
+                }
                 Right<BF16> p[KB];
                 softmax<BF16, DP, KB>(s, col[n], a.c, p);
 #pragma unroll
@@ -238,7 +236,10 @@ __global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(P
             lk.commit(next);
             lv.commit(next + HALF);
         }
-        stage ^= 1;
+    };
+    for (int i = t.t0; i < t.t1; i += 2) {
+        block(i, lds, lds + STAGE);
+        if (i + 1 < t.t1) block(i + 1, lds + STAGE, lds);
     }
 #pragma unroll
     for (int n = 0; n < NQ; ++n)  // a column's two lanes go the same way
@@ -302,7 +303,10 @@ __global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Par
         f32x16_t s[1];
         clear(s[0]);
         rows_times<BF16, DP>(now, 0, q, s[0]);
-        if ((i + 1) * KT > t.least) mask(s[0], i * KT, seen);
+        if ((i + 1) * KT > t.least) {
+            seldom();
+            mask(s[0], i * KT, seen);
+        }
         Right<BF16> p[1];
         softmax<BF16, DP, 1>(s, col, a.c, p);
         columns_times<BF16, DP>(now + HALF, 0, p[0], col.o);

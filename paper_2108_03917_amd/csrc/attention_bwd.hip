@@ -13,6 +13,8 @@
 //                keys are added here.
 // p and t are rounded to bf16 for the products with bf16 tensors (a relative 2^-9
 // of each term), all sums are fp32.
+#include <algorithm>
+
 #include "attention.h"
 
 namespace {
@@ -28,11 +30,58 @@ struct Params {
     int heads, kv_heads, D, group;
     int parts, tile_heads;    // by queries, as in the forward pass
     int units, R, slots, splits;
+    int64_t share;            // by keys: blocks of rows that make a part of a tile
     float c, scale;
     bool zero_rest;
     float *part;              // of the splits, without gaps, one after another
     int32_t *status;
 };
+
+// This lane's part of a row (see load_fragments) to its place in a tile.
+template <bool BF16, int DP>
+__device__ __forceinline__ void load_fragments_to(const View &x, int64_t row, int head, int D, char *tile) {
+    using L = Rows<BF16, DP>;
+    const int lane = threadIdx.x & 63;
+    u32x4_t f[L::STEPS];
+    load_fragments<BF16, DP>(x, row, head, D, f);
+#pragma unroll
+    for (int t = 0; t < L::STEPS; ++t)
+        *reinterpret_cast<u32x4_t *>(tile + L::at(lane & 31, 2 * t + (lane >> 5))) = f[t];
+}
+
+// acc = (32 rows of one tile) (32 rows of another)^T.
+template <bool BF16, int DP>
+__device__ __forceinline__ void rows_times_rows(const char *a, const char *b, f32x16_t &acc) {
+    using L = Rows<BF16, DP>;
+    const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int t = 0; t < L::STEPS; ++t) {
+        const int at = L::at(row, 2 * t + h);
+        mma<BF16>(*reinterpret_cast<const u32x4_t *>(a + at), *reinterpret_cast<const u32x4_t *>(b + at), acc);
+    }
+}
+
+// Add the second group's sums to the first's, by way of LDS (4 wavefronts x 32 x DP).
+template <int DP>
+__device__ __forceinline__ void add_groups(char *lds, int wave, int group, f32x16_t (&x)[DP / 32]) {
+    float4 *room = reinterpret_cast<float4 *>(lds + wave * 32 * DP * 4) + (threadIdx.x & 63);
+    __syncthreads();
+    if (group == 1)
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                room[(4 * d + g) * 64] = make_float4(x[d][4 * g], x[d][4 * g + 1], x[d][4 * g + 2], x[d][4 * g + 3]);
+    __syncthreads();
+    if (group == 0)
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 t = room[(4 * d + g) * 64];
+                x[d][4 * g] += t.x, x[d][4 * g + 1] += t.y, x[d][4 * g + 2] += t.z, x[d][4 * g + 3] += t.w;
+            }
+}
 
 template <bool BF16>
 __device__ __forceinline__ float dot(const u32x4_t &a, const u32x4_t &b) {
@@ -71,9 +120,12 @@ __device__ __forceinline__ void store_column(void *out, float *part, int64_t at,
         }
 }
 
+// Bytes of parts that tiles by keys may be cut into: beyond it there are tiles enough.
+constexpr int64_t kMostParts = (int64_t)1 << 29;
+
 // By queries: 4 wavefronts of 32 columns.
 template <bool BF16, int DP, bool DMA>
-__global__ __launch_bounds__(256) void k_by_queries(Params a) {
+__global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Params a) {
     using L = Rows<BF16, DP>;
     constexpr int KT = 32, HALF = KT * L::BYTES, STAGE = 2 * HALF;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -135,9 +187,7 @@ __global__ __launch_bounds__(256) void k_by_queries(Params a) {
         lk.commit(lds);
         lv.commit(lds + HALF);
     }
-    int stage = 0;
-    for (int i = t0; i < t1; ++i) {
-        char *now = lds + stage * STAGE, *next = lds + (stage ^ 1) * STAGE;
+    auto block = [&](int i, const char *__restrict now, char *__restrict next) {
         gemm::wait_and_barrier<0>();
         const bool more = i + 1 < t1;
         if (more) {
@@ -146,16 +196,19 @@ __global__ __launch_bounds__(256) void k_by_queries(Params a) {
         }
         if (i * KT < wave_most) {
             f32x16_t x, y;
+            gemm::sched_barrier();
             clear(x);
             clear(y);
             rows_times<BF16, DP>(now, 0, q, x);
             rows_times<BF16, DP>(now + HALF, 0, g, y);
-            const int left_keys = (i + 1) * KT > least ? seen - i * KT - 4 * (lane >> 5) : KT;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float p = 8 * (e >> 2) + (e & 3) < left_keys ? exp2_(fmaf(x[e], a.c, -lse2)) : 0.f;
-                x[e] = p * (y[e] - delta);
+            if (BF16) read_ahead<2 * L::STEPS, 2 * L::STEPS, 6>();
+            gemm::sched_barrier();
+            if ((i + 1) * KT > least) {
+                seldom();
+                mask(x, i * KT, seen);
             }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = exp2_(fmaf(x[e], a.c, -lse2)) * (y[e] - delta);
             Right<BF16> t;
             t.set(x);
             columns_times<BF16, DP>(now, 0, t, dq);
@@ -164,24 +217,61 @@ __global__ __launch_bounds__(256) void k_by_queries(Params a) {
             lk.commit(next);
             lv.commit(next + HALF);
         }
-        stage ^= 1;
+    };
+    for (int i = t0; i < t1; i += 2) {
+        block(i, lds, lds + STAGE);
+        if (i + 1 < t1) block(i + 1, lds + STAGE, lds);
     }
     if (mine) store_column<BF16, DP>(a.dq, mine_part, row * a.heads + head, a.D, dq, a.scale);
 }
 
-// By keys: 4 wavefronts of 32 keys.
+// By keys: 128 keys, 32 for each of 4 wavefronts, or of 4 of each of QW groups of
+// them that take the blocks of rows in turns and are added at the end.
+//
+// With K and V as right operands in registers and both results there, 128 channels take
+// 300 registers, one wavefront a SIMD, and nothing runs beside its exponentials and
+// waits (283 TFLOP/s); V is read from LDS instead (KV_LDS), which leaves room for two.
+template <bool BF16, int DP>
+struct ByKeys {
+    static constexpr bool KV_LDS = BF16 && DP == 128;
+    static constexpr int QW = BF16 ? 2 : 1;
+    static constexpr int WAVES = 4 * QW, THREADS = 64 * WAVES;
+    static constexpr int HALF = 32 * Rows<BF16, DP>::BYTES, STAGE = 2 * HALF;   // of a group
+    static constexpr int KV_BYTES = KV_LDS ? 8 * HALF : 0;
+    static constexpr int LDS = 2 * QW * STAGE + KV_BYTES;
+    // a group's result in LDS: 4 wavefronts of 32 x DP
+    static_assert(QW == 1 || 4 * 32 * DP * 4 <= 2 * QW * STAGE, "LDS");
+};
+
+// Parts that a tile with this many blocks is cut into.
+__device__ __forceinline__ int parts_of(const Params &a, int64_t blocks) {
+    const int64_t n = (blocks + a.share - 1) / a.share;
+    return (int)(n < 1 ? 1 : n < a.splits ? n : a.splits);
+}
+// Where the rows begin that see a tile of keys from `first` on.
+constexpr int kRowBlock = 32;
+__device__ __forceinline__ int first_row(const Params &a, const Sequence &s, int first) {
+    const int r = a.pack.causal ? first + s.q_len - s.keys : 0;
+    return (r < 0 ? 0 : r) / kRowBlock * kRowBlock;
+}
+__device__ __forceinline__ int row_blocks(const Params &a, const Sequence &s, int first) {
+    const int r = first_row(a, s, first);
+    return r < s.q_len ? (s.q_len - r + kRowBlock - 1) / kRowBlock : 0;
+}
+
 template <bool BF16, int DP, bool DMA>
-__global__ __launch_bounds__(256) void k_by_keys(Params a) {
+__global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_by_keys(Params a) {
     using L = Rows<BF16, DP>;
-    constexpr int QT = 32, HALF = QT * L::BYTES, STAGE = 2 * HALF;
+    using B = ByKeys<BF16, DP>;
+    constexpr int QT = kRowBlock, QW = B::QW;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][QT];  // lse (of 2) and delta of the block's rows
+    __shared__ __attribute__((aligned(16))) float stats[2][QW][2][QT];  // lse (of 2) and delta of the blocks' rows
     int kv_head, slot, first;
     if (!unit_of(blockIdx.x, a.kv_heads, a.slots, false, kv_head, slot)) return;
     const Sequence s = locate(a.pack, a.R, slot, true, first, a.status);
     if (first >= s.kv_len) return;
     const int split = blockIdx.y;
-    const int lane = threadIdx.x & 63, wave = gemm::wave_index(), h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = gemm::wave_index() & 3, group = gemm::wave_index() >> 2, h = lane >> 5;
     const int64_t size = a.pack.kv_rows * a.kv_heads * a.D;
     const int key = first + wave * 32 + (lane & 31);
     // rows that no key of the tile counts in
@@ -190,45 +280,55 @@ __global__ __launch_bounds__(256) void k_by_keys(Params a) {
         if (a.zero_rest && split == 0)
             for (int j = first; j < end; ++j) {
                 const int64_t at = ((s.k0 + j) * a.kv_heads + kv_head) * a.D * L::E;
-                zero_row<BF16>(reinterpret_cast<char *>(a.dk) + at, a.D, threadIdx.x, 256);
-                zero_row<BF16>(reinterpret_cast<char *>(a.dv) + at, a.D, threadIdx.x, 256);
+                zero_row<BF16>(reinterpret_cast<char *>(a.dk) + at, a.D, threadIdx.x, B::THREADS);
+                zero_row<BF16>(reinterpret_cast<char *>(a.dv) + at, a.D, threadIdx.x, B::THREADS);
             }
         return;
     }
+    // blocks of rows: those of each query head, one head after another
+    const int r0 = first_row(a, s, first), per = row_blocks(a, s, first);
+    const int64_t blocks = (int64_t)per * a.group;
+    const int parts = parts_of(a, blocks);
+    if (split >= parts) return;
+    const int64_t begin = blocks * split / parts, end = blocks * (split + 1) / parts;
+
     const bool counts = key < s.keys;
     const int64_t row = s.k0 + (counts ? key : s.keys - 1);
-    u32x4_t k[L::STEPS], v[L::STEPS];
-    load_fragments<BF16, DP>(a.k, row, kv_head, a.D, k);
-    load_fragments<BF16, DP>(a.v, row, kv_head, a.D, v);
+    u32x4_t k[B::KV_LDS ? 1 : L::STEPS], v[B::KV_LDS ? 1 : L::STEPS];
+    char *k_tile = lds + 2 * QW * B::STAGE + 2 * wave * B::HALF, *v_tile = k_tile + B::HALF;
+    if constexpr (B::KV_LDS) {
+        if (group == 0)
+            load_fragments_to<BF16, DP>(a.k, row, kv_head, a.D, k_tile);
+        else
+            load_fragments_to<BF16, DP>(a.v, row, kv_head, a.D, v_tile);
+    } else {
+        load_fragments<BF16, DP>(a.k, row, kv_head, a.D, k);
+        load_fragments<BF16, DP>(a.v, row, kv_head, a.D, v);
+    }
     f32x16_t dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
         clear(dk[d]);
         clear(dv[d]);
     }
-    // rows from r0 on see the tile's first key; this lane's key is seen from `from` on
-    const int shift = a.pack.causal ? s.q_len - s.keys : -(1 << 30);
-    int r0 = a.pack.causal ? first + shift : 0;
-    r0 = (r0 < 0 ? 0 : r0) / QT * QT;
+    // this lane's key is seen from row `from` on, all keys of the tile from `all_see` on
+    const int shift = a.pack.causal ? s.q_len - s.keys : 0;
     const int from = !counts ? 0x7fffffff : a.pack.causal ? key + shift : 0;
-    const int per = r0 < s.q_len ? (s.q_len - r0 + QT - 1) / QT : 0;  // blocks of a head
-    // rows that see all keys of the tile
     const int all_see = first + a.R <= s.keys ? (a.pack.causal ? first + a.R - 1 + shift : 0) : 0x7fffffff;
-    const int64_t blocks = (int64_t)per * a.group;
-    int64_t i = blocks * split / a.splits;
-    const int64_t end = blocks * (split + 1) / a.splits;
-    int head = per > 0 ? (int)(i / per) : 0, at = per > 0 ? (int)(i % per) : 0;
 
-    float stat = 0.f;  // lanes 0 .. 31 of the first wavefront: lse, the others delta
+    int64_t i = begin + group;
+    int head = per > 0 ? (int)(i / per) : 0, at = per > 0 ? (int)(i % per) : 0;
+    float stat = 0.f;  // lanes 0 .. 31 of a group's first wavefront: lse, the others delta
     Loader<BF16, DP, QT, 4, DMA> lq(a.q, s.q0, kv_head * a.group, a.D, wave), lg(a.g, s.q0, kv_head * a.group, a.D, wave);
     const int64_t q_step = a.q.head * L::E, g_step = a.g.head * L::E;
     const char *q_base = lq.base, *g_base = lg.base;
+    char *own = lds + group * 2 * B::STAGE;
     auto fetch = [&](char *to, int head, int at) {
         lq.base = q_base + head * q_step;
         lg.base = g_base + head * g_step;
         const int r = r0 + at * QT;
         lq.fetch(to, r, s.q_len);
-        lg.fetch(to + HALF, r, s.q_len);
+        lg.fetch(to + B::HALF, r, s.q_len);
         if (wave == 0) {
             const int rr = r + (lane & 31);
             const int64_t where = (kv_head * a.group + head) * a.pack.q_rows + s.q0 + (rr < s.q_len ? rr : s.q_len - 1);
@@ -238,54 +338,77 @@ __global__ __launch_bounds__(256) void k_by_keys(Params a) {
     };
     auto commit = [&](char *to, int stage) {
         lq.commit(to);
-        lg.commit(to + HALF);
-        if (wave == 0) stats[stage][h][lane & 31] = stat;
+        lg.commit(to + B::HALF);
+        if (wave == 0) stats[stage][group][h][lane & 31] = stat;
     };
     if (i < end) {
-        fetch(lds, head, at);
-        commit(lds, 0);
+        fetch(own, head, at);
+        commit(own, 0);
     }
-    int stage = 0;
-    for (; i < end; ++i) {
-        char *now = lds + stage * STAGE, *next = lds + (stage ^ 1) * STAGE;
+    auto block = [&](const char *__restrict now, char *__restrict next, auto stage) {
         gemm::wait_and_barrier<0>();
+        const bool here = i < end, more = i + QW < end;
         const int r = r0 + at * QT;
-        if (++at == per) {
-            at = 0;
+        i += QW;
+        at += QW;
+        while (at >= per) {
+            at -= per;
             ++head;
         }
-        const bool more = i + 1 < end;
         if (more) fetch(next, head, at);
-        f32x16_t x, y;
-        clear(x);
-        clear(y);
-        rows_times<BF16, DP>(now, 0, k, x);
-        rows_times<BF16, DP>(now + HALF, 0, v, y);
-        const int hidden = r >= all_see ? -1 : from - r - 4 * h;  // rows before it do not see this lane's key
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const float4 l = *reinterpret_cast<const float4 *>(&stats[stage][0][8 * b + 4 * h]);
-            const float4 d = *reinterpret_cast<const float4 *>(&stats[stage][1][8 * b + 4 * h]);
-            const float ls[4] = {l.x, l.y, l.z, l.w}, ds[4] = {d.x, d.y, d.z, d.w};
-#pragma unroll
-            for (int k4 = 0; k4 < 4; ++k4) {
-                const int e = 4 * b + k4;
-                const float p = 8 * b + k4 >= hidden ? exp2_(fmaf(x[e], a.c, -ls[k4])) : 0.f;
-                x[e] = p;
-                y[e] = p * (y[e] - ds[k4]);
+        if (here) {
+            f32x16_t x, y;
+            gemm::sched_barrier();
+            clear(x);
+            clear(y);
+            if constexpr (B::KV_LDS) {
+                rows_times_rows<BF16, DP>(now, k_tile, x);
+                rows_times_rows<BF16, DP>(now + B::HALF, v_tile, y);
+            } else {
+                rows_times<BF16, DP>(now, 0, k, x);
+                rows_times<BF16, DP>(now + B::HALF, 0, v, y);
             }
+            if (BF16) read_ahead<2 * L::STEPS, (B::KV_LDS ? 4 : 2) * L::STEPS, 8>();
+            gemm::sched_barrier();
+            if (r < all_see) {
+                seldom();
+                const int hidden = from - r - 4 * h;  // rows before it do not see this lane's key
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e >> 2) + (e & 3) < hidden) x[e] = -INFINITY;
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const float4 l = *reinterpret_cast<const float4 *>(&stats[stage.value][group][0][8 * b + 4 * h]);
+                const float4 d = *reinterpret_cast<const float4 *>(&stats[stage.value][group][1][8 * b + 4 * h]);
+                const float ls[4] = {l.x, l.y, l.z, l.w}, ds[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    const int e = 4 * b + k4;
+                    x[e] = exp2_(fmaf(x[e], a.c, -ls[k4]));
+                    y[e] = x[e] * (y[e] - ds[k4]);
+                }
+            }
+            Right<BF16> p;
+            p.set(x);
+            columns_times<BF16, DP>(now + B::HALF, 0, p, dv);
+            p.set(y);
+            columns_times<BF16, DP>(now, 0, p, dk);
         }
-        Right<BF16> p;
-        p.set(x);
-        columns_times<BF16, DP>(now + HALF, 0, p, dv);
-        p.set(y);
-        columns_times<BF16, DP>(now, 0, p, dk);
-        if (more) commit(next, stage ^ 1);
-        stage ^= 1;
+        if (more) commit(next, 1 - stage.value);
+    };
+    for (int64_t turn = begin; turn < end; turn += 2 * QW) {
+        block(own, own + B::STAGE, std::integral_constant<int, 0>{});
+        if (turn + QW < end) block(own + B::STAGE, own, std::integral_constant<int, 1>{});
+    }
+    if constexpr (QW == 2) {
+        add_groups<DP>(lds, wave, group, dk);
+        add_groups<DP>(lds, wave, group, dv);
+        if (group > 0) return;
     }
     const int64_t at_row = (s.k0 + key) * a.kv_heads + kv_head;
     if (counts) {
-        float *pk = a.splits > 1 ? a.part + split * 2 * size : nullptr, *pv = pk ? pk + size : nullptr;
+        float *pk = parts > 1 ? a.part + split * 2 * size : nullptr, *pv = pk ? pk + size : nullptr;
         store_column<BF16, DP>(a.dk, pk, at_row, a.D, dk, a.scale);
         store_column<BF16, DP>(a.dv, pv, at_row, a.D, dv, 1.f);
     } else if (a.zero_rest && split == 0 && key < s.kv_len && key < first + a.R) {
@@ -294,15 +417,25 @@ __global__ __launch_bounds__(256) void k_by_keys(Params a) {
     }
 }
 
-// Sums of the splits' values in their order, of kJoinRows rows a workgroup:
-// those of a sequence, or of its keys that count.
+// Sums of the splits' values in their order, of a.R (by keys: of a part of a tile's)
+// rows a workgroup: those of a sequence, or of its keys that count.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_join(Params a, bool by_keys) {
     int first;
-    const Sequence s = locate(a.pack, kJoinRows, blockIdx.x, by_keys, first, a.status);
+    const int R = by_keys ? a.R : kJoinRows;
+    const Sequence s = locate(a.pack, R, blockIdx.x, by_keys, first, a.status);
     const int all = by_keys ? s.keys : s.q_len;
     if (!s.real || first >= all) return;
-    const int rows = all - first < kJoinRows ? all - first : kJoinRows;
+    int rows = all - first < R ? all - first : R;
+    int splits = a.splits;
+    if (by_keys) {
+        splits = parts_of(a, (int64_t)row_blocks(a, s, first) * a.group);
+        if (splits == 1) return;
+        const int skip = (int)blockIdx.z * kJoinRows;
+        if (skip >= rows) return;
+        first += skip;
+        rows = rows - skip < kJoinRows ? rows - skip : kJoinRows;
+    }
     const int64_t width = (int64_t)(by_keys ? a.kv_heads : a.heads) * a.D;
     const int64_t size = (by_keys ? a.pack.kv_rows : a.pack.q_rows) * width;
     const int64_t from = ((by_keys ? s.k0 : s.q0) + first) * width;
@@ -311,7 +444,7 @@ __global__ __launch_bounds__(256) void k_join(Params a, bool by_keys) {
     const int64_t step = (by_keys ? 2 : 1) * size;
     for (int64_t i = threadIdx.x; i < rows * width; i += 256) {
         float x = 0.f;
-        for (int n = 0; n < a.splits; ++n) x += part[n * step + i];
+        for (int n = 0; n < splits; ++n) x += part[n * step + i];
         if (BF16)
             reinterpret_cast<uint16_t *>(out)[from + i] = (uint16_t)pack_bf16(x, 0.f);
         else
@@ -371,11 +504,17 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     const int64_t slots = slots_of(starts, sequences, a.kv_rows, b.R), tiles = (a.kv_rows + b.R - 1) / b.R;
     b.slots = (int)slots;
     r.grid_keys = unit_grid(a.kv_heads, slots);
-    b.splits = splits_of(a.kv_heads * (tiles > sequences ? tiles : sequences), rows * p.group, 2 * D->cu_count, 256);
-    if (b.splits > 1) {
-        const int64_t n = (int64_t)b.splits * 2 * a.kv_rows * a.kv_heads * a.D;
-        r.part = r.part > n ? r.part : n;
-    }
+    // A tile's rows, all heads' of them, are cut into parts of about half of what a CU has to do
+    // in all if every sequence had the mean length; only tiles with more than one part are
+    // joined.  The longest sequence may have all the rows.
+    const int64_t each = (rows * p.group + kRowBlock - 1) / kRowBlock, most = (a.q_rows * p.group + kRowBlock - 1) / kRowBlock;
+    const int64_t all = a.kv_heads * (tiles > sequences ? tiles : sequences) * each;
+    b.share = all / (2 * D->cu_count);
+    b.share = b.share < 8 ? 8 : b.share;
+    const int64_t want = (most + b.share - 1) / b.share, part = (int64_t)2 * a.kv_rows * a.kv_heads * a.D;
+    const int64_t room = part > 0 ? kMostParts / (part * 4) : 1;
+    b.splits = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(want, 16), room));
+    if (b.splits > 1) r.part = std::max(r.part, b.splits * part);
     return r;
 }
 
@@ -390,10 +529,11 @@ hipError_t by_queries(lattice_dense *D, const Plan &r) {
 
 template <bool BF16, int DP, bool DMA>
 hipError_t by_keys(lattice_dense *D, const Plan &r) {
-    constexpr int LDS = 2 * 2 * 32 * Rows<BF16, DP>::BYTES;
+    using B = ByKeys<BF16, DP>;
+    constexpr int LDS = B::LDS;
     static std::atomic<uint64_t> done{0};
-    if (LDS + 1024 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_by_keys<BF16, DP, DMA>), LDS, done));
-    hipLaunchKernelGGL((k_by_keys<BF16, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.splits), dim3(256), LDS,
+    if (LDS + 2048 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_by_keys<BF16, DP, DMA>), LDS, done));
+    hipLaunchKernelGGL((k_by_keys<BF16, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.splits), dim3(B::THREADS), LDS,
                        D->stream, r.by_keys);
     return hipGetLastError();
 }
@@ -401,8 +541,8 @@ hipError_t by_keys(lattice_dense *D, const Plan &r) {
 template <bool BF16>
 hipError_t join(lattice_dense *D, const Params &p, bool keys) {
     if (p.splits == 1) return hipSuccess;
-    const int64_t n = slots_of(p.pack.q_starts, p.pack.sequences, keys ? p.pack.kv_rows : p.pack.q_rows, kJoinRows);
-    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)n, keys ? 2 : 1), dim3(256), 0, D->stream, p, keys);
+    const int64_t n = keys ? p.slots : slots_of(p.pack.q_starts, p.pack.sequences, p.pack.q_rows, kJoinRows);
+    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)n, keys ? 2 : 1, keys ? p.R / kJoinRows : 1), dim3(256), 0, D->stream, p, keys);
     return hipGetLastError();
 }
 
