@@ -28,7 +28,7 @@ using gemm::bf16x8_t;
 using gemm::f32x16_t;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kJoinRows = 16;  // of a workgroup that joins splits
+constexpr int kJoinRows = 4;  // of a workgroup that joins parts
 
 // A tensor [rows][heads][D]: values between rows and between heads.
 struct View {
@@ -165,6 +165,19 @@ __device__ __forceinline__ bool unit_of(int64_t b, int units, int n, bool later_
     }
     if (later_first) slot = n - 1 - slot;
     return slot >= 0 && slot < n && unit < units;
+}
+// A tile's blocks (of keys, or of rows) are cut into parts of about `share`, at most
+// `splits`, so that the longest sequences do not keep a few CUs busy after the
+// others are done.  A launch has `splits` workgroups (blockIdx.y) for each tile, of which
+// those past its parts end at once.  (Next to each other in blockIdx.x, those that end
+// left half of an XCD's shader engines, which are taken in turns, without work.)
+struct Cut {
+    int64_t share;
+    int splits;
+};
+__device__ __forceinline__ int parts_of(const Cut &c, int64_t blocks) {
+    const int64_t n = (blocks + c.share - 1) / c.share;
+    return (int)(n < 1 ? 1 : n < c.splits ? n : c.splits);
 }
 inline int64_t unit_grid(int units, int64_t n) {
     if (units % 8 && 8 % units == 0) return (n + 8 / units - 1) / (8 / units) * 8;
@@ -463,11 +476,27 @@ struct Columns {
 inline Packing packing_of(const AttendArgs &a) {
     return {a.q_rows, a.kv_rows, a.q_starts, a.kv_starts, a.kv_lengths, (int)a.sequences, a.causal};
 }
-// As many splits as give `want` workgroups, of `least` rows each at least.
-inline int splits_of(int64_t tiles, int64_t rows, int64_t want, int64_t least) {
-    int64_t n = want / (tiles > 0 ? tiles : 1);
-    n = n < rows / least ? n : rows / least;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+// How a launch of `grid` workgroups cuts its tiles: `tiles` of them have about `blocks`
+// blocks each, and none more than `most`.  A part is what each of `places` workgroups
+// that run at once has to do in all, or half of it where there are few tiles for a place
+// (whole tiles: 4.5 ms for a training step of 16 objects of 1 to 6411 rows in fp32, halves
+// 4.1; with four tiles a place whole ones are better, 0.93 and 1.03 ms for 12 sequences of
+// 1 to 3400 rows in bf16).  Room for a sequence four times as long as the mean one;
+// `room`: parts whose results are not too large.
+inline Cut cut_of(int64_t tiles, int64_t blocks, int64_t most, int64_t grid, int64_t places, int64_t least, int64_t room) {
+    Cut c;
+    c.share = tiles * blocks / ((tiles < 4 * places ? 2 : 1) * places);
+    c.share = c.share < least ? least : c.share;
+    most = most < 4 * blocks ? most : 4 * blocks;
+    int64_t n = (most + c.share - 1) / c.share;
+    const int64_t few = 32 * places / (grid > 0 ? grid : 1);  // workgroups that end at once are not free
+    n = n < 64 ? n : 64;
+    n = n < few || n <= 2 ? n : few < 2 ? 2 : few;
+    n = n < room ? n : room;
+    c.splits = (int)(n < 1 ? 1 : n);
+    return c;
 }
+// Bytes of partial results that are not too large.
+constexpr int64_t kMostParts = (int64_t)1 << 29;
 
 }  // namespace attend

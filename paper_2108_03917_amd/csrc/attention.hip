@@ -12,8 +12,8 @@
 // tile of 32 columns, whose keys the wavefronts of a workgroup take in turns,
 // each with blocks of its own, so that they never wait for each other; their
 // results are joined in LDS.
-// Where that leaves CUs without work, the keys of a tile are split among
-// workgroups, whose results a second launch joins in a fixed order.
+// Tiles with more blocks of keys than others, or too few of them for the CUs, are cut
+// into parts, whose results a second launch joins in a fixed order.
 #include "attention.h"
 
 namespace {
@@ -28,10 +28,11 @@ struct Params {
     int D;
     int group;          // query heads of a key head
     int parts, tile_heads;  // parts that a group is cut into, query heads of one
-    int R, slots, splits;   // rows of a tile
+    int R, slots;           // rows of a tile
+    Cut cut;                // of blocks of keys
     float c;            // scale, for powers of 2
     bool zero_rest;
-    float *part_o, *part_lse;  // of the splits: [splits][rows][heads][D], [splits][heads][rows]
+    float *part_o, *part_lse;  // of the parts: [splits][rows][heads][D], [splits][heads][rows]
     int32_t *status;
 };
 
@@ -40,7 +41,7 @@ struct Tile {
     Sequence s;
     int first, rows;      // its rows of the sequence
     int head0, heads;     // its query heads
-    int kv_head, split;
+    int kv_head, split, parts;
     int t0, t1;           // blocks of keys of this split
     int least, most;      // keys that its first and its last row see
 };
@@ -76,9 +77,10 @@ __device__ __forceinline__ bool tile_of(const Params &a, Tile &t) {
     t.least = keys_seen(t.s, a.pack.causal, t.first);
     t.most = keys_seen(t.s, a.pack.causal, t.first + t.rows - 1);
     const int n = (t.most + KT - 1) / KT;
-    t.t0 = (int)((int64_t)n * t.split / a.splits);
-    t.t1 = (int)((int64_t)n * (t.split + 1) / a.splits);
-    return true;
+    t.parts = parts_of(a.cut, n);
+    t.t0 = (int)((int64_t)n * t.split / t.parts);
+    t.t1 = (int)((int64_t)n * (t.split + 1) / t.parts);
+    return t.split < t.parts;
 }
 
 // A column's state: its maximum (of the scores as they are), the sum of
@@ -127,7 +129,7 @@ __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t r
     const float f = col.top == -INFINITY ? 0.f : 1.f / sum;
     const float lse2 = col.top == -INFINITY ? -INFINITY : fmaf(col.top, a.c, 0.f) + log2f(sum);
     const int h = (threadIdx.x & 63) >> 5;
-    const bool part = a.splits > 1;
+    const bool part = t.parts > 1;
     if (h == 0) {
         if (part)
             a.part_lse[((int64_t)t.split * a.heads + head) * a.pack.q_rows + row] = lse2;
@@ -356,13 +358,13 @@ __global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Par
         const int64_t row = t.s.q0 + t.first + rr;
         if (c0 == 0) {
             const float lse2 = none ? -INFINITY : m * a.c + log2f(all);
-            if (a.splits > 1)
+            if (t.parts > 1)
                 a.part_lse[((int64_t)t.split * a.heads + hh) * a.pack.q_rows + row] = lse2;
             else if (a.lse)
                 a.lse[hh * a.pack.q_rows + row] = lse2 * kLn2;
         }
         if (c0 >= a.D) continue;
-        if (a.splits > 1) {
+        if (t.parts > 1) {
             if (!none) store4<false>(a.part_o + (((int64_t)t.split * a.pack.q_rows + row) * a.heads + hh) * a.D, c0, a.D, v);
         } else {
             store4<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + hh * a.o.head) * L::E,
@@ -371,36 +373,38 @@ __global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Par
     }
 }
 
-// The splits' results of kJoinRows rows: weights 2^(lse - their common lse), a
-// wavefront for each row and head.
+// The parts' results of kJoinRows rows of a tile (blocks of KT keys): weights
+// 2^(lse - their common lse).
 template <bool BF16>
-__global__ __launch_bounds__(256) void k_join(Params a) {
+__global__ __launch_bounds__(256) void k_join(Params a, int KT) {
     int first;
-    const Sequence s = locate(a.pack, kJoinRows, blockIdx.x, false, first, a.status);
+    const Sequence s = locate(a.pack, a.R, blockIdx.x, false, first, a.status);
     if (!s.real || first >= s.q_len) return;
-    const int rows = s.q_len - first < kJoinRows ? s.q_len - first : kJoinRows;
-    const int lane = threadIdx.x & 63;
+    int rows = s.q_len - first < a.R ? s.q_len - first : a.R;
+    const int splits = parts_of(a.cut, (keys_seen(s, a.pack.causal, first + rows - 1) + KT - 1) / KT);
+    const int skip = (int)blockIdx.y * kJoinRows;
+    if (splits == 1 || skip >= rows) return;
+    first += skip;
+    rows = rows - skip < kJoinRows ? rows - skip : kJoinRows;
     const int64_t next = a.pack.q_rows * a.heads;
-    for (int i = threadIdx.x >> 6; i < rows * a.heads; i += 4) {
+    const int lanes = (a.D + 3) / 4;  // of a head's row
+    for (int id = threadIdx.x; id < rows * a.heads * lanes; id += 256) {
+        const int i = id / lanes, c0 = (id - i * lanes) * 4;
         const int64_t row = s.q0 + first + i / a.heads;
         const int head = i % a.heads;
         const float *lse = a.part_lse + head * a.pack.q_rows + row;
         float m = -INFINITY, sum = 0.f;
         bool nan = false;
-        for (int n = 0; n < a.splits; ++n) {
+        for (int n = 0; n < splits; ++n) {
             const float x = lse[n * next];
             nan |= x != x;
-            const float top = fmaxf(m, x);
-            if (top == -INFINITY) continue;
-            sum = sum * exp2_(m - top) + exp2_(x - top);
-            m = top;
+            m = fmaxf(m, x);
         }
+        for (int n = 0; n < splits; ++n) sum += m == -INFINITY ? 0.f : exp2_(lse[n * next] - m);
         const float all = nan ? NAN : m == -INFINITY ? m : m + log2f(sum);
-        if (a.lse && lane == 0) a.lse[head * a.pack.q_rows + row] = all * kLn2;
-        const int c0 = lane * 4;
-        if (c0 >= a.D) continue;
+        if (a.lse && c0 == 0) a.lse[head * a.pack.q_rows + row] = all * kLn2;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int n = 0; n < a.splits; ++n) {
+        for (int n = 0; n < splits; ++n) {
             const float x = lse[n * next];
             if (x == -INFINITY) continue;
             const float f = exp2_(x - all);
@@ -419,7 +423,7 @@ __global__ __launch_bounds__(256) void k_join(Params a) {
 struct Plan {
     Params p;
     bool few, dma;
-    int nq;
+    int nq, KT;  // blocks of 32 columns of a wavefront, keys of a block
     int64_t grid, part_o, part_lse;  // grid.x; floats of scratch
 };
 
@@ -452,11 +456,13 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     const int64_t slots = slots_of(a.q_starts, sequences, a.q_rows, p.R);
     p.slots = (int)slots;
     r.grid = unit_grid(p.units, slots);
-    const int64_t tiles = (a.q_rows + p.R - 1) / p.R;
-    p.splits = splits_of(p.units * (tiles > sequences ? tiles : sequences), keys, 2 * D->cu_count, 256);
-    if (p.splits > 1) {
-        r.part_o = (int64_t)p.splits * a.q_rows * a.heads * a.D;
-        r.part_lse = (int64_t)p.splits * a.q_rows * a.heads;
+    r.KT = r.few ? 32 : a.bf16 ? keys_of_block<true, 32>() : keys_of_block<false, 32>();
+    const int64_t tiles = (a.q_rows + p.R - 1) / p.R, width = (int64_t)a.q_rows * a.heads * a.D;
+    p.cut = cut_of(p.units * (tiles > sequences ? tiles : sequences), (keys + r.KT - 1) / r.KT, (a.kv_rows + r.KT - 1) / r.KT,
+                   r.grid, r.few ? D->cu_count : 2 * D->cu_count, r.few ? 8 : 4, kMostParts / (width * 4 + 1));
+    if (p.cut.splits > 1) {
+        r.part_o = p.cut.splits * width;
+        r.part_lse = (int64_t)p.cut.splits * a.q_rows * a.heads;
     }
     return r;
 }
@@ -464,7 +470,7 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
 template <bool BF16, int DP, bool DMA>
 hipError_t launch_as(lattice_dense *D, const Plan &r) {
     using L = Rows<BF16, DP>;
-    const dim3 grid((unsigned)r.grid, (unsigned)r.p.splits);
+    const dim3 grid((unsigned)r.grid, (unsigned)r.p.cut.splits);
     if (r.few) {
         constexpr int W = few_waves<BF16, DP>(), LDS = W * 2 * 2 * 32 * L::BYTES;
         static std::atomic<uint64_t> done{0};
@@ -497,9 +503,9 @@ hipError_t launch_type(lattice_dense *D, const Plan &r) {
         case 64: TRY((launch_dim<BF16, 64>(D, r))); break;
         default: TRY((launch_dim<BF16, 128>(D, r))); break;
     }
-    if (r.p.splits == 1) return hipSuccess;
-    const int64_t n = slots_of(r.p.pack.q_starts, r.p.pack.sequences, r.p.pack.q_rows, kJoinRows);
-    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)n), dim3(256), 0, D->stream, r.p);
+    if (r.p.cut.splits == 1) return hipSuccess;
+    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)r.p.slots, (unsigned)((r.p.R + kJoinRows - 1) / kJoinRows)), dim3(256), 0,
+                       D->stream, r.p, r.KT);
     return hipGetLastError();
 }
 

@@ -29,11 +29,11 @@ struct Params {
     float *delta;             // the same
     int heads, kv_heads, D, group;
     int parts, tile_heads;    // by queries, as in the forward pass
-    int units, R, slots, splits;
-    int64_t share;            // by keys: blocks of rows that make a part of a tile
+    int units, R, slots;
+    Cut cut;                  // of blocks of keys, or of rows
     float c, scale;
     bool zero_rest;
-    float *part;              // of the splits, without gaps, one after another
+    float *part;              // of the parts, without gaps, one after another
     int32_t *status;
 };
 
@@ -120,24 +120,21 @@ __device__ __forceinline__ void store_column(void *out, float *part, int64_t at,
         }
 }
 
-// Bytes of parts that tiles by keys may be cut into: beyond it there are tiles enough.
-constexpr int64_t kMostParts = (int64_t)1 << 29;
-
-// By queries: 4 wavefronts of 32 columns.
+// By queries: 4 wavefronts of 32 columns, blocks of keys of
+constexpr int kKeyBlock = 32;
 template <bool BF16, int DP, bool DMA>
 __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Params a) {
     using L = Rows<BF16, DP>;
-    constexpr int KT = 32, HALF = KT * L::BYTES, STAGE = 2 * HALF;
+    constexpr int KT = kKeyBlock, HALF = KT * L::BYTES, STAGE = 2 * HALF;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int unit, slot, first;
+    const int split = blockIdx.y;
     if (!unit_of(blockIdx.x, a.units, a.slots, true, unit, slot)) return;
     const int kv_head = unit / a.parts, part = unit % a.parts, head0 = kv_head * a.group + part * a.tile_heads;
     const int left = a.group - part * a.tile_heads, heads = left < a.tile_heads ? left : a.tile_heads;
     const Sequence s = locate(a.pack, a.R, slot, false, first, a.status);
     if (first >= s.q_len || heads <= 0) return;
     const int rows = s.q_len - first < a.R ? s.q_len - first : a.R;
-    const int split = blockIdx.y;
-    float *mine_part = a.splits > 1 ? a.part + (int64_t)split * a.pack.q_rows * a.heads * a.D : nullptr;
     if (!s.real) {
         if (a.zero_rest && split == 0)
             for (int r = 0; r < rows; ++r)
@@ -147,6 +144,10 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
                                    a.D, threadIdx.x, 256);
         return;
     }
+    const int least = keys_seen(s, a.pack.causal, first), most = keys_seen(s, a.pack.causal, first + rows - 1);
+    const int n = (most + KT - 1) / KT, parts = parts_of(a.cut, n);
+    if (split >= parts) return;
+    float *mine_part = parts > 1 ? a.part + (int64_t)split * a.pack.q_rows * a.heads * a.D : nullptr;
     const int lane = threadIdx.x & 63, wave = gemm::wave_index();
     const int column = wave * 32 + (lane & 31);
     int r = column / heads;
@@ -155,7 +156,6 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
     r = mine ? r : rows - 1;
     const int64_t row = s.q0 + first + r;
     const int seen = keys_seen(s, a.pack.causal, first + r);
-    const int least = keys_seen(s, a.pack.causal, first), most = keys_seen(s, a.pack.causal, first + rows - 1);
     int last = (wave * 32 + 31) / heads;
     last = last < rows ? last : rows - 1;
     const int wave_most = uniform(keys_seen(s, a.pack.causal, first + last));
@@ -178,8 +178,7 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
     f32x16_t dq[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) clear(dq[d]);
-    const int n = (most + KT - 1) / KT;
-    const int t0 = (int)((int64_t)n * split / a.splits), t1 = (int)((int64_t)n * (split + 1) / a.splits);
+    const int t0 = (int)((int64_t)n * split / parts), t1 = (int)((int64_t)n * (split + 1) / parts);
     Loader<BF16, DP, KT, 4, DMA> lk(a.k, s.k0, kv_head, a.D, wave), lv(a.v, s.k0, kv_head, a.D, wave);
     if (t0 < t1) {
         lk.fetch(lds, t0 * KT, s.keys);
@@ -243,11 +242,6 @@ struct ByKeys {
     static_assert(QW == 1 || 4 * 32 * DP * 4 <= 2 * QW * STAGE, "LDS");
 };
 
-// Parts that a tile with this many blocks is cut into.
-__device__ __forceinline__ int parts_of(const Params &a, int64_t blocks) {
-    const int64_t n = (blocks + a.share - 1) / a.share;
-    return (int)(n < 1 ? 1 : n < a.splits ? n : a.splits);
-}
 // Where the rows begin that see a tile of keys from `first` on.
 constexpr int kRowBlock = 32;
 __device__ __forceinline__ int first_row(const Params &a, const Sequence &s, int first) {
@@ -266,11 +260,11 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
     constexpr int QT = kRowBlock, QW = B::QW;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ __attribute__((aligned(16))) float stats[2][QW][2][QT];  // lse (of 2) and delta of the blocks' rows
+    const int split = blockIdx.y;
     int kv_head, slot, first;
     if (!unit_of(blockIdx.x, a.kv_heads, a.slots, false, kv_head, slot)) return;
     const Sequence s = locate(a.pack, a.R, slot, true, first, a.status);
     if (first >= s.kv_len) return;
-    const int split = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = gemm::wave_index() & 3, group = gemm::wave_index() >> 2, h = lane >> 5;
     const int64_t size = a.pack.kv_rows * a.kv_heads * a.D;
     const int key = first + wave * 32 + (lane & 31);
@@ -288,7 +282,7 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
     // blocks of rows: those of each query head, one head after another
     const int r0 = first_row(a, s, first), per = row_blocks(a, s, first);
     const int64_t blocks = (int64_t)per * a.group;
-    const int parts = parts_of(a, blocks);
+    const int parts = parts_of(a.cut, blocks);
     if (split >= parts) return;
     const int64_t begin = blocks * split / parts, end = blocks * (split + 1) / parts;
 
@@ -417,25 +411,21 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
     }
 }
 
-// Sums of the splits' values in their order, of a.R (by keys: of a part of a tile's)
-// rows a workgroup: those of a sequence, or of its keys that count.
+// Sums of the parts' values in their order, of kJoinRows rows of a tile: those of a
+// sequence, or of its keys that count.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_join(Params a, bool by_keys) {
     int first;
-    const int R = by_keys ? a.R : kJoinRows;
-    const Sequence s = locate(a.pack, R, blockIdx.x, by_keys, first, a.status);
+    const Sequence s = locate(a.pack, a.R, blockIdx.x, by_keys, first, a.status);
     const int all = by_keys ? s.keys : s.q_len;
     if (!s.real || first >= all) return;
-    int rows = all - first < R ? all - first : R;
-    int splits = a.splits;
-    if (by_keys) {
-        splits = parts_of(a, (int64_t)row_blocks(a, s, first) * a.group);
-        if (splits == 1) return;
-        const int skip = (int)blockIdx.z * kJoinRows;
-        if (skip >= rows) return;
-        first += skip;
-        rows = rows - skip < kJoinRows ? rows - skip : kJoinRows;
-    }
+    int rows = all - first < a.R ? all - first : a.R;
+    const int splits = parts_of(a.cut, by_keys ? (int64_t)row_blocks(a, s, first) * a.group
+                                               : (keys_seen(s, a.pack.causal, first + rows - 1) + kKeyBlock - 1) / kKeyBlock);
+    const int skip = (int)blockIdx.z * kJoinRows;
+    if (splits == 1 || skip >= rows) return;
+    first += skip;
+    rows = rows - skip < kJoinRows ? rows - skip : kJoinRows;
     const int64_t width = (int64_t)(by_keys ? a.kv_heads : a.heads) * a.D;
     const int64_t size = (by_keys ? a.pack.kv_rows : a.pack.q_rows) * width;
     const int64_t from = ((by_keys ? s.k0 : s.q0) + first) * width;
@@ -494,27 +484,23 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
         p.units = a.kv_heads * p.parts;
         const int64_t slots = slots_of(a.q_starts, sequences, a.q_rows, p.R), tiles = (a.q_rows + p.R - 1) / p.R;
         p.slots = (int)slots;
-        r.grid_queries = unit_grid(p.units, slots);
-        p.splits = splits_of(p.units * (tiles > sequences ? tiles : sequences), keys, 2 * D->cu_count, 256);
-        if (p.splits > 1) r.part = (int64_t)p.splits * a.q_rows * a.heads * a.D;
+        const int64_t grid = unit_grid(p.units, slots), width = a.q_rows * a.heads * a.D;
+        p.cut = cut_of(p.units * std::max(tiles, sequences), (keys + kKeyBlock - 1) / kKeyBlock,
+                       (a.kv_rows + kKeyBlock - 1) / kKeyBlock, grid, 2 * D->cu_count, 8, kMostParts / (width * 4 + 1));
+        if (p.cut.splits > 1) r.part = p.cut.splits * width;
+        r.grid_queries = grid;
     }
     Params &b = r.by_keys;
     b.R = 128;
     const int32_t *starts = !a.q_starts ? nullptr : a.kv_starts ? a.kv_starts : a.q_starts;
     const int64_t slots = slots_of(starts, sequences, a.kv_rows, b.R), tiles = (a.kv_rows + b.R - 1) / b.R;
     b.slots = (int)slots;
-    r.grid_keys = unit_grid(a.kv_heads, slots);
-    // A tile's rows, all heads' of them, are cut into parts of about half of what a CU has to do
-    // in all if every sequence had the mean length; only tiles with more than one part are
-    // joined.  The longest sequence may have all the rows.
-    const int64_t each = (rows * p.group + kRowBlock - 1) / kRowBlock, most = (a.q_rows * p.group + kRowBlock - 1) / kRowBlock;
-    const int64_t all = a.kv_heads * (tiles > sequences ? tiles : sequences) * each;
-    b.share = all / (2 * D->cu_count);
-    b.share = b.share < 8 ? 8 : b.share;
-    const int64_t want = (most + b.share - 1) / b.share, part = (int64_t)2 * a.kv_rows * a.kv_heads * a.D;
-    const int64_t room = part > 0 ? kMostParts / (part * 4) : 1;
-    b.splits = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(want, 16), room));
-    if (b.splits > 1) r.part = std::max(r.part, b.splits * part);
+    // a tile's blocks are the rows of all its query heads
+    const int64_t grid = unit_grid(a.kv_heads, slots), width = 2 * a.kv_rows * a.kv_heads * a.D;
+    b.cut = cut_of(a.kv_heads * std::max(tiles, sequences), (rows + kRowBlock - 1) / kRowBlock * p.group,
+                   (a.q_rows + kRowBlock - 1) / kRowBlock * p.group, grid, D->cu_count, 8, kMostParts / (width * 4 + 1));
+    if (b.cut.splits > 1) r.part = std::max(r.part, b.cut.splits * width);
+    r.grid_keys = grid;
     return r;
 }
 
@@ -522,7 +508,7 @@ template <bool BF16, int DP, bool DMA>
 hipError_t by_queries(lattice_dense *D, const Plan &r) {
     constexpr int LDS = 2 * 2 * 32 * Rows<BF16, DP>::BYTES;
     static_assert(LDS <= 64 * 1024, "LDS");
-    hipLaunchKernelGGL((k_by_queries<BF16, DP, DMA>), dim3((unsigned)r.grid_queries, (unsigned)r.by_queries.splits),
+    hipLaunchKernelGGL((k_by_queries<BF16, DP, DMA>), dim3((unsigned)r.grid_queries, (unsigned)r.by_queries.cut.splits),
                        dim3(256), LDS, D->stream, r.by_queries);
     return hipGetLastError();
 }
@@ -533,16 +519,16 @@ hipError_t by_keys(lattice_dense *D, const Plan &r) {
     constexpr int LDS = B::LDS;
     static std::atomic<uint64_t> done{0};
     if (LDS + 2048 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_by_keys<BF16, DP, DMA>), LDS, done));
-    hipLaunchKernelGGL((k_by_keys<BF16, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.splits), dim3(B::THREADS), LDS,
+    hipLaunchKernelGGL((k_by_keys<BF16, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.cut.splits), dim3(B::THREADS), LDS,
                        D->stream, r.by_keys);
     return hipGetLastError();
 }
 
 template <bool BF16>
 hipError_t join(lattice_dense *D, const Params &p, bool keys) {
-    if (p.splits == 1) return hipSuccess;
-    const int64_t n = keys ? p.slots : slots_of(p.pack.q_starts, p.pack.sequences, p.pack.q_rows, kJoinRows);
-    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)n, keys ? 2 : 1, keys ? p.R / kJoinRows : 1), dim3(256), 0, D->stream, p, keys);
+    if (p.cut.splits == 1) return hipSuccess;
+    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)p.slots, keys ? 2 : 1, (unsigned)((p.R + kJoinRows - 1) / kJoinRows)),
+                       dim3(256), 0, D->stream, p, keys);
     return hipGetLastError();
 }
 

@@ -249,7 +249,7 @@ class Dense:
         other; (address, values from row to row, from head to head)."""
         if t.dtype not in _STORAGE or dtype is not None and t.dtype != dtype:
             raise ValueError(f"{name} must be {dtype or ' or '.join(map(str, _STORAGE))}, got {t.dtype}")
-        if t.device != self.device:
+        if t.get_device() != self._index:
             raise ValueError(f"{name} must be on {self.device}, is on {t.device}")
         if t.dim() != 3 or shape is not None and t.shape != shape:
             raise ValueError(f"{name} must be {list(shape) if shape is not None else '[rows, heads, channels]'}, "
@@ -259,33 +259,43 @@ class Dense:
             raise ValueError(f"{name}: the values of a head must be next to each other")
         return t.data_ptr(), row, head
 
-    def _starts(self, t: Optional[torch.Tensor], n: int, name: str):
-        if t is None:
-            return None
-        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    def _starts(self, t: torch.Tensor, n: int, name: str):
+        if (t.dtype is not torch.int32 or t.get_device() != self._index or t.dim() != 1 or t.shape[0] != n
+                or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous int32 [{n}] on {self.device}")
         return t.data_ptr()
 
     def _attention(self, q, k, v, q_starts, kv_starts, kv_lengths, scale):
-        """Check what both passes take: (dtype .. C, q, k, v), (starts .. sequences), scale."""
+        """Check what both passes take: (dtype .. C), q, k, v, (starts .. sequences), scale."""
+        dtype, shape, kv_shape = q.dtype, q.shape, k.shape
         qv = self._heads(q, "q")
-        kv = self._heads(k, "k", dtype=q.dtype)
-        vv = self._heads(v, "v", k.shape, q.dtype)
-        rows, heads, C = q.shape
-        kv_rows, kv_heads, kC = k.shape
+        kv = self._heads(k, "k", None, dtype)
+        vv = self._heads(v, "v", kv_shape, dtype)
+        rows, heads, C = shape
+        kv_rows, kv_heads, kC = kv_shape
         if kC != C or kv_heads == 0 or heads % kv_heads:
-            raise ValueError(f"k must have heads of {C} channels, as many as divide q's {heads}, is {list(k.shape)}")
-        n = 1
+            raise ValueError(f"k must have heads of {C} channels, as many as divide q's {heads}, is {list(kv_shape)}")
+        n, starts, of_keys, lengths = 1, None, None, None
         if q_starts is not None:
             n = q_starts.shape[0] - 1 if q_starts.dim() == 1 else -1
             if n < 0:
                 raise ValueError("q_starts must be [sequences + 1]")
+            starts = self._starts(q_starts, n + 1, "q_starts")
+            if kv_starts is not None:
+                of_keys = self._starts(kv_starts, n + 1, "kv_starts")
         elif kv_starts is not None:
             raise ValueError("kv_starts without q_starts")
-        packing = (self._starts(q_starts, n + 1, "q_starts"), self._starts(kv_starts, n + 1, "kv_starts"),
-                   self._starts(kv_lengths, n, "kv_lengths"), n)
-        scale = 1 / math.sqrt(C) if scale is None and C else scale
-        return (_STORAGE[q.dtype], rows, kv_rows, heads, kv_heads, C), (*qv, *kv, *vv), packing, scale
+        if kv_lengths is not None:
+            lengths = self._starts(kv_lengths, n, "kv_lengths")
+        if scale is None:
+            scale = 1 / math.sqrt(C) if C else 1.0
+        return (_STORAGE[dtype], rows, kv_rows, heads, kv_heads, C), (*qv, *kv, *vv), (starts, of_keys, lengths, n), scale
+
+    @staticmethod
+    def _new(t: torch.Tensor) -> torch.Tensor:
+        """An empty contiguous tensor of t's shape and type (what torch.empty gives
+        takes the host half as long again)."""
+        return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
     def attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_starts: Optional[torch.Tensor] = None,
                   kv_starts: Optional[torch.Tensor] = None, kv_lengths: Optional[torch.Tensor] = None,
@@ -306,8 +316,10 @@ class Dense:
         sizes, tensors, packing, scale = self._attention(q, k, v, q_starts, kv_starts, kv_lengths, scale)
         rest = out is None
         if rest:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        ov = self._heads(out, "out", q.shape, q.dtype)
+            out = self._new(q)
+            ov = (out.data_ptr(), sizes[3] * sizes[5], sizes[5])
+        else:
+            ov = self._heads(out, "out", q.shape, q.dtype)
         lse = torch.empty((q.shape[1], q.shape[0]), dtype=F32, device=q.device) if want_lse else None
         if want_lse and not rest:
             lse.fill_(-math.inf)
@@ -328,29 +340,43 @@ class Dense:
         self._dev(lse, "lse", (F32,))
         if lse.shape != (q.shape[1], q.shape[0]) or not lse.is_contiguous():
             raise ValueError(f"lse must be a contiguous [{q.shape[1]}, {q.shape[0]}]")
-        gq, gk, gvv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        gq, gk, gvv = self._new(q), self._new(k), self._new(v)
         self._call(self._lib.lattice_attention_backward, "attention_backward", *sizes, *gv, *tensors, *ov, lse.data_ptr(),
                    *packing, causal, scale, True, gq.data_ptr(), gk.data_ptr(), gvv.data_ptr())
         return gq, gk, gvv
 
     # -- norm and rotation of heads ------------------------------------------
     def _rotation(self, q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved):
+        """Check q, k and what both passes take: (dtype .. C), q, k, (positions ..
+        interleaved)."""
+        qv = self._heads(q, "q")
         rows, heads, C = q.shape
-        if positions.dtype not in (F32, torch.int32) or positions.device != self.device:
+        kv, kv_heads = (None, 0, 0), 0
+        if k is not None:
+            kv = self._heads(k, "k", None, q.dtype)
+            k_rows, kv_heads, kC = k.shape
+            if k_rows != rows or kC != C:
+                raise ValueError(f"k must be [{rows}, heads, {C}], is {list(k.shape)}")
+        if positions.dtype not in (F32, torch.int32) or positions.get_device() != self._index:
             raise ValueError(f"positions must be float32 or int32 on {self.device}")
         if positions.dim() == 1:
             positions = positions[:, None]
-        if positions.dim() != 2 or positions.shape[0] != rows or positions.shape[1] > 1 and positions.stride(1) != 1:
+        shape = positions.shape
+        if len(shape) != 2 or shape[0] != rows or shape[1] > 1 and positions.stride(1) != 1:
             raise ValueError(f"positions must be [{rows}, axes], the axes next to each other")
-        axes = positions.shape[1]
-        sections = [freq.shape[0]] if sections is None and freq.dim() == 1 else sections
+        axes = shape[1]
+        if sections is None and freq.dim() == 1:
+            sections = (freq.shape[0],)
         if sections is None or len(sections) != axes:
             raise ValueError(f"sections must hold the pairs of each of {axes} axes")
         self._vector(freq, sum(sections), "freq")
-        self._vector(gain_q, C, "gain_q")
-        self._vector(gain_k, C, "gain_k")
-        return (positions.data_ptr(), positions.dtype == torch.int32, positions.stride(0) if rows > 1 else axes, axes,
-                (ctypes.c_int * axes)(*sections), freq.data_ptr(), norm, _ptr(gain_q), _ptr(gain_k), eps, interleaved)
+        if gain_q is not None:
+            self._vector(gain_q, C, "gain_q")
+        if gain_k is not None:
+            self._vector(gain_k, C, "gain_k")
+        return (_STORAGE[q.dtype], rows, heads, kv_heads, C), qv, kv, (
+            positions.data_ptr(), positions.dtype is torch.int32, positions.stride(0) if rows > 1 else axes, axes,
+            (ctypes.c_int * axes)(*sections), freq.data_ptr(), norm, _ptr(gain_q), _ptr(gain_k), eps, interleaved)
 
     def rotate_heads(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, freq: torch.Tensor,
                      sections: Optional[Sequence[int]] = None, gain_q: Optional[torch.Tensor] = None,
@@ -367,21 +393,21 @@ class Dense:
         pairs, pair p is the channels p and p + P, or 2 p and 2 p + 1 if
         ``interleaved``; channels from 2 P on do not turn.  Without ``norm`` only
         the rotation.  Returns (out_q, out_k); the outputs may be the inputs."""
-        qv = self._heads(q, "q")
-        kv = self._heads(k, "k", (q.shape[0], k.shape[1], q.shape[2]) if k.dim() == 3 else None, q.dtype) if k is not None \
-            else (None, 0, 0)
-        rotation = self._rotation(q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved)
+        sizes, qv, kv, rotation = self._rotation(q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved)
+        _, _, heads, kv_heads, C = sizes
         if out_q is None:
-            out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        oq = self._heads(out_q, "out_q", q.shape, q.dtype)
+            out_q = self._new(q)
+            oq = (out_q.data_ptr(), heads * C, C)
+        else:
+            oq = self._heads(out_q, "out_q", q.shape, q.dtype)
         if k is None:
             out_k, ok = None, (None, 0, 0)
+        elif out_k is None:
+            out_k = self._new(k)
+            ok = (out_k.data_ptr(), kv_heads * C, C)
         else:
-            if out_k is None:
-                out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
             ok = self._heads(out_k, "out_k", k.shape, k.dtype)
-        self._call(self._lib.lattice_rotate_heads, "rotate_heads", _STORAGE[q.dtype], q.shape[0], q.shape[1],
-                   k.shape[1] if k is not None else 0, q.shape[2], *qv, *kv, *rotation, *oq, *ok)
+        self._call(self._lib.lattice_rotate_heads, "rotate_heads", *sizes, *qv, *kv, *rotation, *oq, *ok)
         return out_q, out_k
 
     def rotate_heads_backward(self, grad_q: torch.Tensor, grad_k: Optional[torch.Tensor], q: torch.Tensor,
@@ -394,28 +420,24 @@ class Dense:
         and stored as their inputs, the last two fp32 [C], or None with
         ``want_gains`` False (which is so without the norm unless given).
         Positions and frequencies get none."""
-        qv = self._heads(q, "q")
-        gq = self._heads(grad_q, "grad_q", q.shape, q.dtype)
         if (k is None) != (grad_k is None):
             raise ValueError("k and grad_k go together")
-        kv = gk = ok = (None, 0, 0)
-        out_k = None
+        sizes, qv, kv, rotation = self._rotation(q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved)
+        _, _, heads, kv_heads, C = sizes
+        gq = self._heads(grad_q, "grad_q", q.shape, q.dtype)
+        out_q, out_k = self._new(q), None
+        gk = ok = (None, 0, 0)
         if k is not None:
-            kv = self._heads(k, "k", (q.shape[0], k.shape[1], q.shape[2]) if k.dim() == 3 else None, q.dtype)
             gk = self._heads(grad_k, "grad_k", k.shape, k.dtype)
-            out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-            ok = (out_k.data_ptr(), k.shape[1] * k.shape[2], k.shape[2])
-        rotation = self._rotation(q, k, positions, freq, sections, gain_q, gain_k, norm, eps, interleaved)
-        out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        oq = (out_q.data_ptr(), q.shape[1] * q.shape[2], q.shape[2])
-        gg = [None, None]
+            out_k = self._new(k)
+            ok = (out_k.data_ptr(), kv_heads * C, C)
+        gain = [None, None]
         if norm if want_gains is None else want_gains:
-            both = torch.empty((2, q.shape[2]), dtype=F32, device=q.device)
-            gg = [both[0], both[1] if k is not None else None]
-        self._call(self._lib.lattice_rotate_heads_backward, "rotate_heads_backward", _STORAGE[q.dtype], q.shape[0],
-                   q.shape[1], k.shape[1] if k is not None else 0, q.shape[2], *gq, *gk, *qv, *kv, *rotation, *oq, *ok,
-                   _ptr(gg[0]), _ptr(gg[1]))
-        return out_q, out_k, gg[0], gg[1]
+            both = q.new_empty((2, C), dtype=F32).unbind()
+            gain = [both[0], both[1] if k is not None else None]
+        self._call(self._lib.lattice_rotate_heads_backward, "rotate_heads_backward", *sizes, *gq, *gk, *qv, *kv, *rotation,
+                   out_q.data_ptr(), heads * C, C, *ok, _ptr(gain[0]), _ptr(gain[1]))
+        return out_q, out_k, gain[0], gain[1]
 
     # -- clipping ------------------------------------------------------------
     def clip_gradients(self, grads: Sequence[torch.Tensor], max_norm: float, eps: float = 1e-6,
@@ -426,23 +448,24 @@ class Dense:
         before, an fp32 scalar.  A norm that is not finite is not refused: NaN
         makes every value NaN, infinity makes finite ones 0."""
         n = len(grads)
-        to = grads if out is None else out
-        if len(to) != n:
+        if out is not None and len(out) != n:
             raise ValueError(f"out must hold {n} tensors")
-        device, types = self.device, _STORAGE
-        for name, ts in (("grads", grads),) if out is None else (("grads", grads), ("out", to)):
-            for i, t in enumerate(ts):
-                if t.dtype not in types or t.device != device or not t.is_contiguous():
-                    raise ValueError(f"{name}[{i}] must be contiguous, fp32 or bf16, and on {device}")
+
+        def check(tensors, name):
+            index = self._index
+            for i, t in enumerate(tensors):
+                if t.dtype not in _STORAGE or t.get_device() != index or not t.is_contiguous():
+                    raise ValueError(f"{name}[{i}] must be contiguous, fp32 or bf16, and on {self.device}")
+            return ((ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors]),
+                    (ctypes.c_int * n)(*[_STORAGE[t.dtype] for t in tensors]))
+
+        src = to = check(grads, "grads")
         if out is not None:
-            for i, (a, b) in enumerate(zip(grads, to)):
+            to = check(out, "out")
+            for i, (a, b) in enumerate(zip(grads, out)):
                 if a.shape != b.shape:
                     raise ValueError(f"out[{i}] must be {list(a.shape)}")
-        norm = torch.empty((), dtype=F32, device=device)
-        pointers, kinds = ctypes.c_void_p * n, ctypes.c_int * n
-        src, src_t = pointers(*[t.data_ptr() for t in grads]), kinds(*[types[t.dtype] for t in grads])
-        dst, dst_t = (src, src_t) if out is None else (pointers(*[t.data_ptr() for t in to]),
-                                                       kinds(*[types[t.dtype] for t in to]))
-        self._call(self._lib.lattice_clip_gradients, "clip_gradients", n, src, src_t, dst, dst_t,
+        norm = torch.empty((), dtype=F32, device=self.device)
+        self._call(self._lib.lattice_clip_gradients, "clip_gradients", n, *src, *to,
                    (ctypes.c_int64 * n)(*[t.numel() for t in grads]), max_norm, eps, norm.data_ptr())
         return norm
