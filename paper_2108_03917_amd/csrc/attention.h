@@ -5,8 +5,10 @@
 //   p_ij = exp(s_ij - lse_i),  lse_i = log sum_j exp s_ij,  o_i = sum_j p_ij v_j.
 //
 // Products run on the matrix cores in 32 x 32 blocks, v_mfma_f32_32x32x16_bf16
-// for bf16 and v_mfma_f32_32x32x2_f32 for fp32 storage.  An accumulator holds a
-// block transposed to what the next product wants as its right operand: lane l
+// for bf16 and v_mfma_f32_32x32x2_f32 for fp32 storage, or, where there are many of
+// fp32 heads of up to 64 channels, the bf16 ones on three planes of bf16 whose sum
+// is the value (24 bits): of the nine products the six largest, 2.7 times the rate
+// of the fp32 cores.  An accumulator holds a block transposed to what the next product wants as its right operand: lane l
 // has column l % 32 and rows 8 (e / 4) + 4 (l / 32) + e % 4 of it.  Scores are
 // made as k q^T, so that a query's scores lie in the registers of two lanes
 // (maxima and sums need one exchange between them) and the probabilities are,
@@ -15,6 +17,8 @@
 // keys next to each other for each channel, comes out of LDS by the transposing
 // read (ds_read_b64_tr_b16) for bf16 and lane by lane for fp32.
 #pragma once
+
+#include <algorithm>
 
 #include "dense.h"
 #include "gemm.h"
@@ -30,10 +34,18 @@ using gemm::f32x16_t;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kJoinRows = 4;  // of a workgroup that joins parts
 
-// A tensor [rows][heads][D]: values between rows and between heads.
+// How a kernel takes its operands: fp32 words, bf16, or fp32 as three planes of bf16.
+enum Type { F32, BF16, PLANES };
+template <Type T>
+constexpr int kPlanes = T == PLANES ? 3 : 1;
+template <Type T>
+constexpr int kProducts = T == PLANES ? 6 : 1;   // of planes
+
+// A tensor [rows][heads][D]: values between rows and between heads, bytes between
+// planes.
 struct View {
     const void *p;
-    int64_t row, head;
+    int64_t row, head, plane;
 };
 
 // Where the rows of packed sequences lie, and the tiles that a launch cuts the
@@ -203,6 +215,12 @@ struct Rows {
     __device__ static __forceinline__ int at(int row, int chunk) { return row * BYTES + ((chunk ^ key(row)) << 4); }
 };
 
+template <Type T, int DP>
+using RowsOf = Rows<T != F32, DP>;
+// Bytes of a tile of `rows` rows, its planes one behind the other.
+template <Type T, int DP>
+constexpr int tile_bytes(int rows) { return kPlanes<T> * rows * RowsOf<T, DP>::BYTES; }
+
 // acc += a b over 2 x 16 bytes of each row.
 template <bool BF16>
 __device__ __forceinline__ void mma(const u32x4_t &a, const u32x4_t &b, f32x16_t &acc) {
@@ -236,61 +254,102 @@ __device__ __forceinline__ void read_ahead() {
     }
 }
 
-// acc = (rows row0.. of the tile) (fragments b)^T.
-template <bool BF16, int DP>
-__device__ __forceinline__ void rows_times(const char *tile, int row0, const u32x4_t (&b)[Rows<BF16, DP>::STEPS],
-                                           f32x16_t &acc) {
-    using L = Rows<BF16, DP>;
+// A row's values as a right operand: this lane's chunks 2 t + lane / 32.
+template <Type T, int DP>
+struct Fragments {
+    u32x4_t v[kPlanes<T>][RowsOf<T, DP>::STEPS];
+};
+
+// acc = (rows row0.. of a tile of ROWS) (fragments b)^T.  Of planes the smaller
+// products come first.
+template <Type T, int DP, int ROWS>
+__device__ __forceinline__ void rows_times(const char *tile, int row0, const Fragments<T, DP> &b, f32x16_t &acc) {
+    using L = RowsOf<T, DP>;
+    constexpr int P = kPlanes<T>;
     const int lane = threadIdx.x & 63, row = row0 + (lane & 31), h = lane >> 5;
 #pragma unroll
-    for (int t = 0; t < L::STEPS; ++t)
-        mma<BF16>(*reinterpret_cast<const u32x4_t *>(tile + L::at(row, 2 * t + h)), b[t], acc);
+    for (int t = 0; t < L::STEPS; ++t) {
+        u32x4_t a[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            a[p] = *reinterpret_cast<const u32x4_t *>(tile + p * ROWS * L::BYTES + L::at(row, 2 * t + h));
+#pragma unroll
+        for (int sum = P - 1; sum >= 0; --sum)
+#pragma unroll
+            for (int p = 0; p <= sum; ++p) mma<T != F32>(a[p], b.v[sum - p][t], acc);
+    }
+}
+
+// Three bf16 whose sum is x, of two values at a time: of values below 2^-110 the
+// last ones vanish.
+__device__ __forceinline__ void planes_of(float x0, float x1, uint32_t &h, uint32_t &m, uint32_t &l) {
+    h = pack_bf16(x0, x1);
+    const float r0 = x0 - __uint_as_float(h << 16), r1 = x1 - __uint_as_float(h & 0xffff0000u);
+    m = pack_bf16(r0, r1);
+    l = pack_bf16(r0 - __uint_as_float(m << 16), r1 - __uint_as_float(m & 0xffff0000u));
 }
 
 // The right operand made of an accumulator's block: 4 values a register group.
-template <bool BF16>
+template <Type T>
 struct Right {
-    u32x4_t v[BF16 ? 2 : 4];
-    __device__ __forceinline__ void set(const f32x16_t &p) {
-        if constexpr (BF16) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[s][i] = pack_bf16(p[8 * s + 2 * i], p[8 * s + 2 * i + 1]);
-        } else {
+    u32x4_t v[kPlanes<T>][T == F32 ? 4 : 2];
+    __device__ __forceinline__ void set(const f32x16_t &x) {
+        if constexpr (T == F32) {
 #pragma unroll
             for (int g = 0; g < 4; ++g)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[g][i] = __float_as_uint(p[4 * g + i]);
+                for (int i = 0; i < 4; ++i) v[0][g][i] = __float_as_uint(x[4 * g + i]);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x0 = x[8 * s + 2 * i], x1 = x[8 * s + 2 * i + 1];
+                    if constexpr (T == PLANES) {
+                        uint32_t h, m, l;
+                        planes_of(x0, x1, h, m, l);
+                        v[0][s][i] = h, v[1][s][i] = m, v[2][s][i] = l;
+                    } else {
+                        v[0][s][i] = pack_bf16(x0, x1);
+                    }
+                }
         }
     }
 };
 
-// acc[d] += (channels of the tile's rows row0 .. row0 + 31)^T p, for 32 channels
-// a block d.
-template <bool BF16, int DP>
-__device__ __forceinline__ void columns_times(const char *tile, int row0, const Right<BF16> &p,
-                                              f32x16_t (&acc)[DP / 32]) {
-    using L = Rows<BF16, DP>;
+// acc[d] += (channels of rows row0 .. row0 + 31 of a tile of ROWS)^T b, for 32
+// channels a block d.
+template <Type T, int DP, int ROWS>
+__device__ __forceinline__ void columns_times(const char *tile, int row0, const Right<T> &b, f32x16_t (&acc)[DP / 32]) {
+    using L = RowsOf<T, DP>;
+    constexpr int P = kPlanes<T>;
     const int lane = threadIdx.x & 63, h = lane >> 5;
-    if constexpr (BF16) {
+    if constexpr (T != F32) {
         typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+        typedef short s16x8_t __attribute__((ext_vector_type(8)));
         const int j = lane & 15, wide = (lane >> 4) & 1;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
                 const int chunk = 4 * d + 2 * wide + ((j & 3) >> 1);
-                s16x4_t a[2];
+                u32x4_t a[P];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int row = row0 + 16 * s + 8 * u + 4 * h + (j >> 2);
-                    a[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_s16x4 *)(tile + L::at(row, chunk) + 8 * (j & 1)));
+                for (int p = 0; p < P; ++p) {
+                    s16x4_t x[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int row = row0 + 16 * s + 8 * u + 4 * h + (j >> 2);
+                        x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (lds_s16x4 *)(tile + p * ROWS * L::BYTES + L::at(row, chunk) + 8 * (j & 1)));
+                    }
+                    const s16x8_t both = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    a[p] = __builtin_bit_cast(u32x4_t, both);
                 }
-                typedef short s16x8_t __attribute__((ext_vector_type(8)));
-                const s16x8_t both = __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                mma<true>(__builtin_bit_cast(u32x4_t, both), p.v[s], acc[d]);
+#pragma unroll
+                for (int sum = P - 1; sum >= 0; --sum)
+#pragma unroll
+                    for (int p = 0; p <= sum; ++p) mma<true>(a[p], b.v[sum - p][s], acc[d]);
             }
     } else {
         const int c = lane & 31;
@@ -302,25 +361,25 @@ __device__ __forceinline__ void columns_times(const char *tile, int row0, const 
                 for (int i = 0; i < 4; ++i) {
                     const int row = row0 + 8 * g + 4 * h + i;
                     const float x = *reinterpret_cast<const float *>(tile + L::at(row, 8 * d + (c >> 2)) + 4 * (c & 3));
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(p.v[g][i]), acc[d], 0, 0, 0);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(b.v[0][g][i]), acc[d], 0, 0, 0);
                 }
     }
 }
 
-// Fragments of a row of a tensor: this lane's chunks 2 t + lane / 32, zeros past
-// the row's D channels.
-template <bool BF16, int DP>
-__device__ __forceinline__ void load_fragments(const View &x, int64_t row, int head, int D,
-                                               u32x4_t (&f)[Rows<BF16, DP>::STEPS]) {
-    using L = Rows<BF16, DP>;
+// Fragments of a row of a tensor, zeros past the row's D channels.
+template <Type T, int DP>
+__device__ __forceinline__ void load_fragments(const View &x, int64_t row, int head, int D, Fragments<T, DP> &f) {
+    using L = RowsOf<T, DP>;
     const int h = (threadIdx.x & 63) >> 5;
-    const char *p = reinterpret_cast<const char *>(x.p) + (row * x.row + head * x.head) * L::E;
+    const char *from = reinterpret_cast<const char *>(x.p) + (row * x.row + head * x.head) * L::E;
 #pragma unroll
-    for (int t = 0; t < L::STEPS; ++t) {
-        Raw<BF16, L::VEC> u;
-        load_raw<BF16, L::VEC>(p, (2 * t + h) * L::VEC, D, u);
-        f[t] = u32x4_t{u.w[0], u.w[1], u.w[2], u.w[3]};
-    }
+    for (int p = 0; p < kPlanes<T>; ++p)
+#pragma unroll
+        for (int t = 0; t < L::STEPS; ++t) {
+            Raw<T != F32, L::VEC> u;
+            load_raw<T != F32, L::VEC>(from + p * x.plane, (2 * t + h) * L::VEC, D, u);
+            f.v[p][t] = u32x4_t{u.w[0], u.w[1], u.w[2], u.w[3]};
+        }
 }
 
 // Bring ROWS rows of a tensor into LDS with WAVES wavefronts (this one is number
@@ -328,52 +387,73 @@ __device__ __forceinline__ void load_fragments(const View &x, int64_t row, int h
 // whole chunks long) or through registers.  Rows past the last one and chunks
 // past a row's last stand in for those that are not there: their scores are
 // masked, their channels not stored.
-template <bool BF16, int DP, int ROWS, int WAVES, bool DMA>
+template <Type T, int DP, int ROWS, int WAVES, bool DMA>
 struct Loader {
-    using L = Rows<BF16, DP>;
-    static constexpr int ALL = ROWS * L::CHUNKS / 64;  // 1 KB each; small tiles leave wavefronts without one
+    using L = RowsOf<T, DP>;
+    static_assert(T != PLANES || DMA, "planes are laid out for direct loads");
+    static constexpr int EACH = ROWS * L::CHUNKS / 64;  // wavefronts' loads of a plane, 1 KB each
+    static constexpr int ALL = kPlanes<T> * EACH;       // not all wavefronts may have as many
     static constexpr int N = (ALL + WAVES - 1) / WAVES;
-    static_assert(ROWS * L::CHUNKS % 64 == 0 && (ALL < WAVES || ALL % WAVES == 0), "loads of a tile");
+    static_assert(ROWS * L::CHUNKS % 64 == 0, "loads of a tile");
+    __device__ __forceinline__ bool has(int n) const { return ALL % WAVES == 0 || n * WAVES + wave < ALL; }
     const char *base;
-    int64_t stride;  // bytes
+    int64_t stride, plane;  // bytes
     int D, wave;
     uint32_t offset[DMA ? N : 1];  // of this lane's loads from the first row's start
     u32x4_t r[DMA ? 1 : N];
 
     __device__ __forceinline__ Loader(const View &x, int64_t row0, int head, int D, int wave)
-        : base(reinterpret_cast<const char *>(x.p) + (row0 * x.row + head * x.head) * L::E), stride(x.row * L::E), D(D),
-          wave(wave) {
+        : base(reinterpret_cast<const char *>(x.p) + (row0 * x.row + head * x.head) * L::E), stride(x.row * L::E),
+          plane(x.plane), D(D), wave(wave) {
         if constexpr (DMA)
 #pragma unroll
             for (int n = 0; n < N; ++n) offset[n] = offset_of(n, ROWS - 1);
     }
+    // Row and chunk of this lane's load n in its plane.
+    __device__ __forceinline__ void place(int n, int &row, int &chunk) const {
+        const int id = (n * WAVES + wave) % EACH * 64 + (threadIdx.x & 63);
+        row = id / L::CHUNKS;
+        chunk = (id % L::CHUNKS) ^ L::key(row);
+    }
     __device__ __forceinline__ uint32_t offset_of(int n, int last) const {
-        const int id = (n * WAVES + wave) * 64 + (threadIdx.x & 63), row = id / L::CHUNKS, end = D * L::E / 16 - 1;
-        const int chunk = (id % L::CHUNKS) ^ L::key(row);
+        int row, chunk;
+        place(n, row, chunk);
+        const int end = D * L::E / 16 - 1;
         return (uint32_t)(row < last ? row : last) * (uint32_t)stride + (chunk < end ? chunk : end) * 16;
     }
     // Rows first .. of which the tensor has `rows` (more than first).
     __device__ __forceinline__ void fetch(char *tile, int first, int rows) {
-        if (ALL < WAVES && wave >= ALL) return;
         const int last = rows - 1 - first;
         const char *from = base + first * stride;
         if constexpr (DMA) {
-            const gemm::rsrc_t src = gemm::buffer(uniform(from));
-            if (last >= ROWS - 1) {
+            const bool whole = last >= ROWS - 1;
+            if constexpr (T == PLANES) {
 #pragma unroll
-                for (int n = 0; n < N; ++n) gemm::dma16(src, offset[n], 0, tile + (n * WAVES + wave) * 1024);
+                for (int n = 0; n < N; ++n) {
+                    if (!has(n)) continue;
+                    const gemm::rsrc_t src = gemm::buffer(uniform(from + (n * WAVES + wave) / EACH * plane));
+                    gemm::dma16(src, whole ? offset[n] : offset_of(n, last), 0, tile + (n * WAVES + wave) * 1024);
+                }
             } else {
+                const gemm::rsrc_t src = gemm::buffer(uniform(from));
+                if (whole) {
 #pragma unroll
-                for (int n = 0; n < N; ++n) gemm::dma16(src, offset_of(n, last), 0, tile + (n * WAVES + wave) * 1024);
+                    for (int n = 0; n < N; ++n)
+                        if (has(n)) gemm::dma16(src, offset[n], 0, tile + (n * WAVES + wave) * 1024);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        if (has(n)) gemm::dma16(src, offset_of(n, last), 0, tile + (n * WAVES + wave) * 1024);
+                }
             }
         } else {
-            const int lane = threadIdx.x & 63;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const int id = (n * WAVES + wave) * 64 + lane, row = id / L::CHUNKS;
-                const int chunk = (id % L::CHUNKS) ^ L::key(row);
-                Raw<BF16, L::VEC> u;
-                load_raw<BF16, L::VEC>(from + (int64_t)(row < last ? row : last) * stride, chunk * L::VEC, D, u);
+                if (!has(n)) continue;
+                int row, chunk;
+                place(n, row, chunk);
+                Raw<T != F32, L::VEC> u;
+                load_raw<T != F32, L::VEC>(from + (int64_t)(row < last ? row : last) * stride, chunk * L::VEC, D, u);
                 r[n] = u32x4_t{u.w[0], u.w[1], u.w[2], u.w[3]};
             }
         }
@@ -381,11 +461,10 @@ struct Loader {
     // What fetch() holds in registers goes to the tile.
     __device__ __forceinline__ void commit(char *tile) const {
         if constexpr (!DMA) {
-            if (ALL < WAVES && wave >= ALL) return;
             const int lane = threadIdx.x & 63;
 #pragma unroll
             for (int n = 0; n < N; ++n)
-                *reinterpret_cast<u32x4_t *>(tile + ((n * WAVES + wave) * 64 + lane) * 16) = r[n];
+                if (has(n)) *reinterpret_cast<u32x4_t *>(tile + ((n * WAVES + wave) * 64 + lane) * 16) = r[n];
         }
     }
 };
@@ -450,12 +529,66 @@ __device__ __forceinline__ void zero_row(void *row, int D, int lane, int lanes) 
     }
 }
 
+// -- fp32 tensors as planes of bf16 --
+
+// [3][rows][heads][DP] of up to four tensors, one of blockIdx.y each, channels from D on zeros.
+struct PlaneJobs {
+    View x[4];
+    uint16_t *out[4];
+    int64_t rows[4];
+    int heads[4];
+};
+namespace {
+__global__ __launch_bounds__(256) void k_planes(PlaneJobs jobs, int D, int DP) {
+    const int j = blockIdx.y, parts = DP / 8;
+    const View x = jobs.x[j];
+    const int64_t all = jobs.rows[j] * jobs.heads[j] * parts;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t rh = i / parts, row = rh / jobs.heads[j];
+        const int c0 = (int)(i - rh * parts) * 8, head = (int)(rh - row * jobs.heads[j]);
+        Raw<false, 8> u;
+        load_raw<false, 8>(reinterpret_cast<const float *>(x.p) + row * x.row + head * x.head, c0, D, u);
+        u32x4_t p[3];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t h, m, l;
+            planes_of(__uint_as_float(u.w[2 * k]), __uint_as_float(u.w[2 * k + 1]), h, m, l);
+            p[0][k] = h, p[1][k] = m, p[2][k] = l;
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<u32x4_t *>(jobs.out[j] + (k * all + i) * 8) = p[k];
+    }
+}
+}  // namespace
+// Lay x out at `at` (its bytes: plane_bytes), and take it from there.
+inline void add_planes(PlaneJobs &jobs, int j, View &x, int64_t rows, int heads, int DP, void *at) {
+    jobs.x[j] = x;
+    jobs.out[j] = static_cast<uint16_t *>(at);
+    jobs.rows[j] = rows;
+    jobs.heads[j] = heads;
+    x = {at, (int64_t)heads * DP, DP, rows * heads * DP * 2};
+}
+inline int64_t plane_bytes(int64_t rows, int heads, int DP) { return 3 * rows * heads * DP * 2; }
+inline hipError_t launch_planes(lattice_dense *D, const PlaneJobs &jobs, int count, int C, int DP) {
+    int64_t most = 1;
+    for (int j = 0; j < count; ++j) most = std::max(most, jobs.rows[j] * jobs.heads[j] * (DP / 8));
+    hipLaunchKernelGGL(k_planes, dim3(grid_for(most, 256, D->cu_count), (unsigned)count), dim3(256), 0, D->stream, jobs, C, DP);
+    return hipGetLastError();
+}
+
 // -- host side --
 
 // Whether a tensor's rows can go to LDS straight.
 inline bool straight(const View &x, int D, int E) {
     return (D * E) % 16 == 0 && (x.row * E) % 16 == 0 && (x.head * E) % 16 == 0 &&
            reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.row * E < ((int64_t)1 << 25);
+}
+// Whether fp32 products go by planes of bf16: where they take the fp32 cores longer than laying
+// the planes out, a launch of its own.  Wider heads' planes leave no room for two workgroups
+// on a CU.
+constexpr double kPlanesFrom = 4e8;
+inline bool planes_pay(const AttendArgs &a, int64_t keys) {
+    return a.D <= 64 && (double)a.q_rows * a.heads * (double)keys * a.D >= kPlanesFrom;
 }
 inline int padded_dim(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 // Slots of tiles of R rows, see find().

@@ -48,7 +48,7 @@ struct Tile {
 
 // The workgroup's tile; false where there is nothing to compute (then rows of no
 // sequence, or without keys, have been seen to).
-template <bool BF16, int KT>
+template <Type T, int KT>
 __device__ __forceinline__ bool tile_of(const Params &a, Tile &t) {
     int unit, slot;
     t.split = blockIdx.y;
@@ -67,8 +67,8 @@ __device__ __forceinline__ bool tile_of(const Params &a, Tile &t) {
                 for (int h = 0; h < t.heads; ++h) {
                     const int64_t row = t.s.q0 + t.first + r;
                     const int head = t.head0 + h;
-                    zero_row<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) +
-                                       (row * a.o.row + head * a.o.head) * (BF16 ? 2 : 4),
+                    zero_row<T == BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) +
+                                       (row * a.o.row + head * a.o.head) * (T == BF16 ? 2 : 4),
                                    a.D, threadIdx.x, blockDim.x);
                     if (a.lse && threadIdx.x == 0) a.lse[head * a.pack.q_rows + row] = -INFINITY;
                 }
@@ -92,8 +92,8 @@ struct Column {
 };
 
 // Take in a block of KB x 32 scores of a column.
-template <bool BF16, int DP, int KB>
-__device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, float c, Right<BF16> (&p)[KB]) {
+template <Type T, int DP, int KB>
+__device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, float c, Right<T> (&p)[KB]) {
     float m = s[0][0];
 #pragma unroll
     for (int b = 0; b < KB; ++b)
@@ -123,7 +123,7 @@ __device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, floa
 }
 
 // Write a column: 4 channels at a time, by f.
-template <bool BF16, int DP>
+template <Type T, int DP>
 __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t row, int head, Column<DP> &col) {
     const float sum = pair_sum(col.sum);
     const float f = col.top == -INFINITY ? 0.f : 1.f / sum;
@@ -136,7 +136,7 @@ __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t r
         else if (a.lse)
             a.lse[head * a.pack.q_rows + row] = lse2 * kLn2;
     }
-    char *o = const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + head * a.o.head) * (BF16 ? 2 : 4);
+    char *o = const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + head * a.o.head) * (T == BF16 ? 2 : 4);
     float *po = a.part_o + (((int64_t)t.split * a.pack.q_rows + row) * a.heads + head) * a.D;
     if (part && col.top == -INFINITY) return;
 #pragma unroll
@@ -151,29 +151,30 @@ __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t r
             if (part)
                 store4<false>(po, c0, a.D, v);
             else
-                store4<BF16>(o, c0, a.D, v);
+                store4<T == BF16>(o, c0, a.D, v);
         }
 }
 
 // Many rows: 4 wavefronts x NQ blocks of 32 columns.  Keys of a block:
-template <bool BF16, int DP>
-constexpr int keys_of_block() { return BF16 ? 64 : 32; }
+template <Type T>
+constexpr int keys_of_block() { return T == F32 ? 32 : 64; }
 
-template <bool BF16, int DP, int NQ, bool DMA>
-__global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(Params a) {
-    using L = Rows<BF16, DP>;
-    constexpr int KT = keys_of_block<BF16, DP>(), KB = KT / 32;
-    constexpr int HALF = KT * L::BYTES, STAGE = 2 * HALF;
+template <Type T, int DP, int NQ, bool DMA>
+__global__ __launch_bounds__(256, T != F32 || NQ * DP <= 64 ? 2 : 1) void k_attend(Params a) {
+    using L = RowsOf<T, DP>;
+    constexpr int KT = keys_of_block<T>(), KB = KT / 32;
+    constexpr int HALF = tile_bytes<T, DP>(KT), STAGE = 2 * HALF;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Tile t;
-    if (!tile_of<BF16, KT>(a, t)) return;
+    if (!tile_of<T, KT>(a, t)) return;
     const int lane = threadIdx.x & 63, wave = gemm::wave_index();
 
     int seen[NQ];
     int64_t row[NQ];
     int head[NQ];
     bool mine[NQ];
-    u32x4_t q[NQ][L::STEPS];
+    Fragments<T, DP> q[NQ];
+    const int D = T == PLANES ? DP : a.D;  // as the operands are laid out
     Column<DP> col[NQ];
     int wave_most = 0;
 #pragma unroll
@@ -189,12 +190,12 @@ __global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(P
         int last = ((wave * NQ + n) * 32 + 31) / t.heads;
         last = last < t.rows ? last : t.rows - 1;
         wave_most = uniform(keys_seen(t.s, a.pack.causal, t.first + last));
-        load_fragments<BF16, DP>(a.q, row[n], head[n], a.D, q[n]);
+        load_fragments<T, DP>(a.q, row[n], head[n], D, q[n]);
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d) clear(col[n].o[d]);
     }
 
-    Loader<BF16, DP, KT, 4, DMA> lk(a.k, t.s.k0, t.kv_head, a.D, wave), lv(a.v, t.s.k0, t.kv_head, a.D, wave);
+    Loader<T, DP, KT, 4, DMA> lk(a.k, t.s.k0, t.kv_head, D, wave), lv(a.v, t.s.k0, t.kv_head, D, wave);
     if (t.t0 < t.t1) {
         lk.fetch(lds, t.t0 * KT, t.s.keys);
         lv.fetch(lds + HALF, t.t0 * KT, t.s.keys);
@@ -219,19 +220,19 @@ __global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(P
 #pragma unroll
                 for (int b = 0; b < KB; ++b) {
                     clear(s[b]);
-                    rows_times<BF16, DP>(now, 32 * b, q[n], s[b]);
+                    rows_times<T, DP, KT>(now, 32 * b, q[n], s[b]);
                 }
-                if (BF16) read_ahead<KB * L::STEPS, KB * L::STEPS, 6>();
+                if (T != F32) read_ahead<kProducts<T> * KB * L::STEPS, kPlanes<T> * KB * L::STEPS, 6>();
                 gemm::sched_barrier();
                 if ((i + 1) * KT > t.least) {
                     seldom();
 #pragma unroll
                     for (int b = 0; b < KB; ++b) mask(s[b], i * KT + 32 * b, seen[n]);
                 }
-                Right<BF16> p[KB];
-                softmax<BF16, DP, KB>(s, col[n], a.c, p);
+                Right<T> p[KB];
+                softmax<T, DP, KB>(s, col[n], a.c, p);
 #pragma unroll
-                for (int b = 0; b < KB; ++b) columns_times<BF16, DP>(now + HALF, 32 * b, p[b], col[n].o);
+                for (int b = 0; b < KB; ++b) columns_times<T, DP, KT>(now + HALF, 32 * b, p[b], col[n].o);
             }
         }
         if (more) {
@@ -245,17 +246,17 @@ __global__ __launch_bounds__(256, BF16 || NQ * DP <= 64 ? 2 : 1) void k_attend(P
     }
 #pragma unroll
     for (int n = 0; n < NQ; ++n)  // a column's two lanes go the same way
-        if (mine[n]) finish<BF16, DP>(a, t, row[n], head[n], col[n]);
+        if (mine[n]) finish<T, DP>(a, t, row[n], head[n], col[n]);
 }
 
 // Few rows: one tile of 32 columns, WAVES wavefronts with their own keys.
-template <bool BF16, int DP>
-constexpr int few_waves() { return Rows<BF16, DP>::BYTES <= 256 ? 4 : 2; }
+template <Type T, int DP>
+constexpr int few_waves() { return RowsOf<T, DP>::BYTES <= 256 ? 4 : 2; }
 
-template <bool BF16, int DP, bool DMA>
-__global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Params a) {
-    using L = Rows<BF16, DP>;
-    constexpr int KT = 32, WAVES = few_waves<BF16, DP>();
+template <Type T, int DP, bool DMA>
+__global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params a) {
+    using L = RowsOf<T, DP>;
+    constexpr int KT = 32, WAVES = few_waves<T, DP>();
     constexpr int HALF = KT * L::BYTES, STAGE = 2 * HALF;
     constexpr int LOADS = 2 * KT * L::CHUNKS / 64;
     constexpr int PITCH = DP + 4;  // floats of a column's output in LDS
@@ -263,7 +264,7 @@ __global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Par
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ float tops[WAVES][32], sums[WAVES][32];
     Tile t;
-    if (!tile_of<BF16, KT>(a, t)) return;
+    if (!tile_of<T, KT>(a, t)) return;
     const int lane = threadIdx.x & 63, wave = gemm::wave_index();
     char *own = lds + wave * 2 * STAGE;
 
@@ -272,13 +273,13 @@ __global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Par
     const int h = c - r * t.heads;
     r = r < t.rows ? r : t.rows - 1;
     const int seen = keys_seen(t.s, a.pack.causal, t.first + r);
-    u32x4_t q[L::STEPS];
+    Fragments<T, DP> q;
     Column<DP> col;
-    load_fragments<BF16, DP>(a.q, t.s.q0 + t.first + r, t.head0 + h, a.D, q);
+    load_fragments<T, DP>(a.q, t.s.q0 + t.first + r, t.head0 + h, a.D, q);
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) clear(col.o[d]);
 
-    Loader<BF16, DP, KT, 1, DMA> lk(a.k, t.s.k0, t.kv_head, a.D, 0), lv(a.v, t.s.k0, t.kv_head, a.D, 0);
+    Loader<T, DP, KT, 1, DMA> lk(a.k, t.s.k0, t.kv_head, a.D, 0), lv(a.v, t.s.k0, t.kv_head, a.D, 0);
     int i = t.t0 + wave;
     if (i < t.t1) {
         lk.fetch(own, i * KT, t.s.keys);
@@ -304,14 +305,14 @@ __global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Par
         }
         f32x16_t s[1];
         clear(s[0]);
-        rows_times<BF16, DP>(now, 0, q, s[0]);
+        rows_times<T, DP, KT>(now, 0, q, s[0]);
         if ((i + 1) * KT > t.least) {
             seldom();
             mask(s[0], i * KT, seen);
         }
-        Right<BF16> p[1];
-        softmax<BF16, DP, 1>(s, col, a.c, p);
-        columns_times<BF16, DP>(now + HALF, 0, p[0], col.o);
+        Right<T> p[1];
+        softmax<T, DP, 1>(s, col, a.c, p);
+        columns_times<T, DP, KT>(now + HALF, 0, p[0], col.o);
         if (more) {
             lk.commit(next);
             lv.commit(next + HALF);
@@ -367,7 +368,7 @@ __global__ __launch_bounds__((64 * few_waves<BF16, DP>())) void k_attend_few(Par
         if (t.parts > 1) {
             if (!none) store4<false>(a.part_o + (((int64_t)t.split * a.pack.q_rows + row) * a.heads + hh) * a.D, c0, a.D, v);
         } else {
-            store4<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + hh * a.o.head) * L::E,
+            store4<T == BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + hh * a.o.head) * L::E,
                          c0, a.D, v);
         }
     }
@@ -422,7 +423,7 @@ __global__ __launch_bounds__(256) void k_join(Params a, int KT) {
 // What a call does.
 struct Plan {
     Params p;
-    bool few, dma;
+    bool few, dma, planes;
     int nq, KT;  // blocks of 32 columns of a wavefront, keys of a block
     int64_t grid, part_o, part_lse;  // grid.x; floats of scratch
 };
@@ -447,7 +448,9 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     const int64_t sequences = a.sequences > 0 ? a.sequences : 1;
     const int64_t rows = (a.q_rows + sequences - 1) / sequences, keys = (a.kv_rows + sequences - 1) / sequences;
     r.few = rows * p.group <= 64;
-    r.nq = !r.few && a.D <= 64 && a.q_rows * a.heads >= (int64_t)256 * 2 * D->cu_count ? 2 : 1;
+    r.planes = !a.bf16 && !r.few && planes_pay(a, keys);
+    // 64 columns a wavefront halve the reads of LDS; registers of three planes hold 32 channels so
+    r.nq = !r.few && a.D <= (r.planes ? 32 : 64) && a.q_rows * a.heads >= (int64_t)256 * 2 * D->cu_count ? 2 : 1;
     const Columns c(p.group, r.few ? 32 : 128 * r.nq);
     p.parts = c.parts;
     p.tile_heads = c.heads;
@@ -456,7 +459,7 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     const int64_t slots = slots_of(a.q_starts, sequences, a.q_rows, p.R);
     p.slots = (int)slots;
     r.grid = unit_grid(p.units, slots);
-    r.KT = r.few ? 32 : a.bf16 ? keys_of_block<true, 32>() : keys_of_block<false, 32>();
+    r.KT = r.few ? 32 : a.bf16 || r.planes ? keys_of_block<BF16>() : keys_of_block<F32>();
     const int64_t tiles = (a.q_rows + p.R - 1) / p.R, width = (int64_t)a.q_rows * a.heads * a.D;
     p.cut = cut_of(p.units * (tiles > sequences ? tiles : sequences), (keys + r.KT - 1) / r.KT, (a.kv_rows + r.KT - 1) / r.KT,
                    r.grid, r.few ? D->cu_count : 2 * D->cu_count, r.few ? 8 : 4, kMostParts / (width * 4 + 1));
@@ -467,45 +470,51 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     return r;
 }
 
-template <bool BF16, int DP, bool DMA>
-hipError_t launch_as(lattice_dense *D, const Plan &r) {
-    using L = Rows<BF16, DP>;
-    const dim3 grid((unsigned)r.grid, (unsigned)r.p.cut.splits);
-    if (r.few) {
-        constexpr int W = few_waves<BF16, DP>(), LDS = W * 2 * 2 * 32 * L::BYTES;
-        static std::atomic<uint64_t> done{0};
-        if (LDS + 1024 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend_few<BF16, DP, DMA>), LDS, done));
-        hipLaunchKernelGGL((k_attend_few<BF16, DP, DMA>), grid, dim3(64 * W), LDS, D->stream, r.p);
-        return hipGetLastError();
-    }
-    constexpr int LDS = 2 * 2 * keys_of_block<BF16, DP>() * L::BYTES;
-    if constexpr (DP <= 64) {
-        if (r.nq == 2) {
-            hipLaunchKernelGGL((k_attend<BF16, DP, 2, DMA>), grid, dim3(256), LDS, D->stream, r.p);
-            return hipGetLastError();
-        }
-    }
+template <Type T, int DP, int NQ, bool DMA>
+hipError_t launch_many(lattice_dense *D, const Plan &r, dim3 grid) {
+    constexpr int LDS = 2 * 2 * tile_bytes<T, DP>(keys_of_block<T>());
     static std::atomic<uint64_t> done{0};
-    if (LDS > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend<BF16, DP, 1, DMA>), LDS, done));
-    hipLaunchKernelGGL((k_attend<BF16, DP, 1, DMA>), grid, dim3(256), LDS, D->stream, r.p);
+    if (LDS > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend<T, DP, NQ, DMA>), LDS, done));
+    hipLaunchKernelGGL((k_attend<T, DP, NQ, DMA>), grid, dim3(256), LDS, D->stream, r.p);
     return hipGetLastError();
 }
 
-template <bool BF16, int DP>
-hipError_t launch_dim(lattice_dense *D, const Plan &r) {
-    return r.dma ? launch_as<BF16, DP, true>(D, r) : launch_as<BF16, DP, false>(D, r);
+template <Type T, int DP, bool DMA>
+hipError_t launch_as(lattice_dense *D, const Plan &r) {
+    const dim3 grid((unsigned)r.grid, (unsigned)r.p.cut.splits);
+    if constexpr (T != PLANES)
+        if (r.few) {
+            constexpr int W = few_waves<T, DP>(), LDS = W * 2 * 2 * 32 * RowsOf<T, DP>::BYTES;
+            static std::atomic<uint64_t> done{0};
+            if (LDS + 1024 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend_few<T, DP, DMA>), LDS, done));
+            hipLaunchKernelGGL((k_attend_few<T, DP, DMA>), grid, dim3(64 * W), LDS, D->stream, r.p);
+            return hipGetLastError();
+        }
+    if constexpr (DP <= 64 && (T != PLANES || DP == 32))
+        if (r.nq == 2) return launch_many<T, DP, 2, DMA>(D, r, grid);
+    return launch_many<T, DP, 1, DMA>(D, r, grid);
 }
 
-template <bool BF16>
+template <Type T, int DP>
+hipError_t launch_dim(lattice_dense *D, const Plan &r) {
+    if constexpr (T != PLANES)
+        if (!r.dma) return launch_as<T, DP, false>(D, r);
+    return launch_as<T, DP, true>(D, r);
+}
+
+template <Type T>
 hipError_t launch_type(lattice_dense *D, const Plan &r) {
-    switch (padded_dim(r.p.D)) {
-        case 32: TRY((launch_dim<BF16, 32>(D, r))); break;
-        case 64: TRY((launch_dim<BF16, 64>(D, r))); break;
-        default: TRY((launch_dim<BF16, 128>(D, r))); break;
+    const int dp = padded_dim(r.p.D);
+    if (dp == 32) {
+        TRY((launch_dim<T, 32>(D, r)));
+    } else if (dp == 64) {
+        TRY((launch_dim<T, 64>(D, r)));
+    } else if constexpr (T != PLANES) {
+        TRY((launch_dim<T, 128>(D, r)));
     }
     if (r.p.cut.splits == 1) return hipSuccess;
-    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)r.p.slots, (unsigned)((r.p.R + kJoinRows - 1) / kJoinRows)), dim3(256), 0,
-                       D->stream, r.p, r.KT);
+    hipLaunchKernelGGL((k_join<T == BF16>), dim3((unsigned)r.p.slots, (unsigned)((r.p.R + kJoinRows - 1) / kJoinRows)),
+                       dim3(256), 0, D->stream, r.p, r.KT);
     return hipGetLastError();
 }
 
@@ -516,6 +525,11 @@ int64_t attention_scratch(const lattice_dense *D, const AttendArgs &a) {
     ScratchLayout s;
     s.take(r.part_o * 4);
     s.take(r.part_lse * 4);
+    if (r.planes) {
+        const int dp = padded_dim(a.D);
+        s.take(plane_bytes(a.q_rows, a.heads, dp));
+        s.take(2 * plane_bytes(a.kv_rows, a.kv_heads, dp));
+    }
     return s.bytes;
 }
 
@@ -529,5 +543,15 @@ hipError_t launch_attention(lattice_dense *D, const AttendArgs &a) {
     char *ws = static_cast<char *>(D->ws);
     r.p.part_o = reinterpret_cast<float *>(ws + s.take(r.part_o * 4));
     r.p.part_lse = reinterpret_cast<float *>(ws + s.take(r.part_lse * 4));
-    return a.bf16 ? launch_type<true>(D, r) : launch_type<false>(D, r);
+    if (a.bf16) return launch_type<BF16>(D, r);
+    if (!r.planes) return launch_type<F32>(D, r);
+    const int dp = padded_dim(a.D);
+    const int64_t kv = plane_bytes(a.kv_rows, a.kv_heads, dp);
+    PlaneJobs jobs = {};
+    add_planes(jobs, 0, r.p.q, a.q_rows, a.heads, dp, ws + s.take(plane_bytes(a.q_rows, a.heads, dp)));
+    char *at = ws + s.take(2 * kv);
+    add_planes(jobs, 1, r.p.k, a.kv_rows, a.kv_heads, dp, at);
+    add_planes(jobs, 2, r.p.v, a.kv_rows, a.kv_heads, dp, at + kv);
+    TRY(launch_planes(D, jobs, 3, a.D, dp));
+    return launch_type<PLANES>(D, r);
 }

@@ -23,7 +23,8 @@ using namespace attend;
 
 struct Params {
     Packing pack;
-    View q, k, v, o, g;
+    View q, k, v, g;
+    View o, g_stored;         // as they are stored
     void *dq, *dk, *dv;       // without gaps
     const float *lse;         // [heads][rows]
     float *delta;             // the same
@@ -37,27 +38,27 @@ struct Params {
     int32_t *status;
 };
 
-// This lane's part of a row (see load_fragments) to its place in a tile.
-template <bool BF16, int DP>
+// This lane's part of a bf16 row to its place in a tile.
+template <int DP>
 __device__ __forceinline__ void load_fragments_to(const View &x, int64_t row, int head, int D, char *tile) {
-    using L = Rows<BF16, DP>;
+    using L = RowsOf<BF16, DP>;
     const int lane = threadIdx.x & 63;
-    u32x4_t f[L::STEPS];
+    Fragments<BF16, DP> f;
     load_fragments<BF16, DP>(x, row, head, D, f);
 #pragma unroll
     for (int t = 0; t < L::STEPS; ++t)
-        *reinterpret_cast<u32x4_t *>(tile + L::at(lane & 31, 2 * t + (lane >> 5))) = f[t];
+        *reinterpret_cast<u32x4_t *>(tile + L::at(lane & 31, 2 * t + (lane >> 5))) = f.v[0][t];
 }
 
-// acc = (32 rows of one tile) (32 rows of another)^T.
-template <bool BF16, int DP>
+// acc = (32 rows of one bf16 tile) (32 rows of another)^T.
+template <int DP>
 __device__ __forceinline__ void rows_times_rows(const char *a, const char *b, f32x16_t &acc) {
-    using L = Rows<BF16, DP>;
+    using L = RowsOf<BF16, DP>;
     const int lane = threadIdx.x & 63, row = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int t = 0; t < L::STEPS; ++t) {
         const int at = L::at(row, 2 * t + h);
-        mma<BF16>(*reinterpret_cast<const u32x4_t *>(a + at), *reinterpret_cast<const u32x4_t *>(b + at), acc);
+        mma<true>(*reinterpret_cast<const u32x4_t *>(a + at), *reinterpret_cast<const u32x4_t *>(b + at), acc);
     }
 }
 
@@ -83,17 +84,19 @@ __device__ __forceinline__ void add_groups(char *lds, int wave, int group, f32x1
             }
 }
 
+// This lane's share of the product of two rows as they are stored.
 template <bool BF16>
-__device__ __forceinline__ float dot(const u32x4_t &a, const u32x4_t &b) {
+__device__ __forceinline__ float dot(const View &x, const View &y, int64_t row, int head, int D) {
+    constexpr int VEC = BF16 ? 8 : 4, E = BF16 ? 2 : 4;
+    const char *a = reinterpret_cast<const char *>(x.p) + (row * x.row + head * x.head) * E;
+    const char *b = reinterpret_cast<const char *>(y.p) + (row * y.row + head * y.head) * E;
     float s = 0.f;
+    for (int c0 = VEC * ((threadIdx.x & 63) >> 5); c0 < D; c0 += 2 * VEC) {
+        float u[VEC], v[VEC];
+        load_row<BF16, VEC>(a, c0, D, u);
+        load_row<BF16, VEC>(b, c0, D, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (BF16) {
-            s = fmaf(__uint_as_float(a[i] << 16), __uint_as_float(b[i] << 16), s);
-            s = fmaf(__uint_as_float(a[i] & 0xffff0000u), __uint_as_float(b[i] & 0xffff0000u), s);
-        } else {
-            s = fmaf(__uint_as_float(a[i]), __uint_as_float(b[i]), s);
-        }
+        for (int i = 0; i < VEC; ++i) s = fmaf(u[i], v[i], s);
     }
     return s;
 }
@@ -123,10 +126,12 @@ __device__ __forceinline__ void store_column(void *out, float *part, int64_t at,
 // By queries: 4 wavefronts of 32 columns, blocks of keys of
 constexpr int kKeyBlock = 32;
 constexpr int kShort = 256;  // keys of a tile whose delta is made from the scores
-template <bool BF16, int DP, bool DMA>
-__global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Params a) {
-    using L = Rows<BF16, DP>;
-    constexpr int KT = kKeyBlock, HALF = KT * L::BYTES, STAGE = 2 * HALF;
+template <Type T, int DP, bool DMA>
+__global__ __launch_bounds__(256, T != F32 || DP < 128 ? 2 : 1) void k_by_queries(Params a) {
+    using L = RowsOf<T, DP>;
+    constexpr int KT = kKeyBlock, HALF = tile_bytes<T, DP>(KT), STAGE = 2 * HALF;
+    constexpr bool OUT16 = T == BF16;
+    const int D = T == PLANES ? DP : a.D;  // as the operands are laid out
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int unit, slot, first;
     const int split = blockIdx.y;
@@ -140,8 +145,8 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
         if (a.zero_rest && split == 0)
             for (int r = 0; r < rows; ++r)
                 for (int h = 0; h < heads; ++h)
-                    zero_row<BF16>(reinterpret_cast<char *>(a.dq) +
-                                       ((s.q0 + first + r) * a.heads + head0 + h) * a.D * L::E,
+                    zero_row<OUT16>(reinterpret_cast<char *>(a.dq) +
+                                       ((s.q0 + first + r) * a.heads + head0 + h) * a.D * (OUT16 ? 2 : 4),
                                    a.D, threadIdx.x, 256);
         return;
     }
@@ -161,17 +166,10 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
     last = last < rows ? last : rows - 1;
     const int wave_most = uniform(keys_seen(s, a.pack.causal, first + last));
 
-    u32x4_t q[L::STEPS], g[L::STEPS];
-    float delta = 0.f;
-    {
-        u32x4_t o[L::STEPS];
-        load_fragments<BF16, DP>(a.g, row, head, a.D, g);
-        load_fragments<BF16, DP>(a.o, row, head, a.D, o);
-#pragma unroll
-        for (int t = 0; t < L::STEPS; ++t) delta += dot<BF16>(g[t], o[t]);
-        delta = pair_sum(delta);
-    }
-    load_fragments<BF16, DP>(a.q, row, head, a.D, q);
+    Fragments<T, DP> q, g;
+    float delta = pair_sum(dot<OUT16>(a.g_stored, a.o, row, head, a.D));
+    load_fragments<T, DP>(a.g, row, head, D, g);
+    load_fragments<T, DP>(a.q, row, head, D, q);
     const float lse = a.lse[head * a.pack.q_rows + row];
     const float lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
 
@@ -179,7 +177,7 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) clear(dq[d]);
     const int t0 = (int)((int64_t)n * split / parts), t1 = (int)((int64_t)n * (split + 1) / parts);
-    Loader<BF16, DP, KT, 4, DMA> lk(a.k, s.k0, kv_head, a.D, wave), lv(a.v, s.k0, kv_head, a.D, wave);
+    Loader<T, DP, KT, 4, DMA> lk(a.k, s.k0, kv_head, D, wave), lv(a.v, s.k0, kv_head, D, wave);
     // blocks [from, to); ONLY_DELTA: no more than this lane's share of sum p (g . v) is made
     float sum = 0.f;
     auto blocks = [&](int from, int to, auto only_delta) {
@@ -202,9 +200,9 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
                 gemm::sched_barrier();
                 clear(x);
                 clear(y);
-                rows_times<BF16, DP>(now, 0, q, x);
-                rows_times<BF16, DP>(now + HALF, 0, g, y);
-                if (BF16) read_ahead<2 * L::STEPS, 2 * L::STEPS, 6>();
+                rows_times<T, DP, KT>(now, 0, q, x);
+                rows_times<T, DP, KT>(now + HALF, 0, g, y);
+                if (T != F32) read_ahead<2 * kProducts<T> * L::STEPS, 2 * kPlanes<T> * L::STEPS, 6>();
                 gemm::sched_barrier();
                 if ((i + 1) * KT > least) {
                     seldom();
@@ -216,9 +214,9 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
                 } else {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) x[e] = exp2_(fmaf(x[e], a.c, -lse2)) * (y[e] - delta);
-                    Right<BF16> t;
+                    Right<T> t;
                     t.set(x);
-                    columns_times<BF16, DP>(now, 0, t, dq);
+                    columns_times<T, DP, KT>(now, 0, t, dq);
                 }
             }
             if (more) {
@@ -234,14 +232,14 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
     // Of few keys the outputs are as large as the values, and what rounding them to bf16 took
     // from delta shows in dq and dk (2.6e-3 of them for sequences of 1 to 558 rows, 2.3e-3 so;
     // rounding the results alone makes 1.7e-3).  Of many keys it does not.
-    if (BF16 && most <= kShort) {
+    if (T == BF16 && most <= kShort) {
         blocks(0, n, std::true_type{});
         delta = pair_sum(sum);
         gemm::wait_and_barrier<0>();  // the blocks have been read
     }
     if (mine && lane < 32 && split == 0) a.delta[head * a.pack.q_rows + row] = delta;
     blocks(t0, t1, std::false_type{});
-    if (mine) store_column<BF16, DP>(a.dq, mine_part, row * a.heads + head, a.D, dq, a.scale);
+    if (mine) store_column<OUT16, DP>(a.dq, mine_part, row * a.heads + head, a.D, dq, a.scale);
 }
 
 // By keys: 128 keys, 32 for each of 4 wavefronts, or of 4 of each of QW groups of
@@ -250,12 +248,12 @@ __global__ __launch_bounds__(256, BF16 || DP < 128 ? 2 : 1) void k_by_queries(Pa
 // With K and V as right operands in registers and both results there, 128 channels take
 // 300 registers, one wavefront a SIMD, and nothing runs beside its exponentials and
 // waits (283 TFLOP/s); V is read from LDS instead (KV_LDS), which leaves room for two.
-template <bool BF16, int DP>
+template <Type T, int DP>
 struct ByKeys {
-    static constexpr bool KV_LDS = BF16 && DP == 128;
-    static constexpr int QW = BF16 ? 2 : 1;
+    static constexpr bool KV_LDS = T == BF16 && DP == 128;
+    static constexpr int QW = T != F32 ? 2 : 1;
     static constexpr int WAVES = 4 * QW, THREADS = 64 * WAVES;
-    static constexpr int HALF = 32 * Rows<BF16, DP>::BYTES, STAGE = 2 * HALF;   // of a group
+    static constexpr int HALF = tile_bytes<T, DP>(32), STAGE = 2 * HALF;   // of a group
     static constexpr int KV_BYTES = KV_LDS ? 8 * HALF : 0;
     static constexpr int LDS = 2 * QW * STAGE + KV_BYTES;
     // a group's result in LDS: 4 wavefronts of 32 x DP
@@ -273,10 +271,12 @@ __device__ __forceinline__ int row_blocks(const Params &a, const Sequence &s, in
     return r < s.q_len ? (s.q_len - r + kRowBlock - 1) / kRowBlock : 0;
 }
 
-template <bool BF16, int DP, bool DMA>
-__global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_by_keys(Params a) {
-    using L = Rows<BF16, DP>;
-    using B = ByKeys<BF16, DP>;
+template <Type T, int DP, bool DMA>
+__global__ __launch_bounds__((ByKeys<T, DP>::THREADS), T != F32 ? 2 : 1) void k_by_keys(Params a) {
+    using L = RowsOf<T, DP>;
+    using B = ByKeys<T, DP>;
+    constexpr bool OUT16 = T == BF16;
+    const int D = T == PLANES ? DP : a.D;  // as the operands are laid out
     constexpr int QT = kRowBlock, QW = B::QW;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ __attribute__((aligned(16))) float stats[2][QW][2][QT];  // lse (of 2) and delta of the blocks' rows
@@ -293,9 +293,9 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
         const int end = s.kv_len - first < a.R ? s.kv_len : first + a.R;
         if (a.zero_rest && split == 0)
             for (int j = first; j < end; ++j) {
-                const int64_t at = ((s.k0 + j) * a.kv_heads + kv_head) * a.D * L::E;
-                zero_row<BF16>(reinterpret_cast<char *>(a.dk) + at, a.D, threadIdx.x, B::THREADS);
-                zero_row<BF16>(reinterpret_cast<char *>(a.dv) + at, a.D, threadIdx.x, B::THREADS);
+                const int64_t at = ((s.k0 + j) * a.kv_heads + kv_head) * a.D * (OUT16 ? 2 : 4);
+                zero_row<OUT16>(reinterpret_cast<char *>(a.dk) + at, a.D, threadIdx.x, B::THREADS);
+                zero_row<OUT16>(reinterpret_cast<char *>(a.dv) + at, a.D, threadIdx.x, B::THREADS);
             }
         return;
     }
@@ -308,16 +308,16 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
 
     const bool counts = key < s.keys;
     const int64_t row = s.k0 + (counts ? key : s.keys - 1);
-    u32x4_t k[B::KV_LDS ? 1 : L::STEPS], v[B::KV_LDS ? 1 : L::STEPS];
+    Fragments<T, DP> k, v;
     char *k_tile = lds + 2 * QW * B::STAGE + 2 * wave * B::HALF, *v_tile = k_tile + B::HALF;
     if constexpr (B::KV_LDS) {
         if (group == 0)
-            load_fragments_to<BF16, DP>(a.k, row, kv_head, a.D, k_tile);
+            load_fragments_to<DP>(a.k, row, kv_head, D, k_tile);
         else
-            load_fragments_to<BF16, DP>(a.v, row, kv_head, a.D, v_tile);
+            load_fragments_to<DP>(a.v, row, kv_head, D, v_tile);
     } else {
-        load_fragments<BF16, DP>(a.k, row, kv_head, a.D, k);
-        load_fragments<BF16, DP>(a.v, row, kv_head, a.D, v);
+        load_fragments<T, DP>(a.k, row, kv_head, D, k);
+        load_fragments<T, DP>(a.v, row, kv_head, D, v);
     }
     f32x16_t dk[DP / 32], dv[DP / 32];
 #pragma unroll
@@ -333,7 +333,7 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
     int64_t i = begin + group;
     int head = per > 0 ? (int)(i / per) : 0, at = per > 0 ? (int)(i % per) : 0;
     float stat = 0.f;  // lanes 0 .. 31 of a group's first wavefront: lse, the others delta
-    Loader<BF16, DP, QT, 4, DMA> lq(a.q, s.q0, kv_head * a.group, a.D, wave), lg(a.g, s.q0, kv_head * a.group, a.D, wave);
+    Loader<T, DP, QT, 4, DMA> lq(a.q, s.q0, kv_head * a.group, D, wave), lg(a.g, s.q0, kv_head * a.group, D, wave);
     const int64_t q_step = a.q.head * L::E, g_step = a.g.head * L::E;
     const char *q_base = lq.base, *g_base = lg.base;
     char *own = lds + group * 2 * B::STAGE;
@@ -376,13 +376,13 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
             clear(x);
             clear(y);
             if constexpr (B::KV_LDS) {
-                rows_times_rows<BF16, DP>(now, k_tile, x);
-                rows_times_rows<BF16, DP>(now + B::HALF, v_tile, y);
+                rows_times_rows<DP>(now, k_tile, x);
+                rows_times_rows<DP>(now + B::HALF, v_tile, y);
             } else {
-                rows_times<BF16, DP>(now, 0, k, x);
-                rows_times<BF16, DP>(now + B::HALF, 0, v, y);
+                rows_times<T, DP, QT>(now, 0, k, x);
+                rows_times<T, DP, QT>(now + B::HALF, 0, v, y);
             }
-            if (BF16) read_ahead<2 * L::STEPS, (B::KV_LDS ? 4 : 2) * L::STEPS, 8>();
+            if (T != F32) read_ahead<2 * kProducts<T> * L::STEPS, (B::KV_LDS ? 4 : 2 * kPlanes<T>) * L::STEPS, 8>();
             gemm::sched_barrier();
             if (r < all_see) {
                 seldom();
@@ -403,11 +403,11 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
                     y[e] = x[e] * (y[e] - ds[k4]);
                 }
             }
-            Right<BF16> p;
+            Right<T> p;
             p.set(x);
-            columns_times<BF16, DP>(now + B::HALF, 0, p, dv);
+            columns_times<T, DP, QT>(now + B::HALF, 0, p, dv);
             p.set(y);
-            columns_times<BF16, DP>(now, 0, p, dk);
+            columns_times<T, DP, QT>(now, 0, p, dk);
         }
         if (more) commit(next, 1 - stage.value);
     };
@@ -423,11 +423,11 @@ __global__ __launch_bounds__((ByKeys<BF16, DP>::THREADS), BF16 ? 2 : 1) void k_b
     const int64_t at_row = (s.k0 + key) * a.kv_heads + kv_head;
     if (counts) {
         float *pk = parts > 1 ? a.part + split * 2 * size : nullptr, *pv = pk ? pk + size : nullptr;
-        store_column<BF16, DP>(a.dk, pk, at_row, a.D, dk, a.scale);
-        store_column<BF16, DP>(a.dv, pv, at_row, a.D, dv, 1.f);
+        store_column<OUT16, DP>(a.dk, pk, at_row, a.D, dk, a.scale);
+        store_column<OUT16, DP>(a.dv, pv, at_row, a.D, dv, 1.f);
     } else if (a.zero_rest && split == 0 && key < s.kv_len && key < first + a.R) {
-        zero_row<BF16>(reinterpret_cast<char *>(a.dk) + at_row * a.D * L::E, a.D, h, 2);
-        zero_row<BF16>(reinterpret_cast<char *>(a.dv) + at_row * a.D * L::E, a.D, h, 2);
+        zero_row<OUT16>(reinterpret_cast<char *>(a.dk) + at_row * a.D * (OUT16 ? 2 : 4), a.D, h, 2);
+        zero_row<OUT16>(reinterpret_cast<char *>(a.dv) + at_row * a.D * (OUT16 ? 2 : 4), a.D, h, 2);
     }
 }
 
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256) void k_join(Params a, bool by_keys) {
 // The two launches of a call, with their joins.
 struct Plan {
     Params by_queries, by_keys;
-    bool dma_queries, dma_keys;
+    bool dma_queries, dma_keys, planes;
     int64_t grid_queries, grid_keys, part;  // floats that the larger of the joins needs
 };
 
@@ -477,7 +477,7 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     p.k = {a.k, a.k_row, a.k_head};
     p.v = {a.v, a.v_row, a.v_head};
     p.o = {a.out, a.o_row, a.o_head};
-    p.g = {a.grad, a.g_row, a.g_head};
+    p.g = p.g_stored = {a.grad, a.g_row, a.g_head};
     p.dq = a.grad_q;
     p.dk = a.grad_k;
     p.dv = a.grad_v;
@@ -496,6 +496,7 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     r.dma_keys = straight(p.q, a.D, E) && straight(p.g, a.D, E);
     const int64_t sequences = a.sequences > 0 ? a.sequences : 1;
     const int64_t rows = (a.q_rows + sequences - 1) / sequences, keys = (a.kv_rows + sequences - 1) / sequences;
+    r.planes = !a.bf16 && planes_pay(a, keys);
     {
         const Columns c(p.group, 128);
         p.parts = c.parts;
@@ -524,23 +525,23 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     return r;
 }
 
-template <bool BF16, int DP, bool DMA>
+template <Type T, int DP, bool DMA>
 hipError_t by_queries(lattice_dense *D, const Plan &r) {
-    constexpr int LDS = 2 * 2 * 32 * Rows<BF16, DP>::BYTES;
+    constexpr int LDS = 2 * 2 * tile_bytes<T, DP>(kKeyBlock);
     static_assert(LDS <= 64 * 1024, "LDS");
-    hipLaunchKernelGGL((k_by_queries<BF16, DP, DMA>), dim3((unsigned)r.grid_queries, (unsigned)r.by_queries.cut.splits),
+    hipLaunchKernelGGL((k_by_queries<T, DP, DMA>), dim3((unsigned)r.grid_queries, (unsigned)r.by_queries.cut.splits),
                        dim3(256), LDS, D->stream, r.by_queries);
     return hipGetLastError();
 }
 
-template <bool BF16, int DP, bool DMA>
+template <Type T, int DP, bool DMA>
 hipError_t by_keys(lattice_dense *D, const Plan &r) {
-    using B = ByKeys<BF16, DP>;
+    using B = ByKeys<T, DP>;
     constexpr int LDS = B::LDS;
     static std::atomic<uint64_t> done{0};
-    if (LDS + 2048 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_by_keys<BF16, DP, DMA>), LDS, done));
-    hipLaunchKernelGGL((k_by_keys<BF16, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.cut.splits), dim3(B::THREADS), LDS,
-                       D->stream, r.by_keys);
+    if (LDS + 2048 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_by_keys<T, DP, DMA>), LDS, done));
+    hipLaunchKernelGGL((k_by_keys<T, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.cut.splits),
+                       dim3(B::THREADS), LDS, D->stream, r.by_keys);
     return hipGetLastError();
 }
 
@@ -552,26 +553,32 @@ hipError_t join(lattice_dense *D, const Params &p, bool keys) {
     return hipGetLastError();
 }
 
-template <bool BF16, int DP>
+template <Type T, int DP>
 hipError_t launch_dim(lattice_dense *D, const Plan &r) {
     if (r.by_queries.pack.q_rows > 0) {
-        TRY(r.dma_queries ? (by_queries<BF16, DP, true>(D, r)) : (by_queries<BF16, DP, false>(D, r)));
-        TRY(join<BF16>(D, r.by_queries, false));
+        if constexpr (T == PLANES)
+            TRY((by_queries<T, DP, true>(D, r)));
+        else
+            TRY(r.dma_queries ? (by_queries<T, DP, true>(D, r)) : (by_queries<T, DP, false>(D, r)));
+        TRY(join<T == BF16>(D, r.by_queries, false));
     }
     if (r.by_queries.pack.kv_rows > 0) {
-        TRY(r.dma_keys ? (by_keys<BF16, DP, true>(D, r)) : (by_keys<BF16, DP, false>(D, r)));
-        TRY(join<BF16>(D, r.by_keys, true));
+        if constexpr (T == PLANES)
+            TRY((by_keys<T, DP, true>(D, r)));
+        else
+            TRY(r.dma_keys ? (by_keys<T, DP, true>(D, r)) : (by_keys<T, DP, false>(D, r)));
+        TRY(join<T == BF16>(D, r.by_keys, true));
     }
     return hipSuccess;
 }
 
-template <bool BF16>
+template <Type T>
 hipError_t launch_type(lattice_dense *D, const Plan &r) {
-    switch (padded_dim(r.by_queries.D)) {
-        case 32: return launch_dim<BF16, 32>(D, r);
-        case 64: return launch_dim<BF16, 64>(D, r);
-        default: return launch_dim<BF16, 128>(D, r);
-    }
+    const int dp = padded_dim(r.by_queries.D);
+    if (dp == 32) return launch_dim<T, 32>(D, r);
+    if constexpr (T != PLANES)
+        if (dp == 128) return launch_dim<T, 128>(D, r);
+    return launch_dim<T, 64>(D, r);
 }
 
 }  // namespace
@@ -581,6 +588,11 @@ int64_t attention_backward_scratch(const lattice_dense *D, const AttendArgs &a) 
     ScratchLayout s;
     s.take(a.q_rows * a.heads * 4);
     s.take(r.part * 4);
+    if (r.planes) {
+        const int dp = padded_dim(a.D);
+        s.take(2 * plane_bytes(a.q_rows, a.heads, dp));
+        s.take(2 * plane_bytes(a.kv_rows, a.kv_heads, dp));
+    }
     return s.bytes;
 }
 
@@ -595,5 +607,19 @@ hipError_t launch_attention_backward(lattice_dense *D, const AttendArgs &a) {
     char *ws = static_cast<char *>(D->ws);
     r.by_queries.delta = r.by_keys.delta = reinterpret_cast<float *>(ws + s.take(a.q_rows * a.heads * 4));
     r.by_queries.part = r.by_keys.part = reinterpret_cast<float *>(ws + s.take(r.part * 4));
-    return a.bf16 ? launch_type<true>(D, r) : launch_type<false>(D, r);
+    if (a.bf16) return launch_type<BF16>(D, r);
+    if (!r.planes) return launch_type<F32>(D, r);
+    Params &p = r.by_queries;
+    const int dp = padded_dim(a.D);
+    const int64_t q = plane_bytes(a.q_rows, a.heads, dp), kv = plane_bytes(a.kv_rows, a.kv_heads, dp);
+    char *at_q = ws + s.take(2 * q), *at_kv = ws + s.take(2 * kv);
+    PlaneJobs jobs = {};
+    add_planes(jobs, 0, p.q, a.q_rows, a.heads, dp, at_q);
+    add_planes(jobs, 1, p.g, a.q_rows, a.heads, dp, at_q + q);
+    add_planes(jobs, 2, p.k, a.kv_rows, a.kv_heads, dp, at_kv);
+    add_planes(jobs, 3, p.v, a.kv_rows, a.kv_heads, dp, at_kv + kv);
+    TRY(launch_planes(D, jobs, 4, a.D, dp));
+    Params &b = r.by_keys;
+    b.q = p.q, b.g = p.g, b.k = p.k, b.v = p.v;
+    return launch_type<PLANES>(D, r);
 }

@@ -188,6 +188,28 @@ def test_far_keys_are_split(ops, dtype):  # noqa: F811
               kv_starts=starts_of(8000, 1000))
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,heads,kv_heads,lengths", [(20, 8, 2, (2000, 1, 0, 1400)), (32, 4, 4, (2500,)), (36, 6, 1, (1900, 33)),
+                                                      (64, 3, 3, (1, 2100, 64))])
+def test_many_rows(ops, C, heads, kv_heads, lengths, dtype, causal):  # noqa: F811
+    """Enough of them for fp32 products to go by planes of bf16, of strided heads."""
+    n = sum(lengths)
+    qkv = rand(1, n, heads + 2 * kv_heads, C, dtype=dtype)
+    q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:]
+    s = starts_of(*lengths)
+    at = s.tolist()
+    check_all(ops, q, k, v, [(a, m, a, m) for a, m in zip(at, lengths)], causal, g=rand(2, n, heads, C, dtype=dtype),
+              q_starts=s)
+
+
+@pytest.mark.parametrize("size", [1e-12, 1e12])
+def test_many_rows_of_small_and_large_values(ops, size):  # noqa: F811
+    n = 2500
+    q, k, v, g = (rand(i, n, 4, 32) for i in range(4))
+    check_all(ops, q * size, k / size, v * size, [(0, n, 0, n)], True, g=g / size)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("C", [36, 64])
 def test_strides(ops, C, dtype):  # noqa: F811
