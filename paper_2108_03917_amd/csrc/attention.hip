@@ -287,11 +287,9 @@ __global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params
         lk.commit(own);
         lv.commit(own + HALF);
     }
-    int stage = 0;
-    for (; i < t.t1; i += WAVES) {
-        char *now = own + stage * STAGE, *next = own + (stage ^ 1) * STAGE;
+    auto block = [&](const char *__restrict now, char *__restrict next) {
         const bool more = i + WAVES < t.t1;
-        // what lies in `next` has been read: its products are done
+        // what lay in `next` has been read
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) {
             lk.fetch(next, (i + WAVES) * KT, t.s.keys);
@@ -304,8 +302,11 @@ __global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
         f32x16_t s[1];
+        gemm::sched_barrier();
         clear(s[0]);
         rows_times<T, DP, KT>(now, 0, q, s[0]);
+        if (T != F32) read_ahead<L::STEPS, L::STEPS, 8>();
+        gemm::sched_barrier();
         if ((i + 1) * KT > t.least) {
             seldom();
             mask(s[0], i * KT, seen);
@@ -317,7 +318,11 @@ __global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params
             lk.commit(next);
             lv.commit(next + HALF);
         }
-        stage ^= 1;
+        i += WAVES;
+    };
+    while (i < t.t1) {
+        block(own, own + STAGE);
+        if (i < t.t1) block(own + STAGE, own);
     }
     // join: every wavefront's columns to LDS (its own part, whose blocks are done with)
     const float sum = pair_sum(col.sum);

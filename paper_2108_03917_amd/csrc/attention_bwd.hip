@@ -333,6 +333,7 @@ __global__ __launch_bounds__((ByKeys<T, DP>::THREADS), T != F32 ? 2 : 1) void k_
     int64_t i = begin + group;
     int head = per > 0 ? (int)(i / per) : 0, at = per > 0 ? (int)(i % per) : 0;
     float stat = 0.f;  // lanes 0 .. 31 of a group's first wavefront: lse, the others delta
+    bool inside = false;
     Loader<T, DP, QT, 4, DMA> lq(a.q, s.q0, kv_head * a.group, D, wave), lg(a.g, s.q0, kv_head * a.group, D, wave);
     const int64_t q_step = a.q.head * L::E, g_step = a.g.head * L::E;
     const char *q_base = lq.base, *g_base = lg.base;
@@ -346,20 +347,26 @@ __global__ __launch_bounds__((ByKeys<T, DP>::THREADS), T != F32 ? 2 : 1) void k_
         if (wave == 0) {
             const int rr = r + (lane & 31);
             const int64_t where = (kv_head * a.group + head) * a.pack.q_rows + s.q0 + (rr < s.q_len ? rr : s.q_len - 1);
-            const float x = h == 0 ? a.lse[where] : a.delta[where];
-            stat = h == 0 ? (rr < s.q_len && x != -INFINITY ? x * kLog2e : INFINITY) : (rr < s.q_len ? x : 0.f);
+            stat = (h == 0 ? a.lse : a.delta)[where];
+            inside = rr < s.q_len;
         }
     };
     auto commit = [&](char *to, int stage) {
         lq.commit(to);
         lg.commit(to + B::HALF);
-        if (wave == 0) stats[stage][group][h][lane & 31] = stat;
+        // (made here and not where it is loaded: that would wait for the blocks' loads)
+        if (wave == 0)
+            stats[stage][group][h][lane & 31] =
+                h == 0 ? (inside && stat != -INFINITY ? stat * kLog2e : INFINITY) : (inside ? stat : 0.f);
     };
     if (i < end) {
         fetch(own, head, at);
         commit(own, 0);
     }
-    auto block = [&](const char *__restrict now, char *__restrict next, auto stage) {
+    // (all that is read in LDS is told to be apart from where the next block goes: the reads
+    // would wait for its loads)
+    auto block = [&](const char *__restrict now, char *__restrict next, const char *__restrict k_own,
+                     const char *__restrict v_own, const float *__restrict stats_now, auto stage) {
         gemm::wait_and_barrier<0>();
         const bool here = i < end, more = i + QW < end;
         const int r = r0 + at * QT;
@@ -376,8 +383,8 @@ __global__ __launch_bounds__((ByKeys<T, DP>::THREADS), T != F32 ? 2 : 1) void k_
             clear(x);
             clear(y);
             if constexpr (B::KV_LDS) {
-                rows_times_rows<DP>(now, k_tile, x);
-                rows_times_rows<DP>(now + B::HALF, v_tile, y);
+                rows_times_rows<DP>(now, k_own, x);
+                rows_times_rows<DP>(now + B::HALF, v_own, y);
             } else {
                 rows_times<T, DP, QT>(now, 0, k, x);
                 rows_times<T, DP, QT>(now + B::HALF, 0, v, y);
@@ -393,8 +400,8 @@ __global__ __launch_bounds__((ByKeys<T, DP>::THREADS), T != F32 ? 2 : 1) void k_
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const float4 l = *reinterpret_cast<const float4 *>(&stats[stage.value][group][0][8 * b + 4 * h]);
-                const float4 d = *reinterpret_cast<const float4 *>(&stats[stage.value][group][1][8 * b + 4 * h]);
+                const float4 l = *reinterpret_cast<const float4 *>(stats_now + 8 * b + 4 * h);
+                const float4 d = *reinterpret_cast<const float4 *>(stats_now + QT + 8 * b + 4 * h);
                 const float ls[4] = {l.x, l.y, l.z, l.w}, ds[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
                 for (int k4 = 0; k4 < 4; ++k4) {
@@ -412,8 +419,9 @@ __global__ __launch_bounds__((ByKeys<T, DP>::THREADS), T != F32 ? 2 : 1) void k_
         if (more) commit(next, 1 - stage.value);
     };
     for (int64_t turn = begin; turn < end; turn += 2 * QW) {
-        block(own, own + B::STAGE, std::integral_constant<int, 0>{});
-        if (turn + QW < end) block(own + B::STAGE, own, std::integral_constant<int, 1>{});
+        block(own, own + B::STAGE, k_tile, v_tile, stats[0][group][0], std::integral_constant<int, 0>{});
+        if (turn + QW < end)
+            block(own + B::STAGE, own, k_tile, v_tile, stats[1][group][0], std::integral_constant<int, 1>{});
     }
     if constexpr (QW == 2) {
         add_groups<DP>(lds, wave, group, dk);
