@@ -797,7 +797,7 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
  * over the keys j that row i of a sequence sees: all of the sequence's, and if
  * causal those with j <= i + (its keys) - (its rows), i and j from 0 in it.
  *   dtype         storage of q, k, v and out.
- *   q_rows, kv_rows   rows of q and out, and of k and v; 0 .. 2^31 - 1.
+ *   q_rows, kv_rows   rows of q and out, and of k and v; 0 .. 2^30.
  *   heads, kv_heads   1 .. 65536, kv_heads a divisor of heads.   C  1 .. 128.
  *   q_starts      dev int32 [sequences + 1]: sequence b has rows q_starts[b] ..
  *                 q_starts[b + 1] - 1.  NULL: one sequence of all rows
@@ -821,7 +821,7 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
  * whatever they hold.  A value that is not finite in a sequence's own keys or
  * values may reach all of its rows, also those that a causal mask keeps from it.
  */
-#define LATTICE_ATTENTION_MAX_ROWS (((int64_t)1 << 31) - 1)
+#define LATTICE_ATTENTION_MAX_ROWS ((int64_t)1 << 30)
 #define LATTICE_ATTENTION_MAX_HEADS 65536
 #define LATTICE_ATTENTION_MAX_CHANNELS 128
 #define LATTICE_ATTENTION_MAX_SEQUENCES ((int64_t)1 << 24)

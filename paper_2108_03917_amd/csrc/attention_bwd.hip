@@ -125,7 +125,7 @@ __device__ __forceinline__ void store_column(void *out, float *part, int64_t at,
 
 // By queries: 4 wavefronts of 32 columns, blocks of keys of
 constexpr int kKeyBlock = 32;
-constexpr int kShort = 256;  // keys of a tile whose delta is made from the scores
+constexpr int kShort = 128;  // keys of a tile whose delta is made from the scores
 template <Type T, int DP, bool DMA>
 __global__ __launch_bounds__(256, T != F32 || DP < 128 ? 2 : 1) void k_by_queries(Params a) {
     using L = RowsOf<T, DP>;

@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
 from typing import Optional, Sequence
 
 import torch
@@ -444,28 +445,26 @@ class Dense:
                        out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
         """Scale ``grads`` (fp32 or bf16, contiguous, of any shapes) by
         min(1, max_norm / (norm + eps)), where norm is that over all their values,
-        in place or into ``out`` (fp32 or bf16, the same shapes).  Returns the norm
+        in place or into ``out`` (fp32 or bf16, of as many values each).  Returns the norm
         before, an fp32 scalar.  A norm that is not finite is not refused: NaN
         makes every value NaN, infinity makes finite ones 0."""
         n = len(grads)
-        if out is not None and len(out) != n:
-            raise ValueError(f"out must hold {n} tensors")
 
         def check(tensors, name):
-            index = self._index
-            for i, t in enumerate(tensors):
-                if t.dtype not in _STORAGE or t.get_device() != index or not t.is_contiguous():
-                    raise ValueError(f"{name}[{i}] must be contiguous, fp32 or bf16, and on {self.device}")
-            return ((ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors]),
-                    (ctypes.c_int * n)(*[_STORAGE[t.dtype] for t in tensors]))
+            kinds = [_STORAGE.get(t.dtype, -1) for t in tensors]
+            if (-1 in kinds or [t.get_device() for t in tensors].count(self._index) != n
+                    or not all([t.is_contiguous() for t in tensors])):
+                raise ValueError(f"{name} must be {n} contiguous tensors, fp32 or bf16, on {self.device}")
+            return array("Q", [t.data_ptr() for t in tensors]), array("i", kinds)
 
-        src = to = check(grads, "grads")
+        src, src_t = to, to_t = check(grads, "grads")
+        sizes = array("q", [t.numel() for t in grads])
         if out is not None:
-            to = check(out, "out")
-            for i, (a, b) in enumerate(zip(grads, out)):
-                if a.shape != b.shape:
-                    raise ValueError(f"out[{i}] must be {list(a.shape)}")
+            to, to_t = check(out, "out")
+            for i, (a, b) in enumerate(zip(sizes, out)):
+                if a != b.numel():
+                    raise ValueError(f"out[{i}] must hold as many values as grads[{i}], {a}")
         norm = torch.empty((), dtype=F32, device=self.device)
-        self._call(self._lib.lattice_clip_gradients, "clip_gradients", n, *src, *to,
-                   (ctypes.c_int64 * n)(*[t.numel() for t in grads]), max_norm, eps, norm.data_ptr())
+        self._call(self._lib.lattice_clip_gradients, "clip_gradients", n, *[x.buffer_info()[0] for x in (src, src_t, to, to_t,
+                   sizes)], max_norm, eps, norm.data_ptr())
         return norm
