@@ -808,18 +808,21 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
  *                 rows of k and v, the first ones (a cache that is filled in
  *                 part), or NULL for all.
  *   sequences     0 .. 2^24.
- *   scale         > 0.
+ *   scale         > 0, up to 1e30.
  *   zero_rest     rows of no sequence: non-zero makes their out 0 and their lse
  *                 -inf, 0 leaves both as they are.
  *   out           dev [q_rows][heads][C].   lse  dev fp32 [heads][q_rows], or NULL.
- * A row that sees no key gets 0 and an lse of -inf.  Starts that go back or lie
+ * A row that sees no key, or only ones that score -inf, gets 0 and an lse of -inf.  Starts that go back or lie
  * outside the rows, and lengths outside their sequence, are clamped to what there
  * is, and reported by lattice_dense_get_status (LATTICE_E_RANGE).
- * Products of fp32 are fp32 ones; of bf16 values they are exact, and exp(..) is
+ * Products of fp32 values are as exact as fp32 ones (where there are many, of up to
+ * 64 channels, made of three bf16 each: values of 2^127 or more give NaN there, those
+ * below 2^-110 lose their last bits); of bf16 values they are exact, and exp(..) is
  * rounded to bf16 before the product with v.  Sums are fp32.
- * Rows of k and v that belong to no sequence or do not count are not used,
- * whatever they hold.  A value that is not finite in a sequence's own keys or
- * values may reach all of its rows, also those that a causal mask keeps from it.
+ * Rows that belong to no sequence, and keys that do not count, are not used,
+ * whatever they hold.  A value that is not finite in a sequence's own rows may
+ * reach all results of that sequence, also those that a causal mask keeps from it,
+ * and none of another's.
  */
 #define LATTICE_ATTENTION_MAX_ROWS ((int64_t)1 << 30)
 #define LATTICE_ATTENTION_MAX_HEADS 65536

@@ -452,9 +452,14 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     r.dma = straight(p.k, a.D, E) && straight(p.v, a.D, E);
     const int64_t sequences = a.sequences > 0 ? a.sequences : 1;
     const int64_t rows = (a.q_rows + sequences - 1) / sequences, keys = (a.kv_rows + sequences - 1) / sequences;
-    r.few = rows * p.group <= 64;
-    r.planes = !a.bf16 && !r.few && planes_pay(a, keys);
-    // 64 columns a wavefront halve the reads of LDS; registers of three planes hold 32 channels so
+    // One tile's columns hold a sequence's rows and heads, and its keys are many: a token of 16
+    // sequences of 2000 keys 28 us (many rows' tiles 35), of 64 of 4096 keys, 64 columns, 113
+    // (120); 200 sequences of 20 rows and keys 16 (12).
+    r.few = rows * p.group <= 32 && keys >= 4 * rows;
+    r.planes = !a.bf16 && !r.few && planes_pay(a, keys, 1e8);
+    // 64 columns a wavefront halve the reads of LDS, but also the workgroups (8 heads of 64 in bf16:
+    // 16384 rows 623 us, 648 with 32; 4096 rows 99 and 75); registers of three planes hold 32
+    // channels so
     r.nq = !r.few && a.D <= (r.planes ? 32 : 64) && a.q_rows * a.heads >= (int64_t)256 * 2 * D->cu_count ? 2 : 1;
     const Columns c(p.group, r.few ? 32 : 128 * r.nq);
     p.parts = c.parts;

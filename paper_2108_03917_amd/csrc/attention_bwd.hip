@@ -504,7 +504,7 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
     r.dma_keys = straight(p.q, a.D, E) && straight(p.g, a.D, E);
     const int64_t sequences = a.sequences > 0 ? a.sequences : 1;
     const int64_t rows = (a.q_rows + sequences - 1) / sequences, keys = (a.kv_rows + sequences - 1) / sequences;
-    r.planes = !a.bf16 && planes_pay(a, keys);
+    r.planes = !a.bf16 && planes_pay(a, keys, 1e7);
     {
         const Columns c(p.group, 128);
         p.parts = c.parts;

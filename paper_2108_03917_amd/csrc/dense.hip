@@ -209,7 +209,7 @@ lattice_status check_attention(lattice_dense *D, const AttendArgs &a, lattice_dt
                 (long long)a.kv_rows, a.heads, a.kv_heads, a.D);
         return LATTICE_E_ARG;
     }
-    if (!is_storage(dtype) || !(a.scale > 0.f) || !isfinite(a.scale) || a.sequences < 0 ||
+    if (!is_storage(dtype) || !(a.scale > 0.f) || !(a.scale <= 1e30f) || a.sequences < 0 ||
         a.sequences > LATTICE_ATTENTION_MAX_SEQUENCES) {
         set_err(D, "%s: bad type, scale or number of sequences (%lld)", what, (long long)a.sequences);
         return LATTICE_E_ARG;

@@ -252,6 +252,49 @@ def test_rows_of_no_sequence(ops, rows, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_very_many_sequences(ops, dtype):  # noqa: F811
+    """More starts than a wavefront's lanes, and than those squared."""
+    lengths = [i % 4 for i in range(5000)]
+    n = sum(lengths)
+    s = starts_of(*lengths)
+    q, k, v, g = (rand(i, n, 1, 8, dtype=dtype) for i in range(4))
+    owner = torch.repeat_interleave(torch.arange(5000, device=DEV), torch.tensor(lengths, device=DEV))
+    out, lse = ops.attention(q, k, v, s, want_lse=True)
+    got = ops.attention_backward(g, q, k, v, out, lse, s)
+    Q, K, V, G = (x[:, 0].double() for x in (q, k, v, g))
+    z = torch.where(owner[:, None] == owner, Q @ K.t() / math.sqrt(8), -math.inf)
+    p = torch.softmax(z, 1)
+    t = p * (G @ V.t() - (G * (p @ V)).sum(1, keepdim=True))
+    # scores up to 10, two or three keys: 60 u of the sums of |terms|, and the roundings
+    half = 3 * HALF if dtype == "bf16" else 0.0
+    mag = p * (G.abs() @ V.abs().t() + (G.abs() * (p @ V.abs())).sum(1, keepdim=True))
+    rel = 200 * U + half
+    within(out[:, 0], p @ V, rel * (p @ V.abs()), "out")
+    within(got[0][:, 0], t @ K / math.sqrt(8), rel * (mag @ K.abs()), "grad_q")
+    within(got[1][:, 0], t.t() @ Q / math.sqrt(8), rel * (mag.t() @ Q.abs()), "grad_k")
+    within(got[2][:, 0], p.t() @ G, rel * (p.t() @ G.abs()), "grad_v")
+
+
+def test_no_sequences_and_one_with_a_length(ops):  # noqa: F811
+    q, k, v, g = (rand(i, 50, 2, 32) for i in range(4))
+    none = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = ops.attention(q, k, v, none, want_lse=True)
+    assert torch.all(out == 0) and torch.all(lse == -math.inf)
+    assert all(torch.all(x == 0) for x in ops.attention_backward(g, q, k, v, out, lse, none))
+    for m in (0, 1, 33, 50):
+        check_all(ops, q, k, v, [(0, 50, 0, m)], True, g=g, kv_lengths=torch.tensor([m], dtype=torch.int32, device=DEV))
+    empty = rand(5, 0, 2, 32)
+    out, lse = ops.attention(q, empty, empty, want_lse=True)
+    assert torch.all(out == 0)
+    got = ops.attention_backward(g, q, empty, empty, out, lse)
+    assert torch.all(got[0] == 0) and got[1].shape == got[2].shape == (0, 2, 32)
+    out, lse = ops.attention(empty, k, v, want_lse=True)
+    assert out.shape == (0, 2, 32) and lse.shape == (2, 0)
+    got = ops.attention_backward(empty, empty, k, v, out, lse)
+    assert torch.all(got[1] == 0) and torch.all(got[2] == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_scores(ops, dtype):  # noqa: F811
     """Scores of thousands, growing along the keys (the running maximum moves), and
     falling ones."""
