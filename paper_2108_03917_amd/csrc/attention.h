@@ -32,7 +32,9 @@ using gemm::bf16x8_t;
 using gemm::f32x16_t;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kJoinRows = 4;  // of a workgroup that joins parts
+constexpr int kJoinRows = 4;     // of a workgroup that joins parts
+constexpr int kJoinPairs = 16;   // of rows and heads that it takes at a time
+constexpr int kMostSplits = 64;
 
 // How a kernel takes its operands: fp32 words, bf16, or fp32 as three planes of bf16.
 enum Type { F32, BF16, PLANES };
@@ -646,11 +648,17 @@ inline Cut cut_of(int64_t tiles, int64_t blocks, int64_t most, int64_t grid, int
     most = most < 4 * blocks ? most : 4 * blocks;
     int64_t n = (most + c.share - 1) / c.share;
     const int64_t few = 32 * places / (grid > 0 ? grid : 1);  // workgroups that end at once are not free
-    n = n < 64 ? n : 64;
+    n = n < kMostSplits ? n : kMostSplits;
     n = n < few || n <= 2 ? n : few < 2 ? 2 : few;
     n = n < room ? n : room;
     c.splits = (int)(n < 1 ? 1 : n);
     return c;
+}
+// The grid of a join: tiles, their rows by kJoinRows, and what each of these has to do in
+// up to `pieces` where there are not workgroups enough.
+inline dim3 join_grid(int64_t slots, int R, int64_t pieces) {
+    const int64_t y = (R + kJoinRows - 1) / kJoinRows, z = 8192 / (slots * y);
+    return dim3((unsigned)slots, (unsigned)y, (unsigned)(z < 1 ? 1 : z < pieces ? z : pieces));
 }
 // Bytes of partial results that are not too large.
 constexpr int64_t kMostParts = (int64_t)1 << 29;

@@ -393,35 +393,46 @@ __global__ __launch_bounds__(256) void k_join(Params a, int KT) {
     first += skip;
     rows = rows - skip < kJoinRows ? rows - skip : kJoinRows;
     const int64_t next = a.pack.q_rows * a.heads;
-    const int lanes = (a.D + 3) / 4;  // of a head's row
-    for (int id = threadIdx.x; id < rows * a.heads * lanes; id += 256) {
-        const int i = id / lanes, c0 = (id - i * lanes) * 4;
-        const int64_t row = s.q0 + first + i / a.heads;
-        const int head = i % a.heads;
-        const float *lse = a.part_lse + head * a.pack.q_rows + row;
-        float m = -INFINITY, sum = 0.f;
-        bool nan = false;
-        for (int n = 0; n < splits; ++n) {
-            const float x = lse[n * next];
-            nan |= x != x;
-            m = fmaxf(m, x);
+    const int lanes = (a.D + 3) / 4, pairs = rows * a.heads;  // of a head's row; rows' heads
+    __shared__ float lses[kJoinPairs][kMostSplits];
+    for (int base = (int)blockIdx.z * kJoinPairs; base < pairs; base += kJoinPairs * gridDim.z) {
+        const int here = pairs - base < kJoinPairs ? pairs - base : kJoinPairs;
+        __syncthreads();
+        for (int id = threadIdx.x; id < here * splits; id += 256) {
+            const int n = id / here, i = base + id - n * here;
+            lses[id - n * here][n] = a.part_lse[n * next + (i % a.heads) * a.pack.q_rows + s.q0 + first + i / a.heads];
         }
-        for (int n = 0; n < splits; ++n) sum += m == -INFINITY ? 0.f : exp2_(lse[n * next] - m);
-        const float all = nan ? NAN : m == -INFINITY ? m : m + log2f(sum);
-        if (a.lse && c0 == 0) a.lse[head * a.pack.q_rows + row] = all * kLn2;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int n = 0; n < splits; ++n) {
-            const float x = lse[n * next];
-            if (x == -INFINITY) continue;
-            const float f = exp2_(x - all);
-            const float *p = a.part_o + (n * next + row * a.heads + head) * a.D + c0;
+        __syncthreads();
+        for (int id = threadIdx.x; id < here * lanes; id += 256) {
+            const int pair = id / lanes, i = base + pair, c0 = (id - pair * lanes) * 4;
+            const int64_t row = s.q0 + first + i / a.heads;
+            const int head = i % a.heads;
+            const float *lse = lses[pair];
+            float m = -INFINITY, sum = 0.f;
+            bool nan = false;
+            for (int n = 0; n < splits; ++n) {
+                nan |= lse[n] != lse[n];
+                m = fmaxf(m, lse[n]);
+            }
+            for (int n = 0; n < splits; ++n) sum += m == -INFINITY ? 0.f : exp2_(lse[n] - m);
+            const float all = nan ? NAN : m == -INFINITY ? m : m + log2f(sum);
+            if (a.lse && c0 == 0) a.lse[head * a.pack.q_rows + row] = all * kLn2;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            const float *p = a.part_o + (row * a.heads + head) * a.D;
+#pragma unroll 4
+            for (int n = 0; n < splits; ++n) {
+                // a part without keys has written nothing
+                const bool none = lse[n] == -INFINITY;
+                const float f = none ? 0.f : exp2_(lse[n] - all);
+                float x[4];
+                load_row<false, 4>(p + n * next * a.D, c0, a.D, x);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c0 + k < a.D) v[k] += f * p[k];
+                for (int k = 0; k < 4; ++k) v[k] += none ? 0.f : f * x[k];
+            }
+            store4<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) +
+                             (row * a.o.row + head * a.o.head) * (BF16 ? 2 : 4),
+                         c0, a.D, v);
         }
-        store4<BF16>(const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) +
-                         (row * a.o.row + head * a.o.head) * (BF16 ? 2 : 4),
-                     c0, a.D, v);
     }
 }
 
@@ -523,7 +534,7 @@ hipError_t launch_type(lattice_dense *D, const Plan &r) {
         TRY((launch_dim<T, 128>(D, r)));
     }
     if (r.p.cut.splits == 1) return hipSuccess;
-    hipLaunchKernelGGL((k_join<T == BF16>), dim3((unsigned)r.p.slots, (unsigned)((r.p.R + kJoinRows - 1) / kJoinRows)),
+    hipLaunchKernelGGL((k_join<T == BF16>), join_grid(r.p.slots, r.p.R, (kJoinRows * r.p.heads + kJoinPairs - 1) / kJoinPairs),
                        dim3(256), 0, D->stream, r.p, r.KT);
     return hipGetLastError();
 }

@@ -450,23 +450,30 @@ __global__ __launch_bounds__(256) void k_join(Params a, bool by_keys) {
     int rows = all - first < a.R ? all - first : a.R;
     const int splits = parts_of(a.cut, by_keys ? (int64_t)row_blocks(a, s, first) * a.group
                                                : (keys_seen(s, a.pack.causal, first + rows - 1) + kKeyBlock - 1) / kKeyBlock);
-    const int skip = (int)blockIdx.z * kJoinRows;
+    const int skip = (int)blockIdx.y * kJoinRows;
     if (splits == 1 || skip >= rows) return;
     first += skip;
     rows = rows - skip < kJoinRows ? rows - skip : kJoinRows;
     const int64_t width = (int64_t)(by_keys ? a.kv_heads : a.heads) * a.D;
     const int64_t size = (by_keys ? a.pack.kv_rows : a.pack.q_rows) * width;
     const int64_t from = ((by_keys ? s.k0 : s.q0) + first) * width;
-    void *out = !by_keys ? a.dq : blockIdx.y == 0 ? a.dk : a.dv;
-    const float *part = a.part + blockIdx.y * size + from;
-    const int64_t step = (by_keys ? 2 : 1) * size;
-    for (int64_t i = threadIdx.x; i < rows * width; i += 256) {
-        float x = 0.f;
-        for (int n = 0; n < splits; ++n) x += part[n * step + i];
-        if (BF16)
-            reinterpret_cast<uint16_t *>(out)[from + i] = (uint16_t)pack_bf16(x, 0.f);
-        else
-            reinterpret_cast<float *>(out)[from + i] = x;
+    const int64_t step = (by_keys ? 2 : 1) * size, all_values = rows * width;
+    // four values a thread, of both tensors by keys; the last ones of a row of odd width alone
+    const int vec = width % 4 == 0 ? 4 : 1;
+    for (int t = 0; t < (by_keys ? 2 : 1); ++t) {
+        void *out = !by_keys ? a.dq : t == 0 ? a.dk : a.dv;
+        const float *part = a.part + t * size + from;
+        for (int64_t i = ((int64_t)blockIdx.z * 256 + threadIdx.x) * vec; i < all_values; i += (int64_t)256 * vec * gridDim.z) {
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int n = 0; n < splits; ++n) {
+                float p[4];
+                load_row<false, 4>(part + n * step + i, 0, vec, p);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] += p[k];
+            }
+            store4<BF16>(reinterpret_cast<char *>(out) + (from + i) * (BF16 ? 2 : 4), 0, vec, x);
+        }
     }
 }
 
@@ -556,7 +563,7 @@ hipError_t by_keys(lattice_dense *D, const Plan &r) {
 template <bool BF16>
 hipError_t join(lattice_dense *D, const Params &p, bool keys) {
     if (p.cut.splits == 1) return hipSuccess;
-    hipLaunchKernelGGL((k_join<BF16>), dim3((unsigned)p.slots, keys ? 2 : 1, (unsigned)((p.R + kJoinRows - 1) / kJoinRows)),
+    hipLaunchKernelGGL((k_join<BF16>), join_grid(p.slots, p.R, ((int64_t)kJoinRows * (keys ? p.kv_heads : p.heads) * p.D + 1023) / 1024),
                        dim3(256), 0, D->stream, p, keys);
     return hipGetLastError();
 }
