@@ -320,10 +320,7 @@ __global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params
         }
         i += WAVES;
     };
-    while (i < t.t1) {
-        block(own, own + STAGE);
-        if (i < t.t1) block(own + STAGE, own);
-    }
+    for (int stage = 0; i < t.t1; stage ^= 1) block(own + stage * STAGE, own + (stage ^ 1) * STAGE);
     // join: every wavefront's columns to LDS (its own part, whose blocks are done with)
     const float sum = pair_sum(col.sum);
     const int half = lane >> 5;
