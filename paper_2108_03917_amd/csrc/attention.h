@@ -152,7 +152,9 @@ __device__ __forceinline__ Sequence locate(const Packing &p, int R, int slot, bo
             if (p.kv_lengths) keys = p.kv_lengths[b];
         }
         to = to < from ? from : to;
+        // (starts that go back may put the slot before its sequence: none then)
         first = (uniform(slot - i) - (int)((uint32_t)uniform(from) / (uint32_t)R)) * R;
+        first = first < 0 ? 0x7fffffff : first;
         s.real = i > 0 && i <= p.sequences;
         if (!s.real) {
             s.q0 = s.k0 = uniform(from);

@@ -391,6 +391,35 @@ def test_starts_that_do_not_fit_are_clamped_and_reported(ops):  # noqa: F811
     assert ops.status() == OK
 
 
+@pytest.mark.parametrize("sequences", [7, 61, 62, 300])
+def test_starts_in_any_order_touch_nothing_else(ops, sequences):  # noqa: F811
+    """Random starts and lengths, far outside the rows too: what lies around the
+    tensors stays as it is."""
+    from paper_2108_03917_amd.lattice import E_RANGE, OK
+
+    n, C, pad = 500, 32, 4096
+    g = torch.Generator(device=DEV)
+    for seed in range(4):
+        g.manual_seed(seed)
+        far = 2 ** 31 - 1 if seed % 2 else 2 * n
+
+        def starts():
+            return torch.randint(-far, far, (sequences + 1,), generator=g, device=DEV).int()
+
+        room = torch.full((2 * pad + n * 2 * C,), 3.0, device=DEV)
+        out = room[pad:-pad].view(n, 2, C)
+        q, k, v = (rand(i, n, 2, C) for i in range(3))
+        packing = dict(q_starts=starts(), kv_starts=starts(), kv_lengths=starts()[1:])
+        ops.attention(q, k, v, causal=bool(seed & 1), out=out, **packing)
+        o, lse = ops.attention(q, k, v, causal=bool(seed & 1), want_lse=True, **packing)
+        ops.attention_backward(q, q, k, v, o, lse, causal=bool(seed & 1), **packing)
+        assert torch.all(room[:pad] == 3) and torch.all(room[-pad:] == 3)
+        assert ops.status() == E_RANGE
+    s = starts_of(n)
+    ops.attention(q, k, v, s)
+    assert ops.status() == OK
+
+
 def test_refusals(ops):  # noqa: F811
     from paper_2108_03917_amd import LatticeError
 
