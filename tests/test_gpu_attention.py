@@ -228,6 +228,32 @@ def test_strides(ops, C, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,far", [(64, "rows"), (36, "rows"), (64, "heads")])
+def test_offsets_past_32_bits(ops, C, far, dtype):  # noqa: F811
+    """Rows 8 MB apart, or heads 2.1 GB: the last of them lie 6 to 7 GB behind the first."""
+    n, e = 900, 4 if dtype == "f32" else 2
+    gap = (1 << 23) // e if far == "rows" else (2100 << 20) // e
+    heads, kv_heads = 4, 2 if far == "rows" else 4
+    buffer = torch.empty(n * gap if far == "rows" else 3 * gap + (1 << 20), device=DEV, dtype=T[dtype])
+
+    def place(i, h):
+        at = buffer[i * (gap // 8 if far == "rows" else 1 << 17):]
+        x = at.as_strided((n, h, C), (gap, C, 1) if far == "rows" else (C, gap, 1))
+        return x.copy_(rand(i, n, h, C, dtype=dtype))
+
+    q, k, v, g = place(1, heads), place(2, kv_heads), place(3, kv_heads), place(4, heads)
+    s, seqs = starts_of(n - 50, 50), [(0, n - 50, 0, n - 50), (n - 50, 50, n - 50, 50)]
+    out, lse = check_all(ops, q, k, v, seqs, True, g=g, q_starts=s)
+    check_all(ops, q[-1:], k, v, [(0, 1, 0, n)], False, g=g[-1:])
+    if far == "rows":
+        to = place(5, heads)
+        assert torch.equal(ops.attention(q, k, v, s, causal=True, out=to), out)
+        near = ops.attention_backward(g, q, k, v, out, lse, s, causal=True)
+        for a, b in zip(near, ops.attention_backward(g, q, k, v, to, lse, s, causal=True)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [90, 4000])
 def test_rows_of_no_sequence(ops, rows, dtype):  # noqa: F811
     """Left alone in a given out, else zeros; whatever they hold reaches no result."""

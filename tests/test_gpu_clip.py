@@ -55,6 +55,16 @@ def test_clip(ops, sizes, dtype, share):  # noqa: F811
         assert all(torch.equal(a, b) for a, b in zip(before, grads))
 
 
+def test_more_than_2_31_values(ops):  # noqa: F811
+    """The norm and the scaled values are exact here: 2^32 squares of 1/4, and a factor of
+    2^-10; two values behind the 2^31st one are not as the others."""
+    x = torch.full((1 << 32,), 0.5, device=DEV, dtype=torch.bfloat16)
+    x[(1 << 31) + 5], x[-1] = -0.5, -0.5
+    want = x * 2.0 ** -10
+    norm = ops.clip_gradients([x[:5], x[5:]], 2.0 ** 5, 0.0)
+    assert norm.item() == 2.0 ** 15 and torch.equal(x, want)
+
+
 def test_shapes_and_odd_addresses(ops):  # noqa: F811
     flat = rand(1, 10000)
     half = rand(2, 10000, dtype="bf16")

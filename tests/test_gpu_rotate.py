@@ -154,6 +154,18 @@ def test_strides_and_in_place(ops, C, offset, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_past_32_bits(ops, dtype):  # noqa: F811
+    """Rows 32 MB apart: the last lies 4.8 GB behind the first."""
+    n, C, gap = 150, 36, (32 << 20) // (4 if dtype == "f32" else 2)
+    buffer = torch.empty(n * gap, device=DEV, dtype=T[dtype])
+    q, k = (buffer[i * 1000:].as_strided((n, 3, C), (gap, C, 1)).copy_(rand(i, n, 3, C, dtype=dtype)) for i in (1, 2))
+    args, gains = (rand(3, n, 1), frequencies(C // 2), None), (rand(4, C), rand(5, C))
+    want = check(ops, q, k, *args, gains)
+    ops.rotate_heads(q, k, *args, *gains, out_q=q, out_k=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_of_zeros(ops, dtype):  # noqa: F811
     q = torch.zeros(5, 2, 16, device=DEV, dtype=T[dtype])
     y, _ = ops.rotate_heads(q, None, rand(1, 5, 1), frequencies(8))
