@@ -636,6 +636,17 @@ struct Columns {
 inline Packing packing_of(const AttendArgs &a) {
     return {a.q_rows, a.kv_rows, a.q_starts, a.kv_starts, a.kv_lengths, (int)a.sequences, a.causal};
 }
+// Workgroups of a launch; more go in several (the threads along a side have 32 bits).
+constexpr int64_t kMostGrid = (int64_t)1 << 22;
+template <class Params, class Launch>
+hipError_t in_launches(Params p, int64_t grid, Launch launch) {
+    for (p.block0 = 0; p.block0 < grid; p.block0 += kMostGrid) {
+        const int64_t left = grid - p.block0;
+        launch(dim3((unsigned)(left < kMostGrid ? left : kMostGrid), (unsigned)p.cut.splits), p);
+        TRY(hipGetLastError());
+    }
+    return hipSuccess;
+}
 // How a launch of `grid` workgroups cuts its tiles: `tiles` of them have about `blocks`
 // blocks each, and none more than `most`.  A part is what each of `places` workgroups
 // that run at once has to do in all, or half of it where there are few tiles for a place
@@ -653,7 +664,7 @@ inline Cut cut_of(int64_t tiles, int64_t blocks, int64_t most, int64_t grid, int
     n = n < kMostSplits ? n : kMostSplits;
     n = n < few || n <= 2 ? n : few < 2 ? 2 : few;
     n = n < room ? n : room;
-    c.splits = (int)(n < 1 ? 1 : n);
+    c.splits = (int)(n < 1 || grid > kMostGrid ? 1 : n);
     return c;
 }
 // The grid of a join: tiles, their rows by kJoinRows, and what each of these has to do in

@@ -36,6 +36,7 @@ struct Params {
     int group;          // query heads of a key head
     int parts, tile_heads;  // parts that a group is cut into, query heads of one
     int R, slots;           // rows of a tile
+    int64_t block0;         // of the launch's workgroups, among all of them
     Cut cut;                // of blocks of keys
     float c;            // scale, for powers of 2
     bool zero_rest;
@@ -59,7 +60,7 @@ template <Type T, int KT>
 __device__ __forceinline__ bool tile_of(const Params &a, Tile &t) {
     int unit, slot;
     t.split = blockIdx.y;
-    if (!unit_of(blockIdx.x, a.units, a.slots, true, unit, slot)) return false;
+    if (!unit_of(a.block0 + blockIdx.x, a.units, a.slots, true, unit, slot)) return false;
     const int part = unit % a.parts;
     t.kv_head = unit / a.parts;
     t.head0 = t.kv_head * a.group + part * a.tile_heads;
@@ -496,28 +497,29 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
 }
 
 template <Type T, int DP, int NQ, bool DMA>
-hipError_t launch_many(lattice_dense *D, const Plan &r, dim3 grid) {
+hipError_t launch_many(lattice_dense *D, const Plan &r) {
     constexpr int LDS = 2 * 2 * tile_bytes<T, DP>(keys_of_block<T>());
     static std::atomic<uint64_t> done{0};
     if (LDS > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend<T, DP, NQ, DMA>), LDS, done));
-    hipLaunchKernelGGL((k_attend<T, DP, NQ, DMA>), grid, dim3(256), LDS, D->stream, r.p);
-    return hipGetLastError();
+    return in_launches(r.p, r.grid, [&](dim3 grid, const Params &p) {
+        hipLaunchKernelGGL((k_attend<T, DP, NQ, DMA>), grid, dim3(256), LDS, D->stream, p);
+    });
 }
 
 template <Type T, int DP, bool DMA>
 hipError_t launch_as(lattice_dense *D, const Plan &r) {
-    const dim3 grid((unsigned)r.grid, (unsigned)r.p.cut.splits);
     if constexpr (T != PLANES)
         if (r.few) {
             constexpr int W = few_waves<T, DP>(), LDS = W * 2 * 2 * 32 * RowsOf<T, DP>::BYTES;
             static std::atomic<uint64_t> done{0};
             if (LDS + 1024 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_attend_few<T, DP, DMA>), LDS, done));
-            hipLaunchKernelGGL((k_attend_few<T, DP, DMA>), grid, dim3(64 * W), LDS, D->stream, r.p);
-            return hipGetLastError();
+            return in_launches(r.p, r.grid, [&](dim3 grid, const Params &p) {
+                hipLaunchKernelGGL((k_attend_few<T, DP, DMA>), grid, dim3(64 * W), LDS, D->stream, p);
+            });
         }
     if constexpr (DP <= 64 && (T != PLANES || DP == 32))
-        if (r.nq == 2) return launch_many<T, DP, 2, DMA>(D, r, grid);
-    return launch_many<T, DP, 1, DMA>(D, r, grid);
+        if (r.nq == 2) return launch_many<T, DP, 2, DMA>(D, r);
+    return launch_many<T, DP, 1, DMA>(D, r);
 }
 
 template <Type T, int DP>

@@ -35,6 +35,7 @@ struct Params {
     int heads, kv_heads, D, group;
     int parts, tile_heads;    // by queries, as in the forward pass
     int units, R, slots;
+    int64_t block0;           // of the launch's workgroups, among all of them
     Cut cut;                  // of blocks of keys, or of rows
     float c, scale;
     bool zero_rest;
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(256, T != F32 || DP < 128 ? 2 : 1) void k_by_querie
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int unit, slot, first;
     const int split = blockIdx.y;
-    if (!unit_of(blockIdx.x, a.units, a.slots, true, unit, slot)) return;
+    if (!unit_of(a.block0 + blockIdx.x, a.units, a.slots, true, unit, slot)) return;
     const int kv_head = unit / a.parts, part = unit % a.parts, head0 = kv_head * a.group + part * a.tile_heads;
     const int left = a.group - part * a.tile_heads, heads = left < a.tile_heads ? left : a.tile_heads;
     const Sequence s = locate(a.pack, a.R, slot, false, first, a.status);
@@ -286,7 +287,7 @@ __global__ __launch_bounds__((ByKeys<T, DP>::THREADS), T != F32 ? 2 : 1) void k_
     __shared__ __attribute__((aligned(16))) float stats[2][QW][2][QT];  // lse (of 2) and delta of the blocks' rows
     const int split = blockIdx.y;
     int kv_head, slot, first;
-    if (!unit_of(blockIdx.x, a.kv_heads, a.slots, false, kv_head, slot)) return;
+    if (!unit_of(a.block0 + blockIdx.x, a.kv_heads, a.slots, false, kv_head, slot)) return;
     const Sequence s = locate(a.pack, a.R, slot, true, first, a.status);
     if (first >= s.kv_len) return;
     const int lane = threadIdx.x & 63, wave = gemm::wave_index() & 3, group = gemm::wave_index() >> 2, h = lane >> 5;
@@ -548,9 +549,9 @@ template <Type T, int DP, bool DMA>
 hipError_t by_queries(lattice_dense *D, const Plan &r) {
     constexpr int LDS = 2 * 2 * tile_bytes<T, DP>(kKeyBlock);
     static_assert(LDS <= 64 * 1024, "LDS");
-    hipLaunchKernelGGL((k_by_queries<T, DP, DMA>), dim3((unsigned)r.grid_queries, (unsigned)r.by_queries.cut.splits),
-                       dim3(256), LDS, D->stream, r.by_queries);
-    return hipGetLastError();
+    return in_launches(r.by_queries, r.grid_queries, [&](dim3 grid, const Params &p) {
+        hipLaunchKernelGGL((k_by_queries<T, DP, DMA>), grid, dim3(256), LDS, D->stream, p);
+    });
 }
 
 template <Type T, int DP, bool DMA>
@@ -559,9 +560,9 @@ hipError_t by_keys(lattice_dense *D, const Plan &r) {
     constexpr int LDS = B::LDS;
     static std::atomic<uint64_t> done{0};
     if (LDS + 2048 > 64 * 1024) TRY(gemm::allow_lds(reinterpret_cast<const void *>(&k_by_keys<T, DP, DMA>), LDS, done));
-    hipLaunchKernelGGL((k_by_keys<T, DP, DMA>), dim3((unsigned)r.grid_keys, (unsigned)r.by_keys.cut.splits),
-                       dim3(B::THREADS), LDS, D->stream, r.by_keys);
-    return hipGetLastError();
+    return in_launches(r.by_keys, r.grid_keys, [&](dim3 grid, const Params &p) {
+        hipLaunchKernelGGL((k_by_keys<T, DP, DMA>), grid, dim3(B::THREADS), LDS, D->stream, p);
+    });
 }
 
 template <bool BF16>

@@ -263,11 +263,43 @@ void random_sizes() {
     lattice_dense_destroy(D);
 }
 
+// More tiles than the threads along a side of a launch have bits for (32, 512 or fewer of a
+// workgroup): several launches, which have all tiles between them.
+void many_tiles() {
+    lattice_dense *D = handle();
+    static int64_t workgroups = 0;
+    on_launch = [](const Launch &l) {
+        if (l.grid.x >= 1u << 23 || l.grid.y > 65535 || l.grid.z > 65535)
+            fail("%s: a grid of %u x %u x %u", l.name.c_str(), l.grid.x, l.grid.y, l.grid.z);
+        workgroups += (int64_t)l.grid.x * l.grid.y;
+    };
+    for (const lattice_dtype dtype : {LATTICE_BF16, LATTICE_F32})
+        for (const int64_t kv_rows : {(int64_t)700000, (int64_t)2800000})
+            for (const int heads : {1, 32}) {
+                Attention a;
+                a.dtype = dtype;
+                a.sequences = heads == 1 ? LATTICE_ATTENTION_MAX_SEQUENCES : 600000;
+                a.q_rows = 700000;
+                a.kv_rows = kv_rows;
+                a.heads = a.kv_heads = heads;
+                a.C = 8;
+                a.take();
+                workgroups = 0;
+                expect("attention", D, a.forward(D), LATTICE_OK);
+                if (workgroups < heads * a.sequences) fail("attention: %lld workgroups", (long long)workgroups);
+                workgroups = 0;
+                expect("attention_backward", D, a.backward(D), LATTICE_OK);
+                if (workgroups < 2 * heads * a.sequences) fail("attention_backward: %lld workgroups", (long long)workgroups);
+            }
+    lattice_dense_destroy(D);
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
     const std::map<std::string, void (*)()> checks = {
-        {"refusals", refusals}, {"nothing_there", nothing_there}, {"random_sizes", random_sizes}};
+        {"refusals", refusals}, {"nothing_there", nothing_there}, {"random_sizes", random_sizes},
+        {"many_tiles", many_tiles}};
     const auto it = checks.find(argc > 1 ? argv[1] : "");
     if (it == checks.end()) fail("which check?");
     it->second();

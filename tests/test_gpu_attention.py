@@ -301,6 +301,40 @@ def test_very_many_sequences(ops, dtype):  # noqa: F811
     within(got[2][:, 0], p.t() @ G, rel * (p.t() @ G.abs()), "grad_v")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("keys", [1, 4])
+def test_more_tiles_than_a_launch(ops, keys, dtype):  # noqa: F811
+    """140000 sequences of 32 heads, a row and 1 or 4 keys each: 4.5 million tiles, more
+    than the 2^22 of a launch.  The tolerances of attention_ref, a sequence along an axis."""
+    n, heads, C = 140000, 32, 8
+    q, k, v, g = rand(1, n, heads, C, dtype=dtype), rand(2, n * keys, heads, C, dtype=dtype), \
+        rand(3, n * keys, heads, C, dtype=dtype), rand(4, n, heads, C, dtype=dtype)
+    s = torch.arange(n + 1, device=DEV, dtype=torch.int32)
+    out, lse = ops.attention(q, k, v, s, s * keys, want_lse=True)
+    got = ops.attention_backward(g, q, k, v, out, lse, s, s * keys)
+    half, scale = HALF if dtype == "bf16" else 0.0, 1 / math.sqrt(C)
+    Q, G = q.double()[:, None], g.double()[:, None]
+    K, V = k.double().view(n, keys, heads, C), v.double().view(n, keys, heads, C)
+    z = (Q * K).sum(3, keepdim=True) * scale
+    A = (Q * K).abs().sum(3, keepdim=True).amax(1, keepdim=True) * scale
+    l = torch.logsumexp(z, 1, keepdim=True)
+    p = torch.exp(z - l)
+    e_p = U * (2 * (C + 8) * A + 2 * keys + 16)
+    o = (p * V).sum(1, keepdim=True)
+    o_e = ((e_p + U * keys + half) * p * V.abs()).sum(1, keepdim=True) + half * o.abs()
+    within(out, o[:, 0], o_e[:, 0], "out")
+    within(lse.t(), l[:, 0, :, 0], (U * ((C + 8) * A + keys + 8 + 2 * l.abs()))[:, 0, :, 0], "lse")
+    e_p = e_p + 2 * U * l.abs()
+    t = p * ((G * V).sum(3, keepdim=True) - (G * o).sum(3, keepdim=True))
+    mag = (G * V).abs().sum(3, keepdim=True) + (G * o).abs().sum(3, keepdim=True)
+    t_e = p * ((e_p + (C + 4) * U) * mag + (G.abs() * o_e).sum(3, keepdim=True)) + half * t.abs()
+    for x, r, e, name in ((got[0], (t * K).sum(1) * scale, ((t_e + U * keys * t.abs()) * K.abs()).sum(1) * scale, "grad_q"),
+                          (got[1], (t * Q * scale).flatten(0, 1), ((t_e + U * heads * t.abs()) * Q.abs() * scale).flatten(0, 1),
+                           "grad_k"),
+                          (got[2], (p * G).flatten(0, 1), (p * (e_p + U * heads + half) * G.abs()).flatten(0, 1), "grad_v")):
+        within(x, r, e + half * r.abs(), name)
+
+
 def test_no_sequences_and_one_with_a_length(ops):  # noqa: F811
     q, k, v, g = (rand(i, 50, 2, 32) for i in range(4))
     none = torch.zeros(1, dtype=torch.int32, device=DEV)

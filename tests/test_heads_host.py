@@ -24,10 +24,10 @@ def driver(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("check", ["refusals", "nothing_there", "random_sizes"])
+@pytest.mark.parametrize("check", ["refusals", "nothing_there", "random_sizes", "many_tiles"])
 def test_host(driver, check):
     """Bad arguments are refused before anything is enqueued or allocated; calls without
     rows, keys or sequences are none; calls of random sizes launch grids that there are, on the
-    handle's device and stream."""
+    handle's device and stream, and so do ones of very many tiles."""
     r = subprocess.run([driver, check], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", (r.returncode, r.stdout, r.stderr)
