@@ -823,6 +823,8 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
  * whatever they hold.  A value that is not finite in a sequence's own rows may
  * reach all results of that sequence, also those that a causal mask keeps from it,
  * and none of another's.
+ * A tile has up to 256 rows and heads of one sequence and key head; 2^31 tiles or more
+ * are refused.
  */
 #define LATTICE_ATTENTION_MAX_ROWS ((int64_t)1 << 30)
 #define LATTICE_ATTENTION_MAX_HEADS 65536

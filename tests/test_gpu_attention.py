@@ -138,6 +138,26 @@ def test_head_layouts(ops, heads, kv_heads, dtype):  # noqa: F811
 PACKS = [(1,), (1, 1, 1), (5, 0, 7), (0, 0, 0), (64, 64, 64), (1, 200, 3, 0, 129, 1), (33,) * 9, tuple(range(1, 80)), (300, 2, 256)]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,heads,kv_heads,keys", [(2, 65536, 1, 70), (1, 65536, 1, 3000), (3, 4096, 64, 40)])
+def test_very_many_heads(ops, rows, heads, kv_heads, keys, dtype):  # noqa: F811
+    """The query heads of a key head are as many rows of one head."""
+    C, group = 16, heads // kv_heads
+    q, g = rand(1, rows, heads, C, dtype=dtype), rand(4, rows, heads, C, dtype=dtype)
+    k, v = rand(2, keys, kv_heads, C, dtype=dtype), rand(3, keys, kv_heads, C, dtype=dtype)
+
+    def as_rows(x):
+        return x.view(rows, kv_heads, group, -1).transpose(1, 2).reshape(rows * group, kv_heads, -1)
+
+    ref = attention_ref(as_rows(q), k, v, [(0, rows * group, 0, keys)], False, 0.25, as_rows(g))
+    out, lse = ops.attention(q, k, v, want_lse=True)
+    grads = ops.attention_backward(g, q, k, v, out, lse)
+    within(as_rows(out), *ref[0], "out")
+    within(as_rows(lse.t().contiguous())[..., 0].t(), *ref[1], "lse")
+    for x, (r, e), name in zip((as_rows(grads[0]), *grads[1:]), ref[2:], ("grad_q", "grad_k", "grad_v")):
+        within(x, r, e, name)
+
+
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("lengths", PACKS, ids=[str(len(p)) + "x" + str(max(p)) for p in PACKS])

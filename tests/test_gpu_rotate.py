@@ -166,6 +166,12 @@ def test_offsets_past_32_bits(ops, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_very_many_heads(ops, dtype):  # noqa: F811
+    check(ops, rand(1, 2, 65536, 20, dtype=dtype), rand(2, 2, 65536, 20, dtype=dtype), rand(3, 2, 2), frequencies(9), [4, 5],
+          (rand(4, 20), rand(5, 20)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_of_zeros(ops, dtype):  # noqa: F811
     q = torch.zeros(5, 2, 16, device=DEV, dtype=T[dtype])
     y, _ = ops.rotate_heads(q, None, rand(1, 5, 1), frequencies(8))
