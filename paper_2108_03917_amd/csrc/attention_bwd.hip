@@ -252,7 +252,8 @@ __global__ __launch_bounds__(256, T != F32 || DP < 128 ? 2 : 1) void k_by_querie
 //
 // With K and V as right operands in registers and both results there, 128 channels take
 // 300 registers, one wavefront a SIMD, and nothing runs beside its exponentials and
-// waits (283 TFLOP/s); K and V are read from LDS instead (KV_LDS), which leaves room for two (0.63 PFLOP/s).
+// waits (283 TFLOP/s); K and V are read from LDS instead (KV_LDS), which leaves room for
+// two (0.63 PFLOP/s).
 template <Type T, int DP>
 struct ByKeys {
     static constexpr bool KV_LDS = T == BF16 && DP == 128;

@@ -151,8 +151,9 @@ bool apart(int64_t rows, int64_t heads, int64_t C, int64_t row, int64_t head) {
     return (head >= C && row >= (heads - 1) * head + C) || (row >= C && head >= (rows - 1) * row + C);
 }
 
-bool strides_ok(int64_t row, int64_t head) {
-    return row >= 0 && head >= 0 && row <= ((int64_t)1 << 40) && head <= ((int64_t)1 << 40);
+// Strides that go forward, to no more values than there are addresses (2^48 bytes).
+bool strides_ok(int64_t rows, int64_t heads, int64_t row, int64_t head) {
+    return row >= 0 && head >= 0 && (double)(rows - 1) * (double)row + (double)(heads - 1) * (double)head < 0x1p47;
 }
 
 // A tensor that is read, or written, by an operator on heads.
@@ -172,7 +173,7 @@ lattice_status check_heads(lattice_dense *D, const char *what, const Heads *t, i
     };
     for (int i = 0; i < n; ++i) {
         if (t[i].rows <= 0 || t[i].heads <= 0) continue;
-        if (!t[i].p || !strides_ok(t[i].row, t[i].head)) {
+        if (!t[i].p || !strides_ok(t[i].rows, t[i].heads, t[i].row, t[i].head)) {
             set_err(D, "%s: %s is missing or has a bad stride", what, t[i].name);
             return LATTICE_E_ARG;
         }

@@ -124,6 +124,12 @@ void refusals() {
                                  nullptr, nullptr, 1, 0, 1.f, 1, good.out, 128, 32, nullptr);
     });
 
+    refused("strides past all addresses", D, [&] {
+        return lattice_attention(D, LATTICE_F32, LATTICE_ATTENTION_MAX_ROWS, 90, 4, 2, 32, good.q, (int64_t)1 << 34, 32, good.k,
+                                 64, 32, good.v, 64, 32, nullptr, nullptr, nullptr, 1, 0, 1.f, 1, good.out, (int64_t)1 << 34, 32,
+                                 nullptr);
+    });
+
     const Rotation fine = [] { Rotation r; r.take(); return r; }();
     expect("rotate_heads", D, fine.forward(D), LATTICE_OK);
     expect("rotate_heads_backward", D, fine.backward(D), LATTICE_OK);
