@@ -812,12 +812,13 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
  *   zero_rest     rows of no sequence: non-zero makes their out 0 and their lse
  *                 -inf, 0 leaves both as they are.
  *   out           dev [q_rows][heads][C].   lse  dev fp32 [heads][q_rows], or NULL.
- * A row that sees no key, or only ones that score -inf, gets 0 and an lse of -inf.  Starts that go back or lie
+ * A row that sees no key, or only ones that score -inf, gets 0 and an lse of -inf; one that sees
+ * a score that is no number gets NaN, and an lse of NaN.  Starts that go back or lie
  * outside the rows, and lengths outside their sequence, are clamped to what there
  * is, and reported by lattice_dense_get_status (LATTICE_E_RANGE).
  * Products of fp32 values are as exact as fp32 ones (where there are many, of up to
- * 64 channels, made of three bf16 each: values of 2^127 or more give NaN there, those
- * below 2^-110 lose their last bits); of bf16 values they are exact, and exp(..) is
+ * 64 channels, made of three bf16 each: values of 2^127 or more, infinities among them,
+ * give NaN there, those below 2^-110 lose their last bits); of bf16 values they are exact, and exp(..) is
  * rounded to bf16 before the product with v.  Sums are fp32.
  * Rows that belong to no sequence, and keys that do not count, are not used,
  * whatever they hold.  A value that is not finite in a sequence's own rows may

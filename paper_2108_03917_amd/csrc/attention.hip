@@ -92,7 +92,9 @@ __device__ __forceinline__ bool tile_of(const Params &a, Tile &t) {
 }
 
 // A column's state: its maximum (of the scores as they are), the sum of
-// this lane's share of the exponentials, and the output's channels.
+// this lane's share of the exponentials, and the output's channels.  A maximum passes by what
+// is no number, a sum does not: a column has seen no key (or ones that score -inf alone) where its
+// maximum is -inf and its sum is 0, and where the latter is none, the result is none.
 template <int DP>
 struct Column {
     float top = -INFINITY, sum = 0.f;
@@ -134,8 +136,9 @@ __device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, floa
 template <Type T, int DP>
 __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t row, int head, Column<DP> &col) {
     const float sum = pair_sum(col.sum);
-    const float f = col.top == -INFINITY ? 0.f : 1.f / sum;
-    const float lse2 = col.top == -INFINITY ? -INFINITY : fmaf(col.top, a.c, 0.f) + log2f(sum);
+    const bool none = col.top == -INFINITY && sum == 0.f;
+    const float f = none ? 0.f : 1.f / sum;
+    const float lse2 = none ? -INFINITY : fmaf(col.top, a.c, 0.f) + log2f(sum);
     const int h = (threadIdx.x & 63) >> 5;
     const bool part = t.parts > 1;
     if (h == 0) {
@@ -146,7 +149,7 @@ __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t r
     }
     char *o = const_cast<char *>(reinterpret_cast<const char *>(a.o.p)) + (row * a.o.row + head * a.o.head) * (T == BF16 ? 2 : 4);
     float *po = a.part_o + (((int64_t)t.split * a.pack.q_rows + row) * a.heads + head) * a.D;
-    if (part && col.top == -INFINITY) return;
+    if (part && none) return;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -155,7 +158,7 @@ __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t r
             if (c0 >= a.D) continue;
             float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = col.top == -INFINITY ? 0.f : col.o[d][4 * g + i] * f;
+            for (int i = 0; i < 4; ++i) v[i] = none ? 0.f : col.o[d][4 * g + i] * f;
             if (part)
                 store4<false>(po, c0, a.D, v);
             else
@@ -354,14 +357,14 @@ __global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params
         float all = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            if (tops[w][cc] == -INFINITY) continue;
+            if (tops[w][cc] == -INFINITY && sums[w][cc] == 0.f) continue;
             const float f = exp2_((tops[w][cc] - m) * a.c);
             all += f * sums[w][cc];
             const float *x = reinterpret_cast<const float *>(lds + w * 2 * STAGE) + cc * PITCH + c0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] += f * x[k];
         }
-        const bool none = m == -INFINITY;
+        const bool none = m == -INFINITY && all == 0.f;
         const float inv = none ? 0.f : 1.f / all;
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = none ? 0.f : v[k] * inv;

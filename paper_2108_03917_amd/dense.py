@@ -310,8 +310,8 @@ class Dense:
         which ``kv_lengths`` (int32 [sequences]) says how many count.  Without
         starts there is one sequence.  With ``causal`` row i of a sequence of n
         sees the keys up to i + (its keys) - n.  ``scale`` is 1 / sqrt(C) unless
-        given.  A row that sees no key gets zeros; rows of no sequence are left
-        alone in a given ``out``, else zeros.  Returns out, with ``want_lse`` also
+        given.  A row that sees no key gets zeros, one that sees a NaN gets NaN; rows
+        of no sequence are left alone in a given ``out``, else zeros.  Returns out, with ``want_lse`` also
         the log of each row's sum of exponentials (fp32 [heads, rows]), which the
         backward pass takes."""
         sizes, tensors, packing, scale = self._attention(q, k, v, q_starts, kv_starts, kv_lengths, scale)
