@@ -417,7 +417,9 @@ Params params_of(const lattice_dense *D, const RotateArgs &a, bool backward, uns
     while (2 * p.share <= a.heads && (a.rows * p.share < resident || (a.rows * p.share < 4 * resident && a.heads >= 8 * p.share)))
         p.share = 1 << ++p.log_share;
     p.items = a.rows * p.share;
-    grid = grid_for(p.items, groups, D->cu_count, backward ? 4 : 1 << 16);
+    // Forward a group has one item, up to 2^14 workgroups a CU: 2^30 threads (the runtime
+    // refuses 2^32).
+    grid = grid_for(p.items, groups, D->cu_count, backward ? 4 : 1 << 14);
     return p;
 }
 
