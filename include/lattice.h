@@ -878,6 +878,8 @@ lattice_status lattice_attention_backward(lattice_dense *D, lattice_dtype dtype,
  *   norm          0: rotation alone (no gains).
  *   gain_q, gain_k   dev fp32 [C], or NULL for ones.     eps  >= 0.
  *   out_q, out_k  as q and k; may be these themselves (the same strides).
+ * The mean of the squares is taken of values of any size, also where fp32 has no number for
+ * their squares.
  */
 #define LATTICE_ROTATE_MAX_CHANNELS 256
 #define LATTICE_ROTATE_MAX_AXES 8

@@ -15,9 +15,9 @@
 // reduced to a part of a turn in 64 bits: a position of 1e5 has 1.6e4 turns, of
 // which 24 bits would leave 1e-3 of one.
 //
-// Everything is bound by the bytes: 16384 rows of 32 + 8 heads of 128 in bf16, 67 us
-// forward (335 MB, 5.0 TB/s; a large copy 5.6) and 110 backward (503 MB, 4.6 TB/s);
-// 82411 rows of 4 + 4 heads of 36 in fp32, 47 and 98 (4.1 and 2.9 TB/s: 5 of a
+// Everything is bound by the bytes: 16384 rows of 32 + 8 heads of 128 in bf16, 66 us
+// forward (335 MB, 5.0 TB/s; a large copy 5.6) and 113 backward (503 MB, 4.5 TB/s);
+// 82411 rows of 4 + 4 heads of 36 in fp32, 49 and 100 (3.9 and 2.9 TB/s: 5 of a
 // group's 8 lanes have channels).  What got them there from 113 and 364 us: loads without
 // a branch around them, of 4 (backward 2) heads at a time; sums by moves between lanes
 // in place of LDS; addresses made for each head, which leaves room for 5 (4)
@@ -221,6 +221,19 @@ __device__ __forceinline__ float inverse_root(float x) {
     return small ? z * 1.1258999e15f : z;           // 2^50
 }
 
+// Sums of squares, and of products with a gradient, that lose nothing in fp32: their terms that
+// count are normal numbers, and none overflows.  Others (of values from about 1e18 on or, without
+// eps, below 1e-15) are made again from the row times a power of two, in a branch that few rows
+// take: the mean of the squares is 2^-98 to 2^116 there, for values from 2^-149 to 2^128.  The branch
+// for each head costs the rows that do not take it 1 us of 48 forward and 1 of 99 backward (fp32, the
+// sizes above); one branch for the heads side by side keeps their values and cost 17 of 66 in
+// bf16.  Where all gradients are zero the backward pass takes 3 us longer.
+__device__ __forceinline__ bool holds(float sum) { return sum >= 0x1p-100f && sum <= 0x1p120f; }
+// The root of that power of two.
+__device__ __forceinline__ float half_scale_for(float mean) {
+    return mean > 0x1p120f ? 0x1p-35f : mean < 0x1p-100f ? 0x1p50f : 1.f;
+}
+
 // Sine and cosine of `turns` whole turns: the part of a turn (exact in 64 bits),
 // its nearest quarter, and in the eighth of a turn about that the Taylor series
 // about 0, whose first terms left out are below 2^-27.
@@ -333,7 +346,21 @@ __global__ __launch_bounds__(kThreads, 4) void k_rotate(Params p) {
                         float ss = 0.f, w[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-                        const float r = p.norm ? inverse_root(group_sum<G>(ss) * of_all + p.eps) : 1.f;
+                        float r = 1.f;
+                        if (p.norm) {
+                            const float mean = group_sum<G>(ss) * of_all + p.eps;
+                            r = inverse_root(mean);
+                            if (!holds(mean)) {  // the same for a group's lanes
+                                const float h = half_scale_for(mean), f = h * h;
+                                ss = 0.f;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    x[i] *= f;
+                                    ss = fmaf(x[i], x[i], ss);
+                                }
+                                r = inverse_root(group_sum<G>(ss) * of_all + p.eps * f * f);
+                            }
+                        }
 #pragma unroll
                         for (int i = 0; i < 8; ++i) w[i] = x[i] * r * gain[i];
                         turn<INTER, false>(w, cs, sn, y);
@@ -351,11 +378,28 @@ __global__ __launch_bounds__(kThreads, 4) void k_rotate(Params p) {
                             }
                             ss = group_sum<G>(ss);
                             vx = group_sum<G>(vx);
-                            const float r = inverse_root(ss * of_all + p.eps), m = vx * r * of_all;
+                            const float mean = ss * of_all + p.eps;
+                            float r = inverse_root(mean), m = vx * r * of_all, h = 1.f;
+                            if (!holds(mean) || !holds(fabsf(vx))) {  // also gradients of zero
+                                h = half_scale_for(mean);
+                                ss = vx = 0.f;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    x[i] *= h * h;
+                                    ss = fmaf(x[i], x[i], ss);
+                                }
+                                r = inverse_root(group_sum<G>(ss) * of_all + p.eps * (h * h) * (h * h));
+                                const float part = r * of_all;  // (a mean's parts: their sum may overflow)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) vx = fmaf(u[i] * gain[i], x[i] * part, vx);
+                                m = group_sum<G>(vx);
+                            }
+                            // r h h is 1 / sqrt(mean), which need be no normal number
+                            const float rh = r * h;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 const float n = x[i] * r;
-                                y[i] = r * (u[i] * gain[i] - n * m);
+                                y[i] = rh * (u[i] * gain[i] - n * m) * h;
                                 sums[s][i] = fmaf(u[i], n, sums[s][i]);
                             }
                         } else {
