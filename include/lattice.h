@@ -920,10 +920,10 @@ lattice_status lattice_rotate_heads_backward(lattice_dense *D, lattice_dtype dty
  *                 An output may be its own input (of the same type), otherwise
  *                 none overlaps another output or an input.
  *   in_dtype, out_dtype   host: storage of each.
- *   max_norm      >= 0, also infinity (the norm alone, and copies).     eps  >= 0.
+ *   max_norm      >= 0, also infinity (the norm alone, and copies, whatever the norm).     eps  >= 0.
  *   norm          dev fp32 [1].
- * The sum is fp64.  A norm that is not finite scales by what the formula gives:
- * NaN for NaN, and 0 for infinity (with NaN for infinite values).
+ * The sum is fp64.  Under a finite max_norm a norm that is not finite scales by what the
+ * formula gives: NaN for NaN, and 0 for infinity (with NaN for infinite values).
  */
 #define LATTICE_CLIP_MAX_TENSORS 65536
 lattice_status lattice_clip_gradients(lattice_dense *D, int count, const void *const *in, const lattice_dtype *in_dtype,

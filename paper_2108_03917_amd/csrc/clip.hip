@@ -140,11 +140,11 @@ __device__ __forceinline__ void scale(const Tensor &t, int64_t lo, int64_t hi, f
         scale<false, false>(t.in, t.out, lo, hi, f);
 }
 
-// What a norm scales by: a norm that is no number makes every value none; zeros stay
-// zeros without eps too.
+// What a norm scales by: a norm that is no number makes every value none, unless there is no
+// largest norm; zeros stay zeros without eps too.
 __device__ __forceinline__ float factor(double norm, float most, float eps) {
     const double q = (double)most / (norm + (double)eps);
-    return q > 1.0 || norm == 0.0 ? 1.f : (float)q;
+    return q > 1.0 || norm == 0.0 || most == INFINITY ? 1.f : (float)q;
 }
 
 __global__ __launch_bounds__(kThreads) void k_scale(Table table, const double *sums, int parts, float most, float eps,

@@ -447,7 +447,8 @@ class Dense:
         min(1, max_norm / (norm + eps)), where norm is that over all their values,
         in place or into ``out`` (fp32 or bf16, of as many values each).  Returns the norm
         before, an fp32 scalar.  A norm that is not finite is not refused: NaN
-        makes every value NaN, infinity makes finite ones 0."""
+        makes every value NaN, infinity makes finite ones 0, unless ``max_norm``
+        is infinite: then nothing is scaled."""
         n = len(grads)
 
         def check(tensors, name):
