@@ -923,7 +923,8 @@ lattice_status lattice_rotate_heads_backward(lattice_dense *D, lattice_dtype dty
  *   max_norm      >= 0, also infinity (the norm alone, and copies, whatever the norm).     eps  >= 0.
  *   norm          dev fp32 [1].
  * The sum is fp64.  Under a finite max_norm a norm that is not finite scales by what the
- * formula gives: NaN for NaN, and 0 for infinity (with NaN for infinite values).
+ * formula gives: NaN for NaN, and 0 for infinity (with NaN for infinite values).  A norm of
+ * finite values that fp32 has no number for is given as infinity, and scales as what it is.
  */
 #define LATTICE_CLIP_MAX_TENSORS 65536
 lattice_status lattice_clip_gradients(lattice_dense *D, int count, const void *const *in, const lattice_dtype *in_dtype,

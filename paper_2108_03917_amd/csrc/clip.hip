@@ -108,19 +108,35 @@ __global__ __launch_bounds__(kThreads) void k_squares(Table table, double *sums)
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
+// What a norm scales by, f 2^e: a norm that is no number makes every value none, unless there is
+// no largest norm; zeros stay zeros without eps too.  The power of two is there for factors that
+// are no normal fp32 numbers, of norms up to 1e47.
+struct Factor {
+    float f;
+    int e;
+    __device__ __forceinline__ Factor(double norm, float most, float eps) : f(1.f), e(0) {
+        const double q = (double)most / (norm + (double)eps);
+        if (q > 1.0 || norm == 0.0 || most == INFINITY) return;
+        if (q > 0.0 && q < 0x1p-100) e = ilogb(q) + 1;  // f <= 1: no product overflows
+        f = (float)ldexp(q, -e);
+    }
+    __device__ __forceinline__ bool one() const { return f == 1.f && e == 0; }
+    __device__ __forceinline__ float times(float v) const { return ldexpf(v * f, e); }
+};
+
 template <bool IN16, bool OUT16>
-__device__ __forceinline__ void scale(const void *in, void *out, int64_t lo, int64_t hi, float f) {
+__device__ __forceinline__ void scale(const void *in, void *out, int64_t lo, int64_t hi, const Factor &f) {
     int64_t i = lo + threadIdx.x * 8;
     for (; i + 8 <= hi; i += kThreads * 8) {
         float v[8];
         load_row<IN16, 8>(reinterpret_cast<const char *>(in) + i * (IN16 ? 2 : 4), 0, 8, v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= f;
+        for (int k = 0; k < 8; ++k) v[k] = f.times(v[k]);
         store_row<OUT16, 8>(reinterpret_cast<char *>(out) + i * (OUT16 ? 2 : 4), 0, 8, v);
     }
     for (int k = 0; i + k < hi && k < 8; ++k) {
-        const float v = f * (IN16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(in)[i + k])
-                                  : reinterpret_cast<const float *>(in)[i + k]);
+        const float v = f.times(IN16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(in)[i + k])
+                                     : reinterpret_cast<const float *>(in)[i + k]);
         if (OUT16)
             reinterpret_cast<uint16_t *>(out)[i + k] = (uint16_t)pack_bf16(v, 0.f);
         else
@@ -128,7 +144,7 @@ __device__ __forceinline__ void scale(const void *in, void *out, int64_t lo, int
     }
 }
 
-__device__ __forceinline__ void scale(const Tensor &t, int64_t lo, int64_t hi, float f) {
+__device__ __forceinline__ void scale(const Tensor &t, int64_t lo, int64_t hi, const Factor &f) {
     const bool in16 = t.first & kIn16, out16 = t.first & kOut16;
     if (in16 && out16)
         scale<true, true>(t.in, t.out, lo, hi, f);
@@ -140,13 +156,6 @@ __device__ __forceinline__ void scale(const Tensor &t, int64_t lo, int64_t hi, f
         scale<false, false>(t.in, t.out, lo, hi, f);
 }
 
-// What a norm scales by: a norm that is no number makes every value none, unless there is no
-// largest norm; zeros stay zeros without eps too.
-__device__ __forceinline__ float factor(double norm, float most, float eps) {
-    const double q = (double)most / (norm + (double)eps);
-    return q > 1.0 || norm == 0.0 || most == INFINITY ? 1.f : (float)q;
-}
-
 __global__ __launch_bounds__(kThreads) void k_scale(Table table, const double *sums, int parts, float most, float eps,
                                                     float *norm) {
     const Lanes lanes(table);
@@ -154,10 +163,10 @@ __global__ __launch_bounds__(kThreads) void k_scale(Table table, const double *s
     for (int i = threadIdx.x; i < parts; i += kThreads) s += sums[i];
     const double all = sqrt(block_sum<kThreads>(s));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)all;
-    const float f = factor(all, most, eps);
+    const Factor f(all, most, eps);
     for (int64_t c = table.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const Tensor t = lanes.of(c);
-        if (f == 1.f && t.in == t.out) continue;
+        if (f.one() && t.in == t.out) continue;
         const int64_t lo = (c - (t.first & kFirst)) * kChunk, hi = lo + kChunk < t.n ? lo + kChunk : t.n;
         scale(t, lo, hi, f);
     }
@@ -217,7 +226,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few(Table table, float most, fl
         for (int i = 0; i < 8; ++i) s = fma((double)v[k][i], (double)v[k][i], s);
     const double all = sqrt(block_sum<kFewThreads>(s));
     if (threadIdx.x == 0) *norm = (float)all;
-    const float f = factor(all, most, eps);
+    const Factor f(all, most, eps);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
         const int64_t c = wave + k * WAVES;
@@ -225,9 +234,9 @@ __global__ __launch_bounds__(kFewThreads) void k_few(Table table, float most, fl
         const Tensor t = lanes.of(c);
         const int64_t at = (c - (t.first & kFirst)) * kPiece + lane * 8;
         const int left = t.n - at < 8 ? (int)(t.n - at) : 8;
-        if (left <= 0 || (f == 1.f && t.in == t.out)) continue;
+        if (left <= 0 || (f.one() && t.in == t.out)) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] *= f;
+        for (int i = 0; i < 8; ++i) v[k][i] = f.times(v[k][i]);
         if (t.first & kOut16)
             store_row<true, 8>(reinterpret_cast<uint16_t *>(t.out) + at, 0, left, v[k]);
         else

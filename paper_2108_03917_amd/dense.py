@@ -448,7 +448,8 @@ class Dense:
         in place or into ``out`` (fp32 or bf16, of as many values each).  Returns the norm
         before, an fp32 scalar.  A norm that is not finite is not refused: NaN
         makes every value NaN, infinity makes finite ones 0, unless ``max_norm``
-        is infinite: then nothing is scaled."""
+        is infinite: then nothing is scaled.  (A norm of finite values past fp32's
+        largest number is returned as infinity, but scales as what it is.)"""
         n = len(grads)
 
         def check(tensors, name):
