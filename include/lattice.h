@@ -813,7 +813,8 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
  *                 -inf, 0 leaves both as they are.
  *   out           dev [q_rows][heads][C].   lse  dev fp32 [heads][q_rows], or NULL.
  * A row that sees no key, or only ones that score -inf, gets 0 and an lse of -inf; one that sees
- * a score that is no number gets NaN, and an lse of NaN.  Starts that go back or lie
+ * a score that is no number gets NaN, and an lse of NaN.  Finite scores may be of any size (q_i . k_j,
+ * before the scale, of fp32's).  Starts that go back or lie
  * outside the rows, and lengths outside their sequence, are clamped to what there
  * is, and reported by lattice_dense_get_status (LATTICE_E_RANGE).
  * Products of fp32 values are as exact as fp32 ones (where there are many, of up to
@@ -849,7 +850,8 @@ lattice_status lattice_attention(lattice_dense *D, lattice_dtype dtype, int64_t 
  *   zero_rest     rows of no sequence, and keys that do not count: non-zero makes
  *                 their gradients 0, 0 leaves them as they are.
  * The rest as in the forward call; p and t are rounded to bf16 before their
- * products with bf16 values.
+ * products with bf16 values.  An lse has 24 bits, so p is off by 2^-23 |lse_i| of itself, and
+ * gradients of scores of 1e7 or more mean little (from about 1e9 on they need not be finite).
  */
 lattice_status lattice_attention_backward(lattice_dense *D, lattice_dtype dtype, int64_t q_rows, int64_t kv_rows,
                                           int heads, int kv_heads, int C, const void *grad_out, int64_t grad_row,

@@ -40,7 +40,8 @@ struct Params {
     Cut cut;                // of blocks of keys
     float c;            // scale, for powers of 2
     bool zero_rest;
-    float *part_o, *part_lse;  // of the parts: [splits][rows][heads][D], [splits][heads][rows]
+    float *part_o;      // of the parts: [splits][rows][heads][D]
+    float2 *part_stats; // [splits][heads][rows]: maximum and sum (an lse would round what sets the parts' weights)
     int32_t *status;
 };
 
@@ -101,6 +102,9 @@ struct Column {
     f32x16_t o[DP / 32];
 };
 
+// Scores (for powers of 2) that c times themselves rounds by 1/2 at most.
+constexpr float kLargeScore = 0x1p24f;
+
 // Take in a block of KB x 32 scores of a column.
 template <Type T, int DP, int KB>
 __device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, float c, Right<T> (&p)[KB]) {
@@ -120,7 +124,18 @@ __device__ __forceinline__ void softmax(f32x16_t (&s)[KB], Column<DP> &col, floa
 #pragma unroll
             for (int e = 0; e < 16; ++e) col.o[d][e] *= f;
     }
-    const float mc = col.top == -INFINITY ? 0.f : col.top * c;
+    float mc = col.top == -INFINITY ? 0.f : col.top * c;
+    // c times a large score is off by more than an exponential bears: the difference first
+    const bool large = fabsf(mc) > kLargeScore;
+    if (__any(large)) {
+        seldom();
+        const float base = large ? col.top : 0.f;
+        mc = large ? 0.f : mc;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[b][e] -= base;
+    }
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
 #pragma unroll
@@ -143,7 +158,7 @@ __device__ __forceinline__ void finish(const Params &a, const Tile &t, int64_t r
     const bool part = t.parts > 1;
     if (h == 0) {
         if (part)
-            a.part_lse[((int64_t)t.split * a.heads + head) * a.pack.q_rows + row] = lse2;
+            a.part_stats[((int64_t)t.split * a.heads + head) * a.pack.q_rows + row] = make_float2(col.top, sum);
         else if (a.lse)
             a.lse[head * a.pack.q_rows + row] = lse2 * kLn2;
     }
@@ -373,7 +388,7 @@ __global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params
         if (c0 == 0) {
             const float lse2 = none ? -INFINITY : m * a.c + log2f(all);
             if (t.parts > 1)
-                a.part_lse[((int64_t)t.split * a.heads + hh) * a.pack.q_rows + row] = lse2;
+                a.part_stats[((int64_t)t.split * a.heads + hh) * a.pack.q_rows + row] = make_float2(m, all);
             else if (a.lse)
                 a.lse[hh * a.pack.q_rows + row] = lse2 * kLn2;
         }
@@ -387,8 +402,12 @@ __global__ __launch_bounds__((64 * few_waves<T, DP>())) void k_attend_few(Params
     }
 }
 
-// The parts' results of kJoinRows rows of a tile (blocks of KT keys): weights
-// 2^(lse - their common lse).
+// A part's sum as it is under the parts' common maximum.
+__device__ __forceinline__ float weight(float2 stat, float m, float c) {
+    return stat.x == -INFINITY && stat.y == 0.f ? 0.f : exp2_((stat.x - m) * c) * stat.y;
+}
+
+// The parts' results of kJoinRows rows of a tile (blocks of KT keys), weighted so.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_join(Params a, int KT) {
     int first;
@@ -402,36 +421,33 @@ __global__ __launch_bounds__(256) void k_join(Params a, int KT) {
     rows = rows - skip < kJoinRows ? rows - skip : kJoinRows;
     const int64_t next = a.pack.q_rows * a.heads;
     const int lanes = (a.D + 3) / 4, pairs = rows * a.heads;  // of a head's row; rows' heads
-    __shared__ float lses[kJoinPairs][kMostSplits];
+    __shared__ float2 stats[kJoinPairs][kMostSplits];
     for (int base = (int)blockIdx.z * kJoinPairs; base < pairs; base += kJoinPairs * gridDim.z) {
         const int here = pairs - base < kJoinPairs ? pairs - base : kJoinPairs;
         __syncthreads();
         for (int id = threadIdx.x; id < here * splits; id += 256) {
             const int n = id / here, i = base + id - n * here;
-            lses[id - n * here][n] = a.part_lse[n * next + (i % a.heads) * a.pack.q_rows + s.q0 + first + i / a.heads];
+            stats[id - n * here][n] = a.part_stats[n * next + (i % a.heads) * a.pack.q_rows + s.q0 + first + i / a.heads];
         }
         __syncthreads();
         for (int id = threadIdx.x; id < here * lanes; id += 256) {
             const int pair = id / lanes, i = base + pair, c0 = (id - pair * lanes) * 4;
             const int64_t row = s.q0 + first + i / a.heads;
             const int head = i % a.heads;
-            const float *lse = lses[pair];
+            const float2 *stat = stats[pair];
             float m = -INFINITY, sum = 0.f;
-            bool nan = false;
-            for (int n = 0; n < splits; ++n) {
-                nan |= lse[n] != lse[n];
-                m = fmaxf(m, lse[n]);
-            }
-            for (int n = 0; n < splits; ++n) sum += m == -INFINITY ? 0.f : exp2_(lse[n] - m);
-            const float all = nan ? NAN : m == -INFINITY ? m : m + log2f(sum);
-            if (a.lse && c0 == 0) a.lse[head * a.pack.q_rows + row] = all * kLn2;
+            for (int n = 0; n < splits; ++n) m = fmaxf(m, stat[n].x);
+            for (int n = 0; n < splits; ++n) sum += weight(stat[n], m, a.c);
+            const bool nothing = m == -INFINITY && sum == 0.f;
+            if (a.lse && c0 == 0) a.lse[head * a.pack.q_rows + row] = nothing ? -INFINITY : (m * a.c + log2f(sum)) * kLn2;
+            const float inv = nothing ? 0.f : 1.f / sum;
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             const float *p = a.part_o + (row * a.heads + head) * a.D;
 #pragma unroll 4
             for (int n = 0; n < splits; ++n) {
                 // a part without keys has written nothing
-                const bool none = lse[n] == -INFINITY;
-                const float f = none ? 0.f : exp2_(lse[n] - all);
+                const bool none = stat[n].x == -INFINITY && stat[n].y == 0.f;
+                const float f = weight(stat[n], m, a.c) * inv;
                 float x[4];
                 load_row<false, 4>(p + n * next * a.D, c0, a.D, x);
 #pragma unroll
@@ -449,7 +465,7 @@ struct Plan {
     Params p;
     bool few, dma, planes;
     int nq, KT;  // blocks of 32 columns of a wavefront, keys of a block
-    int64_t grid, part_o, part_lse;  // grid.x; floats of scratch
+    int64_t grid, part_o, part_stats;  // grid.x; values of scratch
 };
 
 Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
@@ -494,7 +510,7 @@ Plan plan_of(const lattice_dense *D, const AttendArgs &a) {
                    r.grid, r.few ? D->cu_count : 2 * D->cu_count, r.few ? 8 : 4, kMostParts / (width * 4 + 1));
     if (p.cut.splits > 1) {
         r.part_o = p.cut.splits * width;
-        r.part_lse = (int64_t)p.cut.splits * a.q_rows * a.heads;
+        r.part_stats = (int64_t)p.cut.splits * a.q_rows * a.heads;
     }
     return r;
 }
@@ -554,7 +570,7 @@ int64_t attention_scratch(const lattice_dense *D, const AttendArgs &a) {
     const Plan r = plan_of(D, a);
     ScratchLayout s;
     s.take(r.part_o * 4);
-    s.take(r.part_lse * 4);
+    s.take(r.part_stats * 8);
     if (r.planes) {
         const int dp = padded_dim(a.D);
         s.take(plane_bytes(a.q_rows, a.heads, dp));
@@ -572,7 +588,7 @@ hipError_t launch_attention(lattice_dense *D, const AttendArgs &a) {
     ScratchLayout s;
     char *ws = static_cast<char *>(D->ws);
     r.p.part_o = reinterpret_cast<float *>(ws + s.take(r.part_o * 4));
-    r.p.part_lse = reinterpret_cast<float *>(ws + s.take(r.part_lse * 4));
+    r.p.part_stats = reinterpret_cast<float2 *>(ws + s.take(r.part_stats * 8));
     if (a.bf16) return launch_type<BF16>(D, r);
     if (!r.planes) return launch_type<F32>(D, r);
     const int dp = padded_dim(a.D);
