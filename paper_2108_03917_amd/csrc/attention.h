@@ -509,9 +509,6 @@ __device__ __forceinline__ float pair_sum(float x) {
 }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Row of an accumulator's value e in this lane.
-__device__ __forceinline__ int acc_row(int e) { return gemm::acc_row(e); }
-
 // Scores of keys from `seen` on (of the block from key0 on) count for nothing.
 __device__ __forceinline__ void mask(f32x16_t &s, int key0, int seen) {
     const int n = seen - key0 - 4 * ((threadIdx.x & 63) >> 5);

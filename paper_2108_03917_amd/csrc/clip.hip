@@ -306,12 +306,11 @@ hipError_t launch_clip(lattice_dense *D, const ClipArgs &a) {
         parts += (int)grid;
     }
     bool first = true;
-    for (int at = 0; at < a.count || first;) {
+    for (int at = 0; at < a.count;) {
         at = fill(a, at, kChunk, table);
         const unsigned grid = grid_of(D, table);
-        if (!grid && !(first && at >= a.count)) continue;
-        // one workgroup without tensors still leaves the norm
-        hipLaunchKernelGGL(k_scale, dim3(grid ? grid : 1), dim3(kThreads), 0, D->stream, table, sums, parts, a.most, a.eps,
+        if (!grid) continue;
+        hipLaunchKernelGGL(k_scale, dim3(grid), dim3(kThreads), 0, D->stream, table, sums, parts, a.most, a.eps,
                            first ? a.norm : nullptr);
         TRY(hipGetLastError());
         first = false;
