@@ -820,7 +820,8 @@ lattice_status lattice_orthogonalize(lattice_dense *D, const void *g, lattice_dt
  * Products of fp32 values are as exact as fp32 ones (where there are many, of up to
  * 64 channels, made of three bf16 each: values of 2^127 or more, infinities among them,
  * give NaN there, those below 2^-110 lose their last bits); of bf16 values they are exact, and exp(..) is
- * rounded to bf16 before the product with v.  Sums are fp32.
+ * rounded to bf16 before the product with v: by up to 2^-8 of each term, where bf16 tensors that
+ * the caller widens to fp32 are computed without (and take longer).  Sums are fp32.
  * Rows that belong to no sequence, and keys that do not count, are not used,
  * whatever they hold.  A value that is not finite in a sequence's own rows may
  * reach all results of that sequence, also those that a causal mask keeps from it,
@@ -872,7 +873,8 @@ lattice_status lattice_attention_backward(lattice_dense *D, lattice_dtype dtype,
  * 1, and so on, P in all; pair p is (p, p + P), or (2 p, 2 p + 1) if interleaved.
  * Channels from 2 P on do not turn.
  *   q, k          dev [rows][heads][C] and [rows][kv_heads][C] stored as dtype;
- *                 kv_heads may be 0 (no keys).   C  1 .. 256.
+ *                 kv_heads may be 0 (no keys).   C  1 .. 256 (lattice_attention's
+ *                 heads have up to 128).
  *   positions     dev [rows][axes], position_stride values a row: fp32, or int32
  *                 if integers.    axes  1 .. 8.   sections  host [axes], >= 0.
  *   freq          dev fp32 [P]: radians for a unit of the position.  Angles are

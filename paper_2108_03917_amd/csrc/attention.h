@@ -608,8 +608,10 @@ inline bool straight(const View &x, int D, int E) {
 // Whether fp32 products go by planes of bf16: where they take the fp32 cores longer than laying
 // the planes out, a launch of its own.  4 heads of 32, rows and keys alike, fp32 cores and planes
 // in us: forward 600 rows (5e7 of these products) 20 and 23, 1000 (1.3e8) 31 and 25, 2500 67 and 55;
-// backward 300 rows (1.2e7) 46 and 40, 2500 193 and 130.  Wider heads' planes leave no room
-// for two workgroups on a CU.  (Nor for planes of more than 8 GB.)
+// backward 300 rows (1.2e7) 46 and 40, 2500 193 and 130.  Wider heads are not built so: two
+// stages of 64 keys' planes of 128 channels take 192 KB of LDS, more than there is; blocks of 32
+// keys would fit, with one wavefront a SIMD, which is what the fp32 cores' kernels have there too.
+// (Nor are planes of more than 8 GB made.)
 inline bool planes_pay(const AttendArgs &a, int64_t keys, double from) {
     return a.D <= 64 && (double)a.q_rows * a.heads * (double)keys * a.D >= from &&
            ((double)a.q_rows * a.heads + (double)a.kv_rows * a.kv_heads) * 2 * 6 * 64 <= 8e9;

@@ -19,8 +19,11 @@
 // beside them: 16384 rows of 16 (4) heads of 128, causal, bf16, take 1.01 to 1.23 ms from
 // card to card (1.09 to 0.9 PFLOP/s; a large product reaches 1.6).  32 columns a wavefront
 // there, since 64 leave one wavefront a SIMD.  Few rows are bound by the bytes of the keys and values:
-// 48 tokens against caches of 8192 x 8 heads of 128, bf16, 189 us and 8 for the parts
+// 48 tokens against caches of 8192 x 8 heads of 128, bf16, 190 us and 8 for the parts
 // (5.0 TB/s; a large copy 5.6).  A token against 77 keys takes 6.0 us.
+//
+// Vector registers that do not fit: k_attend<BF16, 64, 2> keeps 8 in memory (21 without direct loads),
+// k_attend<PLANES, 64, 1> 2; no other instance has any.
 #include "attention.h"
 
 namespace {

@@ -11,12 +11,17 @@
 //   by keys      each wavefront has 32 keys of a key head; the rows of all its
 //                query heads go by; makes dk and dv, so that heads which share
 //                keys are added here.
-// p and t are rounded to bf16 for the products with bf16 tensors (a relative 2^-9
-// of each term), all sums are fp32.
+// p and t are rounded to bf16 for the products with bf16 tensors (by up to 2^-8 of
+// each term), all sums are fp32.
 //
-// Both are bound by the matrix cores and what stands between their products: 12
-// sequences of 1 to 3400 rows of 16 (4) heads of 128, causal, bf16, take 280 us by
-// queries (0.77 PFLOP/s) and 463 by keys (0.63), and 16 for the parts of keys.
+// 12 sequences of 1 to 3400 rows of 16 (4) heads of 128, causal, bf16, take 283 us by
+// queries (0.77 PFLOP/s) and 464 by keys (0.63), and 16 for the parts of keys.  Neither keeps one
+// unit busy all the time: the matrix cores work for 0.36 of it by queries and 0.31 by keys (counters),
+// and by keys a wavefront reads 48 KB of LDS for 32 products: eight wavefronts' reads take 3072
+// cycles at 128 bytes each, their products 2048, so LDS is the nearer bound.
+//
+// Vector registers that do not fit: k_by_keys<PLANES, 64> keeps 15 in memory, k_by_keys<F32, 128> without
+// direct loads 31; no other instance has any.
 #include <algorithm>
 
 #include "attention.h"

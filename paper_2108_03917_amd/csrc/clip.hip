@@ -11,6 +11,10 @@
 // another read and a write of everything; the second pass goes backwards, so that what
 // the first read last is still in the memory-side cache.  400 million bf16 values in 48
 // tensors: 154 us (5.2 TB/s) and 287 (5.6); 30 million fp32 in 60: 21 and 40.
+//
+// A launch takes 64 tensors.  More take two for each 64, and every workgroup that scales adds up the
+// sums of all: 1e8 fp32 values take 236 us in 48 tensors (5.1 TB/s), 259 in 65, 350 in 300 and
+// 712 in 1000 (1.7 TB/s), 1e9 in 1000 3300 (3.6 TB/s).
 #include "dense.h"
 
 namespace {

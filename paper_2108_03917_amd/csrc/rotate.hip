@@ -17,11 +17,12 @@
 //
 // Everything is bound by the bytes: 16384 rows of 32 + 8 heads of 128 in bf16, 66 us
 // forward (335 MB, 5.0 TB/s; a large copy 5.6) and 113 backward (503 MB, 4.5 TB/s);
-// 82411 rows of 4 + 4 heads of 36 in fp32, 49 and 100 (3.9 and 2.9 TB/s: 5 of a
+// 82411 rows of 4 + 4 heads of 36 in fp32, 49 and 100 (3.9 and 2.8 TB/s: 5 of a
 // group's 8 lanes have channels).  What got them there from 113 and 364 us: loads without
 // a branch around them, of 4 (backward 2) heads at a time; sums by moves between lanes
 // in place of LDS; addresses made for each head, which leaves room for 5 (4)
-// wavefronts a SIMD.
+// wavefronts a SIMD (backward, fp32 rows that are not whole lanes' keep 3 or 4 vector registers
+// in memory).
 //
 // dgain: each lane adds up its channels in fp32, a workgroup its groups in LDS,
 // and rowsum.h the workgroups in fp64, in a fixed order.

@@ -313,7 +313,9 @@ class Dense:
         given.  A row that sees no key gets zeros, one that sees a NaN gets NaN; rows
         of no sequence are left alone in a given ``out``, else zeros.  Returns out, with ``want_lse`` also
         the log of each row's sum of exponentials (fp32 [heads, rows]), which the
-        backward pass takes."""
+        backward pass takes.  Of bf16 tensors the probabilities, and the backward
+        pass's gradients of scores, are rounded to bf16 for their products; of the
+        same widened to fp32 they are not."""
         sizes, tensors, packing, scale = self._attention(q, k, v, q_starts, kv_starts, kv_lengths, scale)
         rest = out is None
         if rest:
@@ -386,7 +388,7 @@ class Dense:
                      out_k: Optional[torch.Tensor] = None):
         """Divide each head's row of ``q`` [rows, heads, C] and ``k`` [rows,
         kv_heads, C] (or None; both fp32 or both bf16, any strides but along C; C
-        up to 256) by the root of its mean square (and ``eps``), multiply by the
+        up to 256, twice ``attention``'s) by the root of its mean square (and ``eps``), multiply by the
         gains (fp32 [C] or None), and turn its pairs of channels by the row's
         ``positions`` [rows, axes] (fp32 or int32; [rows] for one axis) times
         ``freq`` (fp32, one for each pair, radians): ``sections[a]`` pairs with
