@@ -73,6 +73,32 @@ def test_one_large_head_among_others(ops, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C,P", [(3, 1), (16, 8), (36, 18), (72, 33), (128, 64), (256, 128), (250, 3)])
+def test_some_heads_of_a_wavefront(ops, C, P, dtype):  # noqa: F811
+    """Every third head large, every third small: groups of a wavefront that go different ways,
+    forward and backward, each head as it is alone."""
+    q, g = rand(1, 40, 6, C, dtype=dtype), rand(2, 40, 6, C, dtype=dtype)
+    for i, f in ((0, 2.0 ** 70), (1, 2.0 ** -70)):
+        q[:, i::3] *= f
+        g[:, i::3] *= f
+    q[::5], g[::7] = rand(3, 8, 6, C, dtype=dtype), 0
+    args = (rand(4, 40, 1), frequencies(P), [P], 1 + 0.2 * rand(5, C))
+    y, _ = ops.rotate_heads(q, None, *args, eps=0.0)
+    gx = ops.rotate_heads_backward(g, None, q, None, *args, eps=0.0)[0]
+    for h in range(6):
+        one = ops.rotate_heads(q[:, h:h + 1], None, *args, eps=0.0)[0]
+        back = ops.rotate_heads_backward(g[:, h:h + 1], None, q[:, h:h + 1], None, *args, eps=0.0)[0]
+        assert torch.equal(y[:, h:h + 1], one) and torch.equal(gx[:, h:h + 1], back)
+        for row in (0, 1, 11):                   # and alone in its launch
+            at = slice(row, row + 1)
+            alone = (args[0][at], *args[1:])
+            assert torch.equal(ops.rotate_heads(q[at, h:h + 1], None, *alone, eps=0.0)[0], one[at])
+            assert torch.equal(ops.rotate_heads_backward(g[at, h:h + 1], None, q[at, h:h + 1], None, *alone, eps=0.0)[0], back[at])
+    ref = rotate_ref(q, args[0], args[1], [P], args[3], True, 0.0, False)
+    within(y, *ref, "out")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradients_of_zero(ops, dtype):  # noqa: F811
     q = rand(1, 300, 4, 48, dtype=dtype)
     g = rand(2, 300, 4, 48, dtype=dtype)
