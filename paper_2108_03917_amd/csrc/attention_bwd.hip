@@ -17,8 +17,8 @@
 // 12 sequences of 1 to 3400 rows of 16 (4) heads of 128, causal, bf16, take 283 us by
 // queries (0.77 PFLOP/s) and 464 by keys (0.63), and 16 for the parts of keys.  Neither keeps one
 // unit busy all the time: the matrix cores work for 0.36 of it by queries and 0.31 by keys (counters),
-// and by keys a wavefront reads 48 KB of LDS for 32 products: eight wavefronts' reads take 3072
-// cycles at 128 bytes each, their products 2048, so LDS is the nearer bound.
+// and by keys a wavefront reads 48 KB of LDS for 32 products: eight wavefronts' reads, at 128 bytes
+// a cycle, take half as long again as their products (2048 cycles), so LDS is the nearer bound.
 //
 // Vector registers that do not fit: k_by_keys<PLANES, 64> keeps 15 in memory, k_by_keys<F32, 128> without
 // direct loads 31; no other instance has any.
